@@ -1,0 +1,232 @@
+// Device parts shared by the attention kernels (gfx950, wave64): 16-bit
+// element types and their matrix instructions, tiles in LDS, packed sequences.
+//
+// Matrix instruction used throughout: 32x32x16, D = A B + C. Lane l holds, with
+// r = l % 32 and h = l / 32,
+//   A[r][8h .. 8h+7], B[8h .. 8h+7][r], and D[8g + 4h + i][r] as element 4g + i.
+// The order of the 16 contracted values is free as long as A and B agree, so a
+// product's result feeds the next one without moving between lanes: of D's
+// elements, 8 s .. 8 s + 7 (s = 0, 1) are rows 16 s + 4h + {0..3} and
+// 16 s + 8 + 4h + {0..3} of column r, and B takes them as its eight values when
+// A is loaded in that order (tr_frag).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/opattr_attn.h"
+#include "common.h"
+
+namespace opa {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+struct BF16 {
+  typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+  typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+  // weights are exp2(x + kShift): float16 loses bits below 2^-14, bfloat16 has
+  // float32's range
+  static constexpr float kShift = 0.f;
+  static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a),
+                                                   __builtin_bit_cast(v8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a),
+                                                   __builtin_bit_cast(v8, b), c, 0, 0, 0);
+  }
+  // both rounded to nearest even
+  static __device__ __forceinline__ uint32_t pack(float x, float y) {
+    const f32x2 f = {x, y};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, v2));
+  }
+  static __device__ __forceinline__ float widen(uint16_t x) {
+    return __uint_as_float((uint32_t)x << 16);
+  }
+};
+
+struct F16 {
+  typedef _Float16 v8 __attribute__((ext_vector_type(8)));
+  typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+  static constexpr float kShift = 6.f;
+  static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, a),
+                                                  __builtin_bit_cast(v8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a),
+                                                  __builtin_bit_cast(v8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float x, float y) {
+    const f32x2 f = {x, y};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, v2));
+  }
+  static __device__ __forceinline__ float widen(uint16_t x) {
+    return (float)__builtin_bit_cast(_Float16, x);
+  }
+};
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Maximum and sum over a lane and its partner in the other half of the wave.
+__device__ __forceinline__ float half_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// --------------------------------------------------------------------------
+// Tiles in LDS: rows of DP 16-bit values (DP 64 or 128: head_dim rounded up,
+// the rest zero), in 16-byte chunks. Chunk c of a row lies at place c ^
+// swz(row), so that the reads below meet each bank once a cycle: along a
+// column of chunks (nat_frag: 16 rows, one chunk) and across 4 rows by 4
+// chunks (tr_frag).
+// --------------------------------------------------------------------------
+template <int DP>
+__device__ __forceinline__ int swz(int row) {
+  return DP == 128 ? ((row & 3) << 2) | ((row >> 2) & 3)
+                   : ((row & 2) << 1) | ((row >> 2) & 3);
+}
+
+// Row `row`, values 8 chunk .. 8 chunk + 7.
+template <int DP>
+__device__ __forceinline__ s16x8 nat_frag(const uint16_t *tile, int row, int chunk) {
+  return *reinterpret_cast<const s16x8 *>(tile + row * DP + ((chunk ^ swz<DP>(row)) << 3));
+}
+
+// Column 32 db + l % 32 of rows row0 + 4h + {0..3} and row0 + 8 + 4h + {0..3}
+// (row0 a multiple of 16). The transposing read gives lane i of 16 lanes the
+// column i of four rows, whose four 8-byte pieces lanes 4 r .. 4 r + 3 name.
+template <int DP>
+__device__ __forceinline__ s16x8 tr_frag(const uint16_t *tile, int row0, int db) {
+  typedef s16x4 __attribute__((address_space(3))) * lds4;
+  const int l = lane_id(), i = l & 15;
+  const int row = row0 + ((l >> 5) << 2) + (i >> 2);
+  const int col = (db << 5) + (l & 16) + ((i & 3) << 2);
+  const uint16_t *p0 = tile + row * DP + (((col >> 3) ^ swz<DP>(row)) << 3) + (col & 4);
+  const uint16_t *p1 = tile + (row + 8) * DP + (((col >> 3) ^ swz<DP>(row + 8)) << 3) + (col & 4);
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p0));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p1));
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// ROWS rows from `src` (uniform; row stride `ts` elements, `left` rows exist,
+// head_dim values each) into `tile`, by the NW waves of the block, straight to
+// LDS. Rows and values that do not exist become zero: the buffer's range ends
+// after `left` rows, and a chunk past head_dim asks past any range. The data is
+// there after wait_loads() of every wave and a barrier.
+template <int DP, int ROWS, int NW>
+__device__ __forceinline__ void tile_load(uint16_t *tile, const uint16_t *src, int64_t ts,
+                                          int left, int head_dim, int wave) {
+  constexpr int C = DP / 8;  // chunks a row
+  constexpr int N = ROWS * C / (NW * OPA_WAVE);
+  static_assert(N * NW * OPA_WAVE == ROWS * C, "whole loads");
+  const int n = left < 0 ? 0 : left > ROWS ? ROWS : left;
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint16_t *>(src), (short)0, (int)(n * ts * 2), 0x00027000);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int first = (i * NW + wave) * OPA_WAVE;
+    const int id = first + lane_id();
+    const int row = id / C;
+    const int chunk = (id % C) ^ swz<DP>(row);
+    const uint32_t off = chunk * 8 < head_dim ? (uint32_t)(row * (int)ts * 2 + chunk * 16)
+                                              : 0xfffffff0u;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rsrc, (__attribute__((address_space(3))) void *)(tile + first * 8), 16, (int)off, 0, 0,
+        0);
+  }
+}
+
+// The wave's loads have arrived (also those straight to LDS).
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Barrier of the block after which every wave's LDS accesses before it are done.
+__device__ __forceinline__ void block_sync() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// --------------------------------------------------------------------------
+// Packed sequences
+// --------------------------------------------------------------------------
+__device__ __forceinline__ int clamp_to(int x, int lo, int hi) {
+  return x < lo ? lo : x > hi ? hi : x;
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Sequence b's first row and its count of rows, clamped to [0, n].
+struct Span {
+  int first, count;
+};
+__device__ __forceinline__ Span span_of(const int32_t *cu, int b, int n) {
+  const int s = clamp_to(cu[b], 0, n);
+  const int e = clamp_to(cu[b + 1], s, n);
+  return {s, e - s};
+}
+
+// Tile `tile` of the sequences' tiles of `rows` rows: which sequence, and which
+// of its tiles; false past the last. By whole waves; the result is uniform.
+__device__ __forceinline__ bool find_tile(const int32_t *cu, int n_seqs, int n, int rows,
+                                          int tile, int &seq, int &part) {
+  const int lane = lane_id();
+  for (int base = 0; base < n_seqs; base += OPA_WAVE) {
+    const int b = base + lane;
+    int tiles = 0;
+    if (b < n_seqs) tiles = (span_of(cu, b, n).count + rows - 1) / rows;
+    int inc = tiles;
+#pragma unroll
+    for (int d = 1; d < OPA_WAVE; d <<= 1) {
+      const int o = __shfl_up(inc, d);
+      if (lane >= d) inc += o;
+    }
+    const uint64_t m = __ballot(inc > tile);
+    if (m) {
+      const int w = __ffsll((unsigned long long)m) - 1;
+      seq = base + w;
+      part = uniform(tile - __shfl(inc - tiles, w));
+      return true;
+    }
+    tile -= uniform(__shfl(inc, OPA_WAVE - 1));
+  }
+  return false;
+}
+
+// Errors found in the data, into the record's flags, status and bad_records.
+__device__ inline void report(opattr_diag *diag, uint32_t flag, int bad) {
+  if (!diag || bad <= 0) return;
+  atomicOr(&diag->flags, flag);
+  if (flag & OPATTR_F_DATA) {
+    atomicAdd((unsigned long long *)&diag->bad_records, (unsigned long long)bad);
+    atomicExch(&diag->status, OPATTR_ERR_DATA);
+  } else {
+    const int32_t was = diag->status;
+    if (was != OPATTR_ERR_DATA && was != OPATTR_ERR_ORDER)
+      atomicCAS(&diag->status, was, OPATTR_ERR_LIMIT);
+  }
+}
+
+// Offsets outside [0, n] or decreasing, by one block.
+__device__ inline void check_spans(const int32_t *cu, int n_seqs, int n, opattr_diag *diag) {
+  if (!diag) return;
+  int bad = 0;
+  for (int b = threadIdx.x; b < n_seqs; b += blockDim.x)
+    bad += cu[b] < 0 || cu[b + 1] > n || cu[b + 1] < cu[b];
+  if (bad) report(diag, OPATTR_F_DATA, bad);
+}
+
+}  // namespace opa

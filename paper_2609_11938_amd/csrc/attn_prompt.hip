@@ -1,0 +1,201 @@
+// Attention over whole prompts (opattr_attn_prompt).
+#include <type_traits>
+
+#include "attn_dev.h"
+#include "attn_impl.h"
+
+namespace opa {
+
+constexpr int kWaves = 4;       // waves a block, 32 queries each
+constexpr int kRowsQ = 32 * kWaves;
+constexpr int kRowsK = 64;      // keys a tile
+
+template <class E, int DP>
+__global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs a) {
+  constexpr int KS = DP / 16, DB = DP / 32;
+  __shared__ __align__(16) uint16_t tk[2][kRowsK * DP], tv[2][kRowsK * DP];
+  const int lane = lane_id(), wave = uniform(wave_id());
+  const int r = lane & 31, h = lane >> 5;
+  // a block's key head goes by its index modulo the key heads
+  int id = blockIdx.x;
+  const int hk = id % a.n_kv;
+  id /= a.n_kv;
+  const int head = hk * a.group + id % a.group;
+  int seq, part;
+  if (blockIdx.x == 0) {
+    check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag);
+    check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
+  }
+  if (!find_tile(a.cu_q, a.n_seqs, a.n_q, kRowsQ, id / a.group, seq, part)) return;
+  Span sq = span_of(a.cu_q, seq, a.n_q), sk = span_of(a.cu_k, seq, a.n_k);
+  sq = {uniform(sq.first), uniform(sq.count)};
+  sk = {uniform(sk.first), uniform(sk.count)};
+  // the sequence's last queries, which see the most keys, first
+  const int q0 = ((sq.count + kRowsQ - 1) / kRowsQ - 1 - part) * kRowsQ;
+  const int lead = sk.count - sq.count;
+  const int qrow = q0 + wave * 32 + r;  // this lane's query
+  const bool live = qrow < sq.count;
+  const int last = (q0 + kRowsQ < sq.count ? q0 + kRowsQ : sq.count) - 1;
+  const int keys = a.causal ? clamp_to(last + lead + 1, 0, sk.count) : sk.count;
+  const int tiles = (keys + kRowsK - 1) / kRowsK;
+  // keys below `whole` are seen by every query of this wave
+  const int whole = a.causal ? clamp_to(q0 + wave * 32 + lead + 1, 0, sk.count) : sk.count;
+  const int seen = live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) : sk.count) : 0;
+
+  s16x8 qf[KS];
+  {
+    const uint16_t *qp = a.q.p + (int64_t)(sq.first + (live ? qrow : 0)) * a.q.ts +
+                         (int64_t)head * a.q.hs;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      qf[s] = (s16x8)(0);
+      if (live && 16 * s + 8 * h < a.head_dim)
+        qf[s] = *reinterpret_cast<const s16x8 *>(qp + 16 * s + 8 * h);
+    }
+  }
+  const uint16_t *kp = a.k.p + (int64_t)sk.first * a.k.ts + (int64_t)hk * a.k.hs;
+  const uint16_t *vp = a.v.p + (int64_t)sk.first * a.v.ts + (int64_t)hk * a.v.hs;
+  const float c = a.scale * kLog2e;
+  f32x16 o[DB];
+  float m, l;
+  // One pass over the keys. A weight of 0 times a value that is not finite is no
+  // 0: kCareful adds the values of a tile that not every query of the wave sees
+  // key by key, and only to the queries that see the key.
+  const auto pass = [&](auto careful) {
+    constexpr bool kCareful = decltype(careful)::value;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = (f32x16)(0.f);
+    m = -INFINITY;
+    l = 0.f;
+    if (tiles > 0) {
+      tile_load<DP, kRowsK, kWaves>(tk[0], kp, a.k.ts, sk.count, a.head_dim, wave);
+      tile_load<DP, kRowsK, kWaves>(tv[0], vp, a.v.ts, sk.count, a.head_dim, wave);
+    }
+    for (int t = 0; t < tiles; ++t) {
+      wait_loads();
+      block_sync();
+      const int k0 = t * kRowsK, b = t & 1;
+      if (t + 1 < tiles) {
+        tile_load<DP, kRowsK, kWaves>(tk[b ^ 1], kp + (int64_t)(k0 + kRowsK) * a.k.ts, a.k.ts,
+                                      sk.count - k0 - kRowsK, a.head_dim, wave);
+        tile_load<DP, kRowsK, kWaves>(tv[b ^ 1], vp + (int64_t)(k0 + kRowsK) * a.v.ts, a.v.ts,
+                                      sk.count - k0 - kRowsK, a.head_dim, wave);
+      }
+      f32x16 x[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        x[kb] = (f32x16)(0.f);
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+          x[kb] = E::mfma(nat_frag<DP>(tk[b], 32 * kb + r, 2 * s + h), qf[s], x[kb]);
+      }
+      const bool cut = k0 + kRowsK > whole;
+      float top = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = k0 + 32 * kb + 8 * (i >> 2) + 4 * h + (i & 3);
+          float v = x[kb][i] * c;
+          if (cut && key >= seen) v = -INFINITY;
+          x[kb][i] = v;
+          top = fmaxf(top, v);
+        }
+      const float mn = fmaxf(m, half_max(top));
+      const float ref = mn == -INFINITY ? 0.f : mn;
+      const float old = exp2_fast(m - ref);
+      m = mn;
+      float sum = 0.f;
+      s16x8 pf[4];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          u32x4 w;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p0 = exp2_fast(x[kb][8 * s + 2 * i] - ref + E::kShift);
+            const float p1 = exp2_fast(x[kb][8 * s + 2 * i + 1] - ref + E::kShift);
+            sum += p0 + p1;
+            w[i] = E::pack(p0, p1);
+          }
+          pf[2 * kb + s] = __builtin_bit_cast(s16x8, w);
+        }
+      l = l * old + sum;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= old;
+      if (kCareful && cut) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll 1
+          for (int n = 0; n < 16; ++n) {  // slot n % 8 of half n / 8
+            u32x4 only;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              only[i] = h == n >> 3 && i == (n & 7) >> 1 ? (n & 1 ? 0xffff0000u : 0xffffu) : 0u;
+            const bool sees = k0 + 16 * s + 8 * ((n & 7) >> 2) + 4 * (n >> 3) + (n & 3) < seen;
+            const s16x8 pn = __builtin_bit_cast(s16x8, __builtin_bit_cast(u32x4, pf[s]) & only);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+              const u32x4 v = __builtin_bit_cast(u32x4, tr_frag<DP>(tv[b], 16 * s, d)) & only;
+              const f32x16 with = E::mfma(__builtin_bit_cast(s16x8, v), pn, o[d]);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[d][i] = sees ? with[i] : o[d][i];
+            }
+          }
+      } else {
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int s = 0; s < 4; ++s) o[d] = E::mfma(tr_frag<DP>(tv[b], 16 * s, d), pf[s], o[d]);
+      }
+    }
+  };
+  pass(std::false_type{});
+  if (a.causal) {
+    float zero = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) zero = fmaf(o[d][i], 0.f, zero);
+    if (__syncthreads_or(!(zero == 0.f))) pass(std::true_type{});
+  }
+  l = half_sum(l);
+  if (!live) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint16_t *op = a.out.p + (int64_t)(sq.first + qrow) * a.out.ts + (int64_t)head * a.out.hs;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int col = 32 * d + 8 * g + 4 * h;
+      const u32x2 w = {E::pack(o[d][4 * g] * inv, o[d][4 * g + 1] * inv),
+                       E::pack(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv)};
+      if (col < a.head_dim) *reinterpret_cast<u32x2 *>(op + col) = w;
+    }
+  if (a.lse && h == 0)
+    a.lse[(int64_t)head * a.n_q + sq.first + qrow] =
+        l == 0.f ? -INFINITY : (m + log2f(l) - E::kShift) * kLn2;
+}
+
+template <class E>
+static void launch(const PromptArgs &a, hipStream_t s) {
+  const int64_t tiles = (int64_t)a.n_q / kRowsQ + a.n_seqs;
+  const dim3 grid((uint32_t)(tiles * a.n_heads));
+  if (a.head_dim <= 64)
+    hipLaunchKernelGGL((k_attn_prompt<E, 64>), grid, dim3(kWaves * OPA_WAVE), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_attn_prompt<E, 128>), grid, dim3(kWaves * OPA_WAVE), 0, s, a);
+}
+
+void run_prompt(const PromptArgs &a, int dtype, hipStream_t s) {
+  if (a.n_q == 0 || a.n_seqs == 0) return;
+  if (dtype == OPATTR_BF16)
+    launch<BF16>(a, s);
+  else
+    launch<F16>(a, s);
+}
+
+}  // namespace opa

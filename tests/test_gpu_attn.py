@@ -1,0 +1,642 @@
+"""The attention operators on the GPU against the 64-bit oracle
+(tests/attn_oracle.py) and its bounds: prompts and their gradient, the paged
+cache's attention, append, fork and compact, at the sizes, masks and layouts
+where they can go wrong."""
+import math
+
+import numpy as np
+import pytest
+
+import attn_oracle as O
+from paper_2609_11938_amd import attn, opattr
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+DATA, LIMIT = -9, -10
+
+
+def _torch():
+    import torch
+
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return torch
+
+
+def _dt(name):
+    return getattr(_torch(), name)
+
+
+def _ints(v):
+    torch = _torch()
+    return torch.tensor(np.asarray(v), dtype=torch.int32, device=DEV)
+
+
+def _rand(rng, shape, dtype, gain=1.0):
+    """A device tensor of the type, and its values in 64 bits."""
+    torch = _torch()
+    t = torch.from_numpy((rng.normal(size=shape) * gain).astype(np.float32)).to(DEV, _dt(dtype))
+    return t, _host(t)
+
+
+def _host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _cu(lens):
+    return np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+
+
+def _within(got, want, name):
+    value, bound = want
+    got = _host(got)
+    assert got.shape == value.shape, name
+    inf = np.isinf(value)
+    assert np.array_equal(inf, np.isinf(got)), f"{name}: infinities differ"
+    assert np.array_equal(got[inf], value[inf]), name
+    off = np.abs(np.where(inf, 0, got) - np.where(inf, 0, value))
+    assert np.isfinite(off).all(), f"{name}: not finite"
+    worst = np.argmax(off - bound) if off.size else 0
+    assert (off <= bound).all(), (f"{name}: off by {off.reshape(-1)[worst]:.3g}, bound "
+                                  f"{np.broadcast_to(bound, off.shape).reshape(-1)[worst]:.3g}")
+
+
+def _layout(t, how):
+    """The same values in another layout."""
+    torch = _torch()
+    if how == "heads":  # [heads, tokens, head_dim]
+        return t.transpose(0, 1).contiguous().transpose(0, 1)
+    if how == "packed":  # a slice of wider rows
+        n, h, d = t.shape
+        wide = torch.full((n, h + 3, d + 16), float("nan"), dtype=t.dtype, device=t.device)
+        wide[:, 2:2 + h, 8:8 + d] = t
+        return wide[:, 2:2 + h, 8:8 + d]
+    return t
+
+
+def _prompt(lens_q, lens_k, h, g, d, causal, dtype, layout="plain", scale=None, seed=0,
+            gain=1.0):
+    rng = np.random.default_rng([seed, h, g, d, sum(lens_q), sum(lens_k)])
+    cu_q, cu_k = _cu(lens_q), _cu(lens_k)
+    T, K = int(cu_q[-1]), int(cu_k[-1])
+    q, qh = _rand(rng, (T, h, d), dtype, gain)
+    k, kh = _rand(rng, (K, g, d), dtype)
+    v, vh = _rand(rng, (K, g, d), dtype)
+    do, doh = _rand(rng, (T, h, d), dtype)
+    q, k, v, do = (_layout(t, layout) for t in (q, k, v, do))
+    print(f"case prompt q={lens_q} k={lens_k} heads={h}/{g} d={d} causal={causal} {dtype} "
+          f"{layout}", flush=True)
+    return dict(q=q, k=k, v=v, do=do, qh=qh, kh=kh, vh=vh, doh=doh, cu_q=_ints(cu_q),
+                cu_k=_ints(cu_k), hq=cu_q, hk=cu_k, causal=causal, dtype=dtype,
+                scale=1 / math.sqrt(d) if scale is None else scale)
+
+
+def _check_prompt(s, grad=True, layout="plain"):
+    torch = _torch()
+    args = (s["q"], s["k"], s["v"])
+    kw = dict(causal=s["causal"], scale=s["scale"])
+    diag = attn.new_diag(DEV)
+    out0 = _layout(torch.full(s["q"].shape, float("nan"), dtype=s["q"].dtype, device=DEV), layout)
+    out, lse = attn.opattr_attn_prompt(*args, s["cu_q"], s["cu_k"], out=out0, diag=diag, **kw)
+    torch.cuda.synchronize()
+    want = O.packed(s["qh"], s["kh"], s["vh"], s["hq"], s["hk"], s["scale"], s["causal"],
+                    s["dtype"], s["doh"], _host(out))
+    _within(out, want["out"], "out")
+    _within(lse, want["lse"], "lse")
+    if grad:
+        new = [_layout(torch.full(t.shape, float("nan"), dtype=t.dtype, device=DEV), layout)
+               for t in args]
+        got = attn.opattr_attn_prompt_grad(s["do"], *args, out, lse, s["cu_q"], s["cu_k"],
+                                           dq=new[0], dk=new[1], dv=new[2], diag=diag, **kw)
+        torch.cuda.synchronize()
+        for name, t in zip(("dq", "dk", "dv"), got):
+            _within(t, want[name], name)
+        again = attn.opattr_attn_prompt_grad(s["do"], *args, out, lse, s["cu_q"], s["cu_k"], **kw)
+        for name, t, u in zip(("dq", "dk", "dv"), got, again):
+            assert torch.equal(t, u), f"{name}: runs differ"
+    assert opattr.read_diag(diag)["status"] == 0
+    return out, lse, want
+
+
+SEQS = [([1], [1]), ([5], [5]), ([64], [64]), ([127, 1, 33], [127, 1, 33]), ([129], [129]),
+        ([31, 0, 260, 2], [31, 0, 260, 2]), ([1, 1, 1], [300, 65, 1]),
+        ([100, 40], [37, 0]), ([3, 70], [200, 150])]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens", SEQS, ids=str)
+def test_prompt_lengths(lens, causal):
+    _check_prompt(_prompt(*lens, 4, 2, 64, causal, "bfloat16"))
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("h,g,d", [(1, 1, 8), (3, 1, 24), (2, 2, 64), (6, 3, 72), (4, 4, 128),
+                                   (8, 1, 128), (12, 12, 64), (5, 5, 120)])
+def test_prompt_heads(h, g, d, dtype):
+    _check_prompt(_prompt([70, 131], [70, 131], h, g, d, True, dtype))
+
+
+@pytest.mark.parametrize("layout", ["heads", "packed"])
+@pytest.mark.parametrize("d,dtype", [(64, "float16"), (128, "bfloat16"), (40, "bfloat16")])
+def test_prompt_layouts(layout, d, dtype):
+    _check_prompt(_prompt([90, 7, 130], [90, 7, 130], 4, 2, d, True, dtype, layout), layout=layout)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_long(d, dtype):
+    _check_prompt(_prompt([1000, 515], [1000, 777], 2, 1, d, True, dtype))
+
+
+def test_prompt_sharp_and_flat():
+    """Scores of large size (one key takes all), and none at all."""
+    _check_prompt(_prompt([200], [200], 2, 2, 64, True, "bfloat16", gain=30.0))
+    _check_prompt(_prompt([200], [200], 2, 2, 64, True, "float16", scale=0.0))
+    _check_prompt(_prompt([150], [150], 2, 1, 64, True, "float16", scale=-0.2))
+
+
+def test_prompt_nothing():
+    torch = _torch()
+    z = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device=DEV)
+    out, lse = attn.opattr_attn_prompt(z, z, z, _ints([0]), _ints([0]))
+    assert out.shape == (0, 2, 64) and lse.shape == (2, 0)
+    got = attn.opattr_attn_prompt_grad(z, z, z, z, out, lse, _ints([0, 0]), _ints([0, 0]))
+    assert all(t.numel() == 0 for t in got)
+
+
+def test_prompt_empty_rows_are_zero():
+    """Queries before the first key a causal mask leaves them, and a sequence
+    without keys."""
+    s = _prompt([50, 20], [30, 0], 2, 1, 64, True, "bfloat16")
+    out, lse, _ = _check_prompt(s)
+    assert (out[:20] == 0).all() and (out[50:] == 0).all()
+    assert _torch().isneginf(lse[:, :20]).all() and _torch().isneginf(lse[:, 50:]).all()
+
+
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf"), 3e38])
+def test_prompt_masked_values_do_not_matter(what):
+    """Values that no finite sum survives, at a key that only the last queries
+    see, and in rows outside every sequence."""
+    torch = _torch()
+    s = _prompt([140], [140], 2, 1, 64, True, "bfloat16")
+    out, lse, _ = _check_prompt(s, grad=False)
+    for row in (3, 77, 139):
+        k, v = s["k"].clone(), s["v"].clone()
+        v[row] = what
+        k[row] = what
+        got, gl = attn.opattr_attn_prompt(s["q"], k, v, s["cu_q"], s["cu_k"], causal=True,
+                                          scale=s["scale"])
+        assert torch.equal(got[:row], out[:row]), row
+        assert torch.equal(gl[:, :row], lse[:, :row]), row
+        v = s["v"].clone()
+        v[row, 0, 5] = what
+        got, _ = attn.opattr_attn_prompt(s["q"], s["k"], v, s["cu_q"], s["cu_k"], causal=True,
+                                         scale=s["scale"])
+        assert torch.equal(got[:row], out[:row]), row
+        keep = [c for c in range(64) if c != 5]
+        assert torch.equal(got[:, :, keep], out[:, :, keep]), row
+        if math.isnan(what):
+            assert torch.isnan(got[row:, :, 5]).all()
+    # rows between sequences: the kernels must not touch what lies beside a span
+    q2, k2, v2 = (torch.full((300,) + t.shape[1:], what, dtype=t.dtype, device=DEV)
+                  for t in (s["q"], s["k"], s["v"]))
+    for t, u in ((q2, s["q"]), (k2, s["k"]), (v2, s["v"])):
+        t[100:240] = u
+    cu = _ints([100, 240])
+    got, gl = attn.opattr_attn_prompt(q2, k2, v2, cu, causal=True, scale=s["scale"])
+    assert torch.equal(got[100:240], out) and torch.equal(gl[:, 100:240], lse)
+    grads = attn.opattr_attn_prompt_grad(s["do"], s["q"], s["k"], s["v"], out, lse, s["cu_q"],
+                                         causal=True, scale=s["scale"])
+    do2 = torch.full_like(q2, what)
+    do2[100:240] = s["do"]
+    grads2 = attn.opattr_attn_prompt_grad(do2, q2, k2, v2, got, gl, cu, causal=True,
+                                          scale=s["scale"])
+    for t, u in zip(grads2, grads):
+        assert torch.equal(t[100:240], u)
+
+
+def test_prompt_bad_offsets_are_flagged():
+    torch = _torch()
+    s = _prompt([60, 40], [60, 40], 2, 1, 64, True, "bfloat16")
+    for cu in ([0, 60, 150], [-5, 60, 100], [0, 70, 60]):
+        diag = attn.new_diag(DEV)
+        attn.opattr_attn_prompt(s["q"], s["k"], s["v"], _ints(cu), diag=diag)
+        torch.cuda.synchronize()
+        d = opattr.read_diag(diag)
+        assert d["status"] == DATA and d["bad_records"] > 0, cu
+        diag = attn.new_diag(DEV)
+        out, lse = attn.opattr_attn_prompt(s["q"], s["k"], s["v"], s["cu_q"])
+        attn.opattr_attn_prompt_grad(s["do"], s["q"], s["k"], s["v"], out, lse, _ints(cu),
+                                     diag=diag)
+        assert opattr.read_diag(diag)["status"] == DATA, cu
+
+
+def test_prompt_grad_against_differences():
+    """The gradient times a direction against differences of the 64-bit loss."""
+    s = _prompt([37, 66], [37, 66], 4, 2, 64, True, "bfloat16")
+    out, lse = attn.opattr_attn_prompt(s["q"], s["k"], s["v"], s["cu_q"], scale=s["scale"])
+    got = attn.opattr_attn_prompt_grad(s["do"], s["q"], s["k"], s["v"], out, lse, s["cu_q"],
+                                       scale=s["scale"])
+    host = [s["qh"], s["kh"], s["vh"]]
+
+    def loss(q, k, v):
+        o = O.packed(q, k, v, s["hq"], s["hk"], s["scale"], True, "bfloat16")["out"][0]
+        return (o * s["doh"]).sum()
+
+    want = O.packed(*host, s["hq"], s["hk"], s["scale"], True, "bfloat16", s["doh"], _host(out))
+    rng = np.random.default_rng(1)
+    for at, name in enumerate(("dq", "dk", "dv")):
+        way = rng.normal(size=host[at].shape)
+        up, down = list(host), list(host)
+        h = 1e-5
+        up[at], down[at] = host[at] + h * way, host[at] - h * way
+        diff = (loss(*up) - loss(*down)) / (2 * h)
+        bound = (want[name][1] * np.abs(way)).sum() + 1e-5 * abs(diff) + 1e-7
+        assert abs((_host(got[at]) * way).sum() - diff) <= bound, name
+
+
+def test_prompt_grad_small_and_large():
+    """Gradients far below and above 1 keep their digits (float16 too)."""
+    for dtype, gain in (("float16", 2e-4), ("bfloat16", 1e-12), ("float16", 300.0)):
+        s = _prompt([90], [90], 2, 1, 64, True, dtype)
+        torch = _torch()
+        s["do"] = (s["do"].float() * gain).to(s["do"].dtype)
+        s["doh"] = _host(s["do"])
+        _check_prompt(s)
+        assert torch.isfinite(s["do"]).all()
+
+
+def test_prompt_other_stream_and_own_buffers():
+    """On a stream of the caller's, with no buffers given: right although the
+    current stream goes on allocating."""
+    torch = _torch()
+    s = _prompt([300, 200], [300, 200], 4, 2, 64, True, "bfloat16")
+    want, wl = attn.opattr_attn_prompt(s["q"], s["k"], s["v"], s["cu_q"])
+    grads = attn.opattr_attn_prompt_grad(s["do"], s["q"], s["k"], s["v"], want, wl, s["cu_q"])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out, lse = attn.opattr_attn_prompt(s["q"], s["k"], s["v"], s["cu_q"], stream=side)
+    got = attn.opattr_attn_prompt_grad(s["do"], s["q"], s["k"], s["v"], out, lse, s["cu_q"],
+                                       stream=side)
+    junk = [torch.full((1 << 16,), 7.0, device=DEV) for _ in range(8)]
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, wl)
+    assert all(torch.equal(t, u) for t, u in zip(got, grads)) and junk
+
+
+# --------------------------------------------------------------------------- #
+# paged cache                                                                 #
+# --------------------------------------------------------------------------- #
+
+
+def _cache(rng, lens, g, d, page, dtype, extra=3, width=None, order="nhd"):
+    """A cache whose unused places hold NaN, a table in shuffled order, and the
+    keys and values by token."""
+    torch = _torch()
+    counts = [-(-n // page) for n in lens]
+    pages = sum(counts) + extra
+    width = max(counts, default=0) + 1 if width is None else width
+    ids = rng.permutation(pages)[:sum(counts)]
+    table = np.full((len(lens), width), -1, np.int64)
+    at = 0
+    for b, n in enumerate(counts):
+        table[b, :n] = ids[at:at + n]
+        at += n
+    shape = (2, pages, page, g, d) if order == "nhd" else (2, pages, g, page, d)
+    cache = torch.full(shape, float("nan"), dtype=_dt(dtype), device=DEV)
+    if order != "nhd":
+        cache = cache.transpose(2, 3)
+    kv = []
+    for b, n in enumerate(lens):
+        x, xh = _rand(rng, (2, n, g, d), dtype)
+        for t in range(n):
+            cache[:, table[b, t // page], t % page] = x[:, t]
+        kv.append(xh)
+    return cache, table, kv
+
+
+def _check_paged(lens, h, g, d, page, dtype, seed=0, order="nhd", ws=None):
+    torch = _torch()
+    print(f"case paged lens={lens} heads={h}/{g} d={d} page={page} {dtype} {order}", flush=True)
+    rng = np.random.default_rng([seed, h, g, d, page, len(lens)])
+    cache, table, kv = _cache(rng, lens, g, d, page, dtype, order=order)
+    q, qh = _rand(rng, (len(lens), h, d), dtype, 2.0)
+    scale = 1 / math.sqrt(d)
+    diag = attn.new_diag(DEV)
+    args = (q, cache[0], cache[1], _ints(table), _ints(lens))
+    out, lse = attn.opattr_attn_paged(*args, diag=diag, ws=ws)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lens):
+        for j in range(h):
+            one = O.head(qh[b:b + 1, j], kv[b][0][:, j * g // h], kv[b][1][:, j * g // h], scale,
+                         False, dtype)
+            _within(out[b:b + 1, j], one["out"], f"out[{b}, {j}]")
+            _within(lse[j, b:b + 1], one["lse"], f"lse[{j}, {b}]")
+    assert opattr.read_diag(diag)["status"] == 0
+    again, _ = attn.opattr_attn_paged(*args, ws=ws)
+    assert torch.equal(out, again), "runs differ"
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("h,g,d,page", [(2, 2, 64, 16), (8, 2, 128, 16), (16, 1, 128, 32),
+                                        (3, 1, 72, 1), (4, 4, 8, 64), (12, 12, 64, 4),
+                                        (5, 1, 128, 128), (2, 1, 40, 1024)])
+def test_paged_heads(h, g, d, page, dtype):
+    _check_paged([1, 37, 0, 130], h, g, d, page, dtype)
+
+
+@pytest.mark.parametrize("lens", [[0], [1], [31], [32], [33], [255], [256], [257], [1025], [0, 0],
+                                  [5000, 3, 0, 700], [1] * 70], ids=lambda v: str(v)[:30])
+def test_paged_lengths(lens):
+    _check_paged(lens, 4, 1, 64, 16, "bfloat16")
+
+
+def test_paged_long_split():
+    """One sequence over many shares, beside short ones; the workspace holds
+    another call's partial results."""
+    ws = attn.Workspace(DEV)
+    _check_paged([40000], 4, 2, 64, 16, "float16", ws=ws)
+    _check_paged([20011, 1, 0, 300], 8, 2, 128, 64, "bfloat16", ws=ws)
+
+
+def test_paged_head_major_pages():
+    _check_paged([100, 45], 4, 2, 64, 16, "bfloat16", order="hnd")
+
+
+def test_paged_bad_table_and_lens():
+    """Entries out of range are masked, lengths past the table cut; both flagged."""
+    torch = _torch()
+    rng = np.random.default_rng(5)
+    lens, page = [50, 40], 16
+    cache, table, kv = _cache(rng, lens, 2, 64, page, "bfloat16", width=4)
+    q, qh = _rand(rng, (2, 4, 64), "bfloat16")
+    for where, value in (((0, 1), 10_000), ((1, 0), -3)):
+        bad = table.copy()
+        bad[where] = value
+        diag = attn.new_diag(DEV)
+        out, lse = attn.opattr_attn_paged(q, cache[0], cache[1], _ints(bad), _ints(lens),
+                                          diag=diag)
+        torch.cuda.synchronize()
+        d = opattr.read_diag(diag)
+        assert d["status"] == DATA and d["bad_records"] == page
+        b, s = where
+        keep = [t for t in range(lens[b]) if t // page != s]
+        one = O.head(qh[b:b + 1, 0], kv[b][0][keep, 0], kv[b][1][keep, 0], 0.125, False,
+                     "bfloat16")
+        _within(out[b:b + 1, 0], one["out"], "out")
+        _within(lse[0, b:b + 1], one["lse"], "lse")
+    diag = attn.new_diag(DEV)
+    full = _ints(rng.permutation(cache.shape[1])[:8].reshape(2, 4))
+    cache.nan_to_num_(0.5)
+    want, _ = attn.opattr_attn_paged(q, cache[0], cache[1], full, _ints([64, 0]))
+    got, _ = attn.opattr_attn_paged(q, cache[0], cache[1], full, _ints([9999, -7]), diag=diag)
+    assert torch.equal(got, want)
+    assert opattr.read_diag(diag)["status"] == DATA
+
+
+def test_paged_offsets_past_32_bits():
+    """Pages beyond 2^31 values from the first."""
+    torch = _torch()
+    rng = np.random.default_rng(6)
+    page, g, d = 64, 8, 128
+    pages = (1 << 31) // (page * g * d) + 40
+    cache = torch.zeros(2, pages, page, g, d, dtype=torch.bfloat16, device=DEV)
+    lens = [3 * page - 5]
+    table = np.array([[pages - 1, 3, pages - 2]])
+    x, xh = _rand(rng, (2, lens[0], g, d), "bfloat16")
+    new, _ = x, None
+    after = attn.opattr_kv_append(new[0], new[1], _ints([0, lens[0]]), cache[0], cache[1],
+                                  _ints(table), _ints([0]))
+    assert after.tolist() == lens
+    assert torch.equal(cache[1, pages - 1], x[1, :page])
+    q, qh = _rand(rng, (1, 8, d), "bfloat16")
+    out, _ = attn.opattr_attn_paged(q, cache[0], cache[1], _ints(table), after)
+    for j in range(8):
+        one = O.head(qh[:, j], xh[0][:, j], xh[1][:, j], 1 / math.sqrt(d), False, "bfloat16")
+        _within(out[:, j], one["out"], "out")
+
+
+@pytest.mark.parametrize("g,d,page,order", [(2, 64, 16, "nhd"), (3, 40, 8, "hnd"),
+                                            (1, 128, 1, "nhd"), (12, 64, 32, "nhd")])
+def test_append(g, d, page, order):
+    torch = _torch()
+    rng = np.random.default_rng([g, d, page])
+    before, new = [0, 5, 33, 17, 0], [7, 0, 1, 40, 1]
+    total = [x + y for x, y in zip(before, new)]
+    cache, table, _ = _cache(rng, total, g, d, page, "bfloat16", order=order)
+    cache.fill_(-1)
+    rows, _ = _rand(rng, (sum(new), 2 * g + 1, d), "bfloat16")
+    k, v = rows[:, :g], rows[:, g:2 * g]
+    diag = attn.new_diag(DEV)
+    print(f"case append g={g} d={d} page={page} {order}", flush=True)
+    after = attn.opattr_kv_append(k, v, _ints(_cu(new)), cache[0], cache[1], _ints(table),
+                                  _ints(before), diag=diag)
+    torch.cuda.synchronize()
+    assert after.tolist() == total and opattr.read_diag(diag)["status"] == 0
+    want = torch.full_like(cache, -1)
+    at = 0
+    for b, n in enumerate(new):
+        for t in range(n):
+            pos = before[b] + t
+            want[0, table[b, pos // page], pos % page] = k[at]
+            want[1, table[b, pos // page], pos % page] = v[at]
+            at += 1
+    assert torch.equal(cache, want)
+
+
+def test_append_out_of_place_is_flagged():
+    torch = _torch()
+    rng = np.random.default_rng(9)
+    cache, table, _ = _cache(rng, [20, 20], 2, 64, 16, "bfloat16", width=2)
+    cache.fill_(-1)
+    x, _ = _rand(rng, (30, 2, 64), "bfloat16")
+    bad = table.copy()
+    bad[0, 1] = 5000
+    diag = attn.new_diag(DEV)
+    attn.opattr_kv_append(x, x, _ints([0, 20, 30]), cache[0], cache[1], _ints(bad), _ints([0, 27]),
+                          diag=diag)
+    torch.cuda.synchronize()
+    d = opattr.read_diag(diag)
+    assert d["status"] == DATA and d["bad_records"] == 4 + 5
+    want = torch.full_like(cache, -1)
+    want[:, table[0, 0]] = x[:16]
+    want[:, table[1, 1], 11:] = x[20:25]
+    assert torch.equal(cache, want)
+
+
+# --------------------------------------------------------------------------- #
+# page tables                                                                 #
+# --------------------------------------------------------------------------- #
+
+
+def _turn(rng, rows, n_out, width, page, pages, held_some=False, planes=3, each=40):
+    """A table over distinct pages, lengths, parents and room."""
+    torch = _torch()
+    lens = [int(rng.integers(0, width * page + 1)) for _ in range(rows)]
+    need = [-(-n // page) for n in lens]
+    while sum(need) > pages * 2 // 3:
+        i = int(np.argmax(need))
+        lens[i] //= 2
+        need[i] = -(-lens[i] // page)
+    ids = rng.permutation(pages)
+    table = np.full((rows, width), -1, np.int64)
+    at = 0
+    for i, n in enumerate(need):
+        table[i, :n] = ids[at:at + n]
+        at += n
+    parent = rng.integers(-1, rows, n_out) if rows else np.full(n_out, -1)
+    room = [min(width * page, (lens[p] if p >= 0 else 0) + int(rng.integers(0, 2 * page)))
+            for p in parent]
+    held = None
+    if held_some:
+        held = np.zeros(pages, np.int64)
+        held[ids[at:at + 3]] = 2
+        held[ids[0]] = 1
+    pool = torch.randint(-2 ** 31, 2 ** 31 - 1, (planes, pages, each), dtype=torch.int32,
+                         device=DEV)
+    return pool, table, lens, parent, room, held
+
+
+TURNS = [(1, 1, 3, 16, 10), (5, 7, 6, 16, 60), (8, 3, 5, 1, 64), (40, 60, 9, 4, 700),
+         (300, 500, 12, 8, 9000), (0, 3, 4, 8, 30), (4, 0, 4, 8, 30), (3, 5, 70, 32, 300)]
+
+
+@pytest.mark.parametrize("held", [False, True])
+@pytest.mark.parametrize("rows,n_out,width,page,pages", TURNS)
+def test_fork_and_compact(rows, n_out, width, page, pages, held):
+    torch = _torch()
+    rng = np.random.default_rng([rows, n_out, pages])
+    pool, table, lens, parent, room, hold = _turn(rng, rows, n_out, width, page, pages, held)
+    print(f"case fork rows={rows}->{n_out} width={width} page={page} pages={pages} held={held}",
+          flush=True)
+    hd = None if hold is None else _ints(hold)
+    before = pool.clone()
+    diag = attn.new_diag(DEV)
+    want_t, want_l, want_r, copies, short = O.fork(page, pages, table, lens, parent, room, hold)
+    got = attn.opattr_pages_fork(pool, page, _ints(table), _ints(lens), _ints(parent),
+                                 _ints(room), held=hd, diag=diag)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(got["table"].cpu().numpy(), want_t)
+    np.testing.assert_array_equal(got["lens"].cpu().numpy(), want_l)
+    np.testing.assert_array_equal(got["refs"].cpu().numpy(), want_r)
+    for x, y in copies:
+        before[:, y] = before[:, x]
+    assert torch.equal(pool, before)
+    assert opattr.read_diag(diag)["status"] == (LIMIT if short else 0)
+    want_t, want_m, live, moves = O.compact(pages, want_t, hold)
+    c = attn.opattr_pages_compact(pool, got["table"], held=hd, diag=diag)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(c["table"].cpu().numpy(), want_t)
+    np.testing.assert_array_equal(c["moved"].cpu().numpy(), want_m)
+    assert c["live"].tolist() == [live]
+    for x, y in moves:
+        before[:, y] = before[:, x]
+    assert torch.equal(pool, before)
+    # the table in place
+    t = got["table"].clone()
+    attn.opattr_pages_compact(pool, t, held=hd, table_out=t)
+    np.testing.assert_array_equal(t.cpu().numpy(), want_t)
+
+
+def test_fork_runs_out_of_pages():
+    """Requests past the free pages: -1 entries, LIMIT, and rows whose copy got no
+    page end at their full pages."""
+    torch = _torch()
+    page, pages = 8, 10
+    table = np.array([[0, 1, 2, -1, -1], [4, 5, -1, -1, -1]])
+    lens = [21, 9]
+    parent, room = [0, 0, 1, 1, -1], [24, 30, 9, 9, 20]
+    pool = torch.arange(2 * pages * 4, dtype=torch.int32, device=DEV).view(2, pages, 4)
+    want_t, want_l, want_r, copies, short = O.fork(page, pages, table, lens, parent, room)
+    assert short
+    diag = attn.new_diag(DEV)
+    before = pool.clone()
+    got = attn.opattr_pages_fork(pool, page, _ints(table), _ints(lens), _ints(parent),
+                                 _ints(room), diag=diag)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(got["table"].cpu().numpy(), want_t)
+    np.testing.assert_array_equal(got["lens"].cpu().numpy(), want_l)
+    np.testing.assert_array_equal(got["refs"].cpu().numpy(), want_r)
+    for x, y in copies:
+        before[:, y] = before[:, x]
+    assert torch.equal(pool, before)
+    assert opattr.read_diag(diag)["status"] == LIMIT
+    # none free at all: the copies fail
+    full = np.arange(10).reshape(2, 5)
+    got = attn.opattr_pages_fork(pool, page, _ints(full), _ints([37, 40]), _ints([0, 0, 1]),
+                                 None, diag=diag)
+    want_t, want_l, want_r, copies, short = O.fork(page, pages, full, [37, 40], [0, 0, 1], None)
+    assert short and want_l[1] == 32 and not copies
+    np.testing.assert_array_equal(got["table"].cpu().numpy(), want_t)
+    np.testing.assert_array_equal(got["lens"].cpu().numpy(), want_l)
+    np.testing.assert_array_equal(got["refs"].cpu().numpy(), want_r)
+
+
+def test_pages_bad_entries_are_flagged():
+    torch = _torch()
+    page, pages = 4, 12
+    table = np.array([[3, 99, 5], [-1, 7, -1]])
+    pool = torch.zeros(1, pages, 4, dtype=torch.int32, device=DEV)
+    diag = attn.new_diag(DEV)
+    got = attn.opattr_pages_fork(pool, page, _ints(table), _ints([12, 0]), _ints([0, 5, -2]),
+                                 None, diag=diag)
+    want = O.fork(page, pages, table, [12, 0], [0, 5, -2], None)
+    np.testing.assert_array_equal(got["table"].cpu().numpy(), want[0])
+    d = opattr.read_diag(diag)
+    assert d["status"] == DATA and d["bad_records"] == 3
+    diag = attn.new_diag(DEV)
+    c = attn.opattr_pages_compact(pool, _ints(table), diag=diag)
+    np.testing.assert_array_equal(c["table"].cpu().numpy(), O.compact(pages, table)[0])
+    d = opattr.read_diag(diag)
+    assert d["status"] == DATA and d["bad_records"] == 1
+
+
+def test_binding_refuses():
+    torch = _torch()
+    s = _prompt([20], [20], 2, 1, 64, True, "bfloat16")
+    q, k, v, cu = s["q"], s["k"], s["v"], s["cu_q"]
+    bad = [lambda: attn.opattr_attn_prompt(q.float(), k.float(), v.float(), cu),
+           lambda: attn.opattr_attn_prompt(q, k.half(), v, cu),
+           lambda: attn.opattr_attn_prompt(q, k, v[:10], cu),
+           lambda: attn.opattr_attn_prompt(q, k, v, cu.long()),
+           lambda: attn.opattr_attn_prompt(q, k, v, cu, _ints([0, 10, 20])),
+           lambda: attn.opattr_attn_prompt(q, k, v, cu, out=torch.empty_like(q[:5])),
+           lambda: attn.opattr_attn_prompt(q, k, v, cu, lse=torch.empty(2, 19, device=DEV)),
+           lambda: attn.opattr_attn_prompt(q.transpose(1, 2).contiguous().transpose(1, 2), k, v,
+                                           cu),
+           lambda: attn.opattr_attn_prompt(q[:, :, 1:57], k[:, :, 1:57], v[:, :, 1:57], cu),
+           lambda: attn.opattr_attn_prompt(q.cpu(), k.cpu(), v.cpu(), cu.cpu()),
+           lambda: attn.opattr_pages_compact(torch.zeros(2, 4, 6, device=DEV)[:, :, ::2],
+                                             _ints([[1]]))]
+    for f in bad:
+        with pytest.raises((TypeError, ValueError, RuntimeError)):
+            f()
+    torch.cuda.synchronize()
+
+
+def test_prompt_graph_replays():
+    """Captured with buffers of the caller's, replayed with new inputs between
+    eager work: every replay as the eager call."""
+    torch = _torch()
+    s = _prompt([80, 130], [80, 130], 4, 2, 64, True, "float16")
+    q, k, v, do, cu = s["q"], s["k"], s["v"], s["do"], s["cu_q"]
+    ws = attn.Workspace(DEV)
+    out, lse = attn.opattr_attn_prompt(q, k, v, cu)
+    g = attn.opattr_attn_prompt_grad(do, q, k, v, out, lse, cu, ws=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        attn.opattr_attn_prompt(q, k, v, cu, out=out, lse=lse)
+        attn.opattr_attn_prompt_grad(do, q, k, v, out, lse, cu, dq=g[0], dk=g[1], dv=g[2], ws=ws)
+    for turn in range(3):
+        q.mul_(0.7)
+        do.mul_(0.5)
+        want, wl = attn.opattr_attn_prompt(q, k, v, cu)
+        wg = attn.opattr_attn_prompt_grad(do, q, k, v, want, wl, cu)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, wl), turn
+        assert all(torch.equal(a, b) for a, b in zip(g, wg)), turn
