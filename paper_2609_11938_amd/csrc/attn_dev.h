@@ -71,6 +71,17 @@ struct F16 {
   }
 };
 
+__device__ __forceinline__ int clamp_to(int x, int lo, int hi) {
+  return x < lo ? lo : x > hi ? hi : x;
+}
+// The same value in every lane, kept in a scalar register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const uint16_t *uniform(const uint16_t *p) {
+  const uint64_t x = (uint64_t)p;
+  return (const uint16_t *)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 |
+                            (uint32_t)uniform((int)x));
+}
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -127,7 +138,9 @@ __device__ __forceinline__ s16x8 tr_frag(const uint16_t *tile, int row0, int db)
 // head_dim values each) into `tile`, by the NW waves of the block, straight to
 // LDS. Rows and values that do not exist become zero: the buffer's range ends
 // after `left` rows, and a chunk past head_dim asks past any range. The data is
-// there after wait_loads() of every wave and a barrier.
+// there after wait_loads() of every wave and a barrier. The compiler waits by
+// itself before a read that may meet a load in flight, so that tiles used in
+// turn have to be arrays of their own, each named where it is used.
 template <int DP, int ROWS, int NW>
 __device__ __forceinline__ void tile_load(uint16_t *tile, const uint16_t *src, int64_t ts,
                                           int left, int head_dim, int wave) {
@@ -136,7 +149,7 @@ __device__ __forceinline__ void tile_load(uint16_t *tile, const uint16_t *src, i
   static_assert(N * NW * OPA_WAVE == ROWS * C, "whole loads");
   const int n = left < 0 ? 0 : left > ROWS ? ROWS : left;
   const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint16_t *>(src), (short)0, (int)(n * ts * 2), 0x00027000);
+      const_cast<uint16_t *>(uniform(src)), (short)0, uniform((int)(n * ts * 2)), 0x00027000);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int first = (i * NW + wave) * OPA_WAVE;
@@ -151,12 +164,18 @@ __device__ __forceinline__ void tile_load(uint16_t *tile, const uint16_t *src, i
   }
 }
 
-// The wave's loads have arrived (also those straight to LDS).
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// The wave's loads have arrived (also those straight to LDS). As the builtin, so
+// that the compiler knows it too and does not wait again.
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  asm volatile("" ::: "memory");
+}
 
 // Barrier of the block after which every wave's LDS accesses before it are done.
 __device__ __forceinline__ void block_sync() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -164,10 +183,6 @@ __device__ __forceinline__ void block_sync() {
 // --------------------------------------------------------------------------
 // Packed sequences
 // --------------------------------------------------------------------------
-__device__ __forceinline__ int clamp_to(int x, int lo, int hi) {
-  return x < lo ? lo : x > hi ? hi : x;
-}
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // Sequence b's first row and its count of rows, clamped to [0, n].
 struct Span {

@@ -93,7 +93,7 @@ __global__ void k_attn_zero(uint32_t *p, int n) {
 // that a lane holds one key; P and dS then are the B operands of
 // dv^T = dout^T P and dk^T = q^T dS.
 template <class E, int DP>
-__global__ __launch_bounds__(kGradWaves * OPA_WAVE, 1) void k_attn_dkv(PromptArgs a) {
+__global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
   __shared__ __align__(16) uint16_t tq[2][kStepQ * DP], td[2][kStepQ * DP];
   __shared__ __align__(16) float tl[2][kStepQ], tD[2][kStepQ];
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 1) void k_attn_dkv(PromptArg
 // dq of 32 queries a wave: S^T = K Q^T with the wave's queries as columns;
 // dS^T then is the B operand of dq^T = K^T dS^T.
 template <class E, int DP>
-__global__ __launch_bounds__(kGradWaves * OPA_WAVE, 1) void k_attn_dq(PromptArgs a) {
+__global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
   __shared__ __align__(16) uint16_t tk[2][kStepK * DP], tv[2][kStepK * DP];
   const int lane = lane_id(), wave = uniform(wave_id());

@@ -13,7 +13,8 @@ constexpr int kRowsK = 64;      // keys a tile
 template <class E, int DP>
 __global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
-  __shared__ __align__(16) uint16_t tk[2][kRowsK * DP], tv[2][kRowsK * DP];
+  __shared__ __align__(16) uint16_t tk0[kRowsK * DP], tk1[kRowsK * DP];
+  __shared__ __align__(16) uint16_t tv0[kRowsK * DP], tv1[kRowsK * DP];
   const int lane = lane_id(), wave = uniform(wave_id());
   const int r = lane & 31, h = lane >> 5;
   // a block's key head goes by its index modulo the key heads
@@ -42,115 +43,129 @@ __global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs
   const int whole = a.causal ? clamp_to(q0 + wave * 32 + lead + 1, 0, sk.count) : sk.count;
   const int seen = live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) : sk.count) : 0;
 
+  // scores in units of 1 / c, c > 0: a negative scale turns the queries round
+  const float c = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-120f);
   s16x8 qf[KS];
   {
     const uint16_t *qp = a.q.p + (int64_t)(sq.first + (live ? qrow : 0)) * a.q.ts +
                          (int64_t)head * a.q.hs;
+    const s16x8 turn = (s16x8)(a.scale < 0.f ? (short)0x8000 : (short)0);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       qf[s] = (s16x8)(0);
       if (live && 16 * s + 8 * h < a.head_dim)
-        qf[s] = *reinterpret_cast<const s16x8 *>(qp + 16 * s + 8 * h);
+        qf[s] = *reinterpret_cast<const s16x8 *>(qp + 16 * s + 8 * h) ^ turn;
     }
   }
   const uint16_t *kp = a.k.p + (int64_t)sk.first * a.k.ts + (int64_t)hk * a.k.hs;
   const uint16_t *vp = a.v.p + (int64_t)sk.first * a.v.ts + (int64_t)hk * a.v.hs;
-  const float c = a.scale * kLog2e;
   f32x16 o[DB];
-  float m, l;
-  // One pass over the keys. A weight of 0 times a value that is not finite is no
-  // 0: kCareful adds the values of a tile that not every query of the wave sees
-  // key by key, and only to the queries that see the key.
-  const auto pass = [&](auto careful) {
-    constexpr bool kCareful = decltype(careful)::value;
+  float m, l;  // the reference of the weights, in scores, and this half's sum
+
+  const auto load = [&](uint16_t *k, uint16_t *v, int k0) __attribute__((always_inline)) {
+    tile_load<DP, kRowsK, kWaves>(k, kp + k0 * a.k.ts, a.k.ts, sk.count - k0, a.head_dim, wave);
+    tile_load<DP, kRowsK, kWaves>(v, vp + k0 * a.v.ts, a.v.ts, sk.count - k0, a.head_dim, wave);
+  };
+  const auto step = [&](auto careful, const uint16_t *k, const uint16_t *v,
+                        int k0) __attribute__((always_inline)) {
+    f32x16 x[2];
+    x[0] = x[1] = (f32x16)(0.f);
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+        x[kb] = E::mfma(nat_frag<DP>(k, 32 * kb + r, 2 * s + h), qf[s], x[kb]);
+    const bool cut = k0 + kRowsK > whole;
+    if (cut) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (k0 + 32 * kb + 8 * (i >> 2) + 4 * h + (i & 3) >= seen) x[kb][i] = -INFINITY;
+    }
+    float top = m;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
+    // The weights' reference follows the maximum only when that has passed it by
+    // 8 binary digits: until then they are at most 2^(8 + kShift), and sums and
+    // outputs need no new scale.
+    if (__any(top > m + 8.f / c)) {
+      const float to = half_max(top);
+      const float by = to == -INFINITY ? 1.f : exp2_fast((m - to) * c);
+      m = to;
+      l *= by;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= by;
+    }
+    const float ref = E::kShift - (m == -INFINITY ? 0.f : m * c);
+    s16x8 pf[4];
+    float sum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p0 = exp2_fast(fmaf(x[kb][8 * s + 2 * i], c, ref));
+          const float p1 = exp2_fast(fmaf(x[kb][8 * s + 2 * i + 1], c, ref));
+          sum += p0 + p1;
+          w[i] = E::pack(p0, p1);
+        }
+        pf[2 * kb + s] = __builtin_bit_cast(s16x8, w);
+      }
+    l += sum;
+    if (decltype(careful)::value && cut) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll 1
+        for (int n = 0; n < 16; ++n) {  // slot n % 8 of half n / 8
+          u32x4 only;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            only[i] = h == n >> 3 && i == (n & 7) >> 1 ? (n & 1 ? 0xffff0000u : 0xffffu) : 0u;
+          const bool sees = k0 + 16 * s + 8 * ((n & 7) >> 2) + 4 * (n >> 3) + (n & 3) < seen;
+          const s16x8 pn = __builtin_bit_cast(s16x8, __builtin_bit_cast(u32x4, pf[s]) & only);
+#pragma unroll
+          for (int d = 0; d < DB; ++d) {
+            const u32x4 w = __builtin_bit_cast(u32x4, tr_frag<DP>(v, 16 * s, d)) & only;
+            const f32x16 with = E::mfma(__builtin_bit_cast(s16x8, w), pn, o[d]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = sees ? with[i] : o[d][i];
+          }
+        }
+    } else {
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = E::mfma(tr_frag<DP>(v, 16 * s, d), pf[s], o[d]);
+    }
+  };
+  // One pass over the keys, two tiles in turn. A weight of 0 times a value that
+  // is not finite is no 0: the careful pass adds the values of a tile that not
+  // every query of the wave sees key by key, and only to the queries that see
+  // the key.
+  const auto pass = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = (f32x16)(0.f);
     m = -INFINITY;
     l = 0.f;
-    if (tiles > 0) {
-      tile_load<DP, kRowsK, kWaves>(tk[0], kp, a.k.ts, sk.count, a.head_dim, wave);
-      tile_load<DP, kRowsK, kWaves>(tv[0], vp, a.v.ts, sk.count, a.head_dim, wave);
-    }
-    for (int t = 0; t < tiles; ++t) {
+    if (tiles > 0) load(tk0, tv0, 0);
+    for (int t = 0; t < tiles; t += 2) {
+      const int k0 = t * kRowsK;
       wait_loads();
       block_sync();
-      const int k0 = t * kRowsK, b = t & 1;
-      if (t + 1 < tiles) {
-        tile_load<DP, kRowsK, kWaves>(tk[b ^ 1], kp + (int64_t)(k0 + kRowsK) * a.k.ts, a.k.ts,
-                                      sk.count - k0 - kRowsK, a.head_dim, wave);
-        tile_load<DP, kRowsK, kWaves>(tv[b ^ 1], vp + (int64_t)(k0 + kRowsK) * a.v.ts, a.v.ts,
-                                      sk.count - k0 - kRowsK, a.head_dim, wave);
-      }
-      f32x16 x[2];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        x[kb] = (f32x16)(0.f);
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-          x[kb] = E::mfma(nat_frag<DP>(tk[b], 32 * kb + r, 2 * s + h), qf[s], x[kb]);
-      }
-      const bool cut = k0 + kRowsK > whole;
-      float top = -INFINITY;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = k0 + 32 * kb + 8 * (i >> 2) + 4 * h + (i & 3);
-          float v = x[kb][i] * c;
-          if (cut && key >= seen) v = -INFINITY;
-          x[kb][i] = v;
-          top = fmaxf(top, v);
-        }
-      const float mn = fmaxf(m, half_max(top));
-      const float ref = mn == -INFINITY ? 0.f : mn;
-      const float old = exp2_fast(m - ref);
-      m = mn;
-      float sum = 0.f;
-      s16x8 pf[4];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          u32x4 w;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p0 = exp2_fast(x[kb][8 * s + 2 * i] - ref + E::kShift);
-            const float p1 = exp2_fast(x[kb][8 * s + 2 * i + 1] - ref + E::kShift);
-            sum += p0 + p1;
-            w[i] = E::pack(p0, p1);
-          }
-          pf[2 * kb + s] = __builtin_bit_cast(s16x8, w);
-        }
-      l = l * old + sum;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] *= old;
-      if (kCareful && cut) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll 1
-          for (int n = 0; n < 16; ++n) {  // slot n % 8 of half n / 8
-            u32x4 only;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              only[i] = h == n >> 3 && i == (n & 7) >> 1 ? (n & 1 ? 0xffff0000u : 0xffffu) : 0u;
-            const bool sees = k0 + 16 * s + 8 * ((n & 7) >> 2) + 4 * (n >> 3) + (n & 3) < seen;
-            const s16x8 pn = __builtin_bit_cast(s16x8, __builtin_bit_cast(u32x4, pf[s]) & only);
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-              const u32x4 v = __builtin_bit_cast(u32x4, tr_frag<DP>(tv[b], 16 * s, d)) & only;
-              const f32x16 with = E::mfma(__builtin_bit_cast(s16x8, v), pn, o[d]);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) o[d][i] = sees ? with[i] : o[d][i];
-            }
-          }
-      } else {
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int s = 0; s < 4; ++s) o[d] = E::mfma(tr_frag<DP>(tv[b], 16 * s, d), pf[s], o[d]);
-      }
+      if (t + 1 < tiles) load(tk1, tv1, k0 + kRowsK);
+      step(careful, tk0, tv0, k0);
+      if (t + 1 >= tiles) break;
+      wait_loads();
+      block_sync();
+      if (t + 2 < tiles) load(tk0, tv0, k0 + 2 * kRowsK);
+      step(careful, tk1, tv1, k0 + kRowsK);
     }
   };
   pass(std::false_type{});
@@ -177,7 +192,7 @@ __global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs
     }
   if (a.lse && h == 0)
     a.lse[(int64_t)head * a.n_q + sq.first + qrow] =
-        l == 0.f ? -INFINITY : (m + log2f(l) - E::kShift) * kLn2;
+        l == 0.f ? -INFINITY : (m * c + log2f(l) - E::kShift) * kLn2;
 }
 
 template <class E>
