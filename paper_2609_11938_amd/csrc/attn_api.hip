@@ -146,7 +146,10 @@ int opattr_attn_prompt(const opattr_attn_shape *a, const opattr_rows *q, const o
 
 size_t opattr_attn_prompt_grad_workspace_bytes(const opattr_attn_shape *a) {
   if (!ok_shape(a)) return 0;
-  return align256((size_t)a->n_q * a->n_heads * 4) + align256((size_t)a->n_kv_heads * 8);
+  const size_t dp = a->head_dim <= 64 ? 64 : 128;
+  const int n = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads);
+  return align256((size_t)a->n_q * a->n_heads * 8) + align256((size_t)a->n_kv_heads * 8) +
+         (n > 1 ? (size_t)n * a->n_k * a->n_kv_heads * 2 * dp * 4 : 0);
 }
 
 int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
@@ -172,10 +175,12 @@ int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
   p.dq = rows(dq);
   p.dk = rows(dk);
   p.dv = rows(dv);
-  p.delta = static_cast<float *>(ws);
-  if (a->dtype == OPATTR_F16)
-    p.norms = reinterpret_cast<uint32_t *>(static_cast<char *>(ws) +
-                                           align256((size_t)a->n_q * a->n_heads * 4));
+  char *at = static_cast<char *>(ws);
+  p.rows = reinterpret_cast<float *>(at);
+  at += align256((size_t)a->n_q * a->n_heads * 8);
+  if (a->dtype == OPATTR_F16) p.norms = reinterpret_cast<uint32_t *>(at);
+  p.part = reinterpret_cast<float *>(at + align256((size_t)a->n_kv_heads * 8));
+  p.splits = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads);
   run_prompt_grad(p, a->dtype, (hipStream_t)stream);
   return launched();
 }

@@ -112,25 +112,43 @@ __device__ __forceinline__ int swz(int row) {
                    : ((row & 2) << 1) | ((row >> 2) & 3);
 }
 
-// Row `row`, values 8 chunk .. 8 chunk + 7.
+// Fragments. A lane's place in a tile is one offset (bytes), and the places it
+// reads differ from it in bits that the swizzle leaves to an exclusive or:
+//   nat_frag  row r of 32, values 16 s + 8 h .. + 7
+//   tr_frag   column 32 db + l % 32 of rows 4h + {0..3} and 8 + 4h + {0..3}; the
+//             transposing read gives lane i of 16 lanes the column i of four
+//             rows, whose four 8-byte pieces lanes 4 r .. 4 r + 3 name
+// `row0` is the first row, a multiple of 32 (nat_frag) or 16 (tr_frag).
 template <int DP>
-__device__ __forceinline__ s16x8 nat_frag(const uint16_t *tile, int row, int chunk) {
-  return *reinterpret_cast<const s16x8 *>(tile + row * DP + ((chunk ^ swz<DP>(row)) << 3));
+__device__ __forceinline__ int nat_place() {
+  const int r = lane_id() & 31, h = lane_id() >> 5;
+  return r * DP * 2 + ((h ^ swz<DP>(r)) << 4);
+}
+template <int DP>
+__device__ __forceinline__ int tr_place() {
+  const int l = lane_id(), i = l & 15;
+  const int row = ((l >> 5) << 2) + (i >> 2), col = (l & 16) + ((i & 3) << 2);
+  return row * DP * 2 + (((col >> 3) ^ swz<DP>(row)) << 4) + ((col & 4) << 1);
+}
+// Not a constant of a loop any more: the places above are cheaper to make again
+// than to hold.
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
-// Column 32 db + l % 32 of rows row0 + 4h + {0..3} and row0 + 8 + 4h + {0..3}
-// (row0 a multiple of 16). The transposing read gives lane i of 16 lanes the
-// column i of four rows, whose four 8-byte pieces lanes 4 r .. 4 r + 3 name.
 template <int DP>
-__device__ __forceinline__ s16x8 tr_frag(const uint16_t *tile, int row0, int db) {
+__device__ __forceinline__ s16x8 nat_frag(const uint16_t *tile, int place, int row0, int s) {
+  return *reinterpret_cast<const s16x8 *>(reinterpret_cast<const char *>(tile) +
+                                          row0 * DP * 2 + (place ^ (s << 5)));
+}
+template <int DP>
+__device__ __forceinline__ s16x8 tr_frag(const uint16_t *tile, int place, int row0, int db) {
   typedef s16x4 __attribute__((address_space(3))) * lds4;
-  const int l = lane_id(), i = l & 15;
-  const int row = row0 + ((l >> 5) << 2) + (i >> 2);
-  const int col = (db << 5) + (l & 16) + ((i & 3) << 2);
-  const uint16_t *p0 = tile + row * DP + (((col >> 3) ^ swz<DP>(row)) << 3) + (col & 4);
-  const uint16_t *p1 = tile + (row + 8) * DP + (((col >> 3) ^ swz<DP>(row + 8)) << 3) + (col & 4);
-  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p0));
-  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p1));
+  const char *p = reinterpret_cast<const char *>(tile) + row0 * DP * 2;
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + (place ^ (db << 6))));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds4)(p + 8 * DP * 2 + (place ^ (db << 6) ^ 32)));
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 

@@ -1,11 +1,18 @@
 // Gradient of attention over whole prompts (opattr_attn_prompt_grad).
 //
-// Three launches. k_attn_delta: D_i = dout_i . out_i, and for float16 the
-// largest norms of dout's and v's rows. k_attn_dkv: a wave holds 32 keys of one
-// key head, and dk and dv of them, and passes over the queries that see them of
-// every query head of the group. k_attn_dq: a wave holds 32 queries and passes
-// over their keys. Each recomputes the weights from lse; every sum has one
-// owner and one order, so runs repeat bit for bit.
+// Two passes, each recomputing the weights p from lse; every sum has one owner
+// and one order, so runs repeat bit for bit.
+//   k_attn_dq   a wave holds 32 queries and passes over their keys: dq, and the
+//               rows' D = sum_j p_j dp_j for the second pass
+//   k_attn_dkv  a wave holds 32 keys of one key head, and their dk and dv, and
+//               passes over the queries that see them, of every query head of
+//               the group; where key tiles are few, a tile's passes are split
+//               over several blocks and added up by k_dkv_sum
+// Nine products where seven are needed (with the forward pass), because the
+// scores and dp are computed by both passes: the other way, adding dq in the
+// second pass, needs float32 atomics, whose order changes the result.
+#include <type_traits>
+
 #include "attn_dev.h"
 #include "attn_impl.h"
 
@@ -13,8 +20,8 @@ namespace opa {
 
 constexpr int kGradWaves = 4;
 constexpr int kHeld = 32 * kGradWaves;  // keys (queries) a block holds
-constexpr int kStepQ = 32;              // queries a tile of the dk/dv pass
-constexpr int kStepK = 64;              // keys a tile of the dq pass
+constexpr int kStepK = 64;              // keys a tile of the first pass
+constexpr int kStepQ = 32;              // queries a tile of the second pass
 
 // Weights and their gradients are rounded to 16 bits for the products. For
 // float16 both are scaled by powers of two first: the weights by 2^kWeight, and
@@ -38,13 +45,12 @@ struct Scales<F16> {
   }
 };
 
-// D_i, 4 lanes a row, and the largest squared norms of dout's and v's rows (the
-// bits of non-negative floats order as integers, so the maximum is the same in
-// any order). A block takes kDeltaRows rows of one head: blockIdx.y is a query
-// head, and past those a key head whose values are only measured.
-constexpr int kDeltaRows = 512;
-template <class E>
-__global__ __launch_bounds__(256) void k_attn_delta(PromptArgs a) {
+// float16: the largest squared norms of dout's and v's rows (the bits of
+// non-negative floats order as integers, so the maximum is the same in any
+// order). A block takes kNormRows rows of one head: blockIdx.y is a query head,
+// and past those a key head. 4 lanes a row.
+constexpr int kNormRows = 512;
+__global__ __launch_bounds__(256) void k_attn_norms(PromptArgs a) {
   __shared__ float most[4];
   const int sub = threadIdx.x & 3;
   const bool q = (int)blockIdx.y < a.n_heads;
@@ -52,29 +58,22 @@ __global__ __launch_bounds__(256) void k_attn_delta(PromptArgs a) {
   const int n = q ? a.n_q : a.n_k;
   const Rows x = q ? a.dout : a.v;
   float top = 0.f;
-  for (int64_t t = (int64_t)blockIdx.x * kDeltaRows + (threadIdx.x >> 2);
-       t < n && t < ((int64_t)blockIdx.x + 1) * kDeltaRows; t += 64) {
+  for (int64_t t = (int64_t)blockIdx.x * kNormRows + (threadIdx.x >> 2);
+       t < n && t < ((int64_t)blockIdx.x + 1) * kNormRows; t += 64) {
     const uint16_t *px = x.p + t * x.ts + (int64_t)head * x.hs;
-    const uint16_t *py = q ? a.out.p + t * a.out.ts + (int64_t)head * a.out.hs : px;
-    float dot = 0.f, norm = 0.f;
+    float norm = 0.f;
     for (int c = sub * 8; c < a.head_dim; c += 32) {
       const s16x8 u = *reinterpret_cast<const s16x8 *>(px + c);
-      const s16x8 w = *reinterpret_cast<const s16x8 *>(py + c);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float f = E::widen((uint16_t)u[i]);
-        dot = fmaf(f, E::widen((uint16_t)w[i]), dot);
+        const float f = F16::widen((uint16_t)u[i]);
         norm = fmaf(f, f, norm);
       }
     }
-    dot += __shfl_xor(dot, 1);
-    dot += __shfl_xor(dot, 2);
     norm += __shfl_xor(norm, 1);
     norm += __shfl_xor(norm, 2);
-    if (q && sub == 0) a.delta[(int64_t)head * a.n_q + t] = dot;
     top = fmaxf(top, norm);
   }
-  if (!a.norms) return;
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
   if (lane_id() == 0) most[wave_id()] = top;
@@ -89,35 +88,192 @@ __global__ void k_attn_zero(uint32_t *p, int n) {
   if (i < n) p[i] = 0;
 }
 
+// dq of 32 queries a wave: S^T = K Q^T with the wave's queries as columns;
+// dS^T then is the B operand of dq^T = K^T dS^T. D' = dout . out starts the pass
+// (out's 16 bits make it inexact); the exact D is summed beside it and goes to
+// the second pass with the scaled lse.
+template <class E, int DP>
+__global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
+  constexpr int KS = DP / 16, DB = DP / 32;
+  __shared__ __align__(16) uint16_t tk0[kStepK * DP], tk1[kStepK * DP];
+  __shared__ __align__(16) uint16_t tv0[kStepK * DP], tv1[kStepK * DP];
+  const int lane = lane_id(), wave = uniform(wave_id());
+  const int r = lane & 31, h = lane >> 5;
+  int id = blockIdx.x;
+  const int hk = id % a.n_kv;
+  id /= a.n_kv;
+  const int head = hk * a.group + id % a.group;
+  int seq, part;
+  if (blockIdx.x == 0) {
+    check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag);
+    check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
+  }
+  if (!find_tile(a.cu_q, a.n_seqs, a.n_q, kHeld, id / a.group, seq, part)) return;
+  Span sq = span_of(a.cu_q, seq, a.n_q), sk = span_of(a.cu_k, seq, a.n_k);
+  sq = {uniform(sq.first), uniform(sq.count)};
+  sk = {uniform(sk.first), uniform(sk.count)};
+  const int q0 = ((sq.count + kHeld - 1) / kHeld - 1 - part) * kHeld;
+  const int lead = sk.count - sq.count;
+  const int qrow = q0 + wave * 32 + r;
+  const bool live = qrow < sq.count;
+  const int last = (q0 + kHeld < sq.count ? q0 + kHeld : sq.count) - 1;
+  const int keys = a.causal ? clamp_to(last + lead + 1, 0, sk.count) : sk.count;
+  const int tiles = (keys + kStepK - 1) / kStepK;
+  const int whole = a.causal ? clamp_to(q0 + wave * 32 + lead + 1, 0, sk.count) : sk.count;
+  const int seen = live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) : sk.count) : 0;
+  s16x8 qf[KS], df[KS];
+  float L = INFINITY, D = 0.f, exact = 0.f;
+  {
+    const int64_t tok = sq.first + (live ? qrow : 0);
+    const uint16_t *qp = a.q.p + tok * a.q.ts + (int64_t)head * a.q.hs;
+    const uint16_t *dp = a.dout.p + tok * a.dout.ts + (int64_t)head * a.dout.hs;
+    const uint16_t *op = a.out.p + tok * a.out.ts + (int64_t)head * a.out.hs;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      qf[s] = (s16x8)(0);
+      df[s] = (s16x8)(0);
+      if (live && 16 * s + 8 * h < a.head_dim) {
+        qf[s] = *reinterpret_cast<const s16x8 *>(qp + 16 * s + 8 * h);
+        df[s] = *reinterpret_cast<const s16x8 *>(dp + 16 * s + 8 * h);
+        const s16x8 of = *reinterpret_cast<const s16x8 *>(op + 16 * s + 8 * h);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          D = fmaf(E::widen((uint16_t)df[s][i]), E::widen((uint16_t)of[i]), D);
+      }
+    }
+    D = half_sum(D);
+    if (live) {
+      // a query that sees nothing has weights 0: exp2(x - inf)
+      const float lse = a.lse[(int64_t)head * a.n_q + tok] * kLog2e;
+      L = lse == -INFINITY ? INFINITY : lse;
+    }
+  }
+  const uint16_t *kp = a.k.p + (int64_t)sk.first * a.k.ts + (int64_t)hk * a.k.hs;
+  const uint16_t *vp = a.v.p + (int64_t)sk.first * a.v.ts + (int64_t)hk * a.v.hs;
+  const float c = a.scale * kLog2e;
+  const float up = Scales<E>::ds(a.norms, hk);
+  const int nat0 = nat_place<DP>(), tr0 = tr_place<DP>();
+  f32x16 dq[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) dq[d] = (f32x16)(0.f);
+
+  const auto load = [&](uint16_t *k, uint16_t *v, int k0) __attribute__((always_inline)) {
+    tile_load<DP, kStepK, kGradWaves>(k, kp + k0 * a.k.ts, a.k.ts, sk.count - k0, a.head_dim,
+                                     wave);
+    tile_load<DP, kStepK, kGradWaves>(v, vp + k0 * a.v.ts, a.v.ts, sk.count - k0, a.head_dim,
+                                     wave);
+  };
+  const auto step = [&](const uint16_t *k, const uint16_t *v, int k0)
+                        __attribute__((always_inline)) {
+    const bool cut = k0 + kStepK > whole;
+    const int nat = fresh(nat0), tr = fresh(tr0);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      f32x16 x = (f32x16)(0.f), y = (f32x16)(0.f);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        x = E::mfma(nat_frag<DP>(k, nat, 32 * kb, s), qf[s], x);
+        y = E::mfma(nat_frag<DP>(v, nat, 32 * kb, s), df[s], y);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = exp2_fast(fmaf(x[e], c, -L));
+        float pd = p * y[e];
+        float ds = p * (y[e] - D) * up;
+        if (cut && k0 + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3) >= seen) pd = ds = 0.f;
+        exact += pd;
+        x[e] = ds;
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = E::pack(x[8 * s + 2 * i], x[8 * s + 2 * i + 1]);
+        const s16x8 sf = __builtin_bit_cast(s16x8, w);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+          dq[d] = E::mfma(tr_frag<DP>(k, tr, 32 * kb + 16 * s, d), sf, dq[d]);
+      }
+    }
+  };
+  if (tiles > 0) load(tk0, tv0, 0);
+  for (int t = 0; t < tiles; t += 2) {
+    const int k0 = t * kStepK;
+    wait_loads();
+    block_sync();
+    if (t + 1 < tiles) load(tk1, tv1, k0 + kStepK);
+    step(tk0, tv0, k0);
+    if (t + 1 >= tiles) break;
+    wait_loads();
+    block_sync();
+    if (t + 2 < tiles) load(tk0, tv0, k0 + 2 * kStepK);
+    step(tk1, tv1, k0 + kStepK);
+  }
+  exact = half_sum(exact);
+  if (!live) return;
+  if (h == 0) {
+    const int64_t at = (int64_t)head * a.n_q + sq.first + qrow;
+    *reinterpret_cast<f32x2 *>(a.rows + 2 * at) = f32x2{L - Scales<E>::kWeight, exact};
+  }
+  const float f = a.scale / up;
+  uint16_t *op = a.dq.p + (int64_t)(sq.first + qrow) * a.dq.ts + (int64_t)head * a.dq.hs;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int col = 32 * d + 8 * g + 4 * h;
+      const u32x2 w = {E::pack(dq[d][4 * g] * f, dq[d][4 * g + 1] * f),
+                       E::pack(dq[d][4 * g + 2] * f, dq[d][4 * g + 3] * f)};
+      if (col < a.head_dim) *reinterpret_cast<u32x2 *>(op + col) = w;
+    }
+}
+
+// kStepQ pairs (lse, D) from p to LDS, past `left` of them zero; by one wave.
+__device__ __forceinline__ void row_load(float *to, const float *p, int left) {
+  static_assert(2 * kStepQ == OPA_WAVE, "a float a lane");
+  const int n = left < 0 ? 0 : left > kStepQ ? kStepQ : left;
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<float *>(reinterpret_cast<const float *>(
+          uniform(reinterpret_cast<const uint16_t *>(p)))),
+      (short)0, uniform(n * 8), 0x00027000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)to, 4,
+                                           lane_id() * 4, 0, 0, 0);
+}
+
 // dk and dv of 32 keys a wave: S = Q K^T with the wave's keys as columns, so
 // that a lane holds one key; P and dS then are the B operands of
 // dv^T = dout^T P and dk^T = q^T dS.
 template <class E, int DP>
 __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
-  __shared__ __align__(16) uint16_t tq[2][kStepQ * DP], td[2][kStepQ * DP];
-  __shared__ __align__(16) float tl[2][kStepQ], tD[2][kStepQ];
+  __shared__ __align__(16) uint16_t tq0[kStepQ * DP], tq1[kStepQ * DP];
+  __shared__ __align__(16) uint16_t td0[kStepQ * DP], td1[kStepQ * DP];
+  __shared__ __align__(16) float ts0[2 * kStepQ], ts1[2 * kStepQ];
   const int lane = lane_id(), wave = uniform(wave_id());
   const int r = lane & 31, h = lane >> 5;
-  const int hk = blockIdx.x % a.n_kv;
+  int id = blockIdx.x;
+  const int hk = id % a.n_kv;
+  id /= a.n_kv;
+  const int split = id % a.splits;
   int seq, part;
-  if (blockIdx.x == 0) {
-    check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag);
-    check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
-  }
-  if (!find_tile(a.cu_k, a.n_seqs, a.n_k, kHeld, blockIdx.x / a.n_kv, seq, part)) return;
+  if (!find_tile(a.cu_k, a.n_seqs, a.n_k, kHeld, id / a.splits, seq, part)) return;
   Span sq = span_of(a.cu_q, seq, a.n_q), sk = span_of(a.cu_k, seq, a.n_k);
   sq = {uniform(sq.first), uniform(sq.count)};
   sk = {uniform(sk.first), uniform(sk.count)};
   const int lead = sk.count - sq.count;
   const int key0 = part * kHeld + wave * 32, key = key0 + r;
   const bool live = key < sk.count;
-  // the first query that sees a key of the block, and the first that sees this
-  // lane's
+  // the first query that sees a key of the block, the first that sees every key
+  // of this wave, and the first that sees this lane's
   const int begin = a.causal ? clamp_to(part * kHeld - lead, 0, sq.count) : 0;
+  const int whole = key0 + 32 > sk.count ? sq.count
+                                         : a.causal ? clamp_to(key0 + 31 - lead, 0, sq.count) : 0;
   const int from = live ? (a.causal ? clamp_to(key - lead, 0, sq.count) : 0) : sq.count;
-  const int t0 = begin / kStepQ, t1 = (sq.count + kStepQ - 1) / kStepQ;
-  const int per = t1 - t0, steps = per > 0 ? per * a.group : 0;
+  const int t0 = begin / kStepQ, per = (sq.count + kStepQ - 1) / kStepQ - t0;
+  // this block's steps of the tile's: a head's queries, then the next head's
+  const int all = per > 0 ? per * a.group : 0;
+  const int first = (int)((int64_t)all * split / a.splits);
+  const int steps = (int)((int64_t)all * (split + 1) / a.splits);
   s16x8 kf[KS], vf[KS];
   {
     const int64_t tok = sk.first + (live ? key : 0);
@@ -136,79 +292,104 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   const float c = a.scale * kLog2e;
   const float up = Scales<E>::ds(a.norms, hk);
   const float fv = exp2_fast(-Scales<E>::kWeight), upw = up * fv;
+  const int nat0 = nat_place<DP>(), tr0 = tr_place<DP>();
   f32x16 dk[DB], dv[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) dk[d] = dv[d] = (f32x16)(0.f);
 
-  const auto load = [&](int step, int b) {
-    const int head = hk * a.group + step / per, q0 = (t0 + step % per) * kStepQ;
+  // Queries past the sequence's last, and tiles past this block's last, come as
+  // zero rows with lse and D zero: they add zeros.
+  const auto load = [&](uint16_t *q, uint16_t *dout, float *rows, int t)
+                        __attribute__((always_inline)) {
+    const int g = t / per, q0 = (t0 + t - g * per) * kStepQ, head = hk * a.group + g;
+    const int left = t < steps ? sq.count - q0 : 0;
     const int64_t tok = sq.first + q0;
-    tile_load<DP, kStepQ, kGradWaves>(tq[b], a.q.p + tok * a.q.ts + (int64_t)head * a.q.hs,
-                                      a.q.ts, sq.count - q0, a.head_dim, wave);
-    tile_load<DP, kStepQ, kGradWaves>(td[b],
+    tile_load<DP, kStepQ, kGradWaves>(q, a.q.p + tok * a.q.ts + (int64_t)head * a.q.hs, a.q.ts,
+                                      left, a.head_dim, wave);
+    tile_load<DP, kStepQ, kGradWaves>(dout,
                                       a.dout.p + tok * a.dout.ts + (int64_t)head * a.dout.hs,
-                                      a.dout.ts, sq.count - q0, a.head_dim, wave);
-    // a query that is not there, or sees nothing, has weights 0: exp2(x - inf)
-    if (threadIdx.x < 2 * kStepQ) {
-      const int i = threadIdx.x & (kStepQ - 1), q = q0 + i;
-      const int64_t at = (int64_t)head * a.n_q + tok + i;
-      if (threadIdx.x < kStepQ) {
-        float s = q < sq.count ? a.lse[at] * kLog2e - Scales<E>::kWeight : INFINITY;
-        tl[b][i] = s == -INFINITY ? INFINITY : s;
-      } else {
-        tD[b][i] = q < sq.count ? a.delta[at] : 0.f;
-      }
-    }
+                                      a.dout.ts, left, a.head_dim, wave);
+    if (wave == 0) row_load(rows, a.rows + ((int64_t)head * a.n_q + tok) * 2, left);
   };
-  if (steps > 0) load(0, 0);
-  for (int t = 0; t < steps; ++t) {
-    wait_loads();
-    block_sync();
-    const int b = t & 1, q0 = (t0 + t % per) * kStepQ;
-    if (t + 1 < steps) load(t + 1, b ^ 1);
+  const auto step = [&](const uint16_t *q, const uint16_t *dout, const float *rows, int t)
+                        __attribute__((always_inline)) {
+    const int q0 = (t0 + t % per) * kStepQ;
+    const int nat = fresh(nat0), tr = fresh(tr0);
     f32x16 x = (f32x16)(0.f), y = (f32x16)(0.f);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      x = E::mfma(nat_frag<DP>(tq[b], r, 2 * s + h), kf[s], x);
-      y = E::mfma(nat_frag<DP>(td[b], r, 2 * s + h), vf[s], y);
+      x = E::mfma(nat_frag<DP>(q, nat, 0, s), kf[s], x);
+      y = E::mfma(nat_frag<DP>(dout, nat, 0, s), vf[s], y);
     }
-    s16x8 pf[2], sf[2];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 r0 = *reinterpret_cast<const f32x4 *>(rows + 2 * (8 * g + 4 * h));
+      const f32x4 r1 = *reinterpret_cast<const f32x4 *>(rows + 2 * (8 * g + 4 * h) + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int e = 4 * g + i;
+        const float p = exp2_fast(fmaf(x[e], c, -(i < 2 ? r0[2 * i] : r1[2 * i - 4])));
+        y[e] = p * (y[e] - (i < 2 ? r0[2 * i + 1] : r1[2 * i - 3])) * upw;
+        x[e] = p;
+      }
+    }
+    if (q0 < whole) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (q0 + 8 * (e >> 2) + 4 * h + (e & 3) < from) x[e] = y[e] = 0.f;
+    }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       u32x4 wp, ws;
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const int q = 16 * s + 8 * g + 4 * h;
-        const f32x4 L = *reinterpret_cast<const f32x4 *>(&tl[b][q]);
-        const f32x4 D = *reinterpret_cast<const f32x4 *>(&tD[b][q]);
-        float p[4], ds[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = 8 * s + 4 * g + i;
-          p[i] = exp2_fast(fmaf(x[e], c, -L[i]));
-          ds[i] = p[i] * (y[e] - D[i]) * upw;
-          if (q0 + q + i < from) p[i] = ds[i] = 0.f;
-        }
-        wp[2 * g] = E::pack(p[0], p[1]);
-        wp[2 * g + 1] = E::pack(p[2], p[3]);
-        ws[2 * g] = E::pack(ds[0], ds[1]);
-        ws[2 * g + 1] = E::pack(ds[2], ds[3]);
+      for (int i = 0; i < 4; ++i) {
+        wp[i] = E::pack(x[8 * s + 2 * i], x[8 * s + 2 * i + 1]);
+        ws[i] = E::pack(y[8 * s + 2 * i], y[8 * s + 2 * i + 1]);
       }
-      pf[s] = __builtin_bit_cast(s16x8, wp);
-      sf[s] = __builtin_bit_cast(s16x8, ws);
+      const s16x8 pf = __builtin_bit_cast(s16x8, wp), sf = __builtin_bit_cast(s16x8, ws);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        dv[d] = E::mfma(tr_frag<DP>(dout, tr, 16 * s, d), pf, dv[d]);
+        dk[d] = E::mfma(tr_frag<DP>(q, tr, 16 * s, d), sf, dk[d]);
+      }
     }
+  };
+  // two tiles in turn; no branch in the loop, which would cost copies of dk, dv
+  if (first < steps) load(tq0, td0, ts0, first);
+  for (int t = first; t < steps; t += 2) {
+    wait_loads();
+    block_sync();
+    load(tq1, td1, ts1, t + 1);
+    step(tq0, td0, ts0, t);
+    wait_loads();
+    block_sync();
+    load(tq0, td0, ts0, t + 2);
+    step(tq1, td1, ts1, t + 1);
+  }
+  wait_loads();
+  if (!live) return;
+  const float fk = a.scale / up;
+  const int64_t tok = sk.first + key;
+  if (a.splits > 1) {  // [splits][n_k][n_kv][dk, dv][DP]
+    float *p = a.part + (((int64_t)split * a.n_k + tok) * a.n_kv + hk) * 2 * DP;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        dv[d] = E::mfma(tr_frag<DP>(td[b], 16 * s, d), pf[s], dv[d]);
-        dk[d] = E::mfma(tr_frag<DP>(tq[b], 16 * s, d), sf[s], dk[d]);
+      for (int g = 0; g < 4; ++g) {
+        const int col = 32 * d + 8 * g + 4 * h;
+        f32x4 x, y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = dk[d][4 * g + i] * fk;
+          y[i] = dv[d][4 * g + i] * fv;
+        }
+        *reinterpret_cast<f32x4 *>(p + col) = x;
+        *reinterpret_cast<f32x4 *>(p + DP + col) = y;
       }
+    return;
   }
-  if (!live) return;
-  const float fk = a.scale / up;
-  uint16_t *kp = a.dk.p + (int64_t)(sk.first + key) * a.dk.ts + (int64_t)hk * a.dk.hs;
-  uint16_t *vp = a.dv.p + (int64_t)(sk.first + key) * a.dv.ts + (int64_t)hk * a.dv.hs;
+  uint16_t *kp = a.dk.p + tok * a.dk.ts + (int64_t)hk * a.dk.hs;
+  uint16_t *vp = a.dv.p + tok * a.dv.ts + (int64_t)hk * a.dv.hs;
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -224,140 +405,74 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
     }
 }
 
-// dq of 32 queries a wave: S^T = K Q^T with the wave's queries as columns;
-// dS^T then is the B operand of dq^T = K^T dS^T.
+// The splits' dk and dv of the rows inside a sequence, added in order: 4 values
+// a thread, a wave's all of one row of DP 128 (of two, DP 64).
 template <class E, int DP>
-__global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
-  constexpr int KS = DP / 16, DB = DP / 32;
-  __shared__ __align__(16) uint16_t tk[2][kStepK * DP], tv[2][kStepK * DP];
-  const int lane = lane_id(), wave = uniform(wave_id());
-  const int r = lane & 31, h = lane >> 5;
-  int id = blockIdx.x;
-  const int hk = id % a.n_kv;
-  id /= a.n_kv;
-  const int head = hk * a.group + id % a.group;
-  int seq, part;
-  if (!find_tile(a.cu_q, a.n_seqs, a.n_q, kHeld, id / a.group, seq, part)) return;
-  Span sq = span_of(a.cu_q, seq, a.n_q), sk = span_of(a.cu_k, seq, a.n_k);
-  sq = {uniform(sq.first), uniform(sq.count)};
-  sk = {uniform(sk.first), uniform(sk.count)};
-  const int q0 = ((sq.count + kHeld - 1) / kHeld - 1 - part) * kHeld;
-  const int lead = sk.count - sq.count;
-  const int qrow = q0 + wave * 32 + r;
-  const bool live = qrow < sq.count;
-  const int last = (q0 + kHeld < sq.count ? q0 + kHeld : sq.count) - 1;
-  const int keys = a.causal ? clamp_to(last + lead + 1, 0, sk.count) : sk.count;
-  const int tiles = (keys + kStepK - 1) / kStepK;
-  const int seen = live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) : sk.count) : 0;
-  s16x8 qf[KS], df[KS];
-  float L = INFINITY, D = 0.f;
-  {
-    const int64_t tok = sq.first + (live ? qrow : 0);
-    const uint16_t *qp = a.q.p + tok * a.q.ts + (int64_t)head * a.q.hs;
-    const uint16_t *dp = a.dout.p + tok * a.dout.ts + (int64_t)head * a.dout.hs;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      qf[s] = (s16x8)(0);
-      df[s] = (s16x8)(0);
-      if (live && 16 * s + 8 * h < a.head_dim) {
-        qf[s] = *reinterpret_cast<const s16x8 *>(qp + 16 * s + 8 * h);
-        df[s] = *reinterpret_cast<const s16x8 *>(dp + 16 * s + 8 * h);
-      }
-    }
-    if (live) {
-      const int64_t at = (int64_t)head * a.n_q + tok;
-      L = a.lse[at] * kLog2e;
-      if (L == -INFINITY) L = INFINITY;
-      D = a.delta[at];
-    }
+__global__ __launch_bounds__(256) void k_dkv_sum(PromptArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t n = (int64_t)a.n_k * a.n_kv * 2 * DP;
+  if (i * 4 >= n) return;
+  const int64_t row = i * 4 / (2 * DP);
+  const int64_t tok = row / a.n_kv;
+  const int hk = (int)(row - tok * a.n_kv);
+  const int at = (int)(i * 4 - row * 2 * DP), col = at % DP;
+  if (col >= a.head_dim) return;
+  // rows outside every sequence keep what they hold
+  int lo = 0, hi = a.n_seqs;  // the last sequence that starts at or before tok
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.cu_k[mid] <= tok) lo = mid; else hi = mid;
   }
-  const uint16_t *kp = a.k.p + (int64_t)sk.first * a.k.ts + (int64_t)hk * a.k.hs;
-  const uint16_t *vp = a.v.p + (int64_t)sk.first * a.v.ts + (int64_t)hk * a.v.hs;
-  const float c = a.scale * kLog2e;
-  const float up = Scales<E>::ds(a.norms, hk);
-  f32x16 dq[DB];
-#pragma unroll
-  for (int d = 0; d < DB; ++d) dq[d] = (f32x16)(0.f);
-  if (tiles > 0) {
-    tile_load<DP, kStepK, kGradWaves>(tk[0], kp, a.k.ts, sk.count, a.head_dim, wave);
-    tile_load<DP, kStepK, kGradWaves>(tv[0], vp, a.v.ts, sk.count, a.head_dim, wave);
-  }
-  for (int t = 0; t < tiles; ++t) {
-    wait_loads();
-    block_sync();
-    const int k0 = t * kStepK, b = t & 1;
-    if (t + 1 < tiles) {
-      tile_load<DP, kStepK, kGradWaves>(tk[b ^ 1], kp + (int64_t)(k0 + kStepK) * a.k.ts, a.k.ts,
-                                        sk.count - k0 - kStepK, a.head_dim, wave);
-      tile_load<DP, kStepK, kGradWaves>(tv[b ^ 1], vp + (int64_t)(k0 + kStepK) * a.v.ts, a.v.ts,
-                                        sk.count - k0 - kStepK, a.head_dim, wave);
-    }
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      f32x16 x = (f32x16)(0.f), y = (f32x16)(0.f);
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        x = E::mfma(nat_frag<DP>(tk[b], 32 * kb + r, 2 * s + h), qf[s], x);
-        y = E::mfma(nat_frag<DP>(tv[b], 32 * kb + r, 2 * s + h), df[s], y);
-      }
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        u32x4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float ds[2];
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int e = 8 * s + 2 * i + j;
-            const int key = k0 + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3);
-            ds[j] = exp2_fast(fmaf(x[e], c, -L)) * (y[e] - D) * up;
-            if (key >= seen) ds[j] = 0.f;
-          }
-          w[i] = E::pack(ds[0], ds[1]);
-        }
-        const s16x8 sf = __builtin_bit_cast(s16x8, w);
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-          dq[d] = E::mfma(tr_frag<DP>(tk[b], 32 * kb + 16 * s, d), sf, dq[d]);
-      }
-    }
-  }
-  if (!live) return;
-  const float f = a.scale / up;
-  uint16_t *op = a.dq.p + (int64_t)(sq.first + qrow) * a.dq.ts + (int64_t)head * a.dq.hs;
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int col = 32 * d + 8 * g + 4 * h;
-      const u32x2 w = {E::pack(dq[d][4 * g] * f, dq[d][4 * g + 1] * f),
-                       E::pack(dq[d][4 * g + 2] * f, dq[d][4 * g + 3] * f)};
-      if (col < a.head_dim) *reinterpret_cast<u32x2 *>(op + col) = w;
-    }
+  const Span s = span_of(a.cu_k, lo, a.n_k);
+  if (tok < s.first || tok >= (int64_t)s.first + s.count) return;
+  f32x4 sum = (f32x4)(0.f);
+  for (int k = 0; k < a.splits; ++k)
+    sum += *reinterpret_cast<const f32x4 *>(a.part + k * n + i * 4);
+  const Rows &o = at < DP ? a.dk : a.dv;
+  const u32x2 w = {E::pack(sum[0], sum[1]), E::pack(sum[2], sum[3])};
+  *reinterpret_cast<u32x2 *>(o.p + tok * o.ts + (int64_t)hk * o.hs + col) = w;
 }
 
 template <class E, int DP>
 static void launch(const PromptArgs &a, hipStream_t s) {
   const int64_t kt = (int64_t)a.n_k / kHeld + a.n_seqs, qt = (int64_t)a.n_q / kHeld + a.n_seqs;
   const dim3 block(kGradWaves * OPA_WAVE);
-  if (a.n_k > 0)
-    hipLaunchKernelGGL((k_attn_dkv<E, DP>), dim3((uint32_t)(kt * a.n_kv)), block, 0, s, a);
   if (a.n_q > 0)
     hipLaunchKernelGGL((k_attn_dq<E, DP>), dim3((uint32_t)(qt * a.n_heads)), block, 0, s, a);
+  if (a.n_k == 0) return;
+  hipLaunchKernelGGL((k_attn_dkv<E, DP>), dim3((uint32_t)(kt * a.n_kv * a.splits)), block, 0, s,
+                     a);
+  if (a.splits > 1) {
+    const int64_t n = (int64_t)a.n_k * a.n_kv * 2 * DP / 4;
+    hipLaunchKernelGGL((k_dkv_sum<E, DP>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, s, a);
+  }
 }
 
 template <class E>
 static void grad(const PromptArgs &a, hipStream_t s) {
-  if (a.norms)
+  if (a.norms) {
     hipLaunchKernelGGL(k_attn_zero, dim3((2 * a.n_kv + 63) / 64), dim3(64), 0, s, a.norms,
                        2 * a.n_kv);
-  const int most = a.norms && a.n_k > a.n_q ? a.n_k : a.n_q;
-  const dim3 grid((most + kDeltaRows - 1) / kDeltaRows, a.n_heads + (a.norms ? a.n_kv : 0));
-  if (most > 0) hipLaunchKernelGGL((k_attn_delta<E>), grid, dim3(256), 0, s, a);
+    const int most = a.n_k > a.n_q ? a.n_k : a.n_q;
+    const dim3 grid((most + kNormRows - 1) / kNormRows, a.n_heads + a.n_kv);
+    if (most > 0) hipLaunchKernelGGL(k_attn_norms, grid, dim3(256), 0, s, a);
+  }
   if (a.head_dim <= 64)
     launch<E, 64>(a, s);
   else
     launch<E, 128>(a, s);
+}
+
+// Blocks of a key tile. A tile's steps go one after another, and a causal
+// sequence's first tile has the most: about 2048 blocks keep the chip full to
+// the end, each of 16 steps at least (by the sequences' mean length).
+int grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv) {
+  if (n_seqs == 0 || n_k == 0) return 1;
+  const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
+  const int64_t steps = n_q / n_seqs * (n_heads / n_kv) / kStepQ;
+  int64_t n = (2048 + blocks - 1) / blocks;
+  if (n > steps / 16) n = steps / 16;
+  return n < 1 ? 1 : n > 8 ? 8 : (int)n;
 }
 
 void run_prompt_grad(const PromptArgs &a, int dtype, hipStream_t s) {

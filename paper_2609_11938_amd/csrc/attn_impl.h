@@ -20,10 +20,15 @@ struct PromptArgs {
   int n_q, n_k, n_seqs, n_heads, n_kv, group, head_dim, causal;
   float scale;
   opattr_diag *diag;
-  // the gradient's workspace: D_i [heads][n_q], and two bounds a key head
-  float *delta;
+  // the gradient's workspace: pairs (lse in binary digits, D)
+  // [heads][n_q]; two bounds a key head (float16); the splits' dk and dv
+  float *rows, *part;
   uint32_t *norms;
+  int splits;
 };
+
+// Blocks that share a key tile of the gradient.
+int grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv);
 
 struct PagedArgs {
   const uint16_t *k, *v;

@@ -62,19 +62,22 @@ __global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs
   f32x16 o[DB];
   float m, l;  // the reference of the weights, in scores, and this half's sum
 
+  const int nat0 = nat_place<DP>(), tr0 = tr_place<DP>();
+
   const auto load = [&](uint16_t *k, uint16_t *v, int k0) __attribute__((always_inline)) {
     tile_load<DP, kRowsK, kWaves>(k, kp + k0 * a.k.ts, a.k.ts, sk.count - k0, a.head_dim, wave);
     tile_load<DP, kRowsK, kWaves>(v, vp + k0 * a.v.ts, a.v.ts, sk.count - k0, a.head_dim, wave);
   };
   const auto step = [&](auto careful, const uint16_t *k, const uint16_t *v,
                         int k0) __attribute__((always_inline)) {
+    const int nat = fresh(nat0), tr = fresh(tr0);
     f32x16 x[2];
     x[0] = x[1] = (f32x16)(0.f);
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
-        x[kb] = E::mfma(nat_frag<DP>(k, 32 * kb + r, 2 * s + h), qf[s], x[kb]);
+        x[kb] = E::mfma(nat_frag<DP>(k, nat, 32 * kb, s), qf[s], x[kb]);
     const bool cut = k0 + kRowsK > whole;
     if (cut) {
 #pragma unroll
@@ -132,7 +135,7 @@ __global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs
           const s16x8 pn = __builtin_bit_cast(s16x8, __builtin_bit_cast(u32x4, pf[s]) & only);
 #pragma unroll
           for (int d = 0; d < DB; ++d) {
-            const u32x4 w = __builtin_bit_cast(u32x4, tr_frag<DP>(v, 16 * s, d)) & only;
+            const u32x4 w = __builtin_bit_cast(u32x4, tr_frag<DP>(v, tr, 16 * s, d)) & only;
             const f32x16 with = E::mfma(__builtin_bit_cast(s16x8, w), pn, o[d]);
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = sees ? with[i] : o[d][i];
@@ -142,7 +145,7 @@ __global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs
 #pragma unroll
       for (int s = 0; s < 4; ++s)
 #pragma unroll
-        for (int d = 0; d < DB; ++d) o[d] = E::mfma(tr_frag<DP>(v, 16 * s, d), pf[s], o[d]);
+        for (int d = 0; d < DB; ++d) o[d] = E::mfma(tr_frag<DP>(v, tr, 16 * s, d), pf[s], o[d]);
     }
   };
   // One pass over the keys, two tiles in turn. A weight of 0 times a value that
