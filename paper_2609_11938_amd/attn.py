@@ -15,6 +15,10 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
+import threading
+
+import torch
 
 from . import opattr
 from .opattr import Outputs, Workspace  # noqa: F401  (part of this interface)
@@ -55,6 +59,33 @@ EXPORTS = ("opattr_attn_prompt", "opattr_attn_prompt_grad",
            "opattr_pages_compact_workspace_bytes")
 
 _lib = None
+_call = {}
+
+
+class _Args(threading.local):
+    """The structs of one call, side by side in a buffer of the calling thread's:
+    written by one struct.pack and passed by address, which costs a fraction of
+    building a ctypes Structure for each."""
+
+    def __init__(self, *structs):
+        self.pack_into = struct.Struct("".join(_FORMAT[c] for c in structs)).pack_into
+        self.buf = C.create_string_buffer(sum(C.sizeof(c) for c in structs))
+        at, self.at = C.addressof(self.buf), []
+        for c in structs:
+            self.at.append(at)
+            at += C.sizeof(c)
+
+    def set(self, *values):
+        self.pack_into(self.buf, 0, *values)
+        return self.at
+
+
+_FORMAT = {opattr_rows: "Pqq", opattr_attn_shape: "qqPPiiiiiif4x",
+           opattr_kv_pages: "PPqqqiiPiiiii4x", opattr_page_pool: "PqqiiiiP"}
+_PROMPT = _Args(opattr_attn_shape, *[opattr_rows] * 4)
+_GRAD = _Args(opattr_attn_shape, *[opattr_rows] * 8)
+_PAGED = _Args(opattr_kv_pages, opattr_rows, opattr_rows)
+_POOL = _Args(opattr_page_pool)
 
 
 def library():
@@ -81,8 +112,18 @@ def library():
                                        vp]
     for f in EXPORTS:
         getattr(L, f).restype = sz if f.endswith("_bytes") else C.c_int
+        # the same entry point taking its structs by address
+        _call[f] = L[f]
+        _call[f].restype = getattr(L, f).restype
+        _call[f].argtypes = [vp if isinstance(t, type(rows)) else t for t in getattr(L, f).argtypes]
     _lib = L
     return L
+
+
+def _entry(name):
+    if _lib is None:
+        library()
+    return _call[name]
 
 
 def new_diag(device="cuda:0", stream=None):
@@ -91,78 +132,63 @@ def new_diag(device="cuda:0", stream=None):
 
 
 def _dtype(t):
-    import torch
-
-    if not t.is_cuda:
+    d = t.dtype
+    if t.get_device() < 0:
         raise TypeError("device tensors are taken")
-    if t.dtype is torch.bfloat16:
+    if d is torch.bfloat16:
         return BF16
-    if t.dtype is torch.float16:
+    if d is torch.float16:
         return F16
-    raise TypeError(f"bfloat16 or float16 tensors are taken, not {t.dtype}")
+    raise TypeError(f"bfloat16 or float16 tensors are taken, not {d}")
 
 
-def _rows(t, like, tokens, heads, name):
+def _rows(t, like, shape, name):
     """The opattr_rows of a [tokens, heads, head_dim] tensor of like's type."""
-    if t.dtype is not like.dtype or t.device != like.device:
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
         raise TypeError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
-    d = like.shape[2]
-    if t.shape != (tokens, heads, d):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(tokens, heads, d)}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     ts, hs, es = t.stride()
+    n, heads, d = shape
     if es != 1 and d > 1:
         raise ValueError(f"{name}: the last dimension's values must lie side by side")
-    if tokens <= 1:  # the stride of one row says nothing
-        ts = d
-    if heads == 1:
-        hs = 0
-    return opattr_rows(t.data_ptr(), ts, hs)
+    # the stride of a single row or head says nothing
+    return t.data_ptr(), ts if n > 1 else d, hs if heads > 1 else 0
 
 
-def _int32(t, n, like, name):
-    import torch
-
-    if t.dtype is not torch.int32 or t.device != like.device or not t.is_contiguous():
-        raise TypeError(f"{name}: a contiguous int32 tensor on {like.device} is wanted")
-    if n is not None and t.shape != (n if isinstance(n, tuple) else (n,)):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {n}")
-    return t.data_ptr()
-
-
-def _float32(t, shape, like, name):
-    import torch
-
-    if t.dtype is not torch.float32 or t.device != like.device or not t.is_contiguous():
-        raise TypeError(f"{name}: a contiguous float32 tensor on {like.device} is wanted")
+def _array(t, dtype, like, shape, name):
+    """The address of a contiguous array."""
+    if t.dtype is not dtype or t.get_device() != like.get_device() or not t.is_contiguous():
+        raise TypeError(f"{name}: a contiguous {dtype} tensor on {like.device} is wanted")
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
     return t.data_ptr()
 
 
 def _shape(q, k, cu_q, cu_k, causal, scale):
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("queries and keys are [tokens, heads, head_dim]")
-    n = cu_q.shape[0] - 1
-    if scale is None:
-        scale = 1.0 / math.sqrt(q.shape[2])
-    p = _int32(cu_q, None, q, "cu_q")
-    return opattr_attn_shape(q.shape[0], k.shape[0], p,
-                             p if cu_k is cu_q else _int32(cu_k, n + 1, q, "cu_k"), n,
-                             q.shape[1], k.shape[1], q.shape[2], _dtype(q), 1 if causal else 0,
-                             scale)
+    if q.dim() != 3 or k.dim() != 3 or cu_q.dim() != 1:
+        raise ValueError("queries and keys are [tokens, heads, head_dim], offsets one more than "
+                         "sequences")
+    n_q, heads, d = q.shape
+    n_k, kv_heads, _ = k.shape
+    n = cu_q.shape[0]
+    p = _array(cu_q, torch.int32, q, (n,), "cu_q")
+    return (n_q, n_k, p, p if cu_k is cu_q else _array(cu_k, torch.int32, q, (n,), "cu_k"), n - 1,
+            heads, kv_heads, d, _dtype(q), 1 if causal else 0,
+            1.0 / math.sqrt(d) if scale is None else scale)
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _stream(stream, *made):
-    """The stream's handle. Tensors that a call made itself belong to the
-    current stream: one used on another is kept until that has passed the call."""
-    import torch
-
+def _stream(stream, on, *made):
+    """The stream's handle: the caller's, or the current one of `on`'s device.
+    Tensors that a call made itself belong to the current stream: one used on
+    another is kept until that has passed the call."""
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        # current_stream() builds a Stream object for it: 4 us a call
+        return torch._C._cuda_getCurrentRawStream(on.get_device())
     for t in made:
         t.record_stream(stream)
     return stream.cuda_stream
@@ -174,21 +200,20 @@ def opattr_attn_prompt(q, k, v, cu_q, cu_k=None, causal=True, scale=None, out=No
     q[cu_q[b]:cu_q[b+1]] and keys k[cu_k[b]:cu_k[b+1]] (cu_k None: as cu_q);
     scale None: 1 / sqrt(head_dim). Rows of ``out`` and ``lse`` outside every
     sequence are not written."""
-    import torch
-
-    L = library()
-    cu_k = cu_q if cu_k is None else cu_k
-    a = _shape(q, k, cu_q, cu_k, causal, scale)
+    call = _entry("opattr_attn_prompt")
+    a = _shape(q, k, cu_q, cu_q if cu_k is None else cu_k, causal, scale)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    rows = (a[5], a[0])
     if lse is None:
-        lse = torch.empty((a.n_heads, a.n_q), dtype=torch.float32, device=q.device)
-    rc = L.opattr_attn_prompt(
-        a, _rows(q, q, a.n_q, a.n_heads, "q"), _rows(k, q, a.n_k, a.n_kv_heads, "k"),
-        _rows(v, q, a.n_k, a.n_kv_heads, "v"), _rows(out, q, a.n_q, a.n_heads, "out"),
-        _float32(lse, (a.n_heads, a.n_q), q, "lse"), _ptr(diag),
-        _stream(stream, out, lse))
-    opattr._check(rc, "opattr_attn_prompt")
+        lse = torch.empty(rows, dtype=torch.float32, device=q.device)
+    qs, ks = q.shape, (a[1], a[6], a[7])
+    at = _PROMPT.set(*a, *_rows(q, q, qs, "q"), *_rows(k, q, ks, "k"), *_rows(v, q, ks, "v"),
+                     *_rows(out, q, qs, "out"))
+    rc = call(*at, _array(lse, torch.float32, q, rows, "lse"), _ptr(diag),
+              _stream(stream, q, out, lse))
+    if rc:
+        opattr._check(rc, "opattr_attn_prompt")
     return out, lse
 
 
@@ -197,66 +222,69 @@ def opattr_attn_prompt_grad(dout, q, k, v, out, lse, cu_q, cu_k=None, causal=Tru
                             stream=None):
     """Gradients of sum(out * dout): (dq, dk, dv). out and lse are
     opattr_attn_prompt's for the same inputs."""
-    import torch
-
-    L = library()
-    cu_k = cu_q if cu_k is None else cu_k
-    a = _shape(q, k, cu_q, cu_k, causal, scale)
-    new = [torch.empty(t.shape, dtype=t.dtype, device=t.device) if g is None else g
-           for g, t in ((dq, q), (dk, k), (dv, v))]
-    need = L.opattr_attn_prompt_grad_workspace_bytes(a)
-    buf = (ws or Workspace(q.device)).get(need)
-    rc = L.opattr_attn_prompt_grad(
-        a, _rows(dout, q, a.n_q, a.n_heads, "dout"), _rows(q, q, a.n_q, a.n_heads, "q"),
-        _rows(k, q, a.n_k, a.n_kv_heads, "k"), _rows(v, q, a.n_k, a.n_kv_heads, "v"),
-        _rows(out, q, a.n_q, a.n_heads, "out"), _float32(lse, (a.n_heads, a.n_q), q, "lse"),
-        _rows(new[0], q, a.n_q, a.n_heads, "dq"), _rows(new[1], q, a.n_k, a.n_kv_heads, "dk"),
-        _rows(new[2], q, a.n_k, a.n_kv_heads, "dv"), _ptr(diag), buf.data_ptr(), buf.numel(),
-        _stream(stream, buf, *new))
-    opattr._check(rc, "opattr_attn_prompt_grad")
-    return tuple(new)
+    call, size = _entry("opattr_attn_prompt_grad"), _call["opattr_attn_prompt_grad_workspace_bytes"]
+    a = _shape(q, k, cu_q, cu_q if cu_k is None else cu_k, causal, scale)
+    if dq is None:
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if dk is None:
+        dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    if dv is None:
+        dv = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    qs, ks = q.shape, (a[1], a[6], a[7])
+    at = _GRAD.set(*a, *_rows(dout, q, qs, "dout"), *_rows(q, q, qs, "q"), *_rows(k, q, ks, "k"),
+                   *_rows(v, q, ks, "v"), *_rows(out, q, qs, "out"), *_rows(dq, q, qs, "dq"),
+                   *_rows(dk, q, ks, "dk"), *_rows(dv, q, ks, "dv"))
+    buf = (ws or Workspace(q.device)).get(size(at[0]))
+    rc = call(*at[:6], _array(lse, torch.float32, q, (a[5], a[0]), "lse"), *at[6:], _ptr(diag),
+              buf.data_ptr(), buf.numel(), _stream(stream, q, buf, dq, dk, dv))
+    if rc:
+        opattr._check(rc, "opattr_attn_prompt_grad")
+    return dq, dk, dv
 
 
 def _kv_pages(k_pages, v_pages, table):
-    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or \
-            k_pages.stride() != v_pages.stride() or k_pages.dtype is not v_pages.dtype:
+    """The values of an opattr_kv_pages."""
+    strides = k_pages.stride()
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or strides != v_pages.stride() or \
+            k_pages.dtype is not v_pages.dtype or k_pages.get_device() != v_pages.get_device():
         raise ValueError("k_pages and v_pages are [pages, page_size, kv_heads, head_dim], alike "
                          "in shape, strides and type")
     n, size, heads, d = k_pages.shape
-    ps, ts, hs, es = k_pages.stride()
+    ps, ts, hs, es = strides
     if es != 1 and d > 1:
         raise ValueError("k_pages: the last dimension's values must lie side by side")
     if table.dim() != 2:
         raise ValueError("table is [sequences, entries]")
-    return opattr_kv_pages(k_pages.data_ptr(), v_pages.data_ptr(), ps if n > 1 else 0,
-                           ts if size > 1 else 0, hs if heads > 1 else 0, n, size,
-                           _int32(table, None, k_pages, "table"), table.shape[0], table.shape[1],
-                           heads, d, _dtype(k_pages))
+    b, width = table.shape
+    return (k_pages.data_ptr(), v_pages.data_ptr(), ps if n > 1 else 0, ts if size > 1 else 0,
+            hs if heads > 1 else 0, n, size,
+            _array(table, torch.int32, k_pages, (b, width), "table"), b, width, heads, d,
+            _dtype(k_pages))
 
 
 def opattr_attn_paged(q, k_pages, v_pages, table, lens, scale=None, out=None, lse=None,
                       ws: Workspace | None = None, diag=None, stream=None):
     """Attention of one token a sequence, q [sequences, heads, head_dim], over
     the first lens[b] tokens of each: (out, lse [heads, sequences])."""
-    import torch
-
-    L = library()
+    call, size = _entry("opattr_attn_paged"), _call["opattr_attn_paged_workspace_bytes"]
     c = _kv_pages(k_pages, v_pages, table)
-    b, h = c.n_seqs, q.shape[1]
-    if scale is None:
-        scale = 1.0 / math.sqrt(q.shape[2])
-    if q.dtype is not k_pages.dtype or q.shape[2] != c.head_dim:
-        raise ValueError("q: not of the cache's type and head_dim")
+    b, d = c[8], c[11]
+    if q.dtype is not k_pages.dtype or q.dim() != 3 or q.shape[2] != d:
+        raise ValueError("q: not [sequences, heads, head_dim] of the cache's type")
+    h = q.shape[1]
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if lse is None:
         lse = torch.empty((h, b), dtype=torch.float32, device=q.device)
-    buf = (ws or Workspace(q.device)).get(L.opattr_attn_paged_workspace_bytes(c, h))
-    rc = L.opattr_attn_paged(c, h, _rows(q, q, b, h, "q"), _int32(lens, b, q, "lens"), scale,
-                             _rows(out, q, b, h, "out"), _float32(lse, (h, b), q, "lse"),
-                             _ptr(diag), buf.data_ptr(), buf.numel(),
-                             _stream(stream, buf, out, lse))
-    opattr._check(rc, "opattr_attn_paged")
+    shape = (b, h, d)
+    at = _PAGED.set(*c, *_rows(q, k_pages, shape, "q"), *_rows(out, q, shape, "out"))
+    buf = (ws or Workspace(q.device)).get(size(at[0], h))
+    rc = call(at[0], h, at[1], _array(lens, torch.int32, q, (b,), "lens"),
+              1.0 / math.sqrt(d) if scale is None else scale, at[2],
+              _array(lse, torch.float32, q, (h, b), "lse"), _ptr(diag), buf.data_ptr(),
+              buf.numel(), _stream(stream, q, buf, out, lse))
+    if rc:
+        opattr._check(rc, "opattr_attn_paged")
     return out, lse
 
 
@@ -264,42 +292,41 @@ def opattr_kv_append(k_new, v_new, cu, k_pages, v_pages, table, lens, lens_out=N
                      stream=None):
     """Rows cu[b] .. cu[b+1] of k_new and v_new become the next tokens of
     sequence b, which holds lens[b]; returns the new lengths."""
-    import torch
-
-    L = library()
+    call = _entry("opattr_kv_append")
     c = _kv_pages(k_pages, v_pages, table)
-    n, b = k_new.shape[0], c.n_seqs
-    if k_new.dtype is not k_pages.dtype or k_new.shape[2] != c.head_dim:
-        raise ValueError("k_new: not of the cache's type and head_dim")
+    n, b = k_new.shape[0], c[8]
     if lens_out is None:
         lens_out = torch.empty(b, dtype=torch.int32, device=k_pages.device)
-    rc = L.opattr_kv_append(c, n, _int32(cu, b + 1, k_pages, "cu"),
-                            _rows(k_new, k_new, n, c.n_kv_heads, "k_new"),
-                            _rows(v_new, k_new, n, c.n_kv_heads, "v_new"),
-                            _int32(lens, b, k_pages, "lens"),
-                            _int32(lens_out, b, k_pages, "lens_out"), _ptr(diag),
-                            _stream(stream, lens_out))
-    opattr._check(rc, "opattr_kv_append")
+    shape = (n, c[10], c[11])
+    at = _PAGED.set(*c, *_rows(k_new, k_pages, shape, "k_new"),
+                    *_rows(v_new, k_pages, shape, "v_new"))
+    rc = call(at[0], n, _array(cu, torch.int32, k_pages, (b + 1,), "cu"), at[1], at[2],
+              _array(lens, torch.int32, k_pages, (b,), "lens"),
+              _array(lens_out, torch.int32, k_pages, (b,), "lens_out"), _ptr(diag),
+              _stream(stream, k_pages, lens_out))
+    if rc:
+        opattr._check(rc, "opattr_kv_append")
     return lens_out
 
 
 def _pool(pool, page_size, held):
-    """The opattr_page_pool of a [planes, pages, ...] tensor whose pages lie in
-    one piece each."""
+    """The values of the opattr_page_pool of a [planes, pages, ...] tensor whose
+    pages lie in one piece each."""
     if pool.dim() < 3:
         raise ValueError("pool is [planes, pages, ...]")
-    each = math.prod(pool.shape[2:])
-    inner = 1
-    for n, s in zip(reversed(pool.shape[2:]), reversed(pool.stride()[2:])):
-        if n > 1 and s != inner:
+    if pool.get_device() < 0:
+        raise TypeError("device tensors are taken")
+    shape, strides = pool.shape, pool.stride()
+    each = 1
+    for n, s in zip(shape[:1:-1], strides[:1:-1]):
+        if n > 1 and s != each:
             raise ValueError("a page's values must lie side by side")
-        inner *= n
+        each *= n
     size = pool.element_size()
-    planes, pages = pool.shape[:2]
-    return opattr_page_pool(pool.data_ptr(), pool.stride(0) * size if planes > 1 else 0,
-                            pool.stride(1) * size if pages > 1 else each * size, planes, pages,
-                            each * size, page_size,
-                            None if held is None else _int32(held, pages, pool, "held"))
+    planes, pages = shape[:2]
+    return (pool.data_ptr(), strides[0] * size if planes > 1 else 0,
+            strides[1] * size if pages > 1 else each * size, planes, pages, each * size,
+            page_size, 0 if held is None else _array(held, torch.int32, pool, (pages,), "held"))
 
 
 def opattr_pages_fork(pool, page_size, table, lens, parent, room=None, held=None, table_out=None,
@@ -308,27 +335,30 @@ def opattr_pages_fork(pool, page_size, table, lens, parent, room=None, held=None
     """The next page table: row i continues row parent[i] (-1: empty), with room
     for room[i] tokens. pool [planes, pages, ...] holds the pages that a forked
     row's last, part-filled page is copied in. Returns table, lens and refs."""
-    import torch
-
-    L = library()
-    if table.dim() != 2:
-        raise ValueError("table is [rows, entries]")
+    call, size = _entry("opattr_pages_fork"), _call["opattr_pages_fork_workspace_bytes"]
+    if table.dim() != 2 or parent.dim() != 1:
+        raise ValueError("table is [rows, entries], parent [rows of the next table]")
     p = _pool(pool, page_size, held)
-    rows, width, n = table.shape[0], table.shape[1], parent.shape[0]
+    (rows, width), n, pages = table.shape, parent.shape[0], p[4]
     like = dict(dtype=torch.int32, device=pool.device)
-    table_out = torch.empty((n, width), **like) if table_out is None else table_out
-    lens_out = torch.empty(n, **like) if lens_out is None else lens_out
-    refs = torch.empty(p.n_pages, **like) if refs is None else refs
-    buf = (ws or Workspace(pool.device)).get(
-        L.opattr_pages_fork_workspace_bytes(rows, n, width, p.n_pages))
-    rc = L.opattr_pages_fork(
-        p, _int32(table, None, pool, "table"), _int32(lens, rows, pool, "lens"), rows, width,
-        _int32(parent, n, pool, "parent"),
-        None if room is None else _int32(room, n, pool, "room"), n,
-        _int32(table_out, (n, width), pool, "table_out"), _int32(lens_out, n, pool, "lens_out"),
-        _int32(refs, p.n_pages, pool, "refs"), _ptr(diag), buf.data_ptr(), buf.numel(),
-        _stream(stream, buf, table_out, lens_out, refs))
-    opattr._check(rc, "opattr_pages_fork")
+    if table_out is None:
+        table_out = torch.empty((n, width), **like)
+    if lens_out is None:
+        lens_out = torch.empty(n, **like)
+    if refs is None:
+        refs = torch.empty(pages, **like)
+    buf = (ws or Workspace(pool.device)).get(size(rows, n, width, pages))
+    i32 = torch.int32
+    rc = call(_POOL.set(*p)[0], _array(table, i32, pool, (rows, width), "table"),
+              _array(lens, i32, pool, (rows,), "lens"), rows, width,
+              _array(parent, i32, pool, (n,), "parent"),
+              None if room is None else _array(room, i32, pool, (n,), "room"), n,
+              _array(table_out, i32, pool, (n, width), "table_out"),
+              _array(lens_out, i32, pool, (n,), "lens_out"),
+              _array(refs, i32, pool, (pages,), "refs"), _ptr(diag), buf.data_ptr(), buf.numel(),
+              _stream(stream, pool, buf, table_out, lens_out, refs))
+    if rc:
+        opattr._check(rc, "opattr_pages_fork")
     return Outputs(table=table_out, lens=lens_out, refs=refs)
 
 
@@ -337,23 +367,25 @@ def opattr_pages_compact(pool, table, held=None, table_out=None, moved=None, liv
     """The pages in use moved to the front of the pool. Returns the table with
     their new places, moved (each page's new place, -1: free) and live [1], how
     many are in use."""
-    import torch
-
-    L = library()
+    call, size = _entry("opattr_pages_compact"), _call["opattr_pages_compact_workspace_bytes"]
     if table.dim() != 2:
         raise ValueError("table is [rows, entries]")
     p = _pool(pool, 1, held)
+    (rows, width), pages = table.shape, p[4]
     like = dict(dtype=torch.int32, device=pool.device)
-    table_out = torch.empty(table.shape, **like) if table_out is None else table_out
-    moved = torch.empty(p.n_pages, **like) if moved is None else moved
-    live = torch.empty(1, **like) if live is None else live
-    buf = (ws or Workspace(pool.device)).get(L.opattr_pages_compact_workspace_bytes(p.n_pages))
-    rc = L.opattr_pages_compact(p, _int32(table, None, pool, "table"), table.shape[0],
-                                table.shape[1],
-                                _int32(table_out, tuple(table.shape), pool, "table_out"),
-                                _int32(moved, p.n_pages, pool, "moved"),
-                                _int32(live, 1, pool, "live"), _ptr(diag), buf.data_ptr(),
-                                buf.numel(),
-                                _stream(stream, buf, table_out, moved, live))
-    opattr._check(rc, "opattr_pages_compact")
+    if table_out is None:
+        table_out = torch.empty((rows, width), **like)
+    if moved is None:
+        moved = torch.empty(pages, **like)
+    if live is None:
+        live = torch.empty(1, **like)
+    buf = (ws or Workspace(pool.device)).get(size(pages))
+    i32 = torch.int32
+    rc = call(_POOL.set(*p)[0], _array(table, i32, pool, (rows, width), "table"), rows, width,
+              _array(table_out, i32, pool, (rows, width), "table_out"),
+              _array(moved, i32, pool, (pages,), "moved"), _array(live, i32, pool, (1,), "live"),
+              _ptr(diag), buf.data_ptr(), buf.numel(),
+              _stream(stream, pool, buf, table_out, moved, live))
+    if rc:
+        opattr._check(rc, "opattr_pages_compact")
     return Outputs(table=table_out, moved=moved, live=live)

@@ -5,6 +5,8 @@
 // and its waves take tiles of 32 tokens in turn. Shares are equal but for a
 // sequence's last, of a size that makes about kBlocks blocks of all the work;
 // where a sequence has more than one, a second launch joins them in order.
+#include <limits.h>
+
 #include "attn_dev.h"
 #include "attn_impl.h"
 
@@ -69,12 +71,30 @@ __device__ __forceinline__ int first_share(const PagedArgs &a, int c, int seq) {
   return uniform(sum);
 }
 
-// Results of a share: [items][n_heads][DP + 2]: values, then m and l.
+// A row's result from its values' sum, its weights' sum and reference.
+template <class E>
+__device__ __forceinline__ void paged_store(const PagedArgs &a, int seq, int head, int d, f32x4 v,
+                                            float top, float l) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const u32x2 w = {E::pack(v[0] * inv, v[1] * inv), E::pack(v[2] * inv, v[3] * inv)};
+  if (d < a.head_dim)
+    *reinterpret_cast<u32x2 *>(a.out.p + seq * a.out.ts + (int64_t)head * a.out.hs + d) = w;
+  if (d == 0 && a.lse)
+    a.lse[(int64_t)head * a.n_seqs + seq] =
+        l == 0.f ? -INFINITY : (top + log2f(l) - E::kShift) * kLn2;
+}
+
+// Results of a share: [items][n_heads][DP + 4]: values, then reference and sum of
+// the weights.
 template <class E, int DP>
 __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedArgs a) {
-  constexpr int KS = DP / 32, DB = DP / 16;
-  __shared__ __align__(16) uint16_t tv[kPagedWaves][kTile * DP];
-  __shared__ float so[kPagedWaves][16][DP + 1], sm[kPagedWaves][16], sl[kPagedWaves][16];
+  constexpr int KS = DP / 32, DB = DP / 16, C = DP / 8, N = kTile * C / OPA_WAVE;
+  // each wave's tile of values; at the end the waves' sums
+  __shared__ __align__(16) union {
+    uint16_t v[kPagedWaves][kTile * DP];
+    float o[kPagedWaves][16][DP + 4];
+  } t;
+  __shared__ float sm[kPagedWaves][16], sl[kPagedWaves][16];
   const int lane = lane_id(), wave = uniform(wave_id());
   const int r = lane & 15, g = lane >> 4;
   const int hk = blockIdx.x % a.n_kv, item = blockIdx.x / a.n_kv;
@@ -87,65 +107,99 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedA
   if (threadIdx.x == 0 && part == 0 && hk == 0 && a.lens[seq] != len)
     report(a.diag, OPATTR_F_DATA, 1);
 
+  const uint16_t *qrow = a.q.p + seq * a.q.ts + (int64_t)hk * a.group * a.q.hs;
   s16x8 qf[KS];
-  {
-    const uint16_t *qp = a.q.p + seq * a.q.ts + (int64_t)(hk * a.group + r) * a.q.hs;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      qf[s] = (s16x8)(0);
-      if (r < a.group && 32 * s + 8 * g < a.head_dim)
-        qf[s] = *reinterpret_cast<const s16x8 *>(qp + 32 * s + 8 * g);
-    }
+  for (int s = 0; s < KS; ++s) {
+    qf[s] = (s16x8)(0);
+    if (r < a.group && 32 * s + 8 * g < a.head_dim)
+      qf[s] = *reinterpret_cast<const s16x8 *>(qrow + r * a.q.hs + 32 * s + 8 * g);
   }
   const float c = a.scale * kLog2e;
+  const int mask = (1 << a.shift) - 1, last = a.head_dim / 8 - 1;
   f32x4 o[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) o[d] = (f32x4)(0.f);
   float m = -INFINITY, l = 0.f;
-  const int mask = (1 << a.shift) - 1;
   int bad = 0;
-  for (int k0 = t0 + wave * kTile; k0 < t1; k0 += kTile * kPagedWaves) {
-    // lane t % 32 finds token k0 + t; -1: none
-    int64_t at = -1;
-    {
-      const int tok = k0 + (lane & 31);
-      if (tok < t1) {
-        const int page = table[tok >> a.shift];
-        if (page >= 0 && page < a.n_pages)
-          at = page * a.ps + (tok & mask) * a.ts + (int64_t)hk * a.hs;
-        else if (lane < 32)
-          ++bad;
-      }
-    }
-    // values, a row's chunks side by side, to LDS
-    constexpr int C = DP / 8, N = kTile * C / OPA_WAVE;
-    s16x8 vr[N];
+
+  // The page of token k0 + lane % 32 (kNone past the share's last), and where the
+  // token lies; -1: nowhere. The page is only looked at a tile later: its load
+  // comes after that tile's and would be waited for with them.
+  constexpr int kNone = INT_MIN;
+  const auto page_of = [&](int k0) __attribute__((always_inline)) {
+    const int tok = k0 + (lane & 31);
+    return tok < t1 ? table[tok >> a.shift] : kNone;
+  };
+  const auto place = [&](int page, int k0) __attribute__((always_inline)) {
+    const bool ok = page >= 0 && page < a.n_pages;
+    bad += page != kNone && !ok && lane < 32;
+    const int64_t at = page * a.ps + ((k0 + (lane & 31)) & mask) * a.ts + (int64_t)hk * a.hs;
+    return ok ? at : (int64_t)-1;
+  };
+  // A tile's values (a row's chunks side by side) and keys (as A operands).
+  // Tokens that are not there read the query instead, chunks past head_dim the
+  // last one; neither is used.
+  s16x8 vr[N], kr[2][KS];
+  const auto load = [&](int64_t at) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int id = i * OPA_WAVE + lane;
+      const int id = i * OPA_WAVE + lane, ch = id % C < last ? id % C : last;
       const int64_t p = __shfl(at, id / C);
-      vr[i] = (s16x8)(0);
-      if (p >= 0 && (id % C) * 8 < a.head_dim)
-        vr[i] = *reinterpret_cast<const s16x8 *>(a.v + p + (id % C) * 8);
+      vr[i] = *reinterpret_cast<const s16x8 *>((p >= 0 ? a.v + p : qrow) + ch * 8);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int64_t p = __shfl(at, 16 * u + r);
+      const uint16_t *kp = p >= 0 ? a.k + p : qrow;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const int ch = 4 * s + g < last ? 4 * s + g : last;
+        kr[u][s] = *reinterpret_cast<const s16x8 *>(kp + ch * 8);
+      }
+    }
+  };
+
+  int k0 = t0 + wave * kTile;
+  int64_t at = -1;
+  int next = kNone;
+  if (k0 < t1) {
+    at = place(page_of(k0), k0);
+    load(at);
+    next = page_of(k0 + kTile * kPagedWaves);
+  }
+  for (; k0 < t1; k0 += kTile * kPagedWaves) {
+    const uint64_t there = __ballot(at >= 0);  // the tokens, in both halves
+    if (there != ~0ull) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (!((there >> ((i * OPA_WAVE + lane) / C)) & 1)) vr[i] = (s16x8)(0);
+    }
+    if (a.head_dim < DP) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if ((i * OPA_WAVE + lane) % C > last) vr[i] = (s16x8)(0);
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        if (4 * s + g > last) kr[0][s] = kr[1][s] = (s16x8)(0);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int id = i * OPA_WAVE + lane, row = id / C;
+      *reinterpret_cast<s16x8 *>(&t.v[wave][row * DP + (((id % C) ^ swz<DP>(row)) << 3)]) = vr[i];
     }
     f32x4 x[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int64_t p = __shfl(at, 16 * u + r);
       x[u] = (f32x4)(0.f);
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        s16x8 kf = (s16x8)(0);
-        if (p >= 0 && 32 * s + 8 * g < a.head_dim)
-          kf = *reinterpret_cast<const s16x8 *>(a.k + p + 32 * s + 8 * g);
-        x[u] = E::mfma16(kf, qf[s], x[u]);
-      }
+      for (int s = 0; s < KS; ++s) x[u] = E::mfma16(kr[u][s], qf[s], x[u]);
     }
-    const uint64_t there = __ballot(at >= 0);  // tokens in both halves of the wave
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int id = i * OPA_WAVE + lane, row = id / C;
-      *reinterpret_cast<s16x8 *>(&tv[wave][row * DP + (((id % C) ^ swz<DP>(row)) << 3)]) = vr[i];
+    // the next tile's loads, before this one's softmax; places one tile further
+    if (k0 + kTile * kPagedWaves < t1) {
+      at = place(next, k0 + kTile * kPagedWaves);
+      load(at);
+      next = page_of(k0 + 2 * kTile * kPagedWaves);
     }
     float top = -INFINITY;
 #pragma unroll
@@ -175,13 +229,11 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedA
       }
     l = l * old + sum;
     const s16x8 pf = __builtin_bit_cast(s16x8, w);
-    // the tile's rows were written by this wave
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
       typedef s16x4 __attribute__((address_space(3))) * lds4;
       const int i = lane & 15, row = 4 * g + (i >> 2), col = 16 * d + 4 * (i & 3);
-      const uint16_t *p0 = &tv[wave][row * DP + (((col >> 3) ^ swz<DP>(row)) << 3) + (col & 4)];
+      const uint16_t *p0 = &t.v[wave][row * DP + (((col >> 3) ^ swz<DP>(row)) << 3) + (col & 4)];
       const uint16_t *p1 = p0 + 16 * DP;  // swz repeats every 16 rows
       const s16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p0);
       const s16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p1);
@@ -190,80 +242,91 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedA
       for (int e = 0; e < 4; ++e) o[d][e] *= old;
       o[d] = E::mfma16(vf, pf, o[d]);
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
   if (hk == 0 && bad) report(a.diag, OPATTR_F_DATA, bad);
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
+  __syncthreads();
 #pragma unroll
   for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) so[wave][r][16 * d + 4 * g + e] = o[d][e];
+    *reinterpret_cast<f32x4 *>(&t.o[wave][r][16 * d + 4 * g]) = o[d];
   if (g == 0) {
     sm[wave][r] = m;
     sl[wave][r] = l;
   }
   __syncthreads();
   const bool whole = shares_of(len, share) == 1;
-  for (int i = threadIdx.x; i < a.group * DP; i += kPagedWaves * OPA_WAVE) {
-    const int row = i / DP, d = i % DP, head = hk * a.group + row;
+  for (int i = threadIdx.x; i < a.group * (DP / 4); i += kPagedWaves * OPA_WAVE) {
+    const int row = i / (DP / 4), d = i % (DP / 4) * 4, head = hk * a.group + row;
     float top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kPagedWaves; ++w) top = fmaxf(top, sm[w][row]);
     const float ref = top == -INFINITY ? 0.f : top;
-    float v = 0.f, ls = 0.f;
+    f32x4 v = (f32x4)(0.f);
+    float ls = 0.f;
 #pragma unroll
     for (int w = 0; w < kPagedWaves; ++w) {
       const float f = exp2_fast(sm[w][row] - ref);
-      v = fmaf(so[w][row][d], f, v);
+      v += *reinterpret_cast<const f32x4 *>(&t.o[w][row][d]) * f;
       ls = fmaf(sl[w][row], f, ls);
     }
     if (whole) {
-      const float y = ls == 0.f ? 0.f : v / ls;
-      if (d < a.head_dim)
-        a.out.p[seq * a.out.ts + (int64_t)head * a.out.hs + d] = (uint16_t)E::pack(y, y);
-      if (d == 0 && a.lse)
-        a.lse[(int64_t)head * a.n_seqs + seq] =
-            ls == 0.f ? -INFINITY : (top + log2f(ls) - E::kShift) * kLn2;
+      paged_store<E>(a, seq, head, d, v, top, ls);
     } else {
-      float *p = a.part + ((int64_t)item * a.n_heads + head) * (DP + 2);
-      p[d] = v;
-      if (d == 0) {
-        p[DP] = top;
-        p[DP + 1] = ls;
-      }
+      float *p = a.part + ((int64_t)item * a.n_heads + head) * (DP + 4);
+      *reinterpret_cast<f32x4 *>(p + d) = v;
+      if (d == 0) *reinterpret_cast<f32x4 *>(p + DP) = f32x4{top, ls, 0.f, 0.f};
     }
   }
 }
 
-// A block a sequence and key head: its shares joined in order.
+// A block a sequence and head: its shares joined. The weights' factors first,
+// then the shares in kJoin interleaved runs, each added in order, and the runs
+// in order.
+constexpr int kJoin = 8;
 template <class E, int DP>
-__global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
-  const int hk = blockIdx.x % a.n_kv, seq = blockIdx.x / a.n_kv;
+__global__ __launch_bounds__(kJoin * DP / 4) void k_paged_join(PagedArgs a) {
+  constexpr int kThreads = kJoin * DP / 4;
+  __shared__ float f[kBlocks + 64];  // sized for the most shares of a sequence
+  __shared__ __align__(16) f32x4 sums[kJoin][DP / 4];
+  __shared__ float wave_top[kThreads / OPA_WAVE], run_l[kJoin];
+  const int head = blockIdx.x % a.n_heads, seq = blockIdx.x / a.n_heads;
   const int share = share_size(a);
   const int n = shares_of(uniform(paged_len(a, seq)), share);
   if (n == 1) return;
-  const int first = first_share(a, share, seq);
-  for (int i = threadIdx.x; i < a.group * DP; i += 256) {
-    const int row = i / DP, d = i % DP, head = hk * a.group + row;
-    const int64_t step = (int64_t)a.n_heads * (DP + 2);
-    const float *p = a.part + ((int64_t)first * a.n_heads + head) * (DP + 2);
-    float top = -INFINITY;
-    for (int k = 0; k < n; ++k) top = fmaxf(top, p[k * step + DP]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float v = 0.f, ls = 0.f;
-    for (int k = 0; k < n; ++k) {
-      const float f = exp2_fast(p[k * step + DP] - ref);
-      v = fmaf(p[k * step + d], f, v);
-      ls = fmaf(p[k * step + DP + 1], f, ls);
-    }
-    const float y = ls == 0.f ? 0.f : v / ls;
-    if (d < a.head_dim)
-      a.out.p[seq * a.out.ts + (int64_t)head * a.out.hs + d] = (uint16_t)E::pack(y, y);
-    if (d == 0 && a.lse)
-      a.lse[(int64_t)head * a.n_seqs + seq] =
-          ls == 0.f ? -INFINITY : (top + log2f(ls) - E::kShift) * kLn2;
+  const int64_t step = (int64_t)a.n_heads * (DP + 4);
+  const float *p = a.part + ((int64_t)first_share(a, share, seq) * a.n_heads + head) * (DP + 4);
+  float top = -INFINITY;
+  for (int k = threadIdx.x; k < n; k += kThreads) {
+    f[k] = p[k * step + DP];
+    top = fmaxf(top, f[k]);
   }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane_id() == 0) wave_top[wave_id()] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kThreads / OPA_WAVE; ++w) top = fmaxf(top, wave_top[w]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  const int run = threadIdx.x / (DP / 4), d = threadIdx.x % (DP / 4) * 4;
+  f32x4 v = (f32x4)(0.f);
+  float l = 0.f;
+#pragma unroll 4
+  for (int k = run; k < n; k += kJoin) {
+    const float w = exp2_fast(f[k] - ref);
+    v += *reinterpret_cast<const f32x4 *>(p + k * step + d) * w;
+    l = fmaf(p[k * step + DP + 1], w, l);
+  }
+  sums[run][d / 4] = v;
+  if (d == 0) run_l[run] = l;
+  __syncthreads();
+  if (run) return;
+#pragma unroll
+  for (int k = 1; k < kJoin; ++k) {
+    v += sums[k][d / 4];
+    l += run_l[k];
+  }
+  paged_store<E>(a, seq, head, d, v, top, l);
 }
 
 // Shares at most: sum of ceil(len / c) with c >= kMinShare and c >= sum / (kBlocks
@@ -276,7 +339,7 @@ static int64_t most_items(int n_seqs, int n_kv, int slots) {
 
 size_t paged_workspace(int n_seqs, int n_kv, int n_heads, int slots) {
   if (slots <= kMinShare) return 0;  // no sequence has two shares
-  return (size_t)most_items(n_seqs, n_kv, slots) * n_heads * (128 + 2) * sizeof(float);
+  return (size_t)most_items(n_seqs, n_kv, slots) * n_heads * (128 + 4) * sizeof(float);
 }
 
 template <class E, int DP>
@@ -285,8 +348,8 @@ static void launch(const PagedArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((k_attn_paged<E, DP>), dim3((uint32_t)(items * a.n_kv)),
                      dim3(kPagedWaves * OPA_WAVE), 0, s, a);
   if (a.slots > kMinShare)
-    hipLaunchKernelGGL((k_paged_join<E, DP>), dim3((uint32_t)(a.n_seqs * a.n_kv)), dim3(256), 0,
-                       s, a);
+    hipLaunchKernelGGL((k_paged_join<E, DP>), dim3((uint32_t)(a.n_seqs * a.n_heads)),
+                       dim3(kJoin * DP / 4), 0, s, a);
 }
 
 void run_paged(const PagedArgs &a, int dtype, hipStream_t s) {
