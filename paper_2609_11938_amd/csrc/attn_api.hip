@@ -97,7 +97,10 @@ static bool ok_table(int64_t rows, int64_t width) {
   return rows >= 0 && rows < 1 << 20 && width >= 0 && rows * width < (int64_t)1 << 31;
 }
 
-static int page_blocks(int n_pages) { return (n_pages + kPageBlock - 1) / kPageBlock; }
+// a bit a page, and the set bits before each word and in all
+static size_t bits_bytes(int n_pages) {
+  return align256((size_t)(n_pages / 32 + 1) * 4) + align256((size_t)(n_pages / 32 + 2) * 4);
+}
 
 static PagesArgs pages_args(const opattr_page_pool *p, opattr_diag *diag) {
   PagesArgs a{};
@@ -263,8 +266,7 @@ size_t opattr_pages_fork_workspace_bytes(int32_t n_rows, int32_t n_out, int32_t 
                                          int32_t n_pages) {
   if (!ok_table(n_rows, width) || !ok_table(n_out, width) || n_pages < 0 || n_pages > kMaxPages)
     return 0;
-  return align256((size_t)n_pages * 4) + align256((size_t)page_blocks(n_pages) * 4) +
-         align256(((size_t)n_out + 1) * 4);
+  return bits_bytes(n_pages) + align256(((size_t)n_out + 1) * 4);
 }
 
 int opattr_pages_fork(const opattr_page_pool *p, const int32_t *table, const int32_t *lens,
@@ -290,8 +292,8 @@ int opattr_pages_fork(const opattr_page_pool *p, const int32_t *table, const int
   a.lens_out = lens_out;
   a.refs = refs;
   char *at = static_cast<char *>(ws);
-  a.used = take(at, p->n_pages);
-  a.count = take(at, page_blocks(p->n_pages));
+  a.words = reinterpret_cast<uint32_t *>(take(at, p->n_pages / 32 + 1));
+  a.sums = take(at, p->n_pages / 32 + 2);
   a.row_at = take(at, (size_t)n_out + 1);
   run_fork(a, (hipStream_t)stream);
   return launched();
@@ -299,8 +301,7 @@ int opattr_pages_fork(const opattr_page_pool *p, const int32_t *table, const int
 
 size_t opattr_pages_compact_workspace_bytes(int32_t n_pages) {
   if (n_pages < 0 || n_pages > kMaxPages) return 0;
-  return 3 * align256((size_t)n_pages * 4) + align256((size_t)page_blocks(n_pages) * 4) +
-         align256(8);
+  return bits_bytes(n_pages);
 }
 
 int opattr_pages_compact(const opattr_page_pool *p, const int32_t *table, int32_t n_rows,
@@ -319,11 +320,8 @@ int opattr_pages_compact(const opattr_page_pool *p, const int32_t *table, int32_
   a.moved = moved;
   a.live = live;
   char *at = static_cast<char *>(ws);
-  a.used = take(at, p->n_pages);
-  a.holes = take(at, p->n_pages);
-  a.highs = take(at, p->n_pages);
-  a.count = take(at, page_blocks(p->n_pages));
-  a.total = take(at, 2);
+  a.words = reinterpret_cast<uint32_t *>(take(at, p->n_pages / 32 + 1));
+  a.sums = take(at, p->n_pages / 32 + 2);
   run_compact(a, (hipStream_t)stream);
   return launched();
 }

@@ -56,8 +56,6 @@ struct AppendArgs {
   opattr_diag *diag;
 };
 
-constexpr int kPageBlock = 4096;  // pages a block of the page scans takes
-
 struct PagesArgs {
   char *data;
   int64_t plane, page;  // strides in bytes
@@ -67,8 +65,10 @@ struct PagesArgs {
   int n_rows, width, n_out;
   int32_t *table_out, *lens_out, *refs, *moved, *live;
   opattr_diag *diag;
-  // workspace
-  int32_t *used, *count, *row_at, *holes, *highs, *total;
+  // workspace: a bit a page, the set bits before each word, each row's requests
+  uint32_t *words;
+  int32_t *sums, *row_at;
+  int give, copy_planes;  // blocks that write tables; blocks a row that copy
 };
 
 void run_paged(const PagedArgs &a, int dtype, hipStream_t s);

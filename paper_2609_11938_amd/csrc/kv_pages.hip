@@ -56,13 +56,28 @@ void run_append(const AppendArgs &a, hipStream_t s) {
 }
 
 // --------------------------------------------------------------------------
-// scans over a block of 1024 threads
+// Which pages are in use: a bit each, and the set bits before each word. With
+// both, the pages before one, the r-th free page and the r-th page in use are
+// found by any thread at any time, so that one launch plans, writes the tables
+// and copies, each block for itself. The rest of a call is how the bits come
+// about (kHow):
+//   kSelf   every block sets them in LDS from the table: one launch, for small
+//           tables (8 sequences, 176 entries: a fork of 10 us where five
+//           launches took 20 and their gaps; a table of 160 sequences, 41k
+//           entries, would be 166 KB for every block to read)
+//   kWords  a launch before sets them in memory, each block sums them in LDS
+//   kSums   so does the sum, by a launch of its own: pools past kLdsPages pages
+//           or tables past kLdsRows rows
 // --------------------------------------------------------------------------
-constexpr int kScan = 1024;
+enum { kSelf, kWords, kSums };
+constexpr int kSelfPages = 4096, kSelfEntries = 8192, kSelfRows = 256;
+constexpr int kLdsPages = 65536, kLdsRows = 4096;
+constexpr int kThreads = 256;
 
-// Exclusive sum over the block's threads, and the total. Ends with a barrier
-// before `part` may be used again.
-__device__ __forceinline__ int block_scan(int x, int *part, int &total) {
+// Exclusive sum over the threads of a block of kT, and the total.
+template <int kT>
+__device__ __forceinline__ int block_scan(int x, int &total) {
+  __shared__ int part[kT / OPA_WAVE];
   const int lane = lane_id(), wave = wave_id();
   int inc = x;
 #pragma unroll
@@ -74,7 +89,7 @@ __device__ __forceinline__ int block_scan(int x, int *part, int &total) {
   __syncthreads();
   int before = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < kScan / OPA_WAVE; ++w) {
+  for (int w = 0; w < kT / OPA_WAVE; ++w) {
     const int p = part[w];
     if (w < wave) before += p;
     all += p;
@@ -84,23 +99,99 @@ __device__ __forceinline__ int block_scan(int x, int *part, int &total) {
   return before + inc - x;
 }
 
-// Sum of x over the block, for every thread.
-__device__ __forceinline__ int block_sum(int x, int *part) {
-  int total;
-  block_scan(x, part, total);
-  return total;
+// to[i] = sum of f(0 .. i-1), i = 0 .. n, by a block of kT threads; ends with a
+// barrier. `to` may be where f reads.
+template <int kT, class F>
+__device__ __forceinline__ void prefix(int *to, int n, F f) {
+  int base = 0;
+  for (int i0 = 0; i0 < n; i0 += kT) {
+    const int i = i0 + threadIdx.x;
+    int total;
+    const int at = block_scan<kT>(i < n ? f(i) : 0, total);
+    if (i < n) to[i] = base + at;
+    base += total;
+  }
+  if (threadIdx.x == 0) to[n] = base;
+  __syncthreads();
 }
 
-__global__ void k_pages_zero(int32_t *p, int n) {
-  const int i = blockIdx.x * blockDim.x + threadIdx.x;
-  if (i < n) p[i] = 0;
+struct Bits {
+  const uint32_t *word;  // a set bit: in use, or past the last page
+  const int *sum;        // set bits before each word
+  int words, pages;
+};
+
+__device__ __forceinline__ int words_of(int pages) { return (pages + 31) / 32; }
+// Word w's bits past the last page.
+__device__ __forceinline__ uint32_t past(int w, int pages) {
+  const int n = pages - 32 * w;
+  return n >= 32 ? 0u : ~0u << n;
+}
+__device__ __forceinline__ int free_pages(const Bits &b) { return 32 * b.words - b.sum[b.words]; }
+__device__ __forceinline__ int used_before(const Bits &b, int x) {
+  return x >= 32 * b.words ? b.sum[b.words]
+                           : b.sum[x >> 5] + __popc(b.word[x >> 5] & ((1u << (x & 31)) - 1));
+}
+// The r-th set bit of a word.
+__device__ __forceinline__ int nth_bit(uint32_t w, int r) {
+  for (int k = 0; k < r; ++k) w &= w - 1;
+  return __ffs(w) - 1;
+}
+// The r-th page in use (kSet) or free; there are more than r.
+template <bool kSet>
+__device__ __forceinline__ int nth_page(const Bits &b, int r) {
+  int lo = 0, hi = b.words;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if ((kSet ? b.sum[mid] : 32 * mid - b.sum[mid]) <= r) lo = mid; else hi = mid;
+  }
+  const int before = kSet ? b.sum[lo] : 32 * lo - b.sum[lo];
+  return 32 * lo + nth_bit(kSet ? b.word[lo] : ~b.word[lo], r - before);
+}
+
+__device__ __forceinline__ void set_bit(uint32_t *words, int x) {
+  atomicOr(&words[x >> 5], 1u << (x & 31));
+}
+
+// The words before anything of the table is in: pages held from outside, and
+// bits past the last page.
+__device__ __forceinline__ uint32_t first_word(const PagesArgs &a, int w) {
+  uint32_t v = past(w, a.n_pages);
+  if (a.held)
+    for (int i = 0; i < 32; ++i) {
+      const int x = 32 * w + i;
+      if (x < a.n_pages && a.held[x] > 0) v |= 1u << i;
+    }
+  return v;
+}
+
+__global__ __launch_bounds__(kThreads) void k_pages_start(PagesArgs a) {
+  const int i = blockIdx.x * kThreads + threadIdx.x;
+  if (i < words_of(a.n_pages)) a.words[i] = first_word(a, i);
+  if (a.refs && i < a.n_pages) a.refs[i] = a.held ? a.held[i] : 0;
+}
+
+// kSums: the sums of the words, and the requests before each row.
+__global__ __launch_bounds__(1024) void k_pages_sums(PagesArgs a) {
+  prefix<1024>(a.sums, words_of(a.n_pages), [&](int w) { return __popc(a.words[w]); });
+  if (a.row_at) prefix<1024>(a.row_at, a.n_out, [&](int i) { return a.row_at[i]; });
 }
 
 // Page x of plane l copied to page y, by the block.
 __device__ __forceinline__ void copy_page(const PagesArgs &a, int plane, int x, int y) {
   const u32x4 *from = reinterpret_cast<const u32x4 *>(a.data + plane * a.plane + x * a.page);
   u32x4 *to = reinterpret_cast<u32x4 *>(a.data + plane * a.plane + y * a.page);
-  for (int i = threadIdx.x; i < a.bytes / 16; i += blockDim.x) to[i] = from[i];
+  const int n = a.bytes / 16;
+  int i = threadIdx.x;
+  for (; i + 3 * kThreads < n; i += 4 * kThreads) {
+    const u32x4 w0 = from[i], w1 = from[i + kThreads], w2 = from[i + 2 * kThreads],
+                w3 = from[i + 3 * kThreads];
+    to[i] = w0;
+    to[i + kThreads] = w1;
+    to[i + 2 * kThreads] = w2;
+    to[i + 3 * kThreads] = w3;
+  }
+  for (; i < n; i += kThreads) to[i] = from[i];
 }
 
 // --------------------------------------------------------------------------
@@ -129,145 +220,199 @@ __device__ __forceinline__ ForkRow fork_row(const PagesArgs &a, int i) {
   return r;
 }
 
-// A block a row: the entries it keeps, counted in `used`; row_at[i] = new pages
-// it asks for.
-__global__ __launch_bounds__(256) void k_fork_keep(PagesArgs a) {
+// What of row i is out of range.
+__device__ __forceinline__ int fork_row_bad(const PagesArgs &a, int i, const ForkRow &r) {
+  const int64_t most = (int64_t)a.width * a.size;
+  const int p = a.parent[i];
+  int bad = p < -1 || p >= a.n_rows;
+  if (r.parent >= 0) bad += a.lens[r.parent] < 0 || a.lens[r.parent] > most;
+  if (a.room) bad += a.room[i] > most;
+  return bad;
+}
+
+// A page that row i keeps from its parent; -1: the entry is out of range.
+__device__ __forceinline__ int kept_page(const PagesArgs &a, const ForkRow &r, int slot) {
+  const int id = a.table[(int64_t)r.parent * a.width + slot];
+  return id >= 0 && id < a.n_pages ? id : -1;
+}
+
+// kWords, kSums: a block a row marks what the row keeps and counts it in refs;
+// row_at[i] = the new pages that it asks for.
+__global__ __launch_bounds__(kThreads) void k_fork_keep(PagesArgs a) {
   const int i = blockIdx.x;
   const ForkRow r = fork_row(a, i);
-  __shared__ int earlier;
-  if (threadIdx.x == 0) earlier = 0;
-  __syncthreads();
-  if (r.parent >= 0 && r.part) {
-    bool e = false;
-    for (int j = threadIdx.x; j < i; j += blockDim.x) e |= a.parent[j] == r.parent;
-    if (e) earlier = 1;
-  }
-  __syncthreads();
-  const int kept = r.full + (r.part && !earlier);
+  int e = 0;
+  if (r.part)
+    for (int j = threadIdx.x; j < i; j += kThreads) e |= a.parent[j] == r.parent;
+  const int kept = r.full + (r.part && !__syncthreads_or(e));
   int bad = 0;
-  for (int s = threadIdx.x; s < a.width; s += blockDim.x) {
-    int id = -1;
-    if (s < kept) {
-      id = a.table[(int64_t)r.parent * a.width + s];
-      if (id < 0 || id >= a.n_pages) {
-        id = -1;
-        ++bad;
-      } else {
-        atomicAdd(&a.used[id], 1);
-      }
+  for (int s = threadIdx.x; s < kept; s += kThreads) {
+    const int id = kept_page(a, r, s);
+    if (id < 0) {
+      ++bad;
+      continue;
     }
-    a.table_out[(int64_t)i * a.width + s] = id;
+    set_bit(a.words, id);
+    if (a.refs) atomicAdd(&a.refs[id], 1);
   }
   if (threadIdx.x == 0) {
     a.row_at[i] = r.want - kept;
-    a.lens_out[i] = r.n;
-    const int p = a.parent[i];
-    bad += p < -1 || p >= a.n_rows;
-    if (r.parent >= 0)
-      bad += a.lens[r.parent] < 0 || a.lens[r.parent] > (int64_t)a.width * a.size;
-    if (a.room) bad += a.room[i] > (int64_t)a.width * a.size;
+    bad += fork_row_bad(a, i, r);
   }
   if (bad) report(a.diag, OPATTR_F_DATA, bad);
 }
 
-__device__ __forceinline__ bool is_free(const PagesArgs &a, int x) {
-  return x < a.n_pages && a.used[x] == 0 && !(a.held && a.held[x] > 0);
-}
-
-// Free pages of every block of pages; the last block instead turns row_at into
-// the requests before each row, row_at[n_out] their total.
-__global__ __launch_bounds__(kScan) void k_fork_count(PagesArgs a) {
-  __shared__ int part[kScan / OPA_WAVE];
-  if (blockIdx.x + 1 == gridDim.x) {
-    int base = 0;
-    for (int i0 = 0; i0 < a.n_out; i0 += kScan) {
-      const int i = i0 + threadIdx.x;
-      int total;
-      const int at = block_scan(i < a.n_out ? a.row_at[i] : 0, part, total);
-      if (i < a.n_out) a.row_at[i] = base + at;
-      base += total;
+// Request k of the rows' (row by row) takes the k-th free page. The first
+// a.give blocks write the tables; the others copy: row (block / planes), planes
+// in turn.
+template <int kHow>
+__global__ __launch_bounds__(kThreads) void k_fork(PagesArgs a) {
+  constexpr int kMost = kHow == kSelf ? kSelfPages : kLdsPages;
+  constexpr int kRows = kHow == kSelf ? kSelfRows : kLdsRows;
+  __shared__ uint32_t words[kHow == kSums ? 1 : kMost / 32];
+  __shared__ int sums[kHow == kSums ? 1 : kMost / 32 + 1];
+  __shared__ int rows[kHow == kSums ? 1 : kRows + 1];
+  __shared__ int refs[kHow == kSelf ? kMost : 1];
+  const bool copier = (int)blockIdx.x >= a.give;
+  const int mine = copier ? ((int)blockIdx.x - a.give) / a.copy_planes : 0;
+  if (copier) {  // a row without a part-filled page, or the first of its parent, copies none
+    const ForkRow r = fork_row(a, mine);
+    if (!r.part) return;
+    int e = 0;
+    if (kHow == kSelf) {
+      for (int j = threadIdx.x; j < mine; j += kThreads) e |= a.parent[j] == r.parent;
+      e = __syncthreads_or(e);
+    } else {
+      const int asks = kHow == kSums ? a.row_at[mine + 1] - a.row_at[mine] : a.row_at[mine];
+      e = r.want - asks == r.full;
     }
-    if (threadIdx.x == 0) a.row_at[a.n_out] = base;
+    if (!e) return;
+  }
+  const int nw = words_of(a.n_pages);
+  Bits b{words, sums, nw, a.n_pages};
+  const int *row_at = rows;
+  const bool count = kHow == kSelf && blockIdx.x == 0;
+  if (kHow == kSums) {
+    b.word = a.words;
+    b.sum = a.sums;
+    row_at = a.row_at;
+  } else {
+    if (kHow == kSelf) {
+      for (int w = threadIdx.x; w < nw; w += kThreads) words[w] = first_word(a, w);
+      if (count)
+        for (int x = threadIdx.x; x < a.n_pages; x += kThreads) refs[x] = a.held ? a.held[x] : 0;
+      for (int i = threadIdx.x; i < a.n_out; i += kThreads) {
+        const ForkRow r = fork_row(a, i);
+        bool e = false;
+        if (r.part)
+          for (int j = 0; j < i; ++j) e |= a.parent[j] == r.parent;
+        rows[i] = r.want - r.full - (r.part && !e);
+        if (count) {
+          const int bad = fork_row_bad(a, i, r);
+          if (bad) report(a.diag, OPATTR_F_DATA, bad);
+        }
+      }
+      __syncthreads();
+      int bad = 0;
+      for (int i = threadIdx.x / OPA_WAVE; i < a.n_out; i += kThreads / OPA_WAVE) {
+        const ForkRow r = fork_row(a, i);
+        for (int s = lane_id(); s < r.want - rows[i]; s += OPA_WAVE) {
+          const int id = kept_page(a, r, s);
+          if (id < 0) {
+            ++bad;
+            continue;
+          }
+          set_bit(words, id);
+          if (count) atomicAdd(&refs[id], 1);
+        }
+      }
+      if (count && bad) report(a.diag, OPATTR_F_DATA, bad);
+    } else {
+      for (int w = threadIdx.x; w < nw; w += kThreads) words[w] = a.words[w];
+    }
+    __syncthreads();
+    prefix<kThreads>(sums, nw, [&](int w) { return __popc(words[w]); });
+    prefix<kThreads>(rows, a.n_out, [&](int i) { return kHow == kSelf ? rows[i] : a.row_at[i]; });
+  }
+  const int free = free_pages(b), wanted = row_at[a.n_out];
+  if (copier) {
+    const ForkRow r = fork_row(a, mine);
+    if (row_at[mine] >= free) return;
+    const int x = kept_page(a, r, r.full), y = nth_page<false>(b, row_at[mine]);
+    if (x < 0) return;
+    for (int l = ((int)blockIdx.x - a.give) % a.copy_planes; l < a.n_planes; l += a.copy_planes)
+      copy_page(a, l, x, y);
     return;
   }
-  int n = 0;
-  for (int j = 0; j < kPageBlock / kScan; ++j)
-    n += is_free(a, blockIdx.x * kPageBlock + j * kScan + threadIdx.x);
-  n = block_sum(n, part);
-  if (threadIdx.x == 0) a.count[blockIdx.x] = n;
-}
-
-// The free page of rank r answers request r. Requests past the free pages stay
-// -1; a row whose copy is among them ends at its full pages.
-__global__ __launch_bounds__(kScan) void k_fork_give(PagesArgs a) {
-  __shared__ int part[kScan / OPA_WAVE];
-  int before = 0;
-  for (int j = threadIdx.x; j < (int)blockIdx.x; j += kScan) before += a.count[j];
-  before = block_sum(before, part);
-  const int wanted = a.row_at[a.n_out];
-  for (int j = 0; j < kPageBlock / kScan; ++j) {
-    const int x = blockIdx.x * kPageBlock + j * kScan + threadIdx.x;
-    const bool f = is_free(a, x);
-    int total;
-    const int rank = before + block_scan(f, part, total);
-    before += total;
-    const bool give = f && rank < wanted;
-    if (give) {
-      int lo = 0, hi = a.n_out;  // the last row with row_at <= rank
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.row_at[mid] <= rank) lo = mid; else hi = mid;
-      }
-      const ForkRow r = fork_row(a, lo);
-      const int slot = r.want - (a.row_at[lo + 1] - a.row_at[lo]) + rank - a.row_at[lo];
-      a.table_out[(int64_t)lo * a.width + slot] = x;
-    }
-    if (a.refs && x < a.n_pages) a.refs[x] = a.used[x] + (a.held ? a.held[x] : 0) + give;
+  const int64_t step = (int64_t)a.give * kThreads;
+  const int64_t from = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  for (int64_t at = from; at < (int64_t)a.n_out * a.width; at += step) {
+    const int i = (int)(at / a.width), s = (int)(at - (int64_t)i * a.width);
+    const ForkRow r = fork_row(a, i);
+    const int kept = r.want - (row_at[i + 1] - row_at[i]), k = row_at[i] + s - kept;
+    a.table_out[at] = s < kept                  ? kept_page(a, r, s)
+                      : s < r.want && k < free ? nth_page<false>(b, k)
+                                               : -1;
   }
-  if (blockIdx.x + 1 == gridDim.x && before < wanted) {
-    for (int i = threadIdx.x; i < a.n_out; i += kScan) {
-      const ForkRow r = fork_row(a, i);
-      const bool copy = r.part && r.want - (a.row_at[i + 1] - a.row_at[i]) == r.full;
-      if (copy && a.row_at[i] >= before) a.lens_out[i] = r.full * a.size;
-    }
-    if (threadIdx.x == 0) report(a.diag, OPATTR_F_LIMIT, wanted - before);
+  for (int64_t i = from; i < a.n_out; i += step) {
+    const ForkRow r = fork_row(a, (int)i);
+    const bool copy = r.part && r.want - (row_at[i + 1] - row_at[i]) == r.full;
+    a.lens_out[i] = copy && row_at[i] >= free ? r.full * a.size : r.n;
   }
+  if (a.refs && kHow != kSelf)  // a page given has no other reference
+    for (int64_t k = from; k < wanted && k < free; k += step) a.refs[nth_page<false>(b, (int)k)] = 1;
+  if (a.refs && count) {
+    for (int x = threadIdx.x; x < a.n_pages; x += kThreads) {
+      const bool f = !((words[x >> 5] >> (x & 31)) & 1);
+      a.refs[x] = f ? x - used_before(b, x) < wanted : refs[x];
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0 && wanted > free)
+    report(a.diag, OPATTR_F_LIMIT, wanted - free);
 }
 
-__global__ __launch_bounds__(256) void k_fork_copy(PagesArgs a) {
-  const int i = blockIdx.x;
-  const ForkRow r = fork_row(a, i);
-  if (!r.part || r.want - (a.row_at[i + 1] - a.row_at[i]) != r.full) return;
-  const int x = a.table[(int64_t)r.parent * a.width + r.full];
-  const int y = a.table_out[(int64_t)i * a.width + r.full];
-  if (x < 0 || x >= a.n_pages || y < 0) return;
-  for (int l = blockIdx.y; l < a.n_planes; l += gridDim.y) copy_page(a, l, x, y);
+static int blocks_for(int64_t n, int most) {
+  const int64_t b = (n + kThreads - 1) / kThreads;
+  return b < 1 ? 1 : b > most ? most : (int)b;
 }
 
-void run_fork(const PagesArgs &a, hipStream_t s) {
-  const int blocks = (a.n_pages + kPageBlock - 1) / kPageBlock;
-  if (a.n_pages > 0)
-    hipLaunchKernelGGL(k_pages_zero, dim3((a.n_pages + 255) / 256), dim3(256), 0, s, a.used,
-                       a.n_pages);
-  if (a.n_out > 0) hipLaunchKernelGGL(k_fork_keep, dim3(a.n_out), dim3(256), 0, s, a);
-  hipLaunchKernelGGL(k_fork_count, dim3(blocks + 1), dim3(kScan), 0, s, a);
-  hipLaunchKernelGGL(k_fork_give, dim3(blocks > 0 ? blocks : 1), dim3(kScan), 0, s, a);
-  if (a.n_out > 0 && a.n_planes > 0 && a.n_pages > 0)
-    hipLaunchKernelGGL(k_fork_copy, dim3(a.n_out, a.n_planes < 256 ? a.n_planes : 256),
-                       dim3(256), 0, s, a);
+void run_fork(const PagesArgs &args, hipStream_t s) {
+  PagesArgs a = args;
+  const int64_t entries = (int64_t)a.n_out * a.width;
+  if (a.n_out == 0 && !a.refs) return;
+  const bool self = a.n_pages <= kSelfPages && a.n_out <= kSelfRows && entries <= kSelfEntries;
+  const bool lds = a.n_pages <= kLdsPages && a.n_out <= kLdsRows;
+  // a table writer's setup is worth some entries; planes are shared out so that
+  // a copy of many pages is many blocks, and its setup is paid a few times only
+  a.give = blocks_for(entries / (self ? 2 : 4), self ? 16 : 256);
+  a.copy_planes = a.n_planes < 32 ? a.n_planes : 32;
+  const int64_t blocks = a.give + (a.n_pages > 0 ? (int64_t)a.n_out * a.copy_planes : 0);
+  if (!self) {
+    hipLaunchKernelGGL(k_pages_start, dim3((a.n_pages + kThreads) / kThreads), dim3(kThreads), 0,
+                       s, a);
+    if (a.n_out > 0) hipLaunchKernelGGL(k_fork_keep, dim3(a.n_out), dim3(kThreads), 0, s, a);
+    if (!lds) hipLaunchKernelGGL(k_pages_sums, dim3(1), dim3(1024), 0, s, a);
+  }
+  const dim3 grid((uint32_t)blocks), block(kThreads);
+  if (self)
+    hipLaunchKernelGGL(k_fork<kSelf>, grid, block, 0, s, a);
+  else if (lds)
+    hipLaunchKernelGGL(k_fork<kWords>, grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL(k_fork<kSums>, grid, block, 0, s, a);
 }
 
 // --------------------------------------------------------------------------
 // compact
 // --------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void k_compact_mark(PagesArgs a) {
-  const int64_t n = (int64_t)a.n_rows * a.width;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+// kWords, kSums: the pages that the table names.
+__global__ __launch_bounds__(kThreads) void k_compact_mark(PagesArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   bool bad = false;
-  if (i < n) {
+  if (i < (int64_t)a.n_rows * a.width) {
     const int id = a.table[i];
     if (id >= 0 && id < a.n_pages)
-      a.used[id] = 1;
+      set_bit(a.words, id);
     else
       bad = id != -1;
   }
@@ -275,103 +420,78 @@ __global__ __launch_bounds__(256) void k_compact_mark(PagesArgs a) {
   if (wrong && lane_id() == 0) report(a.diag, OPATTR_F_DATA, wrong);
 }
 
-__device__ __forceinline__ bool in_use(const PagesArgs &a, int x) {
-  return x < a.n_pages && (a.used[x] != 0 || (a.held && a.held[x] > 0));
-}
-
-__global__ __launch_bounds__(kScan) void k_compact_count(PagesArgs a) {
-  __shared__ int part[kScan / OPA_WAVE];
-  int n = 0;
-  for (int j = 0; j < kPageBlock / kScan; ++j)
-    n += in_use(a, blockIdx.x * kPageBlock + j * kScan + threadIdx.x);
-  n = block_sum(n, part);
-  if (threadIdx.x == 0) a.count[blockIdx.x] = n;
-}
-
-// m pages are in use. holes[j]: the j-th free page below m; highs[j]: the j-th
-// page in use at or above m; there are as many of one as of the other. moved of
-// a high page is its j for now.
-__global__ __launch_bounds__(kScan) void k_compact_list(PagesArgs a) {
-  __shared__ int part[kScan / OPA_WAVE];
-  const int blocks = gridDim.x;
-  int before = 0, all = 0;
-  for (int j = threadIdx.x; j < blocks; j += kScan) {
-    const int c = a.count[j];
-    all += c;
-    if (j < (int)blockIdx.x) before += c;
-  }
-  const int m = block_sum(all, part);
-  before = block_sum(before, part);
-  // pages in use below m: the blocks before m's, and the part of that block
-  int low = 0;
-  const int mb = m / kPageBlock;
-  for (int j = threadIdx.x; j < mb; j += kScan) low += a.count[j];
-  for (int x = mb * kPageBlock + threadIdx.x; x < m; x += kScan) low += in_use(a, x);
-  low = block_sum(low, part);
-  for (int j = 0; j < kPageBlock / kScan; ++j) {
-    const int x = blockIdx.x * kPageBlock + j * kScan + threadIdx.x;
-    const bool u = in_use(a, x);
-    int total;
-    const int at = before + block_scan(u, part, total);
-    before += total;
-    if (x >= a.n_pages) continue;
-    if (u) {
-      a.moved[x] = x < m ? x : at - low;
-      if (x >= m) a.highs[at - low] = x;
+// m pages are in use. The j-th of those at or above m takes the j-th free place
+// below m; there are as many of one as of the other.
+template <int kHow>
+__global__ __launch_bounds__(kThreads) void k_compact(PagesArgs a) {
+  constexpr int kMost = kHow == kSelf ? kSelfPages : kLdsPages;
+  __shared__ uint32_t words[kHow == kSums ? 1 : kMost / 32];
+  __shared__ int sums[kHow == kSums ? 1 : kMost / 32 + 1];
+  const int nw = words_of(a.n_pages);
+  const int64_t entries = (int64_t)a.n_rows * a.width;
+  Bits b{words, sums, nw, a.n_pages};
+  if (kHow == kSums) {
+    b.word = a.words;
+    b.sum = a.sums;
+  } else {
+    if (kHow == kSelf) {
+      for (int w = threadIdx.x; w < nw; w += kThreads) words[w] = first_word(a, w);
+      __syncthreads();
+      int bad = 0;
+      for (int i = threadIdx.x; i < entries; i += kThreads) {
+        const int id = a.table[i];
+        if (id >= 0 && id < a.n_pages)
+          set_bit(words, id);
+        else
+          bad += id != -1;
+      }
+      if (blockIdx.x == 0 && bad) report(a.diag, OPATTR_F_DATA, bad);
     } else {
-      a.moved[x] = -1;
-      if (x < m) a.holes[x - at] = x;
+      for (int w = threadIdx.x; w < nw; w += kThreads) words[w] = a.words[w];
     }
+    __syncthreads();
+    prefix<kThreads>(sums, nw, [&](int w) { return __popc(words[w]); });
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    a.total[0] = m;
-    a.total[1] = m - low;
-    if (a.live) *a.live = m;
-  }
-}
-
-// Page moves, then entries of the table and of `moved` of the high pages.
-__global__ __launch_bounds__(256) void k_compact_move(PagesArgs a) {
-  const int m = a.total[0], n = a.total[1];
+  const int m = a.n_pages - free_pages(b), low = used_before(b, m), n = m - low;
+  const auto place = [&](int x) {
+    return x < m ? x : nth_page<false>(b, used_before(b, x) - low);
+  };
   const int64_t jobs = (int64_t)n * a.n_planes;
   for (int64_t j = blockIdx.x; j < jobs; j += gridDim.x) {
     const int at = (int)(j / a.n_planes), plane = (int)(j - (int64_t)at * a.n_planes);
-    copy_page(a, plane, a.highs[at], a.holes[at]);
+    copy_page(a, plane, nth_page<true>(b, low + at), nth_page<false>(b, at));
   }
-  const int64_t entries = (int64_t)a.n_rows * a.width, step = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < entries; i += step) {
+  const int64_t step = (int64_t)gridDim.x * kThreads;
+  const int64_t from = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  for (int64_t i = from; i < entries; i += step) {
     const int id = a.table[i];
-    int to = -1;
-    if (id >= 0 && id < a.n_pages) {
-      to = id;
-      if (id >= m) {  // its place in `highs`
-        int lo = 0, hi = n;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (a.highs[mid] <= id) lo = mid; else hi = mid;
-        }
-        to = a.holes[lo];
-      }
-    }
-    a.table_out[i] = to;
+    a.table_out[i] = id >= 0 && id < a.n_pages ? place(id) : -1;
   }
-  for (int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x; j < n; j += step)
-    a.moved[a.highs[j]] = a.holes[j];
+  for (int64_t x = from; x < a.n_pages; x += step)
+    a.moved[x] = (b.word[x >> 5] >> (x & 31)) & 1 ? place((int)x) : -1;
+  if (a.live && blockIdx.x == 0 && threadIdx.x == 0) *a.live = m;
 }
 
 void run_compact(const PagesArgs &a, hipStream_t s) {
-  const int blocks = (a.n_pages + kPageBlock - 1) / kPageBlock;
   const int64_t entries = (int64_t)a.n_rows * a.width;
-  if (a.n_pages > 0)
-    hipLaunchKernelGGL(k_pages_zero, dim3((a.n_pages + 255) / 256), dim3(256), 0, s, a.used,
-                       a.n_pages);
-  if (entries > 0)
-    hipLaunchKernelGGL(k_compact_mark, dim3((uint32_t)((entries + 255) / 256)), dim3(256), 0, s,
-                       a);
-  if (a.n_pages > 0)
-    hipLaunchKernelGGL(k_compact_count, dim3(blocks), dim3(kScan), 0, s, a);
-  hipLaunchKernelGGL(k_compact_list, dim3(blocks > 0 ? blocks : 1), dim3(kScan), 0, s, a);
-  hipLaunchKernelGGL(k_compact_move, dim3(2048), dim3(256), 0, s, a);
+  // in place, no block may read the table after another has written it
+  const bool self = a.n_pages <= kSelfPages && entries <= kSelfEntries && a.table_out != a.table;
+  const bool lds = a.n_pages <= kLdsPages;
+  if (!self) {
+    hipLaunchKernelGGL(k_pages_start, dim3((a.n_pages + kThreads) / kThreads), dim3(kThreads), 0,
+                       s, a);
+    if (entries > 0)
+      hipLaunchKernelGGL(k_compact_mark, dim3((uint32_t)((entries + kThreads - 1) / kThreads)),
+                         dim3(kThreads), 0, s, a);
+    if (!lds) hipLaunchKernelGGL(k_pages_sums, dim3(1), dim3(1024), 0, s, a);
+  }
+  const dim3 block(kThreads);
+  if (self)
+    hipLaunchKernelGGL(k_compact<kSelf>, dim3(512), block, 0, s, a);
+  else if (lds)
+    hipLaunchKernelGGL(k_compact<kWords>, dim3(2048), block, 0, s, a);
+  else
+    hipLaunchKernelGGL(k_compact<kSums>, dim3(2048), block, 0, s, a);
 }
 
 }  // namespace opa

@@ -500,7 +500,9 @@ def _turn(rng, rows, n_out, width, page, pages, held_some=False, planes=3, each=
 
 
 TURNS = [(1, 1, 3, 16, 10), (5, 7, 6, 16, 60), (8, 3, 5, 1, 64), (40, 60, 9, 4, 700),
-         (300, 500, 12, 8, 9000), (0, 3, 4, 8, 30), (4, 0, 4, 8, 30), (3, 5, 70, 32, 300)]
+         (300, 500, 12, 8, 9000), (0, 3, 4, 8, 30), (4, 0, 4, 8, 30), (3, 5, 70, 32, 300),
+         (250, 256, 32, 2, 4096), (20, 30, 60, 4, 70_001), (100, 5000, 3, 4, 9000),
+         (2, 2, 3, 16, 31), (2, 2, 3, 16, 32), (7, 9, 1, 16, 33)]
 
 
 @pytest.mark.parametrize("held", [False, True])
