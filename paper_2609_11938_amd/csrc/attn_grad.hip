@@ -213,17 +213,22 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs
     }
   };
   if (tiles > 0) load(tk0, tv0, 0);
-  for (int t = 0; t < tiles; t += 2) {
-    const int k0 = t * kStepK;
+  int k0 = 0;
+  for (int t = 1; t < tiles; t += 2) {
     wait_loads();
     block_sync();
-    if (t + 1 < tiles) load(tk1, tv1, k0 + kStepK);
+    load(tk1, tv1, k0 + kStepK);
     step(tk0, tv0, k0);
-    if (t + 1 >= tiles) break;
     wait_loads();
     block_sync();
-    if (t + 2 < tiles) load(tk0, tv0, k0 + 2 * kStepK);
+    load(tk0, tv0, k0 + 2 * kStepK);  // (past the last: zeros)
     step(tk1, tv1, k0 + kStepK);
+    k0 += 2 * kStepK;
+  }
+  wait_loads();
+  if (tiles & 1) {
+    block_sync();
+    step(tk0, tv0, k0);
   }
   exact = half_sum(exact);
   if (!live) return;

@@ -148,37 +148,53 @@ __global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs
         for (int d = 0; d < DB; ++d) o[d] = E::mfma(tr_frag<DP>(v, tr, 16 * s, d), pf[s], o[d]);
     }
   };
-  // One pass over the keys, two tiles in turn. A weight of 0 times a value that
-  // is not finite is no 0: the careful pass adds the values of a tile that not
-  // every query of the wave sees key by key, and only to the queries that see
-  // the key.
-  const auto pass = [&](auto careful) __attribute__((always_inline)) {
+  const auto start = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = (f32x16)(0.f);
     m = -INFINITY;
     l = 0.f;
-    if (tiles > 0) load(tk0, tv0, 0);
-    for (int t = 0; t < tiles; t += 2) {
-      const int k0 = t * kRowsK;
-      wait_loads();
-      block_sync();
-      if (t + 1 < tiles) load(tk1, tv1, k0 + kRowsK);
-      step(careful, tk0, tv0, k0);
-      if (t + 1 >= tiles) break;
-      wait_loads();
-      block_sync();
-      if (t + 2 < tiles) load(tk0, tv0, k0 + 2 * kRowsK);
-      step(careful, tk1, tv1, k0 + kRowsK);
-    }
   };
-  pass(std::false_type{});
+  // Two tiles in turn, the next one's loads in flight. No branch leaves the loop
+  // between them: that would cost copies of o.
+  const std::false_type fast;
+  start();
+  if (tiles > 0) load(tk0, tv0, 0);
+  int k0 = 0;
+  for (int t = 1; t < tiles; t += 2) {
+    wait_loads();
+    block_sync();
+    load(tk1, tv1, k0 + kRowsK);
+    step(fast, tk0, tv0, k0);
+    wait_loads();
+    block_sync();
+    load(tk0, tv0, k0 + 2 * kRowsK);  // (past the last: zeros)
+    step(fast, tk1, tv1, k0 + kRowsK);
+    k0 += 2 * kRowsK;
+  }
+  wait_loads();
+  if (tiles & 1) {
+    block_sync();
+    step(fast, tk0, tv0, k0);
+  }
+  // A weight of 0 times a value that is not finite is no 0: where a sum is not
+  // finite, a second pass adds the values of a tile that not every query of the
+  // wave sees key by key, and only to the queries that see the key.
   if (a.causal) {
     float zero = 0.f;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) zero = fmaf(o[d][i], 0.f, zero);
-    if (__syncthreads_or(!(zero == 0.f))) pass(std::true_type{});
+    if (__syncthreads_or(!(zero == 0.f))) {
+      start();
+      for (int t = 0; t < tiles; ++t) {
+        load(tk0, tv0, t * kRowsK);
+        wait_loads();
+        block_sync();
+        step(std::true_type{}, tk0, tv0, t * kRowsK);
+        block_sync();
+      }
+    }
   }
   l = half_sum(l);
   if (!live) return;
