@@ -13,6 +13,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/opattr_attn.h"
 #include "common.h"
 
@@ -196,6 +198,36 @@ __device__ __forceinline__ void block_sync() {
   __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
+}
+
+// Tiles 0 .. n-1 through two buffers in turn, the next one's loads in flight
+// while one is worked on. load(i, t) starts the loads of tile t into buffer i
+// (tiles past the last too: they give zeros), step(i, t) works on it. No branch
+// leaves the loop between steps: that would cost copies of the accumulators.
+// Ends with no load in flight. (A third buffer changed nothing: 12 packed
+// documents' gradient, 1 sequence of 512 a head.)
+template <class Load, class Step>
+__device__ __forceinline__ void run_tiles(int n, const Load &load, const Step &step) {
+  const std::integral_constant<int, 0> b0;
+  const std::integral_constant<int, 1> b1;
+  if (n <= 0) return;
+  load(b0, 0);
+  int t = 0;
+  for (; t + 1 < n; t += 2) {
+    wait_loads();
+    block_sync();
+    load(b1, t + 1);
+    step(b0, t);
+    wait_loads();
+    block_sync();
+    load(b0, t + 2);
+    step(b1, t + 1);
+  }
+  wait_loads();
+  if (t < n) {
+    block_sync();
+    step(b0, t);
+  }
 }
 
 // --------------------------------------------------------------------------

@@ -11,8 +11,6 @@
 // Nine products where seven are needed (with the forward pass), because the
 // scores and dp are computed by both passes: the other way, adding dq in the
 // second pass, needs float32 atomics, whose order changes the result.
-#include <type_traits>
-
 #include "attn_dev.h"
 #include "attn_impl.h"
 
@@ -20,8 +18,8 @@ namespace opa {
 
 constexpr int kGradWaves = 4;
 constexpr int kHeld = 32 * kGradWaves;  // keys (queries) a block holds
-constexpr int kStepK = 64;              // keys a tile of the first pass
-constexpr int kStepQ = 32;              // queries a tile of the second pass
+// Keys a tile of the first pass, queries a tile of the second. Registers hold the scores of 32 at a time of head_dim 128.
+constexpr int kStep(int dp) { return dp <= 64 ? 64 : 32; }
 
 // Weights and their gradients are rounded to 16 bits for the products. For
 // float16 both are scaled by powers of two first: the weights by 2^kWeight, and
@@ -95,8 +93,8 @@ __global__ void k_attn_zero(uint32_t *p, int n) {
 template <class E, int DP>
 __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
-  __shared__ __align__(16) uint16_t tk0[kStepK * DP], tk1[kStepK * DP];
-  __shared__ __align__(16) uint16_t tv0[kStepK * DP], tv1[kStepK * DP];
+  constexpr int kStepK = kStep(DP), kTile = kStepK * DP;
+  __shared__ __align__(16) uint16_t tk0[kTile], tk1[kTile], tv0[kTile], tv1[kTile];
   const int lane = lane_id(), wave = uniform(wave_id());
   const int r = lane & 31, h = lane >> 5;
   int id = blockIdx.x;
@@ -168,7 +166,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs
     const bool cut = k0 + kStepK > whole;
     const int nat = fresh(nat0), tr = fresh(tr0);
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int kb = 0; kb < kStepK / 32; ++kb) {
       f32x16 x = (f32x16)(0.f), y = (f32x16)(0.f);
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
@@ -212,24 +210,14 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs
       }
     }
   };
-  if (tiles > 0) load(tk0, tv0, 0);
-  int k0 = 0;
-  for (int t = 1; t < tiles; t += 2) {
-    wait_loads();
-    block_sync();
-    load(tk1, tv1, k0 + kStepK);
-    step(tk0, tv0, k0);
-    wait_loads();
-    block_sync();
-    load(tk0, tv0, k0 + 2 * kStepK);  // (past the last: zeros)
-    step(tk1, tv1, k0 + kStepK);
-    k0 += 2 * kStepK;
-  }
-  wait_loads();
-  if (tiles & 1) {
-    block_sync();
-    step(tk0, tv0, k0);
-  }
+  run_tiles(
+      tiles,
+      [&](auto i, int t) __attribute__((always_inline)) {
+        load(i == 0 ? tk0 : tk1, i == 0 ? tv0 : tv1, t * kStepK);
+      },
+      [&](auto i, int t) __attribute__((always_inline)) {
+        step(i == 0 ? tk0 : tk1, i == 0 ? tv0 : tv1, t * kStepK);
+      });
   exact = half_sum(exact);
   if (!live) return;
   if (h == 0) {
@@ -249,10 +237,9 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs
     }
 }
 
-// kStepQ pairs (lse, D) from p to LDS, past `left` of them zero; by one wave.
+// 32 pairs (lse, D) from p to LDS, past `left` of them zero; by a whole wave.
 __device__ __forceinline__ void row_load(float *to, const float *p, int left) {
-  static_assert(2 * kStepQ == OPA_WAVE, "a float a lane");
-  const int n = left < 0 ? 0 : left > kStepQ ? kStepQ : left;
+  const int n = left < 0 ? 0 : left > 32 ? 32 : left;
   const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<float *>(reinterpret_cast<const float *>(
           uniform(reinterpret_cast<const uint16_t *>(p)))),
@@ -267,8 +254,8 @@ __device__ __forceinline__ void row_load(float *to, const float *p, int left) {
 template <class E, int DP>
 __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
-  __shared__ __align__(16) uint16_t tq0[kStepQ * DP], tq1[kStepQ * DP];
-  __shared__ __align__(16) uint16_t td0[kStepQ * DP], td1[kStepQ * DP];
+  constexpr int kStepQ = kStep(DP), kTile = kStepQ * DP, kQB = kStepQ / 32;
+  __shared__ __align__(16) uint16_t tq0[kTile], tq1[kTile], td0[kTile], td1[kTile];
   __shared__ __align__(16) float ts0[2 * kStepQ], ts1[2 * kStepQ];
   const int lane = lane_id(), wave = uniform(wave_id());
   const int r = lane & 31, h = lane >> 5;
@@ -330,64 +317,65 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
     tile_load<DP, kStepQ, kGradWaves>(dout,
                                       a.dout.p + tok * a.dout.ts + (int64_t)head * a.dout.hs,
                                       a.dout.ts, left, a.head_dim, wave);
-    if (wave == 0) row_load(rows, a.rows + ((int64_t)head * a.n_q + tok) * 2, left);
+#pragma unroll
+    for (int b = 0; b < kQB; ++b)
+      if (wave == b)
+        row_load(rows + 64 * b, a.rows + ((int64_t)head * a.n_q + tok + 32 * b) * 2, left - 32 * b);
   };
   const auto step = [&](const uint16_t *q, const uint16_t *dout, const float *rows, int t)
                         __attribute__((always_inline)) {
     const int q0 = (t0 + t % per) * kStepQ;
     const int nat = fresh(nat0), tr = fresh(tr0);
-    f32x16 x = (f32x16)(0.f), y = (f32x16)(0.f);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      x = E::mfma(nat_frag<DP>(q, nat, 0, s), kf[s], x);
-      y = E::mfma(nat_frag<DP>(dout, nat, 0, s), vf[s], y);
-    }
+    for (int qb = 0; qb < kQB; ++qb) {
+      f32x16 x = (f32x16)(0.f), y = (f32x16)(0.f);
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const f32x4 r0 = *reinterpret_cast<const f32x4 *>(rows + 2 * (8 * g + 4 * h));
-      const f32x4 r1 = *reinterpret_cast<const f32x4 *>(rows + 2 * (8 * g + 4 * h) + 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int e = 4 * g + i;
-        const float p = exp2_fast(fmaf(x[e], c, -(i < 2 ? r0[2 * i] : r1[2 * i - 4])));
-        y[e] = p * (y[e] - (i < 2 ? r0[2 * i + 1] : r1[2 * i - 3])) * upw;
-        x[e] = p;
+      for (int s = 0; s < KS; ++s) {
+        x = E::mfma(nat_frag<DP>(q, nat, 32 * qb, s), kf[s], x);
+        y = E::mfma(nat_frag<DP>(dout, nat, 32 * qb, s), vf[s], y);
       }
-    }
-    if (q0 < whole) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (q0 + 8 * (e >> 2) + 4 * h + (e & 3) < from) x[e] = y[e] = 0.f;
-    }
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 r0 = *reinterpret_cast<const f32x4 *>(rows + 64 * qb + 2 * (8 * g + 4 * h));
+        const f32x4 r1 = *reinterpret_cast<const f32x4 *>(rows + 64 * qb + 2 * (8 * g + 4 * h) + 4);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u32x4 wp, ws;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        wp[i] = E::pack(x[8 * s + 2 * i], x[8 * s + 2 * i + 1]);
-        ws[i] = E::pack(y[8 * s + 2 * i], y[8 * s + 2 * i + 1]);
+        for (int i = 0; i < 4; ++i) {
+          const int e = 4 * g + i;
+          const float p = exp2_fast(fmaf(x[e], c, -(i < 2 ? r0[2 * i] : r1[2 * i - 4])));
+          y[e] = p * (y[e] - (i < 2 ? r0[2 * i + 1] : r1[2 * i - 3])) * upw;
+          x[e] = p;
+        }
       }
-      const s16x8 pf = __builtin_bit_cast(s16x8, wp), sf = __builtin_bit_cast(s16x8, ws);
+      if (q0 < whole) {
 #pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        dv[d] = E::mfma(tr_frag<DP>(dout, tr, 16 * s, d), pf, dv[d]);
-        dk[d] = E::mfma(tr_frag<DP>(q, tr, 16 * s, d), sf, dk[d]);
+        for (int e = 0; e < 16; ++e)
+          if (q0 + 32 * qb + 8 * (e >> 2) + 4 * h + (e & 3) < from) x[e] = y[e] = 0.f;
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4 wp, ws;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          wp[i] = E::pack(x[8 * s + 2 * i], x[8 * s + 2 * i + 1]);
+          ws[i] = E::pack(y[8 * s + 2 * i], y[8 * s + 2 * i + 1]);
+        }
+        const s16x8 pf = __builtin_bit_cast(s16x8, wp), sf = __builtin_bit_cast(s16x8, ws);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          dv[d] = E::mfma(tr_frag<DP>(dout, tr, 32 * qb + 16 * s, d), pf, dv[d]);
+          dk[d] = E::mfma(tr_frag<DP>(q, tr, 32 * qb + 16 * s, d), sf, dk[d]);
+        }
       }
     }
   };
-  // two tiles in turn; no branch in the loop, which would cost copies of dk, dv
-  if (first < steps) load(tq0, td0, ts0, first);
-  for (int t = first; t < steps; t += 2) {
-    wait_loads();
-    block_sync();
-    load(tq1, td1, ts1, t + 1);
-    step(tq0, td0, ts0, t);
-    wait_loads();
-    block_sync();
-    load(tq0, td0, ts0, t + 2);
-    step(tq1, td1, ts1, t + 1);
-  }
-  wait_loads();
+  run_tiles(
+      steps - first,
+      [&](auto i, int t) __attribute__((always_inline)) {
+        load(i == 0 ? tq0 : tq1, i == 0 ? td0 : td1, i == 0 ? ts0 : ts1, first + t);
+      },
+      [&](auto i, int t) __attribute__((always_inline)) {
+        step(i == 0 ? tq0 : tq1, i == 0 ? td0 : td1, i == 0 ? ts0 : ts1, first + t);
+      });
   if (!live) return;
   const float fk = a.scale / up;
   const int64_t tok = sk.first + key;
@@ -490,7 +478,7 @@ static void grad(const PromptArgs &a, hipStream_t s) {
 int grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv) {
   if (n_seqs == 0 || n_k == 0) return 1;
   const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
-  const int64_t steps = n_q / n_seqs * (n_heads / n_kv) / kStepQ;
+  const int64_t steps = n_q / n_seqs * (n_heads / n_kv) / 32;
   int64_t n = (2048 + blocks - 1) / blocks;
   if (n > steps / 16) n = steps / 16;
   return n < 1 ? 1 : n > 8 ? 8 : (int)n;

@@ -1,6 +1,4 @@
 // Attention over whole prompts (opattr_attn_prompt).
-#include <type_traits>
-
 #include "attn_dev.h"
 #include "attn_impl.h"
 
@@ -10,12 +8,19 @@ constexpr int kWaves = 4;       // waves a block, 32 queries each
 constexpr int kRowsQ = 32 * kWaves;
 constexpr int kRowsK = 64;      // keys a tile
 
-template <class E, int DP>
-__global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs a) {
+// (one sequence of 6000, 4 heads, 192 blocks: 107 us with one group, 85 with two;
+// 3 of 1500, 16 heads, 608 blocks: 48 and 55)
+constexpr int kFewBlocks = 384;
+
+// G groups of kWaves waves take the key tiles in turn and join their sums at the
+// end: the waves that a few rows would leave a compute unit without.
+template <class E, int DP, int G>
+__global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
-  __shared__ __align__(16) uint16_t tk0[kRowsK * DP], tk1[kRowsK * DP];
-  __shared__ __align__(16) uint16_t tv0[kRowsK * DP], tv1[kRowsK * DP];
-  const int lane = lane_id(), wave = uniform(wave_id());
+  constexpr int kTile = kRowsK * DP;
+  // a group's two tiles of keys, two of values; its sums at the end
+  __shared__ __align__(16) uint16_t tk0[G][kTile], tk1[G][kTile], tv0[G][kTile], tv1[G][kTile];
+  const int lane = lane_id(), all = uniform(wave_id()), wave = all % kWaves, group = all / kWaves;
   const int r = lane & 31, h = lane >> 5;
   // a block's key head goes by its index modulo the key heads
   int id = blockIdx.x;
@@ -148,34 +153,59 @@ __global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs
         for (int d = 0; d < DB; ++d) o[d] = E::mfma(tr_frag<DP>(v, tr, 16 * s, d), pf[s], o[d]);
     }
   };
+  // The second group's sums, through LDS, into the first's, whose lanes hold the
+  // same queries: half of o in the place of each pair of key tiles.
+  const auto join = [&]() __attribute__((always_inline)) {
+    static_assert(G <= 2, "one other group");
+    const int t = threadIdx.x % (kWaves * OPA_WAVE);
+    f32x4 *const so[2] = {reinterpret_cast<f32x4 *>(tk0[0]), reinterpret_cast<f32x4 *>(tk1[0])};
+    f32x2 *const sm = reinterpret_cast<f32x2 *>(tv0[0]);
+    block_sync();
+    if (group) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          so[2 * d / DB][((d % (DB / 2)) * 4 + i) * kWaves * OPA_WAVE + t] =
+              f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+      sm[t] = f32x2{m, l};
+    }
+    block_sync();
+    if (group == 0) {
+      const f32x2 other = sm[t];
+      const float to = fmaxf(m, other[0]);
+      const float by = to == -INFINITY ? 1.f : exp2_fast((m - to) * c);
+      const float with = to == -INFINITY ? 1.f : exp2_fast((other[0] - to) * c);
+      m = to;
+      l = l * by + other[1] * with;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 v = so[2 * d / DB][((d % (DB / 2)) * 4 + i) * kWaves * OPA_WAVE + t];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[d][4 * i + e] = o[d][4 * i + e] * by + v[e] * with;
+        }
+    }
+  };
   const auto start = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = (f32x16)(0.f);
     m = -INFINITY;
     l = 0.f;
   };
-  // Two tiles in turn, the next one's loads in flight. No branch leaves the loop
-  // between them: that would cost copies of o.
-  const std::false_type fast;
   start();
-  if (tiles > 0) load(tk0, tv0, 0);
-  int k0 = 0;
-  for (int t = 1; t < tiles; t += 2) {
-    wait_loads();
-    block_sync();
-    load(tk1, tv1, k0 + kRowsK);
-    step(fast, tk0, tv0, k0);
-    wait_loads();
-    block_sync();
-    load(tk0, tv0, k0 + 2 * kRowsK);  // (past the last: zeros)
-    step(fast, tk1, tv1, k0 + kRowsK);
-    k0 += 2 * kRowsK;
-  }
-  wait_loads();
-  if (tiles & 1) {
-    block_sync();
-    step(fast, tk0, tv0, k0);
-  }
+  run_tiles(
+      (tiles + G - 1) / G,
+      [&](auto i, int t) __attribute__((always_inline)) {
+        load(i == 0 ? tk0[group] : tk1[group], i == 0 ? tv0[group] : tv1[group],
+             (t * G + group) * kRowsK);
+      },
+      [&](auto i, int t) __attribute__((always_inline)) {
+        step(std::false_type{}, i == 0 ? tk0[group] : tk1[group],
+             i == 0 ? tv0[group] : tv1[group], (t * G + group) * kRowsK);
+      });
+  if constexpr (G > 1) join();
   // A weight of 0 times a value that is not finite is no 0: where a sum is not
   // finite, a second pass adds the values of a tile that not every query of the
   // wave sees key by key, and only to the queries that see the key.
@@ -185,17 +215,19 @@ __global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) zero = fmaf(o[d][i], 0.f, zero);
-    if (__syncthreads_or(!(zero == 0.f))) {
+    if (__syncthreads_or(group == 0 && !(zero == 0.f))) {
       start();
-      for (int t = 0; t < tiles; ++t) {
-        load(tk0, tv0, t * kRowsK);
+      for (int k0 = group * kRowsK; k0 < tiles * kRowsK + group * kRowsK; k0 += G * kRowsK) {
+        load(tk0[group], tv0[group], k0);
         wait_loads();
         block_sync();
-        step(std::true_type{}, tk0, tv0, t * kRowsK);
+        step(std::true_type{}, tk0[group], tv0[group], k0);
         block_sync();
       }
+      if constexpr (G > 1) join();
     }
   }
+  if (group) return;
   l = half_sum(l);
   if (!live) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -214,22 +246,23 @@ __global__ __launch_bounds__(kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs
         l == 0.f ? -INFINITY : (m * c + log2f(l) - E::kShift) * kLn2;
 }
 
-template <class E>
+template <class E, int DP>
 static void launch(const PromptArgs &a, hipStream_t s) {
-  const int64_t tiles = (int64_t)a.n_q / kRowsQ + a.n_seqs;
-  const dim3 grid((uint32_t)(tiles * a.n_heads));
-  if (a.head_dim <= 64)
-    hipLaunchKernelGGL((k_attn_prompt<E, 64>), grid, dim3(kWaves * OPA_WAVE), 0, s, a);
+  const int64_t blocks = ((int64_t)a.n_q / kRowsQ + a.n_seqs) * a.n_heads;
+  if (blocks <= kFewBlocks)
+    hipLaunchKernelGGL((k_attn_prompt<E, DP, 2>), dim3((uint32_t)blocks),
+                       dim3(2 * kWaves * OPA_WAVE), 0, s, a);
   else
-    hipLaunchKernelGGL((k_attn_prompt<E, 128>), grid, dim3(kWaves * OPA_WAVE), 0, s, a);
+    hipLaunchKernelGGL((k_attn_prompt<E, DP, 1>), dim3((uint32_t)blocks),
+                       dim3(kWaves * OPA_WAVE), 0, s, a);
 }
 
 void run_prompt(const PromptArgs &a, int dtype, hipStream_t s) {
   if (a.n_q == 0 || a.n_seqs == 0) return;
   if (dtype == OPATTR_BF16)
-    launch<BF16>(a, s);
+    a.head_dim <= 64 ? launch<BF16, 64>(a, s) : launch<BF16, 128>(a, s);
   else
-    launch<F16>(a, s);
+    a.head_dim <= 64 ? launch<F16, 64>(a, s) : launch<F16, 128>(a, s);
 }
 
 }  // namespace opa
