@@ -1,0 +1,69 @@
+"""The attention workload end to end: tokens generated from the paged cache,
+across a fork and a compaction, have the outputs that attention over the whole
+sequence gives; its trace is attributed to the operators that issued it."""
+import json
+
+import numpy as np
+import pytest
+
+import attn_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+
+def _host(t):
+    return t.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_generated_tokens_match_whole_sequences(dtype):
+    import torch
+
+    from paper_2609_11938_amd import workload
+
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    print(f"case serve {dtype}", flush=True)
+    lens, steps = (50, 9, 33), 5
+    alive = workload.serve(workload.Recorder(), lens=lens, steps=steps, layers=2, heads=4,
+                           kv_heads=2, head_dim=64, page_size=8, dtype=getattr(torch, dtype))
+    assert [seq[0][0].shape[0] for seq in alive] == [60, 60, 43]
+    for seq in alive:
+        for q, k, v, out in seq:
+            q, k, v, out = (_host(t) for t in (q, k, v, out))
+            for h in range(4):
+                want, bound = O.head(q[:, h], k[:, h // 2], v[:, h // 2], 0.125, True,
+                                     dtype)["out"]
+                assert (np.abs(out[:, h] - want) <= bound).all()
+    # the fork's two rows share their past and nothing after it
+    past = slice(0, lens[0] + steps)
+    assert torch.equal(alive[0][0][1][past], alive[1][0][1][past])
+    assert not torch.equal(alive[0][0][1], alive[1][0][1])
+
+
+def test_profile_of_the_workload(tmp_path):
+    from paper_2609_11938_amd import profile, workload
+
+    rec = workload.Recorder()
+    workload.serve(rec, lens=(40, 20), steps=3, layers=2)
+    workload.train(rec)
+    print(f"case workload profile: {len(rec.launches)} launches", flush=True)
+    doc = workload.profile(rec)
+    path = tmp_path / "profile.json"
+    profile.write(str(path), doc)
+    doc = json.loads(path.read_text())
+    assert doc["unattributed_kernels"] == []
+    calls = {}
+    for entry in doc["operators"]:
+        names = {k["kernel_name"] for k in entry["kernels"]}
+        calls.setdefault(entry["operator_name"], []).append((len(entry["kernels"]), names))
+        agg = entry["aggregated"]
+        assert agg["total_duration_ns"] == sum(k["duration_ns"] for k in entry["kernels"]) > 0
+        assert agg["l1_hit_rate"] is None and agg["dram_bytes_read"] > 0
+    # 2 layers: a prompt, 2 x 3 steps, one training pass; an append each but the last
+    assert len(calls["aten::attention"]) == 2 + 2 * 3 * 2 + 1
+    assert {n for _, s in calls["aten::attention"] for n in s} == {"attn_prompt", "attn_paged"}
+    assert calls["cache::append"] == [(1, {"kv_append"})] * (2 + 2 * 3 * 2)
+    assert calls["cache::turn"] == [(2, {"pages_fork", "pages_compact"})] * 2
+    assert calls["aten::attention_backward"] == [(1, {"attn_prompt_grad"})]
+    kernels = sum(len(e["kernels"]) for e in doc["operators"])
+    assert kernels == len(rec.launches)
