@@ -244,15 +244,18 @@ __device__ __forceinline__ Span span_of(const int32_t *cu, int b, int n) {
   return {s, e - s};
 }
 
-// Tile `tile` of the sequences' tiles of `rows` rows: which sequence, and which
-// of its tiles; false past the last. By whole waves; the result is uniform.
-__device__ __forceinline__ bool find_tile(const int32_t *cu, int n_seqs, int n, int rows,
-                                          int tile, int &seq, int &part) {
+// Tile `tile` of the tiles of `rows` rows that the sequences of `cu` have: which
+// of the sequence's tiles it is, and the sequence's spans in both offset arrays;
+// false past the last. By whole waves; the result is uniform. Each lane loads a
+// sequence's four offsets at once: what follows waits for one load.
+__device__ __forceinline__ bool find_tile(const int32_t *cu, int n, const int32_t *other,
+                                          int n_other, int n_seqs, int rows, int tile, Span &mine,
+                                          Span &its, int &part) {
   const int lane = lane_id();
   for (int base = 0; base < n_seqs; base += OPA_WAVE) {
-    const int b = base + lane;
-    int tiles = 0;
-    if (b < n_seqs) tiles = (span_of(cu, b, n).count + rows - 1) / rows;
+    const int b = base + lane < n_seqs ? base + lane : n_seqs - 1;
+    const Span x = span_of(cu, b, n), y = span_of(other, b, n_other);
+    const int tiles = base + lane < n_seqs ? (x.count + rows - 1) / rows : 0;
     int inc = tiles;
 #pragma unroll
     for (int d = 1; d < OPA_WAVE; d <<= 1) {
@@ -262,11 +265,13 @@ __device__ __forceinline__ bool find_tile(const int32_t *cu, int n_seqs, int n, 
     const uint64_t m = __ballot(inc > tile);
     if (m) {
       const int w = __ffsll((unsigned long long)m) - 1;
-      seq = base + w;
-      part = uniform(tile - __shfl(inc - tiles, w));
+      const auto from = [&](int v) { return __builtin_amdgcn_readlane(v, w); };
+      mine = {from(x.first), from(x.count)};
+      its = {from(y.first), from(y.count)};
+      part = tile - from(inc - tiles);
       return true;
     }
-    tile -= uniform(__shfl(inc, OPA_WAVE - 1));
+    tile -= __builtin_amdgcn_readlane(inc, OPA_WAVE - 1);
   }
   return false;
 }

@@ -101,15 +101,14 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs
   const int hk = id % a.n_kv;
   id /= a.n_kv;
   const int head = hk * a.group + id % a.group;
-  int seq, part;
   if (blockIdx.x == 0) {
     check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag);
     check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
   }
-  if (!find_tile(a.cu_q, a.n_seqs, a.n_q, kHeld, id / a.group, seq, part)) return;
-  Span sq = span_of(a.cu_q, seq, a.n_q), sk = span_of(a.cu_k, seq, a.n_k);
-  sq = {uniform(sq.first), uniform(sq.count)};
-  sk = {uniform(sk.first), uniform(sk.count)};
+  Span sq, sk;
+  int part;
+  if (!find_tile(a.cu_q, a.n_q, a.cu_k, a.n_k, a.n_seqs, kHeld, id / a.group, sq, sk, part))
+    return;
   const int q0 = ((sq.count + kHeld - 1) / kHeld - 1 - part) * kHeld;
   const int lead = sk.count - sq.count;
   const int qrow = q0 + wave * 32 + r;
@@ -263,11 +262,10 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   const int hk = id % a.n_kv;
   id /= a.n_kv;
   const int split = id % a.splits;
-  int seq, part;
-  if (!find_tile(a.cu_k, a.n_seqs, a.n_k, kHeld, id / a.splits, seq, part)) return;
-  Span sq = span_of(a.cu_q, seq, a.n_q), sk = span_of(a.cu_k, seq, a.n_k);
-  sq = {uniform(sq.first), uniform(sq.count)};
-  sk = {uniform(sk.first), uniform(sk.count)};
+  Span sq, sk;
+  int part;
+  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, id / a.splits, sk, sq, part))
+    return;
   const int lead = sk.count - sq.count;
   const int key0 = part * kHeld + wave * 32, key = key0 + r;
   const bool live = key < sk.count;

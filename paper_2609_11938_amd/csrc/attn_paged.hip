@@ -22,10 +22,21 @@ __device__ __forceinline__ int paged_len(const PagedArgs &a, int b) {
   return b < a.n_seqs ? clamp_to(a.lens[b], 0, a.slots) : 0;
 }
 
-// Tokens of a share; by whole waves.
-__device__ __forceinline__ int share_size(const PagedArgs &a) {
-  int64_t sum = 0;
-  for (int base = 0; base < a.n_seqs; base += OPA_WAVE) sum += paged_len(a, base + lane_id());
+__device__ __forceinline__ int shares_of(int len, int c) { return len > c ? (len + c - 1) / c : 1; }
+
+// Sequences one to a lane; past 64, loops of as many.
+struct Share {
+  int size;   // tokens of every share but a sequence's last
+  int seq, part, len;
+  int first;  // the sequence's first share, as the shares are counted
+};
+
+// Tokens of a share, from every sequence's length: as many as make kBlocks shares
+// of the work of all key heads. mine: this lane's sequence's length.
+__device__ __forceinline__ int share_size(const PagedArgs &a, int mine) {
+  if (a.slots <= kMinShare) return kMinShare;
+  int64_t sum = mine;
+  for (int b = OPA_WAVE + lane_id(); b < a.n_seqs; b += OPA_WAVE) sum += paged_len(a, b);
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
   const int64_t each = (sum * a.n_kv + kBlocks - 1) / kBlocks;
@@ -34,41 +45,50 @@ __device__ __forceinline__ int share_size(const PagedArgs &a) {
   return uniform((int)(c < kMinShare ? kMinShare : c));
 }
 
-__device__ __forceinline__ int shares_of(int len, int c) { return len > c ? (len + c - 1) / c : 1; }
-
-// Share `item` of all the sequences' shares: its sequence and which of its
-// shares it is; false past the last.
-__device__ __forceinline__ bool find_share(const PagedArgs &a, int c, int item, int &seq,
-                                           int &part) {
+// Share `item` of all the sequences' shares; false past the last. By whole waves.
+__device__ __forceinline__ bool find_share(const PagedArgs &a, int item, Share &s) {
   const int lane = lane_id();
+  const int mine = paged_len(a, lane);
+  s.size = share_size(a, mine);
+  int done = 0;
   for (int base = 0; base < a.n_seqs; base += OPA_WAVE) {
     const int b = base + lane;
-    const int n = b < a.n_seqs ? shares_of(paged_len(a, b), c) : 0;
+    const int len = base ? paged_len(a, b) : mine;
+    const int n = b < a.n_seqs ? shares_of(len, s.size) : 0;
     int inc = n;
 #pragma unroll
     for (int d = 1; d < OPA_WAVE; d <<= 1) {
       const int o = __shfl_up(inc, d);
       if (lane >= d) inc += o;
     }
-    const uint64_t m = __ballot(inc > item);
+    const uint64_t m = __ballot(done + inc > item);
     if (m) {
       const int w = __ffsll((unsigned long long)m) - 1;
-      seq = base + w;
-      part = uniform(item - __shfl(inc - n, w));
+      s.seq = base + w;
+      s.first = done + __builtin_amdgcn_readlane(inc - n, w);
+      s.part = item - s.first;
+      s.len = __builtin_amdgcn_readlane(len, w);
       return true;
     }
-    item -= uniform(__shfl(inc, OPA_WAVE - 1));
+    done += __builtin_amdgcn_readlane(inc, OPA_WAVE - 1);
   }
   return false;
 }
 
-// The first share of sequence seq (as find_share counts them).
-__device__ __forceinline__ int first_share(const PagedArgs &a, int c, int seq) {
-  int sum = 0;
-  for (int b = lane_id(); b < seq; b += OPA_WAVE) sum += shares_of(paged_len(a, b), c);
+// The shares of sequence seq. By whole waves.
+__device__ __forceinline__ Share shares_at(const PagedArgs &a, int seq) {
+  const int lane = lane_id();
+  Share s{};
+  const int mine = paged_len(a, lane);
+  s.size = share_size(a, mine);
+  s.seq = seq;
+  s.len = uniform(paged_len(a, seq));
+  int sum = lane < seq ? shares_of(mine, s.size) : 0;
+  for (int b = OPA_WAVE + lane; b < seq; b += OPA_WAVE) sum += shares_of(paged_len(a, b), s.size);
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-  return uniform(sum);
+  s.first = uniform(sum);
+  return s;
 }
 
 // A row's result from its values' sum, its weights' sum and reference.
@@ -98,22 +118,21 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedA
   const int lane = lane_id(), wave = uniform(wave_id());
   const int r = lane & 15, g = lane >> 4;
   const int hk = blockIdx.x % a.n_kv, item = blockIdx.x / a.n_kv;
-  const int share = share_size(a);
-  int seq, part;
-  if (!find_share(a, share, item, seq, part)) return;
-  const int len = uniform(paged_len(a, seq));
-  const int t0 = part * share, t1 = len < t0 + share ? len : t0 + share;
+  Share s;
+  if (!find_share(a, item, s)) return;
+  const int seq = s.seq, len = s.len;
+  const int t0 = s.part * s.size, t1 = len < t0 + s.size ? len : t0 + s.size;
   const int32_t *table = a.table + (int64_t)seq * a.width;
-  if (threadIdx.x == 0 && part == 0 && hk == 0 && a.lens[seq] != len)
+  if (a.diag && threadIdx.x == 0 && s.part == 0 && hk == 0 && a.lens[seq] != len)
     report(a.diag, OPATTR_F_DATA, 1);
 
   const uint16_t *qrow = a.q.p + seq * a.q.ts + (int64_t)hk * a.group * a.q.hs;
   s16x8 qf[KS];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    qf[s] = (s16x8)(0);
-    if (r < a.group && 32 * s + 8 * g < a.head_dim)
-      qf[s] = *reinterpret_cast<const s16x8 *>(qrow + r * a.q.hs + 32 * s + 8 * g);
+  for (int e = 0; e < KS; ++e) {
+    qf[e] = (s16x8)(0);
+    if (r < a.group && 32 * e + 8 * g < a.head_dim)
+      qf[e] = *reinterpret_cast<const s16x8 *>(qrow + r * a.q.hs + 32 * e + 8 * g);
   }
   const float c = a.scale * kLog2e;
   const int mask = (1 << a.shift) - 1, last = a.head_dim / 8 - 1;
@@ -153,9 +172,9 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedA
       const int64_t p = __shfl(at, 16 * u + r);
       const uint16_t *kp = p >= 0 ? a.k + p : qrow;
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int ch = 4 * s + g < last ? 4 * s + g : last;
-        kr[u][s] = *reinterpret_cast<const s16x8 *>(kp + ch * 8);
+      for (int e = 0; e < KS; ++e) {
+        const int ch = 4 * e + g < last ? 4 * e + g : last;
+        kr[u][e] = *reinterpret_cast<const s16x8 *>(kp + ch * 8);
       }
     }
   };
@@ -180,8 +199,8 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedA
       for (int i = 0; i < N; ++i)
         if ((i * OPA_WAVE + lane) % C > last) vr[i] = (s16x8)(0);
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
-        if (4 * s + g > last) kr[0][s] = kr[1][s] = (s16x8)(0);
+      for (int e = 0; e < KS; ++e)
+        if (4 * e + g > last) kr[0][e] = kr[1][e] = (s16x8)(0);
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -193,7 +212,7 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedA
     for (int u = 0; u < 2; ++u) {
       x[u] = (f32x4)(0.f);
 #pragma unroll
-      for (int s = 0; s < KS; ++s) x[u] = E::mfma16(kr[u][s], qf[s], x[u]);
+      for (int e = 0; e < KS; ++e) x[u] = E::mfma16(kr[u][e], qf[e], x[u]);
     }
     // the next tile's loads, before this one's softmax; places one tile further
     if (k0 + kTile * kPagedWaves < t1) {
@@ -255,7 +274,7 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedA
     sl[wave][r] = l;
   }
   __syncthreads();
-  const bool whole = shares_of(len, share) == 1;
+  const bool whole = shares_of(len, s.size) == 1;
   for (int i = threadIdx.x; i < a.group * (DP / 4); i += kPagedWaves * OPA_WAVE) {
     const int row = i / (DP / 4), d = i % (DP / 4) * 4, head = hk * a.group + row;
     float top = -INFINITY;
@@ -291,11 +310,11 @@ __global__ __launch_bounds__(kJoin * DP / 4) void k_paged_join(PagedArgs a) {
   __shared__ __align__(16) f32x4 sums[kJoin][DP / 4];
   __shared__ float wave_top[kThreads / OPA_WAVE], run_l[kJoin];
   const int head = blockIdx.x % a.n_heads, seq = blockIdx.x / a.n_heads;
-  const int share = share_size(a);
-  const int n = shares_of(uniform(paged_len(a, seq)), share);
+  const Share s = shares_at(a, seq);
+  const int n = shares_of(s.len, s.size);
   if (n == 1) return;
   const int64_t step = (int64_t)a.n_heads * (DP + 4);
-  const float *p = a.part + ((int64_t)first_share(a, share, seq) * a.n_heads + head) * (DP + 4);
+  const float *p = a.part + ((int64_t)s.first * a.n_heads + head) * (DP + 4);
   float top = -INFINITY;
   for (int k = threadIdx.x; k < n; k += kThreads) {
     f[k] = p[k * step + DP];

@@ -27,15 +27,14 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
   const int hk = id % a.n_kv;
   id /= a.n_kv;
   const int head = hk * a.group + id % a.group;
-  int seq, part;
   if (blockIdx.x == 0) {
     check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag);
     check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
   }
-  if (!find_tile(a.cu_q, a.n_seqs, a.n_q, kRowsQ, id / a.group, seq, part)) return;
-  Span sq = span_of(a.cu_q, seq, a.n_q), sk = span_of(a.cu_k, seq, a.n_k);
-  sq = {uniform(sq.first), uniform(sq.count)};
-  sk = {uniform(sk.first), uniform(sk.count)};
+  Span sq, sk;
+  int part;
+  if (!find_tile(a.cu_q, a.n_q, a.cu_k, a.n_k, a.n_seqs, kRowsQ, id / a.group, sq, sk, part))
+    return;
   // the sequence's last queries, which see the most keys, first
   const int q0 = ((sq.count + kRowsQ - 1) / kRowsQ - 1 - part) * kRowsQ;
   const int lead = sk.count - sq.count;

@@ -20,6 +20,15 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   }
   const int t = blockIdx.x * 4 + wave_id();
   if (t >= a.n_new) return;
+  const int per = a.head_dim / 8, n = a.n_kv * per;
+  const uint16_t *kr = a.kn.p + t * a.kn.ts, *vr = a.vn.p + t * a.vn.ts;
+  // the first pieces' loads, before the place they go to is known
+  int g = lane / per, c = (lane - g * per) * 8;
+  u32x4 x = (u32x4)(0u), y = (u32x4)(0u);
+  if (lane < n) {
+    x = *reinterpret_cast<const u32x4 *>(kr + g * a.kn.hs + c);
+    y = *reinterpret_cast<const u32x4 *>(vr + g * a.vn.hs + c);
+  }
   // its sequence: as many as end at or before it
   int seq = 0;
   for (int base = 0; base < a.n_seqs; base += OPA_WAVE) {
@@ -39,13 +48,14 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
     return;
   }
   const int64_t to = page * a.ps + (at & ((1 << a.shift) - 1)) * a.ts;
-  const int per = a.head_dim / 8, n = a.n_kv * per;
   for (int i = lane; i < n; i += OPA_WAVE) {
-    const int g = i / per, c = (i - g * per) * 8;
-    const u32x4 x = *reinterpret_cast<const u32x4 *>(a.kn.p + t * a.kn.ts + g * a.kn.hs + c);
-    const u32x4 y = *reinterpret_cast<const u32x4 *>(a.vn.p + t * a.vn.ts + g * a.vn.hs + c);
     *reinterpret_cast<u32x4 *>(a.k + to + g * a.hs + c) = x;
     *reinterpret_cast<u32x4 *>(a.v + to + g * a.hs + c) = y;
+    if (i + OPA_WAVE >= n) break;
+    g = (i + OPA_WAVE) / per;
+    c = (i + OPA_WAVE - g * per) * 8;
+    x = *reinterpret_cast<const u32x4 *>(kr + g * a.kn.hs + c);
+    y = *reinterpret_cast<const u32x4 *>(vr + g * a.vn.hs + c);
   }
 }
 
