@@ -86,16 +86,22 @@ __global__ void k_attn_zero(uint32_t *p, int n) {
   if (i < n) p[i] = 0;
 }
 
+// Two groups of waves share the keys where the blocks are this few (one sequence
+// of 6000, 4 heads, 192 blocks: a training pass of 378 us with one, 340 with two).
+constexpr int kFewBlocks = 256;
+
 // dq of 32 queries a wave: S^T = K Q^T with the wave's queries as columns;
 // dS^T then is the B operand of dq^T = K^T dS^T. D' = dout . out starts the pass
 // (out's 16 bits make it inexact); the exact D is summed beside it and goes to
 // the second pass with the scaled lse.
-template <class E, int DP>
-__global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
+template <class E, int DP, int G>
+__global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
   constexpr int kStepK = kStep(DP), kTile = kStepK * DP;
-  __shared__ __align__(16) uint16_t tk0[kTile], tk1[kTile], tv0[kTile], tv1[kTile];
-  const int lane = lane_id(), wave = uniform(wave_id());
+  // a group's two tiles of keys, two of values; the second's sums at the end
+  __shared__ __align__(16) uint16_t tk0[G][kTile], tk1[G][kTile], tv0[G][kTile], tv1[G][kTile];
+  const int lane = lane_id(), all = uniform(wave_id());
+  const int wave = all % kGradWaves, group = all / kGradWaves;
   const int r = lane & 31, h = lane >> 5;
   int id = blockIdx.x;
   const int hk = id % a.n_kv;
@@ -210,13 +216,44 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs
     }
   };
   run_tiles(
-      tiles,
+      (tiles + G - 1) / G,
       [&](auto i, int t) __attribute__((always_inline)) {
-        load(i == 0 ? tk0 : tk1, i == 0 ? tv0 : tv1, t * kStepK);
+        load(i == 0 ? tk0[group] : tk1[group], i == 0 ? tv0[group] : tv1[group],
+             (t * G + group) * kStepK);
       },
       [&](auto i, int t) __attribute__((always_inline)) {
-        step(i == 0 ? tk0 : tk1, i == 0 ? tv0 : tv1, t * kStepK);
+        step(i == 0 ? tk0[group] : tk1[group], i == 0 ? tv0[group] : tv1[group],
+             (t * G + group) * kStepK);
       });
+  if constexpr (G > 1) {
+    // the second group's sums into the first's: a part of dq in each of the four
+    // tiles' places, one after the other
+    static_assert(G == 2, "one other group");
+    constexpr int kEach = G * kTile * 2 / 16 / (kGradWaves * OPA_WAVE);  // pieces a lane
+    static_assert(4 * kEach >= DB * 4, "they fit");
+    const int t = threadIdx.x % (kGradWaves * OPA_WAVE);
+    f32x4 *const at[4] = {reinterpret_cast<f32x4 *>(tk0[0]), reinterpret_cast<f32x4 *>(tk1[0]),
+                          reinterpret_cast<f32x4 *>(tv0[0]), reinterpret_cast<f32x4 *>(tv1[0])};
+    __shared__ float other[kGradWaves * OPA_WAVE];
+    block_sync();
+    if (group) {
+#pragma unroll
+      for (int i = 0; i < DB * 4; ++i)
+        at[i / kEach][i % kEach * kGradWaves * OPA_WAVE + t] =
+            f32x4{dq[i / 4][i % 4 * 4], dq[i / 4][i % 4 * 4 + 1], dq[i / 4][i % 4 * 4 + 2],
+                  dq[i / 4][i % 4 * 4 + 3]};
+      other[t] = exact;
+    }
+    block_sync();
+    if (group) return;
+#pragma unroll
+    for (int i = 0; i < DB * 4; ++i) {
+      const f32x4 v = at[i / kEach][i % kEach * kGradWaves * OPA_WAVE + t];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dq[i / 4][i % 4 * 4 + e] += v[e];
+    }
+    exact += other[t];
+  }
   exact = half_sum(exact);
   if (!live) return;
   if (h == 0) {
@@ -247,6 +284,25 @@ __device__ __forceinline__ void row_load(float *to, const float *p, int left) {
                                            lane_id() * 4, 0, 0, 0);
 }
 
+// Tiles of queries that key tile `part` of a sequence meets: the first, and how many.
+template <int DP>
+__device__ __forceinline__ Span tile_queries(const PromptArgs &a, const Span &sq, const Span &sk,
+                                             int part) {
+  const int begin =
+      a.causal ? clamp_to(part * kHeld - (sk.count - sq.count), 0, sq.count) : 0;
+  const int first = begin / kStep(DP), end = (sq.count + kStep(DP) - 1) / kStep(DP);
+  return {first, end - first};
+}
+// Blocks that share the tile: at least kSplitSteps steps of 32 queries each, at
+// most a.splits.
+constexpr int kSplitSteps = 24;
+template <int DP>
+__device__ __forceinline__ int tile_splits(const PromptArgs &a, const Span &sq, const Span &sk,
+                                           int part) {
+  const int steps = tile_queries<DP>(a, sq, sk, part).count * a.group * (kStep(DP) / 32);
+  return clamp_to((steps + kSplitSteps - 1) / kSplitSteps, 1, a.splits);
+}
+
 // dk and dv of 32 keys a wave: S = Q K^T with the wave's keys as columns, so
 // that a lane holds one key; P and dS then are the B operands of
 // dv^T = dout^T P and dk^T = q^T dS.
@@ -269,17 +325,18 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   const int lead = sk.count - sq.count;
   const int key0 = part * kHeld + wave * 32, key = key0 + r;
   const bool live = key < sk.count;
-  // the first query that sees a key of the block, the first that sees every key
-  // of this wave, and the first that sees this lane's
-  const int begin = a.causal ? clamp_to(part * kHeld - lead, 0, sq.count) : 0;
+  // the first query that sees every key of this wave, and the first that sees
+  // this lane's
   const int whole = key0 + 32 > sk.count ? sq.count
                                          : a.causal ? clamp_to(key0 + 31 - lead, 0, sq.count) : 0;
   const int from = live ? (a.causal ? clamp_to(key - lead, 0, sq.count) : 0) : sq.count;
-  const int t0 = begin / kStepQ, per = (sq.count + kStepQ - 1) / kStepQ - t0;
+  const Span met = tile_queries<DP>(a, sq, sk, part);
+  const int t0 = met.first, per = met.count;
   // this block's steps of the tile's: a head's queries, then the next head's
-  const int all = per > 0 ? per * a.group : 0;
-  const int first = (int)((int64_t)all * split / a.splits);
-  const int steps = (int)((int64_t)all * (split + 1) / a.splits);
+  const int splits = tile_splits<DP>(a, sq, sk, part), all = per * a.group;
+  if (split >= splits) return;
+  const int first = (int)((int64_t)all * split / splits);
+  const int steps = (int)((int64_t)all * (split + 1) / splits);
   s16x8 kf[KS], vf[KS];
   {
     const int64_t tok = sk.first + (live ? key : 0);
@@ -377,7 +434,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   if (!live) return;
   const float fk = a.scale / up;
   const int64_t tok = sk.first + key;
-  if (a.splits > 1) {  // [splits][n_k][n_kv][dk, dv][DP]
+  if (splits > 1) {  // [splits][n_k][n_kv][dk, dv][DP]
     float *p = a.part + (((int64_t)split * a.n_k + tok) * a.n_kv + hk) * 2 * DP;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -412,47 +469,52 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
     }
 }
 
-// The splits' dk and dv of the rows inside a sequence, added in order: 4 values
-// a thread, a wave's all of one row of DP 128 (of two, DP 64).
+// A key tile's dk and dv from those of its blocks, added in order; a tile of one
+// block is done already. kSumParts blocks a tile and key head.
+constexpr int kSumParts = 4;
 template <class E, int DP>
 __global__ __launch_bounds__(256) void k_dkv_sum(PromptArgs a) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t n = (int64_t)a.n_k * a.n_kv * 2 * DP;
-  if (i * 4 >= n) return;
-  const int64_t row = i * 4 / (2 * DP);
-  const int64_t tok = row / a.n_kv;
-  const int hk = (int)(row - tok * a.n_kv);
-  const int at = (int)(i * 4 - row * 2 * DP), col = at % DP;
-  if (col >= a.head_dim) return;
-  // rows outside every sequence keep what they hold
-  int lo = 0, hi = a.n_seqs;  // the last sequence that starts at or before tok
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.cu_k[mid] <= tok) lo = mid; else hi = mid;
+  constexpr int kRow = 2 * DP / 4;  // pieces of four values of a key: dk, dv
+  int id = blockIdx.x;
+  const int rows = id % kSumParts;
+  id /= kSumParts;
+  const int hk = id % a.n_kv;
+  Span sq, sk;
+  int part;
+  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, id / a.n_kv, sk, sq, part)) return;
+  const int splits = tile_splits<DP>(a, sq, sk, part);
+  if (splits == 1) return;
+  const int64_t plane = (int64_t)a.n_k * a.n_kv * 2 * DP;
+  for (int i = threadIdx.x; i < kHeld / kSumParts * kRow; i += 256) {
+    const int key = part * kHeld + rows * (kHeld / kSumParts) + i / kRow;
+    const int at = i % kRow * 4, col = at % DP;
+    if (key >= sk.count || col >= a.head_dim) continue;
+    const int64_t tok = sk.first + key;
+    const float *p = a.part + (tok * a.n_kv + hk) * 2 * DP + at;
+    f32x4 sum = (f32x4)(0.f);
+#pragma unroll 4
+    for (int k = 0; k < splits; ++k) sum += *reinterpret_cast<const f32x4 *>(p + k * plane);
+    const Rows &o = at < DP ? a.dk : a.dv;
+    const u32x2 w = {E::pack(sum[0], sum[1]), E::pack(sum[2], sum[3])};
+    *reinterpret_cast<u32x2 *>(o.p + tok * o.ts + (int64_t)hk * o.hs + col) = w;
   }
-  const Span s = span_of(a.cu_k, lo, a.n_k);
-  if (tok < s.first || tok >= (int64_t)s.first + s.count) return;
-  f32x4 sum = (f32x4)(0.f);
-  for (int k = 0; k < a.splits; ++k)
-    sum += *reinterpret_cast<const f32x4 *>(a.part + k * n + i * 4);
-  const Rows &o = at < DP ? a.dk : a.dv;
-  const u32x2 w = {E::pack(sum[0], sum[1]), E::pack(sum[2], sum[3])};
-  *reinterpret_cast<u32x2 *>(o.p + tok * o.ts + (int64_t)hk * o.hs + col) = w;
 }
 
 template <class E, int DP>
 static void launch(const PromptArgs &a, hipStream_t s) {
   const int64_t kt = (int64_t)a.n_k / kHeld + a.n_seqs, qt = (int64_t)a.n_q / kHeld + a.n_seqs;
   const dim3 block(kGradWaves * OPA_WAVE);
-  if (a.n_q > 0)
-    hipLaunchKernelGGL((k_attn_dq<E, DP>), dim3((uint32_t)(qt * a.n_heads)), block, 0, s, a);
+  const dim3 rows((uint32_t)(qt * a.n_heads));
+  if (a.n_q > 0 && qt * a.n_heads <= kFewBlocks)
+    hipLaunchKernelGGL((k_attn_dq<E, DP, 2>), rows, dim3(2 * kGradWaves * OPA_WAVE), 0, s, a);
+  else if (a.n_q > 0)
+    hipLaunchKernelGGL((k_attn_dq<E, DP, 1>), rows, block, 0, s, a);
   if (a.n_k == 0) return;
   hipLaunchKernelGGL((k_attn_dkv<E, DP>), dim3((uint32_t)(kt * a.n_kv * a.splits)), block, 0, s,
                      a);
-  if (a.splits > 1) {
-    const int64_t n = (int64_t)a.n_k * a.n_kv * 2 * DP / 4;
-    hipLaunchKernelGGL((k_dkv_sum<E, DP>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, s, a);
-  }
+  if (a.splits > 1)
+    hipLaunchKernelGGL((k_dkv_sum<E, DP>), dim3((uint32_t)(kt * a.n_kv * kSumParts)), dim3(256),
+                       0, s, a);
 }
 
 template <class E>
@@ -470,16 +532,19 @@ static void grad(const PromptArgs &a, hipStream_t s) {
     launch<E, 128>(a, s);
 }
 
-// Blocks of a key tile. A tile's steps go one after another, and a causal
+// Blocks of a key tile at most. A tile's steps go one after another, and a causal
 // sequence's first tile has the most: about 2048 blocks keep the chip full to
-// the end, each of 16 steps at least (by the sequences' mean length).
+// the end (12 packed documents of up to 4001, 512 blocks without: 1110 us, 2048:
+// 900 us, 4096: 1000 us). By the mean length: blocks that find their tile not
+// split cost what the others gain (8 sequences of 512: 46 us unsplit, 57 us with
+// six blocks a tile that do nothing).
 int grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv) {
   if (n_seqs == 0 || n_k == 0) return 1;
   const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
-  const int64_t steps = n_q / n_seqs * (n_heads / n_kv) / 32;
+  const int64_t steps = n_q * (n_heads / n_kv) / 32 / n_seqs;
   int64_t n = (2048 + blocks - 1) / blocks;
-  if (n > steps / 16) n = steps / 16;
-  return n < 1 ? 1 : n > 8 ? 8 : (int)n;
+  if (n > steps / kSplitSteps) n = steps / kSplitSteps;
+  return n < 1 ? 1 : n > 16 ? 16 : (int)n;
 }
 
 void run_prompt_grad(const PromptArgs &a, int dtype, hipStream_t s) {
