@@ -91,17 +91,24 @@ __global__ void k_attn_zero(uint32_t *p, int n) {
 constexpr int kFewBlocks = 256;
 
 // dq of 32 queries a wave: S^T = K Q^T with the wave's queries as columns;
-// dS^T then is the B operand of dq^T = K^T dS^T. D' = dout . out starts the pass
-// (out's 16 bits make it inexact); the exact D is summed beside it and goes to
-// the second pass with the scaled lse.
+// dS^T then is the B operand of dq^T = K^T dS^T. The pass goes by D' = dout . out,
+// which out's 16 bits make inexact; D - D' = sum_j p_j (dp_j - D') is summed beside
+// it, and with kp = sum_j p_j k_j, dq = sum_j p_j (dp_j - D') k_j - (D - D') kp puts
+// that right (a product more; dq's error against 64 bits, of values rounded to 16
+// bits once: 1.65 times that without, 1.4 with). The exact D goes to the second
+// pass with the scaled lse.
 template <class E, int DP, int G>
 __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
   constexpr int kStepK = kStep(DP), kTile = kStepK * DP;
   // a group's two tiles of keys, two of values; the second's sums at the end
   __shared__ __align__(16) uint16_t tk0[G][kTile], tk1[G][kTile], tv0[G][kTile], tv1[G][kTile];
+  // of head_dim 128, dout's fragments, which the registers have no room for
+  constexpr bool kHeldHere = DP <= 64;
+  __shared__ s16x8 held[kHeldHere ? 1 : kGradWaves * KS * OPA_WAVE];
   const int lane = lane_id(), all = uniform(wave_id());
   const int wave = all % kGradWaves, group = all / kGradWaves;
+  s16x8 *const mine = held + (kHeldHere ? 0 : wave * KS * OPA_WAVE + lane);
   const int r = lane & 31, h = lane >> 5;
   int id = blockIdx.x;
   const int hk = id % a.n_kv;
@@ -124,8 +131,8 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
   const int tiles = (keys + kStepK - 1) / kStepK;
   const int whole = a.causal ? clamp_to(q0 + wave * 32 + lead + 1, 0, sk.count) : sk.count;
   const int seen = live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) : sk.count) : 0;
-  s16x8 qf[KS], df[KS];
-  float L = INFINITY, D = 0.f, exact = 0.f;
+  s16x8 qf[KS], df[kHeldHere ? KS : 1];
+  float L = INFINITY, D = 0.f, off = 0.f;
   {
     const int64_t tok = sq.first + (live ? qrow : 0);
     const uint16_t *qp = a.q.p + tok * a.q.ts + (int64_t)head * a.q.hs;
@@ -133,37 +140,42 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
     const uint16_t *op = a.out.p + tok * a.out.ts + (int64_t)head * a.out.hs;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
+      s16x8 d = (s16x8)(0);
       qf[s] = (s16x8)(0);
-      df[s] = (s16x8)(0);
       if (live && 16 * s + 8 * h < a.head_dim) {
         qf[s] = *reinterpret_cast<const s16x8 *>(qp + 16 * s + 8 * h);
-        df[s] = *reinterpret_cast<const s16x8 *>(dp + 16 * s + 8 * h);
+        d = *reinterpret_cast<const s16x8 *>(dp + 16 * s + 8 * h);
         const s16x8 of = *reinterpret_cast<const s16x8 *>(op + 16 * s + 8 * h);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          D = fmaf(E::widen((uint16_t)df[s][i]), E::widen((uint16_t)of[i]), D);
+          D = fmaf(E::widen((uint16_t)d[i]), E::widen((uint16_t)of[i]), D);
       }
+      if constexpr (kHeldHere)
+        df[s] = d;
+      else if (group == 0)
+        mine[s * OPA_WAVE] = d;
     }
     D = half_sum(D);
     if (live) {
       // a query that sees nothing has weights 0: exp2(x - inf)
       const float lse = a.lse[(int64_t)head * a.n_q + tok] * kLog2e;
-      L = lse == -INFINITY ? INFINITY : lse;
+      L = lse == -INFINITY ? INFINITY : lse - Scales<E>::kWeight;
     }
   }
-  const uint16_t *kp = a.k.p + (int64_t)sk.first * a.k.ts + (int64_t)hk * a.k.hs;
-  const uint16_t *vp = a.v.p + (int64_t)sk.first * a.v.ts + (int64_t)hk * a.v.hs;
+  const uint16_t *k0p = a.k.p + (int64_t)sk.first * a.k.ts + (int64_t)hk * a.k.hs;
+  const uint16_t *v0p = a.v.p + (int64_t)sk.first * a.v.ts + (int64_t)hk * a.v.hs;
   const float c = a.scale * kLog2e;
   const float up = Scales<E>::ds(a.norms, hk);
+  const float fw = exp2_fast(-Scales<E>::kWeight), upw = up * fw;
   const int nat0 = nat_place<DP>(), tr0 = tr_place<DP>();
-  f32x16 dq[DB];
+  f32x16 dq[DB], kp[DB];
 #pragma unroll
-  for (int d = 0; d < DB; ++d) dq[d] = (f32x16)(0.f);
+  for (int d = 0; d < DB; ++d) dq[d] = kp[d] = (f32x16)(0.f);
 
   const auto load = [&](uint16_t *k, uint16_t *v, int k0) __attribute__((always_inline)) {
-    tile_load<DP, kStepK, kGradWaves>(k, kp + k0 * a.k.ts, a.k.ts, sk.count - k0, a.head_dim,
+    tile_load<DP, kStepK, kGradWaves>(k, k0p + k0 * a.k.ts, a.k.ts, sk.count - k0, a.head_dim,
                                      wave);
-    tile_load<DP, kStepK, kGradWaves>(v, vp + k0 * a.v.ts, a.v.ts, sk.count - k0, a.head_dim,
+    tile_load<DP, kStepK, kGradWaves>(v, v0p + k0 * a.v.ts, a.v.ts, sk.count - k0, a.head_dim,
                                      wave);
   };
   const auto step = [&](const uint16_t *k, const uint16_t *v, int k0)
@@ -176,41 +188,36 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         x = E::mfma(nat_frag<DP>(k, nat, 32 * kb, s), qf[s], x);
-        y = E::mfma(nat_frag<DP>(v, nat, 32 * kb, s), df[s], y);
+        y = E::mfma(nat_frag<DP>(v, nat, 32 * kb, s),
+                    kHeldHere ? df[kHeldHere ? s : 0] : mine[s * OPA_WAVE], y);
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[e] = exp2_fast(fmaf(x[e], c, -L));
       if (cut) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (k0 + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3) >= seen) x[e] = y[e] = 0.f;
+          if (k0 + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3) >= seen) x[e] = 0.f;
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        exact = fmaf(x[e], y[e], exact);
-        x[e] *= (y[e] - D) * up;
+        y[e] = x[e] * (y[e] - D) * upw;
       }
 #pragma unroll
+      for (int e = 0; e < 16; e += 4) off += (y[e] + y[e + 1]) + (y[e + 2] + y[e + 3]);
+#pragma unroll
       for (int s = 0; s < 2; ++s) {
-        u32x4 w;
+        u32x4 wp, ws;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = E::pack(x[8 * s + 2 * i], x[8 * s + 2 * i + 1]);
-        const s16x8 sf = __builtin_bit_cast(s16x8, w);
-        // D' is off by out's rounding, which dq takes whole; what rounding ds
-        // loses is therefore added by a product of its own (dq's error against
-        // 64 bits, of values rounded to bfloat16 once: 1.65 times that without,
-        // 1.35 with; 6% of a training pass of 12 packed documents)
-        u32x4 u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          u[i] = E::pack(x[8 * s + 2 * i] - E::widen((uint16_t)w[i]),
-                         x[8 * s + 2 * i + 1] - E::widen((uint16_t)(w[i] >> 16)));
-        const s16x8 sl = __builtin_bit_cast(s16x8, u);
+        for (int i = 0; i < 4; ++i) {
+          wp[i] = E::pack(x[8 * s + 2 * i], x[8 * s + 2 * i + 1]);
+          ws[i] = E::pack(y[8 * s + 2 * i], y[8 * s + 2 * i + 1]);
+        }
+        const s16x8 pf = __builtin_bit_cast(s16x8, wp), sf = __builtin_bit_cast(s16x8, ws);
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
           const s16x8 kt = tr_frag<DP>(k, tr, 32 * kb + 16 * s, d);
           dq[d] = E::mfma(kt, sf, dq[d]);
-          dq[d] = E::mfma(kt, sl, dq[d]);
+          kp[d] = E::mfma(kt, pf, kp[d]);
         }
       }
     }
@@ -225,24 +232,33 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
         step(i == 0 ? tk0[group] : tk1[group], i == 0 ? tv0[group] : tv1[group],
              (t * G + group) * kStepK);
       });
-  if constexpr (G > 1) {
-    // the second group's sums into the first's: a part of dq in each of the four
-    // tiles' places, one after the other
+  off = half_sum(off);
+  const int t = threadIdx.x % (kGradWaves * OPA_WAVE);
+  if constexpr (G > 1) {  // of both groups' keys
     static_assert(G == 2, "one other group");
+    __shared__ float sum[G][kGradWaves * OPA_WAVE];
+    sum[group][t] = off;
+    block_sync();
+    off = sum[0][t] + sum[1][t];
+  }
+  const float f = 1.f / up;
+  off *= f;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dq[d][i] = a.scale * (dq[d][i] * f - off * fw * kp[d][i]);
+  if constexpr (G > 1) {
+    // the second group's dq to the first's: a part in each of the four tiles' places
     constexpr int kEach = G * kTile * 2 / 16 / (kGradWaves * OPA_WAVE);  // pieces a lane
     static_assert(4 * kEach >= DB * 4, "they fit");
-    const int t = threadIdx.x % (kGradWaves * OPA_WAVE);
     f32x4 *const at[4] = {reinterpret_cast<f32x4 *>(tk0[0]), reinterpret_cast<f32x4 *>(tk1[0]),
                           reinterpret_cast<f32x4 *>(tv0[0]), reinterpret_cast<f32x4 *>(tv1[0])};
-    __shared__ float other[kGradWaves * OPA_WAVE];
-    block_sync();
     if (group) {
 #pragma unroll
       for (int i = 0; i < DB * 4; ++i)
         at[i / kEach][i % kEach * kGradWaves * OPA_WAVE + t] =
             f32x4{dq[i / 4][i % 4 * 4], dq[i / 4][i % 4 * 4 + 1], dq[i / 4][i % 4 * 4 + 2],
                   dq[i / 4][i % 4 * 4 + 3]};
-      other[t] = exact;
     }
     block_sync();
     if (group) return;
@@ -252,23 +268,20 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
 #pragma unroll
       for (int e = 0; e < 4; ++e) dq[i / 4][i % 4 * 4 + e] += v[e];
     }
-    exact += other[t];
   }
-  exact = half_sum(exact);
   if (!live) return;
   if (h == 0) {
     const int64_t at = (int64_t)head * a.n_q + sq.first + qrow;
-    *reinterpret_cast<f32x2 *>(a.rows + 2 * at) = f32x2{L - Scales<E>::kWeight, exact};
+    *reinterpret_cast<f32x2 *>(a.rows + 2 * at) = f32x2{L, D + off};
   }
-  const float f = a.scale / up;
   uint16_t *op = a.dq.p + (int64_t)(sq.first + qrow) * a.dq.ts + (int64_t)head * a.dq.hs;
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const int col = 32 * d + 8 * g + 4 * h;
-      const u32x2 w = {E::pack(dq[d][4 * g] * f, dq[d][4 * g + 1] * f),
-                       E::pack(dq[d][4 * g + 2] * f, dq[d][4 * g + 3] * f)};
+      const u32x2 w = {E::pack(dq[d][4 * g], dq[d][4 * g + 1]),
+                       E::pack(dq[d][4 * g + 2], dq[d][4 * g + 3])};
       if (col < a.head_dim) *reinterpret_cast<u32x2 *>(op + col) = w;
     }
 }
