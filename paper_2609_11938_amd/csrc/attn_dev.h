@@ -244,6 +244,18 @@ __device__ __forceinline__ Span span_of(const int32_t *cu, int b, int n) {
   return {s, e - s};
 }
 
+// Inclusive sum over the wave, in data-parallel-primitive moves: by shifts inside
+// rows of 16 lanes, then the last lane of a row to the next, and of 32 to the others.
+__device__ __forceinline__ int wave_sums(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
+  return x;
+}
+
 // Tile `tile` of the tiles of `rows` rows that the sequences of `cu` have: which
 // of the sequence's tiles it is, and the sequence's spans in both offset arrays;
 // false past the last. By whole waves; the result is uniform. Each lane loads a
@@ -256,12 +268,7 @@ __device__ __forceinline__ bool find_tile(const int32_t *cu, int n, const int32_
     const int b = base + lane < n_seqs ? base + lane : n_seqs - 1;
     const Span x = span_of(cu, b, n), y = span_of(other, b, n_other);
     const int tiles = base + lane < n_seqs ? (x.count + rows - 1) / rows : 0;
-    int inc = tiles;
-#pragma unroll
-    for (int d = 1; d < OPA_WAVE; d <<= 1) {
-      const int o = __shfl_up(inc, d);
-      if (lane >= d) inc += o;
-    }
+    const int inc = wave_sums(tiles);
     const uint64_t m = __ballot(inc > tile);
     if (m) {
       const int w = __ffsll((unsigned long long)m) - 1;

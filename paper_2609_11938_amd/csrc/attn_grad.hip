@@ -88,7 +88,7 @@ __global__ void k_attn_zero(uint32_t *p, int n) {
 
 // Two groups of waves share the keys where the blocks are this few (one sequence
 // of 6000, 4 heads, 192 blocks: a training pass of 378 us with one, 340 with two).
-constexpr int kFewBlocks = 256;
+constexpr int kFewBlocks = 256, kManyKeys = 768;
 
 // dq of 32 queries a wave: S^T = K Q^T with the wave's queries as columns;
 // dS^T then is the B operand of dq^T = K^T dS^T. The pass goes by D' = dout . out,
@@ -518,7 +518,7 @@ static void launch(const PromptArgs &a, hipStream_t s) {
   const int64_t kt = (int64_t)a.n_k / kHeld + a.n_seqs, qt = (int64_t)a.n_q / kHeld + a.n_seqs;
   const dim3 block(kGradWaves * OPA_WAVE);
   const dim3 rows((uint32_t)(qt * a.n_heads));
-  if (a.n_q > 0 && qt * a.n_heads <= kFewBlocks)
+  if (a.n_q > 0 && qt * a.n_heads <= kFewBlocks && a.n_k >= (int64_t)kManyKeys * a.n_seqs)
     hipLaunchKernelGGL((k_attn_dq<E, DP, 2>), rows, dim3(2 * kGradWaves * OPA_WAVE), 0, s, a);
   else if (a.n_q > 0)
     hipLaunchKernelGGL((k_attn_dq<E, DP, 1>), rows, block, 0, s, a);

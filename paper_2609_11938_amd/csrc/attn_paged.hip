@@ -55,12 +55,7 @@ __device__ __forceinline__ bool find_share(const PagedArgs &a, int item, Share &
     const int b = base + lane;
     const int len = base ? paged_len(a, b) : mine;
     const int n = b < a.n_seqs ? shares_of(len, s.size) : 0;
-    int inc = n;
-#pragma unroll
-    for (int d = 1; d < OPA_WAVE; d <<= 1) {
-      const int o = __shfl_up(inc, d);
-      if (lane >= d) inc += o;
-    }
+    const int inc = wave_sums(n);
     const uint64_t m = __ballot(done + inc > item);
     if (m) {
       const int w = __ffsll((unsigned long long)m) - 1;
@@ -85,9 +80,7 @@ __device__ __forceinline__ Share shares_at(const PagedArgs &a, int seq) {
   s.len = uniform(paged_len(a, seq));
   int sum = lane < seq ? shares_of(mine, s.size) : 0;
   for (int b = OPA_WAVE + lane; b < seq; b += OPA_WAVE) sum += shares_of(paged_len(a, b), s.size);
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-  s.first = uniform(sum);
+  s.first = __builtin_amdgcn_readlane(wave_sums(sum), OPA_WAVE - 1);
   return s;
 }
 

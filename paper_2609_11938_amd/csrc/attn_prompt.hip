@@ -9,8 +9,9 @@ constexpr int kRowsQ = 32 * kWaves;
 constexpr int kRowsK = 64;      // keys a tile
 
 // (one sequence of 6000, 4 heads, 192 blocks: 107 us with one group, 85 with two;
-// 3 of 1500, 16 heads, 608 blocks: 48 and 55)
-constexpr int kFewBlocks = 384;
+// 3 of 1500, 16 heads, 608 blocks: 48 and 55; 4 of 128, where there is a tile for
+// each group: 6.9 and 7.6)
+constexpr int kFewBlocks = 384, kManyKeys = 768;
 
 // G groups of kWaves waves take the key tiles in turn and join their sums at the
 // end: the waves that a few rows would leave a compute unit without.
@@ -248,7 +249,7 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
 template <class E, int DP>
 static void launch(const PromptArgs &a, hipStream_t s) {
   const int64_t blocks = ((int64_t)a.n_q / kRowsQ + a.n_seqs) * a.n_heads;
-  if (blocks <= kFewBlocks)
+  if (blocks <= kFewBlocks && a.n_k >= (int64_t)kManyKeys * a.n_seqs)
     hipLaunchKernelGGL((k_attn_prompt<E, DP, 2>), dim3((uint32_t)blocks),
                        dim3(2 * kWaves * OPA_WAVE), 0, s, a);
   else

@@ -89,12 +89,7 @@ template <int kT>
 __device__ __forceinline__ int block_scan(int x, int &total) {
   __shared__ int part[kT / OPA_WAVE];
   const int lane = lane_id(), wave = wave_id();
-  int inc = x;
-#pragma unroll
-  for (int d = 1; d < OPA_WAVE; d <<= 1) {
-    const int o = __shfl_up(inc, d);
-    if (lane >= d) inc += o;
-  }
+  const int inc = wave_sums(x);
   if (lane == OPA_WAVE - 1) part[wave] = inc;
   __syncthreads();
   int before = 0, all = 0;
@@ -283,14 +278,20 @@ __global__ __launch_bounds__(kThreads) void k_fork(PagesArgs a) {
   __shared__ int sums[kHow == kSums ? 1 : kMost / 32 + 1];
   __shared__ int rows[kHow == kSums ? 1 : kRows + 1];
   __shared__ int refs[kHow == kSelf ? kMost : 1];
+  __shared__ ForkRow row_info[kHow == kSelf ? kRows : 1];
+  const auto row_of = [&](int i) { return kHow == kSelf ? row_info[i] : fork_row(a, i); };
+  if (kHow == kSelf) {  // every row's facts, once
+    for (int i = threadIdx.x; i < a.n_out; i += kThreads) row_info[i] = fork_row(a, i);
+    __syncthreads();
+  }
   const bool copier = (int)blockIdx.x >= a.give;
   const int mine = copier ? ((int)blockIdx.x - a.give) / a.copy_planes : 0;
   if (copier) {  // a row without a part-filled page, or the first of its parent, copies none
-    const ForkRow r = fork_row(a, mine);
+    const ForkRow r = row_of(mine);
     if (!r.part) return;
     int e = 0;
     if (kHow == kSelf) {
-      for (int j = threadIdx.x; j < mine; j += kThreads) e |= a.parent[j] == r.parent;
+      for (int j = threadIdx.x; j < mine; j += kThreads) e |= row_info[j].parent == r.parent;
       e = __syncthreads_or(e);
     } else {
       const int asks = kHow == kSums ? a.row_at[mine + 1] - a.row_at[mine] : a.row_at[mine];
@@ -312,10 +313,10 @@ __global__ __launch_bounds__(kThreads) void k_fork(PagesArgs a) {
       if (count)
         for (int x = threadIdx.x; x < a.n_pages; x += kThreads) refs[x] = a.held ? a.held[x] : 0;
       for (int i = threadIdx.x; i < a.n_out; i += kThreads) {
-        const ForkRow r = fork_row(a, i);
+        const ForkRow r = row_info[i];
         bool e = false;
         if (r.part)
-          for (int j = 0; j < i; ++j) e |= a.parent[j] == r.parent;
+          for (int j = 0; j < i; ++j) e |= row_info[j].parent == r.parent;
         rows[i] = r.want - r.full - (r.part && !e);
         if (count) {
           const int bad = fork_row_bad(a, i, r);
@@ -325,7 +326,7 @@ __global__ __launch_bounds__(kThreads) void k_fork(PagesArgs a) {
       __syncthreads();
       int bad = 0;
       for (int i = threadIdx.x / OPA_WAVE; i < a.n_out; i += kThreads / OPA_WAVE) {
-        const ForkRow r = fork_row(a, i);
+        const ForkRow r = row_of(i);
         for (int s = lane_id(); s < r.want - rows[i]; s += OPA_WAVE) {
           const int id = kept_page(a, r, s);
           if (id < 0) {
@@ -346,7 +347,7 @@ __global__ __launch_bounds__(kThreads) void k_fork(PagesArgs a) {
   }
   const int free = free_pages(b), wanted = row_at[a.n_out];
   if (copier) {
-    const ForkRow r = fork_row(a, mine);
+    const ForkRow r = row_of(mine);
     if (row_at[mine] >= free) return;
     const int x = kept_page(a, r, r.full), y = nth_page<false>(b, row_at[mine]);
     if (x < 0) return;
@@ -358,14 +359,14 @@ __global__ __launch_bounds__(kThreads) void k_fork(PagesArgs a) {
   const int64_t from = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   for (int64_t at = from; at < (int64_t)a.n_out * a.width; at += step) {
     const int i = (int)(at / a.width), s = (int)(at - (int64_t)i * a.width);
-    const ForkRow r = fork_row(a, i);
+    const ForkRow r = row_of(i);
     const int kept = r.want - (row_at[i + 1] - row_at[i]), k = row_at[i] + s - kept;
     a.table_out[at] = s < kept                  ? kept_page(a, r, s)
                       : s < r.want && k < free ? nth_page<false>(b, k)
                                                : -1;
   }
   for (int64_t i = from; i < a.n_out; i += step) {
-    const ForkRow r = fork_row(a, (int)i);
+    const ForkRow r = row_of((int)i);
     const bool copy = r.part && r.want - (row_at[i + 1] - row_at[i]) == r.full;
     a.lens_out[i] = copy && row_at[i] >= free ? r.full * a.size : r.n;
   }

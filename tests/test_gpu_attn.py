@@ -215,6 +215,20 @@ def test_prompt_masked_values_do_not_matter(what):
         assert torch.equal(t[100:240], u)
 
 
+def test_prompt_masked_values_do_not_matter_over_many_keys():
+    """As above, where two groups of waves share a row's keys."""
+    torch = _torch()
+    s = _prompt([900], [900], 2, 1, 64, True, "float16")
+    _, lse, want = _check_prompt(s, grad=False)
+    for row in (70, 513, 899):
+        k, v = s["k"].clone(), s["v"].clone()
+        k[row] = v[row] = float("nan")
+        got, gl = attn.opattr_attn_prompt(s["q"], k, v, s["cu_q"], s["cu_k"], causal=True,
+                                          scale=s["scale"])
+        _within(got[:row], tuple(t[:row] for t in want["out"]), f"out before {row}")
+        assert torch.equal(gl[:, :row], lse[:, :row]) and torch.isnan(got[row:]).all()
+
+
 def test_prompt_bad_offsets_are_flagged():
     torch = _torch()
     s = _prompt([60, 40], [60, 40], 2, 1, 64, True, "bfloat16")
