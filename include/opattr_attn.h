@@ -33,8 +33,11 @@
  *
  * A query that sees no key (an empty sequence, or a causal mask that hides all
  * of them) has output 0, row statistic -inf, and gives and takes no gradient.
- * Keys and values that no query of their sequence may see are never used,
- * whatever their bits; a NaN or an infinity in a masked score is masked too.
+ * What a query does not see takes no part in its output, whatever its bits: rows
+ * beside a sequence, tokens past a length, keys and values that the causal mask
+ * hides, NaN and infinities among them. The gradient is defined for finite
+ * inputs: in a sequence that holds others, also rows that do not see them may
+ * become NaN.
  */
 #ifndef OPATTR_ATTN_H
 #define OPATTR_ATTN_H
@@ -92,7 +95,7 @@ int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
 /* One layer's paged cache: key (value) head g of token t of page x is at
    k (v) + x page_stride + t token_stride + g head_stride (elements, the same
    for both; 16-byte aligned, multiples of 8). page_size is a power of two
-   in [1, 1024]; token n of sequence b is on page table[b * table_stride + n /
+   in [1, 1024], a table names fewer than 2^30 tokens; token n of sequence b is on page table[b * table_stride + n /
    page_size], slot n % page_size. */
 typedef struct {
   void *k, *v;
@@ -149,8 +152,8 @@ typedef struct {
    refs (or NULL) [n_pages] receives the references from table_out and held.
    When the free pages run out the remaining entries are -1, LIMIT is flagged,
    and a row whose copy got no page ends at its full pages. A parent out of
-   range reads as -1 and a kept entry out of range becomes -1, both flagged
-   DATA. table and table_out are [rows][width]; they, lens and lens_out do not
+   range reads as -1, a kept entry out of range becomes -1, a length or room
+   past what the table can name is cut; all flagged DATA. table and table_out are [rows][width]; they, lens and lens_out do not
    overlap. */
 size_t opattr_pages_fork_workspace_bytes(int32_t n_rows, int32_t n_out, int32_t width,
                                          int32_t n_pages);

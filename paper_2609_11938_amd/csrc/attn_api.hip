@@ -70,7 +70,7 @@ static bool ok_pages(const opattr_kv_pages *c) {
       !ok_type(c->dtype) || !ok_heads(c->n_kv_heads, c->n_kv_heads, c->head_dim))
     return false;
   if (c->n_seqs > 0 && c->table_stride > 0 && !c->table) return false;
-  if ((int64_t)c->table_stride * c->page_size >= (int64_t)1 << 31) return false;
+  if ((int64_t)c->table_stride * c->page_size >= (int64_t)1 << 30) return false;
   if (c->n_pages == 0) return true;
   const int64_t most = (int64_t)1 << 40;
   return c->k && c->v && (((uintptr_t)c->k | (uintptr_t)c->v) & 15) == 0 &&

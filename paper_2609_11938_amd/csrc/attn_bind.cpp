@@ -10,6 +10,7 @@
 // when `ws` is None or smaller; otherwise None.
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 
 #include <cmath>
@@ -163,6 +164,7 @@ opattr_attn_shape shape(const at::Tensor &q, PyObject *ko, PyObject *cu_q, PyObj
 // q k v cu_q cu_k causal scale out lse diag stream
 PyObject *attn_prompt(PyObject *const *o) {
   const at::Tensor &q = tensor(o[0], "q");
+  const c10::DeviceGuard on(q.device());
   const opattr_attn_shape a = shape(q, o[1], o[3], o[4], o[5], o[6]);
   const int64_t h = a.n_heads, g = a.n_kv_heads, d = a.head_dim;
   const opattr_rows rq = rows(o[0], q, a.n_q, h, d, "q"), rk = rows(o[1], q, a.n_k, g, d, "k"),
@@ -176,6 +178,7 @@ PyObject *attn_prompt(PyObject *const *o) {
 // dout q k v out lse cu_q cu_k causal scale dq dk dv ws diag stream
 PyObject *attn_prompt_grad(PyObject *const *o) {
   const at::Tensor &q = tensor(o[1], "q");
+  const c10::DeviceGuard on(q.device());
   const opattr_attn_shape a = shape(q, o[2], o[6], o[7], o[8], o[9]);
   const int64_t h = a.n_heads, g = a.n_kv_heads, d = a.head_dim;
   const opattr_rows rd = rows(o[0], q, a.n_q, h, d, "dout"), rq = rows(o[1], q, a.n_q, h, d, "q"),
@@ -223,6 +226,7 @@ opattr_kv_pages kv_pages(PyObject *ko, PyObject *vo, PyObject *to) {
 // q k_pages v_pages table lens scale out lse ws diag stream
 PyObject *attn_paged(PyObject *const *o) {
   const at::Tensor &q = tensor(o[0], "q");
+  const c10::DeviceGuard on(q.device());
   const opattr_kv_pages c = kv_pages(o[1], o[2], o[3]);
   if (q.dim() != 3) throw ValueError("q is [sequences, heads, head_dim]");
   alike(q, THPVariable_Unpack(o[1]), "q");
@@ -241,6 +245,7 @@ PyObject *attn_paged(PyObject *const *o) {
 // k_new v_new cu k_pages v_pages table lens lens_out diag stream
 PyObject *kv_append(PyObject *const *o) {
   const at::Tensor &k = tensor(o[0], "k_new"), &cache = tensor(o[3], "k_pages");
+  const c10::DeviceGuard on(cache.device());
   const opattr_kv_pages c = kv_pages(o[3], o[4], o[5]);
   const int64_t b = c.n_seqs, n = k.dim() ? k.size(0) : 0;
   const opattr_rows rk = rows(o[0], cache, n, c.n_kv_heads, c.head_dim, "k_new"),
@@ -280,6 +285,7 @@ PyObject *pages_fork(PyObject *const *o) {
                    &parent = tensor(o[4], "parent");
   if (table.dim() != 2 || parent.dim() != 1)
     throw ValueError("table is [rows, entries], parent [rows of the next table]");
+  const c10::DeviceGuard on(pool.device());
   const opattr_page_pool p = page_pool(pool, integer(o[1]), o[6]);
   const int64_t rows = table.size(0), width = table.size(1), n = parent.size(0);
   const Work ws(o[10]);
@@ -301,6 +307,7 @@ PyObject *pages_fork(PyObject *const *o) {
 PyObject *pages_compact(PyObject *const *o) {
   const at::Tensor &pool = tensor(o[0], "pool"), &table = tensor(o[1], "table");
   if (table.dim() != 2) throw ValueError("table is [rows, entries]");
+  const c10::DeviceGuard on(pool.device());
   const opattr_page_pool p = page_pool(pool, 1, o[2]);
   const int64_t rows = table.size(0), width = table.size(1);
   const Work ws(o[6]);

@@ -42,7 +42,7 @@ __device__ __forceinline__ int share_size(const PagedArgs &a, int mine) {
   const int64_t each = (sum * a.n_kv + kBlocks - 1) / kBlocks;
   const int64_t c = (each + kTile * kPagedWaves - 1) / (kTile * kPagedWaves) *
                     (kTile * kPagedWaves);
-  return uniform((int)(c < kMinShare ? kMinShare : c));
+  return uniform((int)(c < kMinShare ? kMinShare : c < 1 << 30 ? c : 1 << 30));
 }
 
 // Share `item` of all the sequences' shares; false past the last. By whole waves.
