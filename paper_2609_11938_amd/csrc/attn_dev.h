@@ -184,6 +184,34 @@ __device__ __forceinline__ void tile_load(uint16_t *tile, const uint16_t *src, i
   }
 }
 
+// 32 rows that a wave holds as columns (row l % 32 in lane l, values 32 d + 8 g +
+// 4 h .. + 3 as elements 4 g .. of acc[d]), scaled and rounded, to rows of `out`,
+// `left` of which exist: through the wave's own 32 * DP values of LDS, so that
+// whole rows are written together (from the registers, 16 bytes of 32 rows a store:
+// 16 prompts of 1024 tokens, head_dim 128: 111 us that way, 104 this).
+template <class E, int DP>
+__device__ __forceinline__ void store_rows(uint16_t *lds, const f32x16 (&acc)[DP / 32], float f,
+                                           uint16_t *out, int64_t ts, int left, int head_dim) {
+  constexpr int C = DP / 8;
+  const int l = lane_id(), r = l & 31, h = l >> 5;
+  char *const at = reinterpret_cast<char *>(lds);
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<u32x2 *>(at + r * DP * 2 + (((4 * d + g) ^ swz<DP>(r)) << 4) + h * 8) =
+          u32x2{E::pack(acc[d][4 * g] * f, acc[d][4 * g + 1] * f),
+                E::pack(acc[d][4 * g + 2] * f, acc[d][4 * g + 3] * f)};
+#pragma unroll
+  for (int i = 0; i < 32 * C / OPA_WAVE; ++i) {
+    const int id = i * OPA_WAVE + l, row = id / C, c = id % C;
+    const u32x4 v =
+        *reinterpret_cast<const u32x4 *>(at + row * DP * 2 + ((c ^ swz<DP>(row)) << 4));
+    if (row < left && c * 8 < head_dim)
+      *reinterpret_cast<u32x4 *>(out + row * ts + c * 8) = v;
+  }
+}
+
 // The wave's loads have arrived (also those straight to LDS). As the builtin, so
 // that the compiler knows it too and does not wait again.
 __device__ __forceinline__ void wait_loads() {

@@ -261,29 +261,30 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
                   dq[i / 4][i % 4 * 4 + 3]};
     }
     block_sync();
-    if (group) return;
+    if (group == 0) {
 #pragma unroll
-    for (int i = 0; i < DB * 4; ++i) {
-      const f32x4 v = at[i / kEach][i % kEach * kGradWaves * OPA_WAVE + t];
+      for (int i = 0; i < DB * 4; ++i) {
+        const f32x4 v = at[i / kEach][i % kEach * kGradWaves * OPA_WAVE + t];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) dq[i / 4][i % 4 * 4 + e] += v[e];
+        for (int e = 0; e < 4; ++e) dq[i / 4][i % 4 * 4 + e] += v[e];
+      }
     }
   }
-  if (!live) return;
-  if (h == 0) {
+  if (group == 0 && live && h == 0) {
     const int64_t at = (int64_t)head * a.n_q + sq.first + qrow;
     *reinterpret_cast<f32x2 *>(a.rows + 2 * at) = f32x2{L, D + off};
   }
-  uint16_t *op = a.dq.p + (int64_t)(sq.first + qrow) * a.dq.ts + (int64_t)head * a.dq.hs;
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int col = 32 * d + 8 * g + 4 * h;
-      const u32x2 w = {E::pack(dq[d][4 * g], dq[d][4 * g + 1]),
-                       E::pack(dq[d][4 * g + 2], dq[d][4 * g + 3])};
-      if (col < a.head_dim) *reinterpret_cast<u32x2 *>(op + col) = w;
-    }
+  block_sync();  // the tiles' last readers are done
+  if (group) return;
+  constexpr int kFit = G * kTile / (32 * DP);  // waves' rows in one tile's place
+  uint16_t *const place = wave / kFit == 0 ? tk0[0]
+                          : wave / kFit == 1 ? tk1[0]
+                          : wave / kFit == 2 ? tv0[0]
+                                             : tv1[0];
+  store_rows<E, DP>(place + wave % kFit * 32 * DP, dq, 1.f,
+                    a.dq.p + (int64_t)(sq.first + q0 + wave * 32) * a.dq.ts +
+                        (int64_t)head * a.dq.hs,
+                    a.dq.ts, sq.count - q0 - wave * 32, a.head_dim);
 }
 
 // 32 pairs (lse, D) from p to LDS, past `left` of them zero; by a whole wave.
@@ -444,11 +445,10 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
       [&](auto i, int t) __attribute__((always_inline)) {
         step(i == 0 ? tq0 : tq1, i == 0 ? td0 : td1, i == 0 ? ts0 : ts1, first + t);
       });
-  if (!live) return;
   const float fk = a.scale / up;
-  const int64_t tok = sk.first + key;
   if (splits > 1) {  // [splits][n_k][n_kv][dk, dv][DP]
-    float *p = a.part + (((int64_t)split * a.n_k + tok) * a.n_kv + hk) * 2 * DP;
+    if (!live) return;
+    float *p = a.part + (((int64_t)split * a.n_k + sk.first + key) * a.n_kv + hk) * 2 * DP;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -465,21 +465,17 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
       }
     return;
   }
-  uint16_t *kp = a.dk.p + tok * a.dk.ts + (int64_t)hk * a.dk.hs;
-  uint16_t *vp = a.dv.p + tok * a.dv.ts + (int64_t)hk * a.dv.hs;
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int col = 32 * d + 8 * g + 4 * h;
-      if (col >= a.head_dim) continue;
-      const u32x2 w = {E::pack(dk[d][4 * g] * fk, dk[d][4 * g + 1] * fk),
-                       E::pack(dk[d][4 * g + 2] * fk, dk[d][4 * g + 3] * fk)};
-      const u32x2 u = {E::pack(dv[d][4 * g] * fv, dv[d][4 * g + 1] * fv),
-                       E::pack(dv[d][4 * g + 2] * fv, dv[d][4 * g + 3] * fv)};
-      *reinterpret_cast<u32x2 *>(kp + col) = w;
-      *reinterpret_cast<u32x2 *>(vp + col) = u;
-    }
+  block_sync();  // the tiles' last readers are done
+  constexpr int kFit = kTile / (32 * DP);  // waves' rows in one tile's place
+  uint16_t *const place = (wave / kFit == 0 ? tq0 : wave / kFit == 1 ? tq1
+                                                  : wave / kFit == 2 ? td0
+                                                                     : td1) +
+                          wave % kFit * 32 * DP;
+  const int64_t tok = sk.first + key0;
+  store_rows<E, DP>(place, dk, fk, a.dk.p + tok * a.dk.ts + (int64_t)hk * a.dk.hs, a.dk.ts,
+                    sk.count - key0, a.head_dim);
+  store_rows<E, DP>(place, dv, fv, a.dv.p + tok * a.dv.ts + (int64_t)hk * a.dv.hs, a.dv.ts,
+                    sk.count - key0, a.head_dim);
 }
 
 // A key tile's dk and dv from those of its blocks, added in order; a tile of one

@@ -227,21 +227,15 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
       if constexpr (G > 1) join();
     }
   }
-  if (group) return;
   l = half_sum(l);
-  if (!live) return;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint16_t *op = a.out.p + (int64_t)(sq.first + qrow) * a.out.ts + (int64_t)head * a.out.hs;
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int col = 32 * d + 8 * g + 4 * h;
-      const u32x2 w = {E::pack(o[d][4 * g] * inv, o[d][4 * g + 1] * inv),
-                       E::pack(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv)};
-      if (col < a.head_dim) *reinterpret_cast<u32x2 *>(op + col) = w;
-    }
-  if (a.lse && h == 0)
+  block_sync();  // the tiles' last readers are done
+  if (group) return;
+  store_rows<E, DP>((wave < 2 ? tk0[0] : tk1[0]) + wave % 2 * (kTile / 2), o,
+                    l == 0.f ? 0.f : 1.f / l,
+                    a.out.p + (int64_t)(sq.first + q0 + wave * 32) * a.out.ts +
+                        (int64_t)head * a.out.hs,
+                    a.out.ts, sq.count - q0 - wave * 32, a.head_dim);
+  if (a.lse && live && h == 0)
     a.lse[(int64_t)head * a.n_q + sq.first + qrow] =
         l == 0.f ? -INFINITY : (m * c + log2f(l) - E::kShift) * kLn2;
 }
