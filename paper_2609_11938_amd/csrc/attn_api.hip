@@ -152,7 +152,7 @@ size_t opattr_attn_prompt_grad_workspace_bytes(const opattr_attn_shape *a) {
   const size_t dp = a->head_dim <= 64 ? 64 : 128;
   const int n = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads);
   return align256((size_t)a->n_q * a->n_heads * 8) + align256((size_t)a->n_kv_heads * 8) +
-         (n > 1 ? (size_t)n * a->n_k * a->n_kv_heads * 2 * dp * 4 : 0);
+         (n > 1 ? (size_t)n * (a->n_k / 128 + a->n_seqs) * 128 * a->n_kv_heads * 2 * dp * 4 : 0);
 }
 
 int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,

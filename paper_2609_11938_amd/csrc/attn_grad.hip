@@ -317,6 +317,16 @@ __device__ __forceinline__ int tile_splits(const PromptArgs &a, const Span &sq, 
   return clamp_to((steps + kSplitSteps - 1) / kSplitSteps, 1, a.splits);
 }
 
+// Where a wave of one of a tile's blocks leaves its dk and dv, as its registers hold
+// them: [splits][tiles][n_kv][waves][dk, dv][DP / 8][64 lanes] of four values.
+template <int DP>
+__device__ __forceinline__ f32x4 *part_of(const PromptArgs &a, int split, int tile, int hk,
+                                          int wave) {
+  const int64_t tiles = a.n_k / kHeld + a.n_seqs;
+  const int64_t at = ((split * tiles + tile) * a.n_kv + hk) * kGradWaves + wave;
+  return reinterpret_cast<f32x4 *>(a.part) + at * (2 * DP / 8 * OPA_WAVE) + lane_id();
+}
+
 // dk and dv of 32 keys a wave: S = Q K^T with the wave's keys as columns, so
 // that a lane holds one key; P and dS then are the B operands of
 // dv^T = dout^T P and dk^T = q^T dS.
@@ -446,22 +456,20 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
         step(i == 0 ? tq0 : tq1, i == 0 ? td0 : td1, i == 0 ? ts0 : ts1, first + t);
       });
   const float fk = a.scale / up;
-  if (splits > 1) {  // [splits][n_k][n_kv][dk, dv][DP]
-    if (!live) return;
-    float *p = a.part + (((int64_t)split * a.n_k + sk.first + key) * a.n_kv + hk) * 2 * DP;
+  if (splits > 1) {
+    f32x4 *p = part_of<DP>(a, split, id / a.splits, hk, wave);
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const int col = 32 * d + 8 * g + 4 * h;
         f32x4 x, y;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           x[i] = dk[d][4 * g + i] * fk;
           y[i] = dv[d][4 * g + i] * fv;
         }
-        *reinterpret_cast<f32x4 *>(p + col) = x;
-        *reinterpret_cast<f32x4 *>(p + DP + col) = y;
+        p[(4 * d + g) * OPA_WAVE] = x;
+        p[(4 * DB + 4 * d + g) * OPA_WAVE] = y;
       }
     return;
   }
@@ -479,34 +487,35 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
 }
 
 // A key tile's dk and dv from those of its blocks, added in order; a tile of one
-// block is done already. kSumParts blocks a tile and key head.
-constexpr int kSumParts = 4;
+// block is done already. A wave takes dk or dv of 32 keys.
 template <class E, int DP>
-__global__ __launch_bounds__(256) void k_dkv_sum(PromptArgs a) {
-  constexpr int kRow = 2 * DP / 4;  // pieces of four values of a key: dk, dv
-  int id = blockIdx.x;
-  const int rows = id % kSumParts;
-  id /= kSumParts;
-  const int hk = id % a.n_kv;
+__global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArgs a) {
+  constexpr int DB = DP / 32;
+  __shared__ __align__(16) uint16_t rows[2 * kGradWaves][32 * DP];
+  const int hk = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv;
+  const int all = uniform(wave_id()), wave = all / 2, which = all % 2;
   Span sq, sk;
   int part;
-  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, id / a.n_kv, sk, sq, part)) return;
+  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part)) return;
   const int splits = tile_splits<DP>(a, sq, sk, part);
-  if (splits == 1) return;
-  const int64_t plane = (int64_t)a.n_k * a.n_kv * 2 * DP;
-  for (int i = threadIdx.x; i < kHeld / kSumParts * kRow; i += 256) {
-    const int key = part * kHeld + rows * (kHeld / kSumParts) + i / kRow;
-    const int at = i % kRow * 4, col = at % DP;
-    if (key >= sk.count || col >= a.head_dim) continue;
-    const int64_t tok = sk.first + key;
-    const float *p = a.part + (tok * a.n_kv + hk) * 2 * DP + at;
-    f32x4 sum = (f32x4)(0.f);
-#pragma unroll 4
-    for (int k = 0; k < splits; ++k) sum += *reinterpret_cast<const f32x4 *>(p + k * plane);
-    const Rows &o = at < DP ? a.dk : a.dv;
-    const u32x2 w = {E::pack(sum[0], sum[1]), E::pack(sum[2], sum[3])};
-    *reinterpret_cast<u32x2 *>(o.p + tok * o.ts + (int64_t)hk * o.hs + col) = w;
+  const int key0 = part * kHeld + wave * 32;
+  if (splits == 1 || key0 >= sk.count) return;
+  f32x16 sum[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) sum[d] = (f32x16)(0.f);
+  for (int k = 0; k < splits; ++k) {
+    const f32x4 *p = part_of<DP>(a, k, tile, hk, wave) + which * 4 * DB * OPA_WAVE;
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) {
+      const f32x4 v = p[i * OPA_WAVE];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[i / 4][i % 4 * 4 + e] += v[e];
+    }
   }
+  const Rows &o = which ? a.dv : a.dk;
+  store_rows<E, DP>(rows[all], sum, 1.f,
+                    o.p + (int64_t)(sk.first + key0) * o.ts + (int64_t)hk * o.hs, o.ts,
+                    sk.count - key0, a.head_dim);
 }
 
 template <class E, int DP>
@@ -522,8 +531,8 @@ static void launch(const PromptArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((k_attn_dkv<E, DP>), dim3((uint32_t)(kt * a.n_kv * a.splits)), block, 0, s,
                      a);
   if (a.splits > 1)
-    hipLaunchKernelGGL((k_dkv_sum<E, DP>), dim3((uint32_t)(kt * a.n_kv * kSumParts)), dim3(256),
-                       0, s, a);
+    hipLaunchKernelGGL((k_dkv_sum<E, DP>), dim3((uint32_t)(kt * a.n_kv)),
+                       dim3(2 * kGradWaves * OPA_WAVE), 0, s, a);
 }
 
 template <class E>
