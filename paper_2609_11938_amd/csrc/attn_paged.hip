@@ -4,7 +4,14 @@
 // query heads that read it (at most 16: the columns of a 16x16x32 product),
 // and its waves take tiles of 32 tokens in turn. Shares are equal but for a
 // sequence's last, of a size that makes about kBlocks blocks of all the work;
-// where a sequence has more than one, a second launch joins them in order.
+// where a sequence has more than one, a second launch joins them in order:
+// with a share's sums o_s = sum_j 2^(x_j - m_s) v_j, l_s = sum_j 2^(x_j - m_s),
+// out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s, m the largest m_s.
+//
+// Bound by the cache's bytes, each read once, with the next tile's keys and values in
+// registers and its pages a tile further: 2 sequences of 131000 tokens, 32 heads on 8
+// of 128: 192 us, 5.6 TB/s; 96 of up to 9001: 111 us, 4.9 TB/s, and 8 us for the join.
+// 4 of 150, 12 heads of 64: 5.5 us, the chain of length, table, keys and values.
 #include <limits.h>
 
 #include "attn_dev.h"

