@@ -52,19 +52,31 @@ struct Scales<F16> {
 
 // float16: the largest squared norms of dout's and v's rows (the bits of
 // non-negative floats order as integers, so the maximum is the same in any
-// order). A block takes kNormRows rows of one head: blockIdx.y is a query head,
-// and past those a key head. 4 lanes a row.
+// order), of the rows from the lowest offset to the highest: what lies beside the
+// sequences has no part in the scale. A block takes kNormRows rows of one head:
+// blockIdx.y is a query head, and past those a key head. 4 lanes a row.
 constexpr int kNormRows = 512;
 __global__ __launch_bounds__(256) void k_attn_norms(PromptArgs a) {
   __shared__ float most[4];
+  __shared__ int low, high;
   const int sub = threadIdx.x & 3;
   const bool q = (int)blockIdx.y < a.n_heads;
   const int head = q ? blockIdx.y : blockIdx.y - a.n_heads;
   const int n = q ? a.n_q : a.n_k;
   const Rows x = q ? a.dout : a.v;
+  const int32_t *cu = q ? a.cu_q : a.cu_k;
+  if (threadIdx.x == 0) low = n, high = 0;
+  __syncthreads();
+  for (int b = threadIdx.x; b <= a.n_seqs; b += blockDim.x) {
+    const int at = clamp_to(cu[b], 0, n);
+    atomicMin(&low, at);
+    atomicMax(&high, at);
+  }
+  __syncthreads();
   float top = 0.f;
   for (int64_t t = (int64_t)blockIdx.x * kNormRows + (threadIdx.x >> 2);
-       t < n && t < ((int64_t)blockIdx.x + 1) * kNormRows; t += 64) {
+       t < high && t < ((int64_t)blockIdx.x + 1) * kNormRows; t += 64) {
+    if (t < low) continue;
     const uint16_t *px = x.p + t * x.ts + (int64_t)head * x.hs;
     float norm = 0.f;
     for (int c = sub * 8; c < a.head_dim; c += 32) {

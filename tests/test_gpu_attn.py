@@ -215,6 +215,30 @@ def test_prompt_masked_values_do_not_matter(what):
         assert torch.equal(t[100:240], u)
 
 
+@pytest.mark.parametrize("what", [6e4, float("inf"), float("nan")])
+def test_prompt_grad_float16_rows_beside_sequences(what):
+    """The scale of float16's weights' gradients goes by the sequences' rows
+    alone: the same bits with other rows beside them."""
+    torch = _torch()
+    s = _prompt([70, 61], [70, 61], 4, 2, 64, True, "float16")
+    s["do"] *= 1e-3
+    out, lse = attn.opattr_attn_prompt(s["q"], s["k"], s["v"], s["cu_q"])
+    grads = attn.opattr_attn_prompt_grad(s["do"], s["q"], s["k"], s["v"], out, lse, s["cu_q"])
+
+    def wide(t):
+        w = torch.full((700,) + t.shape[1:], what, dtype=t.dtype, device=DEV)
+        w[520:651] = t
+        return w
+
+    args = [wide(s[n]) for n in "qkv"]
+    cu = s["cu_q"] + 520
+    out2, lse2 = attn.opattr_attn_prompt(*args, cu)
+    assert torch.equal(out2[520:651], out)
+    got = attn.opattr_attn_prompt_grad(wide(s["do"]), *args, out2, lse2, cu)
+    for name, t, u in zip(("dq", "dk", "dv"), got, grads):
+        assert torch.equal(t[520:651], u), name
+
+
 def test_prompt_masked_values_do_not_matter_over_many_keys():
     """As above, where two groups of waves share a row's keys."""
     torch = _torch()
