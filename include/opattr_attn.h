@@ -61,7 +61,8 @@ typedef struct {
    clamped and flagged DATA. Rows outside every sequence are not written.
    Query head h reads key head h / (n_heads / n_kv_heads). With causal, query i
    of a sequence sees key j when j <= i + (keys - queries): the last query sees
-   every key. scale multiplies q.k. */
+   every key. scale multiplies q.k. (max(n_q, n_k) / 128 + n_seqs) n_heads is
+   below 2^24. */
 typedef struct {
   int64_t n_q, n_k;
   const int32_t *cu_q, *cu_k;
@@ -95,8 +96,8 @@ int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
 /* One layer's paged cache: key (value) head g of token t of page x is at
    k (v) + x page_stride + t token_stride + g head_stride (elements, the same
    for both; 16-byte aligned, multiples of 8). page_size is a power of two
-   in [1, 1024], a table names fewer than 2^30 tokens; token n of sequence b is on page table[b * table_stride + n /
-   page_size], slot n % page_size. */
+   in [1, 1024], a table names fewer than 2^30 tokens; token n of sequence b is on
+   page table[b * table_stride + n / page_size], slot n % page_size. */
 typedef struct {
   void *k, *v;
   int64_t page_stride, token_stride, head_stride;
@@ -109,7 +110,7 @@ typedef struct {
 
 /* One query token a sequence: out[b] over the first lens[b] tokens of sequence
    b. q and out have n_seqs rows of n_heads heads (n_heads / n_kv_heads at most
-   16); lse (or NULL) receives [n_heads][n_seqs]. lens[b] is clamped to what the
+   16, n_seqs n_heads below 2^23); lse (or NULL) receives [n_heads][n_seqs]. lens[b] is clamped to what the
    table can name; tokens on a page outside [0, n_pages) are masked; both are
    flagged DATA. Partial results of a sequence's shares are joined in their
    order: the same bits on every run. */
@@ -118,7 +119,7 @@ int opattr_attn_paged(const opattr_kv_pages *c, int32_t n_heads, const opattr_ro
                       const int32_t *lens, float scale, const opattr_rows *out, float *lse,
                       opattr_diag *diag, void *ws, size_t ws_bytes, void *stream);
 
-/* Rows cu[b] .. cu[b+1]) of k_new and v_new (n_new rows) become tokens lens[b],
+/* Rows cu[b] .. cu[b+1]) of k_new and v_new (n_new rows, fewer than 2^26 - 4) become tokens lens[b],
    lens[b] + 1, ... of sequence b. lens_out (or NULL; not lens itself) receives
    lens[b] + (cu[b+1] - cu[b]). Tokens past the table's width or on a page
    outside [0, n_pages) are not written and flagged DATA; no two tokens may

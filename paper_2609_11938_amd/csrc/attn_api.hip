@@ -7,7 +7,8 @@ namespace opa {
 
 constexpr int64_t kMaxTokenStride = 1 << 22;
 constexpr int64_t kMaxHeadStride = (int64_t)1 << 40;
-constexpr int64_t kMaxGrid = 0x7fffffff;
+// a launch takes fewer than 2^32 threads: blocks of 256
+constexpr int64_t kMaxGrid = ((int64_t)1 << 24) - 1;
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -199,7 +200,7 @@ int opattr_attn_paged(const opattr_kv_pages *c, int32_t n_heads, const opattr_ro
   if (!ok_pages(c) || !ok_heads(n_heads, c->n_kv_heads, c->head_dim) ||
       n_heads / c->n_kv_heads > 16 || !isfinite(scale) ||
       !ok_rows(q, c->n_seqs, c->head_dim) || !ok_rows(out, c->n_seqs, c->head_dim) ||
-      (c->n_seqs > 0 && !lens) || (int64_t)c->n_seqs * n_heads > (int64_t)1 << 27)
+      (c->n_seqs > 0 && !lens) || (int64_t)c->n_seqs * n_heads > kMaxGrid / 2)
     return OPATTR_ERR_INVALID_ARG;
   if (!ok_ws(ws, ws_bytes, opattr_attn_paged_workspace_bytes(c, n_heads)))
     return OPATTR_ERR_WORKSPACE;
@@ -233,7 +234,7 @@ int opattr_attn_paged(const opattr_kv_pages *c, int32_t n_heads, const opattr_ro
 int opattr_kv_append(const opattr_kv_pages *c, int64_t n_new, const int32_t *cu,
                      const opattr_rows *k_new, const opattr_rows *v_new, const int32_t *lens,
                      int32_t *lens_out, opattr_diag *diag, void *stream) {
-  if (!ok_pages(c) || n_new < 0 || n_new >= (int64_t)1 << 30 ||
+  if (!ok_pages(c) || n_new < 0 || n_new > kMaxGrid * 4 ||
       !ok_rows(k_new, n_new, c->head_dim) || !ok_rows(v_new, n_new, c->head_dim) ||
       (c->n_seqs > 0 && (!cu || !lens)) || (lens_out && lens_out == lens))
     return OPATTR_ERR_INVALID_ARG;

@@ -388,6 +388,9 @@ static int blocks_for(int64_t n, int most) {
   return b < 1 ? 1 : b > most ? most : (int)b;
 }
 
+// a launch takes fewer than 2^32 threads
+constexpr int kMaxCopiers = 1 << 23;
+
 void run_fork(const PagesArgs &args, hipStream_t s) {
   PagesArgs a = args;
   const int64_t entries = (int64_t)a.n_out * a.width;
@@ -397,7 +400,8 @@ void run_fork(const PagesArgs &args, hipStream_t s) {
   // a table writer's setup is worth some entries; planes are shared out so that
   // a copy of many pages is many blocks, and its setup is paid a few times only
   a.give = blocks_for(entries / (self ? 2 : 4), self ? 16 : 256);
-  a.copy_planes = a.n_planes < 32 ? a.n_planes : 32;
+  const int each = a.n_out > 1 << 18 ? kMaxCopiers / a.n_out : 32;
+  a.copy_planes = a.n_planes < each ? a.n_planes : each;
   const int64_t blocks = a.give + (a.n_pages > 0 ? (int64_t)a.n_out * a.copy_planes : 0);
   if (!self) {
     hipLaunchKernelGGL(k_pages_start, dim3((a.n_pages + kThreads) / kThreads), dim3(kThreads), 0,

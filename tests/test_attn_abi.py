@@ -267,3 +267,16 @@ def test_oracle_bounds_fail_a_wrong_result():
             value, bound = good[name]
             value, bound = value[-len(bad[name][0]):], bound[-len(bad[name][0]):]
             assert (np.abs(bad[name][0] - value) > bound).any(), (what, name)
+
+
+def test_calls_past_one_launch_are_refused(lib):
+    """A launch takes fewer than 2^32 threads: what would need more is an
+    argument error, found before anything is enqueued."""
+    r = _rows()
+    a = _shape(n_heads=64, n_kv_heads=64, n_seqs=1 << 19)
+    assert lib.opattr_attn_prompt(a, r, r, r, r, FAKE, None, None) == INVALID
+    assert lib.opattr_attn_prompt_grad_workspace_bytes(a) == 0
+    c = _pages(n_seqs=1 << 19)
+    assert lib.opattr_attn_paged(c, 32, r, FAKE, 0.1, r, FAKE, None, FAKE, 1 << 30,
+                                 None) == INVALID
+    assert lib.opattr_kv_append(_pages(), 1 << 27, FAKE, r, r, FAKE, None, None, None) == INVALID
