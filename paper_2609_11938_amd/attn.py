@@ -111,26 +111,31 @@ def new_diag(device="cuda:0", stream=None):
     return opattr._new_diag(device, stream)
 
 
-def _on(stream, *made):
-    """The stream's handle, -1 for the current one. Tensors that a call made
-    itself belong to the current stream: one used on another is kept until that
-    has passed the call."""
-    if stream is None:
-        return -1
-    for t in made:
-        if t is not None:
+def _on(stream, call, *args, ws=None, **kw):
+    """The call with ``stream`` as the current one, so that what it allocates is
+    that stream's own: memory that the present stream still works on is not given
+    out. The memory of every tensor it uses is kept until the stream has passed
+    the call, that of its results also for the present stream."""
+    before = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        if ws is not None:
+            kw["ws"] = ws
+        result = call(*args, **kw)
+    made = [result] if torch.is_tensor(result) else \
+        list(result.values() if isinstance(result, dict) else result)
+    for t in (*args, *kw.values(), *made, ws and ws.buf):
+        if torch.is_tensor(t):
             t.record_stream(stream)
-    return stream.cuda_stream
+    for t in made:
+        t.record_stream(before)
+    return result
 
 
-def _with_workspace(call, ws, device, stream, before, diag):
-    """call(*before, workspace, diag, stream), with as large a workspace as it
-    asks for."""
-    buf = None if ws is None else ws.buf
-    need = call(*before, buf, diag, _on(stream, buf))
+def _with_workspace(call, ws, device, before, diag):
+    """call(*before, workspace, diag), with as large a workspace as it asks for."""
+    need = call(*before, None if ws is None else ws.buf, diag)
     if need is not None:
-        buf = (ws or Workspace(device)).get(need)
-        call(*before, buf, diag, _on(stream, buf))
+        call(*before, (ws or Workspace(device)).get(need), diag)
 
 
 def opattr_attn_prompt(q, k, v, cu_q, cu_k=None, causal=True, scale=None, out=None, lse=None,
@@ -139,12 +144,14 @@ def opattr_attn_prompt(q, k, v, cu_q, cu_k=None, causal=True, scale=None, out=No
     q[cu_q[b]:cu_q[b+1]] and keys k[cu_k[b]:cu_k[b+1]] (cu_k None: as cu_q);
     scale None: 1 / sqrt(head_dim). Rows of ``out`` and ``lse`` outside every
     sequence are not written."""
+    if stream is not None:
+        return _on(stream, opattr_attn_prompt, q, k, v, cu_q, cu_k, causal,
+                   scale, out, lse, diag=diag)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if lse is None:
         lse = torch.empty(q.shape[1::-1], dtype=torch.float32, device=q.device)
-    (_bind or binding()).attn_prompt(q, k, v, cu_q, cu_k, causal, scale, out, lse, diag,
-                                     -1 if stream is None else _on(stream, out, lse))
+    (_bind or binding()).attn_prompt(q, k, v, cu_q, cu_k, causal, scale, out, lse, diag)
     return out, lse
 
 
@@ -153,15 +160,16 @@ def opattr_attn_prompt_grad(dout, q, k, v, out, lse, cu_q, cu_k=None, causal=Tru
                             stream=None):
     """Gradients of sum(out * dout): (dq, dk, dv). out and lse are
     opattr_attn_prompt's for the same inputs."""
+    if stream is not None:
+        return _on(stream, opattr_attn_prompt_grad, dout, q, k, v, out, lse,
+                   cu_q, cu_k, causal, scale, dq, dk, dv, ws=ws, diag=diag)
     if dq is None:
         dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if dk is None:
         dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
     if dv is None:
         dv = torch.empty(k.shape, dtype=q.dtype, device=q.device)
-    if stream is not None:
-        _on(stream, dq, dk, dv)
-    _with_workspace((_bind or binding()).attn_prompt_grad, ws, q.device, stream,
+    _with_workspace((_bind or binding()).attn_prompt_grad, ws, q.device,
                     (dout, q, k, v, out, lse, cu_q, cu_k, causal, scale, dq, dk, dv), diag)
     return dq, dk, dv
 
@@ -170,13 +178,14 @@ def opattr_attn_paged(q, k_pages, v_pages, table, lens, scale=None, out=None, ls
                       ws: Workspace | None = None, diag=None, stream=None):
     """Attention of one token a sequence, q [sequences, heads, head_dim], over
     the first lens[b] tokens of each: (out, lse [heads, sequences])."""
+    if stream is not None:
+        return _on(stream, opattr_attn_paged, q, k_pages, v_pages, table, lens,
+                   scale, out, lse, ws=ws, diag=diag)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if lse is None:
         lse = torch.empty(q.shape[1::-1], dtype=torch.float32, device=q.device)
-    if stream is not None:
-        _on(stream, out, lse)
-    _with_workspace((_bind or binding()).attn_paged, ws, q.device, stream,
+    _with_workspace((_bind or binding()).attn_paged, ws, q.device,
                     (q, k_pages, v_pages, table, lens, scale, out, lse), diag)
     return out, lse
 
@@ -185,10 +194,13 @@ def opattr_kv_append(k_new, v_new, cu, k_pages, v_pages, table, lens, lens_out=N
                      stream=None):
     """Rows cu[b] .. cu[b+1] of k_new and v_new become the next tokens of
     sequence b, which holds lens[b]; returns the new lengths."""
+    if stream is not None:
+        return _on(stream, opattr_kv_append, k_new, v_new, cu, k_pages, v_pages,
+                   table, lens, lens_out, diag=diag)
     if lens_out is None:
         lens_out = torch.empty(lens.shape, dtype=torch.int32, device=k_pages.device)
     (_bind or binding()).kv_append(k_new, v_new, cu, k_pages, v_pages, table, lens, lens_out,
-                                   diag, -1 if stream is None else _on(stream, lens_out))
+                                   diag)
     return lens_out
 
 
@@ -198,6 +210,9 @@ def opattr_pages_fork(pool, page_size, table, lens, parent, room=None, held=None
     """The next page table: row i continues row parent[i] (-1: empty), with room
     for room[i] tokens. pool [planes, pages, ...] holds the pages that a forked
     row's last, part-filled page is copied in. Returns table, lens and refs."""
+    if stream is not None:
+        return _on(stream, opattr_pages_fork, pool, page_size, table, lens,
+                   parent, room, held, table_out, lens_out, refs, ws=ws, diag=diag)
     like = dict(dtype=torch.int32, device=pool.device)
     if table_out is None:
         table_out = torch.empty((parent.shape[0], table.shape[1]), **like)
@@ -205,9 +220,7 @@ def opattr_pages_fork(pool, page_size, table, lens, parent, room=None, held=None
         lens_out = torch.empty(parent.shape, **like)
     if refs is None:
         refs = torch.empty(pool.shape[1], **like)
-    if stream is not None:
-        _on(stream, table_out, lens_out, refs)
-    _with_workspace((_bind or binding()).pages_fork, ws, pool.device, stream,
+    _with_workspace((_bind or binding()).pages_fork, ws, pool.device,
                     (pool, page_size, table, lens, parent, room, held, table_out, lens_out,
                      refs), diag)
     return Outputs(table=table_out, lens=lens_out, refs=refs)
@@ -218,6 +231,9 @@ def opattr_pages_compact(pool, table, held=None, table_out=None, moved=None, liv
     """The pages in use moved to the front of the pool. Returns the table with
     their new places, moved (each page's new place, -1: free) and live [1], how
     many are in use."""
+    if stream is not None:
+        return _on(stream, opattr_pages_compact, pool, table, held, table_out,
+                   moved, live, ws=ws, diag=diag)
     like = dict(dtype=torch.int32, device=pool.device)
     if table_out is None:
         table_out = torch.empty(table.shape, **like)
@@ -225,8 +241,6 @@ def opattr_pages_compact(pool, table, held=None, table_out=None, moved=None, liv
         moved = torch.empty(pool.shape[1], **like)
     if live is None:
         live = torch.empty(1, **like)
-    if stream is not None:
-        _on(stream, table_out, moved, live)
-    _with_workspace((_bind or binding()).pages_compact, ws, pool.device, stream,
+    _with_workspace((_bind or binding()).pages_compact, ws, pool.device,
                     (pool, table, held, table_out, moved, live), diag)
     return Outputs(table=table_out, moved=moved, live=live)

@@ -5,8 +5,8 @@
 // an append against 3.8 us for the launch alone).
 //
 // Every function takes its arguments by position, checked by attn.py's
-// signatures; a stream of -1 is the current one of the first tensor's device. A
-// function with a workspace returns the bytes it needs, having done nothing,
+// signatures, and goes to the current stream of its tensors' device. A function
+// with a workspace returns the bytes it needs, having done nothing,
 // when `ws` is None or smaller; otherwise None.
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -88,9 +88,10 @@ float *floats(PyObject *o, const at::Tensor &like, c10::IntArrayRef shape, const
   return static_cast<float *>(array(o, at::kFloat, like, shape, name));
 }
 
-opattr_diag *diag_of(PyObject *o) {
+opattr_diag *diag_of(PyObject *o, const at::Tensor &like) {
   if (o == Py_None) return nullptr;
   const at::Tensor &t = tensor(o, "diag");
+  if (t.get_device() != like.get_device()) throw TypeError("diag: not on the others' device");
   if (t.nbytes() < sizeof(opattr_diag)) throw ValueError("diag: not a diag record");
   return static_cast<opattr_diag *>(t.data_ptr());
 }
@@ -101,10 +102,9 @@ int64_t integer(PyObject *o) {
   return x;
 }
 
-void *stream_of(PyObject *o, const at::Tensor &on) {
-  const int64_t s = integer(o);
-  return s == -1 ? static_cast<void *>(c10::hip::getCurrentHIPStream(on.get_device()).stream())
-                 : reinterpret_cast<void *>(s);
+// The current stream of the tensor's device.
+void *stream_of(const at::Tensor &on) {
+  return c10::hip::getCurrentHIPStream(on.get_device()).stream();
 }
 
 int32_t small(int64_t x) {
@@ -122,9 +122,11 @@ PyObject *done(int rc, const char *name) {
 struct Work {
   void *p = nullptr;
   size_t bytes = 0;
-  explicit Work(PyObject *o) {
+  Work(PyObject *o, const at::Tensor &like) {
     if (o == Py_None) return;
     const at::Tensor &t = tensor(o, "ws");
+    if (t.get_device() != like.get_device() || !t.is_contiguous())
+      throw TypeError("ws: a contiguous tensor on the others' device is wanted");
     p = t.data_ptr();
     bytes = t.nbytes();
   }
@@ -161,7 +163,7 @@ opattr_attn_shape shape(const at::Tensor &q, PyObject *ko, PyObject *cu_q, PyObj
   return a;
 }
 
-// q k v cu_q cu_k causal scale out lse diag stream
+// q k v cu_q cu_k causal scale out lse diag
 PyObject *attn_prompt(PyObject *const *o) {
   const at::Tensor &q = tensor(o[0], "q");
   const c10::DeviceGuard on(q.device());
@@ -171,11 +173,11 @@ PyObject *attn_prompt(PyObject *const *o) {
                     rv = rows(o[2], q, a.n_k, g, d, "v"),
                     ro = rows(o[7], q, a.n_q, h, d, "out");
   return done(opattr_attn_prompt(&a, &rq, &rk, &rv, &ro, floats(o[8], q, {h, a.n_q}, "lse"),
-                                 diag_of(o[9]), stream_of(o[10], q)),
+                                 diag_of(o[9], q), stream_of(q)),
               "opattr_attn_prompt");
 }
 
-// dout q k v out lse cu_q cu_k causal scale dq dk dv ws diag stream
+// dout q k v out lse cu_q cu_k causal scale dq dk dv ws diag
 PyObject *attn_prompt_grad(PyObject *const *o) {
   const at::Tensor &q = tensor(o[1], "q");
   const c10::DeviceGuard on(q.device());
@@ -188,11 +190,11 @@ PyObject *attn_prompt_grad(PyObject *const *o) {
                     sk = rows(o[11], q, a.n_k, g, d, "dk"),
                     sv = rows(o[12], q, a.n_k, g, d, "dv");
   const float *lse = floats(o[5], q, {h, a.n_q}, "lse");
-  const Work ws(o[13]);
+  const Work ws(o[13], q);
   const size_t need = opattr_attn_prompt_grad_workspace_bytes(&a);
   if (need > ws.bytes) return PyLong_FromSize_t(need);
   return done(opattr_attn_prompt_grad(&a, &rd, &rq, &rk, &rv, &ro, lse, &sq, &sk, &sv,
-                                      diag_of(o[14]), ws.p, ws.bytes, stream_of(o[15], q)),
+                                      diag_of(o[14], q), ws.p, ws.bytes, stream_of(q)),
               "opattr_attn_prompt_grad");
 }
 
@@ -223,7 +225,7 @@ opattr_kv_pages kv_pages(PyObject *ko, PyObject *vo, PyObject *to) {
   return c;
 }
 
-// q k_pages v_pages table lens scale out lse ws diag stream
+// q k_pages v_pages table lens scale out lse ws diag
 PyObject *attn_paged(PyObject *const *o) {
   const at::Tensor &q = tensor(o[0], "q");
   const c10::DeviceGuard on(q.device());
@@ -234,15 +236,15 @@ PyObject *attn_paged(PyObject *const *o) {
   const opattr_rows rq = rows(o[0], q, b, h, d, "q"), ro = rows(o[6], q, b, h, d, "out");
   const int32_t *lens = ints(o[4], q, {b}, "lens");
   float *lse = floats(o[7], q, {h, b}, "lse");
-  const Work ws(o[8]);
+  const Work ws(o[8], q);
   const size_t need = opattr_attn_paged_workspace_bytes(&c, small(h));
   if (need > ws.bytes) return PyLong_FromSize_t(need);
   return done(opattr_attn_paged(&c, small(h), &rq, lens, scale_of(o[5], d), &ro, lse,
-                                diag_of(o[9]), ws.p, ws.bytes, stream_of(o[10], q)),
+                                diag_of(o[9], q), ws.p, ws.bytes, stream_of(q)),
               "opattr_attn_paged");
 }
 
-// k_new v_new cu k_pages v_pages table lens lens_out diag stream
+// k_new v_new cu k_pages v_pages table lens lens_out diag
 PyObject *kv_append(PyObject *const *o) {
   const at::Tensor &k = tensor(o[0], "k_new"), &cache = tensor(o[3], "k_pages");
   const c10::DeviceGuard on(cache.device());
@@ -252,8 +254,8 @@ PyObject *kv_append(PyObject *const *o) {
                     rv = rows(o[1], cache, n, c.n_kv_heads, c.head_dim, "v_new");
   return done(opattr_kv_append(&c, n, ints(o[2], cache, {b + 1}, "cu"), &rk, &rv,
                                ints(o[6], cache, {b}, "lens"),
-                               ints(o[7], cache, {b}, "lens_out"), diag_of(o[8]),
-                               stream_of(o[9], cache)),
+                               ints(o[7], cache, {b}, "lens_out"), diag_of(o[8], cache),
+                               stream_of(cache)),
               "opattr_kv_append");
 }
 
@@ -279,7 +281,7 @@ opattr_page_pool page_pool(const at::Tensor &t, int64_t page_size, PyObject *hel
   return p;
 }
 
-// pool page_size table lens parent room held table_out lens_out refs ws diag stream
+// pool page_size table lens parent room held table_out lens_out refs ws diag
 PyObject *pages_fork(PyObject *const *o) {
   const at::Tensor &pool = tensor(o[0], "pool"), &table = tensor(o[2], "table"),
                    &parent = tensor(o[4], "parent");
@@ -288,7 +290,7 @@ PyObject *pages_fork(PyObject *const *o) {
   const c10::DeviceGuard on(pool.device());
   const opattr_page_pool p = page_pool(pool, integer(o[1]), o[6]);
   const int64_t rows = table.size(0), width = table.size(1), n = parent.size(0);
-  const Work ws(o[10]);
+  const Work ws(o[10], pool);
   const size_t need =
       opattr_pages_fork_workspace_bytes(small(rows), small(n), small(width), p.n_pages);
   if (need > ws.bytes) return PyLong_FromSize_t(need);
@@ -299,25 +301,25 @@ PyObject *pages_fork(PyObject *const *o) {
                         o[5] == Py_None ? nullptr : ints(o[5], pool, {n}, "room"), small(n),
                         ints(o[7], pool, {n, width}, "table_out"),
                         ints(o[8], pool, {n}, "lens_out"), ints(o[9], pool, {p.n_pages}, "refs"),
-                        diag_of(o[11]), ws.p, ws.bytes, stream_of(o[12], pool)),
+                        diag_of(o[11], pool), ws.p, ws.bytes, stream_of(pool)),
       "opattr_pages_fork");
 }
 
-// pool table held table_out moved live ws diag stream
+// pool table held table_out moved live ws diag
 PyObject *pages_compact(PyObject *const *o) {
   const at::Tensor &pool = tensor(o[0], "pool"), &table = tensor(o[1], "table");
   if (table.dim() != 2) throw ValueError("table is [rows, entries]");
   const c10::DeviceGuard on(pool.device());
   const opattr_page_pool p = page_pool(pool, 1, o[2]);
   const int64_t rows = table.size(0), width = table.size(1);
-  const Work ws(o[6]);
+  const Work ws(o[6], pool);
   const size_t need = opattr_pages_compact_workspace_bytes(p.n_pages);
   if (need > ws.bytes) return PyLong_FromSize_t(need);
   return done(opattr_pages_compact(&p, ints(o[1], pool, {rows, width}, "table"), small(rows),
                                    small(width), ints(o[3], pool, {rows, width}, "table_out"),
                                    ints(o[4], pool, {p.n_pages}, "moved"),
-                                   ints(o[5], pool, {1}, "live"), diag_of(o[7]), ws.p, ws.bytes,
-                                   stream_of(o[8], pool)),
+                                   ints(o[5], pool, {1}, "live"), diag_of(o[7], pool), ws.p, ws.bytes,
+                                   stream_of(pool)),
               "opattr_pages_compact");
 }
 
@@ -348,12 +350,12 @@ PyMethodDef method(const char *name) {
           METH_FASTCALL, nullptr};
 }
 
-PyMethodDef methods[] = {method<attn_prompt, 11>("attn_prompt"),
-                         method<attn_prompt_grad, 16>("attn_prompt_grad"),
-                         method<attn_paged, 11>("attn_paged"),
-                         method<kv_append, 10>("kv_append"),
-                         method<pages_fork, 13>("pages_fork"),
-                         method<pages_compact, 9>("pages_compact"),
+PyMethodDef methods[] = {method<attn_prompt, 10>("attn_prompt"),
+                         method<attn_prompt_grad, 15>("attn_prompt_grad"),
+                         method<attn_paged, 10>("attn_paged"),
+                         method<kv_append, 9>("kv_append"),
+                         method<pages_fork, 12>("pages_fork"),
+                         method<pages_compact, 8>("pages_compact"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "attn_bind", nullptr, -1, methods,
                           nullptr, nullptr, nullptr, nullptr};

@@ -323,6 +323,42 @@ def test_prompt_other_stream_and_own_buffers():
     assert all(torch.equal(t, u) for t, u in zip(got, grads)) and junk
 
 
+def test_calls_on_another_stream_allocate_there():
+    """What a call on another stream allocates is that stream's own: a block that
+    the present stream has just let go, and still works on, is not given out."""
+    torch = _torch()
+    s = _prompt([300, 200], [300, 200], 4, 2, 64, True, "bfloat16")
+    q, k, v, cu = s["q"], s["k"], s["v"], s["cu_q"]
+    want, wl = attn.opattr_attn_prompt(q, k, v, cu)
+    grads = attn.opattr_attn_prompt_grad(s["do"], q, k, v, want, wl, cu)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    gone = [torch.empty_like(t) for t in (want, wl, *grads)]
+    places = {t.data_ptr() for t in gone}
+    del gone
+    ws = attn.Workspace(DEV)
+    out, lse = attn.opattr_attn_prompt(q, k, v, cu, stream=side)
+    got = attn.opattr_attn_prompt_grad(s["do"], q, k, v, out, lse, cu, ws=ws, stream=side)
+    assert not places & {t.data_ptr() for t in (out, lse, *got, ws.buf)}
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, wl)
+    assert all(torch.equal(t, u) for t, u in zip(got, grads))
+
+
+def test_binding_refuses_workspaces_elsewhere():
+    torch = _torch()
+    s = _prompt([20], [20], 2, 1, 64, True, "bfloat16")
+    args = (s["q"], s["k"], s["v"])
+    out, lse = attn.opattr_attn_prompt(*args, s["cu_q"])
+    ws = attn.Workspace("cpu")
+    ws.get(1 << 20)
+    with pytest.raises(TypeError):
+        attn.opattr_attn_prompt_grad(s["do"], *args, out, lse, s["cu_q"], ws=ws)
+    with pytest.raises(TypeError):
+        attn.opattr_attn_prompt(*args, s["cu_q"], diag=torch.zeros(64, dtype=torch.uint8))
+
+
 # --------------------------------------------------------------------------- #
 # paged cache                                                                 #
 # --------------------------------------------------------------------------- #
