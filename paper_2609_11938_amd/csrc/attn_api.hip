@@ -151,7 +151,7 @@ int opattr_attn_prompt(const opattr_attn_shape *a, const opattr_rows *q, const o
 size_t opattr_attn_prompt_grad_workspace_bytes(const opattr_attn_shape *a) {
   if (!ok_shape(a)) return 0;
   const size_t dp = a->head_dim <= 64 ? 64 : 128;
-  const int n = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads);
+  const int n = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads).most;
   return align256((size_t)a->n_q * a->n_heads * 8) + align256((size_t)a->n_kv_heads * 8) +
          (n > 1 ? (size_t)n * (a->n_k / 128 + a->n_seqs) * 128 * a->n_kv_heads * 2 * dp * 4 : 0);
 }
@@ -184,7 +184,9 @@ int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
   at += align256((size_t)a->n_q * a->n_heads * 8);
   if (a->dtype == OPATTR_F16) p.norms = reinterpret_cast<uint32_t *>(at);
   p.part = reinterpret_cast<float *>(at + align256((size_t)a->n_kv_heads * 8));
-  p.splits = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads);
+  const GradSplits x = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads);
+  p.splits = x.most;
+  p.split_steps = x.steps;
   run_prompt_grad(p, a->dtype, (hipStream_t)stream);
   return launched();
 }

@@ -326,14 +326,13 @@ __device__ __forceinline__ Span tile_queries(const PromptArgs &a, const Span &sq
   const int first = begin / kStep(DP), end = (sq.count + kStep(DP) - 1) / kStep(DP);
   return {first, end - first};
 }
-// Blocks that share the tile: at least kSplitSteps steps of 32 queries each, at
+// Blocks that share the tile: at least a.split_steps steps of 32 queries each, at
 // most a.splits.
-constexpr int kSplitSteps = 24;
 template <int DP>
 __device__ __forceinline__ int tile_splits(const PromptArgs &a, const Span &sq, const Span &sk,
                                            int part) {
   const int steps = tile_queries<DP>(a, sq, sk, part).count * a.group * (kStep(DP) / 32);
-  return clamp_to((steps + kSplitSteps - 1) / kSplitSteps, 1, a.splits);
+  return clamp_to((steps + a.split_steps - 1) / a.split_steps, 1, a.splits);
 }
 
 // Where a wave of one of a tile's blocks leaves its dk and dv, as its registers hold
@@ -574,14 +573,21 @@ static void grad(const PromptArgs &a, hipStream_t s) {
 // the end (12 packed documents of up to 4001, 512 blocks without: 1110 us, 2048:
 // 900 us, 4096: 1000 us). By the mean length: blocks that find their tile not
 // split cost what the others gain (8 sequences of 512: 46 us unsplit, 57 us with
-// six blocks a tile that do nothing).
-int grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv) {
-  if (n_seqs == 0 || n_k == 0) return 1;
+// six blocks a tile that do nothing). Where the tiles leave compute units without a
+// block, a block takes fewer steps (4 sequences of 512, 8 heads on 4 of 128, 64 tiles
+// of up to 32 steps: a training pass of 85 us unsplit, 69 us by 8 steps, of which the
+// sums take 10; of 20 steps 48 and 47: not below 24).
+constexpr int kSplitSteps = 24, kFewSteps = 8, kFewTiles = 192;
+GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv) {
+  GradSplits x{1, kSplitSteps};
+  if (n_seqs == 0 || n_k == 0) return x;
   const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
   const int64_t steps = n_q * (n_heads / n_kv) / 32 / n_seqs;
+  if (blocks <= kFewTiles && steps >= kSplitSteps) x.steps = kFewSteps;
   int64_t n = (2048 + blocks - 1) / blocks;
-  if (n > steps / kSplitSteps) n = steps / kSplitSteps;
-  return n < 1 ? 1 : n > 16 ? 16 : (int)n;
+  if (n > steps / x.steps) n = steps / x.steps;
+  x.most = n < 1 ? 1 : n > 16 ? 16 : (int)n;
+  return x;
 }
 
 void run_prompt_grad(const PromptArgs &a, int dtype, hipStream_t s) {

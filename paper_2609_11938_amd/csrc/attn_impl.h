@@ -24,11 +24,15 @@ struct PromptArgs {
   // [heads][n_q]; two bounds a key head (float16); the splits' dk and dv
   float *rows, *part;
   uint32_t *norms;
-  int splits;
+  int splits, split_steps;
 };
 
-// Blocks that share a key tile of the gradient.
-int grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv);
+// Blocks that share a key tile of the gradient at most, and the steps of 32 queries
+// that each has at least.
+struct GradSplits {
+  int most, steps;
+};
+GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv);
 
 struct PagedArgs {
   const uint16_t *k, *v;
