@@ -211,15 +211,14 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
                     kHeldHere ? df[kHeldHere ? s : 0] : mine[s * OPA_WAVE], y);
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = exp2_fast(fmaf(x[e], c, -L));
-      if (cut) {
+      for (int e = 0; e < 16; ++e) {
+        x[e] = exp2_fast(fmaf(x[e], c, -L));
+        y[e] = x[e] * (y[e] - D) * upw;
+      }
+      if (cut) {  // both: of a hidden key either may be past float32
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (k0 + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3) >= seen) x[e] = 0.f;
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        y[e] = x[e] * (y[e] - D) * upw;
+          if (k0 + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3) >= seen) x[e] = y[e] = 0.f;
       }
 #pragma unroll
       for (int e = 0; e < 16; e += 4) off += (y[e] + y[e + 1]) + (y[e + 2] + y[e + 3]);

@@ -716,3 +716,18 @@ def test_prompt_graph_replays():
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(lse, wl), turn
         assert all(torch.equal(a, b) for a, b in zip(g, wg)), turn
+
+
+@pytest.mark.parametrize("lens,d", [([140], 64), ([140], 128), ([900], 64)], ids=str)
+def test_prompt_grad_hidden_finite_values(lens, d):
+    """A finite value whose product with dout no float32 holds, at a key that only
+    queries without a gradient see: nothing of it reaches any gradient."""
+    torch = _torch()
+    s = _prompt(lens, lens, 2, 1, d, True, "bfloat16")
+    row = 100
+    s["v"][row] = 1e36
+    s["do"][:row] *= 1e3
+    s["do"][row:] = 0
+    s["vh"], s["doh"] = _host(s["v"]), _host(s["do"])
+    assert not torch.isfinite(s["do"][:row, 0].float() @ s["v"][row, 0].float()).any()
+    _check_prompt(s)
