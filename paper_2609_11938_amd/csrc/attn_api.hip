@@ -61,6 +61,13 @@ static PromptArgs prompt_args(const opattr_attn_shape *a, opattr_diag *diag) {
   return p;
 }
 
+// float16: the largest norms of each sequence and head
+static size_t norms_bytes(const opattr_attn_shape *a) {
+  return a->dtype == OPATTR_F16
+             ? align256((size_t)a->n_seqs * (a->n_heads + a->n_kv_heads) * 4)
+             : 0;
+}
+
 static bool ok_ws(const void *ws, size_t have, size_t need) {
   return need == 0 || (ws && ((uintptr_t)ws & 255) == 0 && have >= need);
 }
@@ -152,7 +159,7 @@ size_t opattr_attn_prompt_grad_workspace_bytes(const opattr_attn_shape *a) {
   if (!ok_shape(a)) return 0;
   const size_t dp = a->head_dim <= 64 ? 64 : 128;
   const int n = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads).most;
-  return align256((size_t)a->n_q * a->n_heads * 8) + align256((size_t)a->n_kv_heads * 8) +
+  return align256((size_t)a->n_q * a->n_heads * 8) + norms_bytes(a) +
          (n > 1 ? (size_t)n * (a->n_k / 128 + a->n_seqs) * 128 * a->n_kv_heads * 2 * dp * 4 : 0);
 }
 
@@ -183,7 +190,7 @@ int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
   p.rows = reinterpret_cast<float *>(at);
   at += align256((size_t)a->n_q * a->n_heads * 8);
   if (a->dtype == OPATTR_F16) p.norms = reinterpret_cast<uint32_t *>(at);
-  p.part = reinterpret_cast<float *>(at + align256((size_t)a->n_kv_heads * 8));
+  p.part = reinterpret_cast<float *>(at + norms_bytes(a));
   const GradSplits x = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads);
   p.splits = x.most;
   p.split_steps = x.steps;

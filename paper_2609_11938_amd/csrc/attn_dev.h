@@ -285,12 +285,12 @@ __device__ __forceinline__ int wave_sums(int x) {
 }
 
 // Tile `tile` of the tiles of `rows` rows that the sequences of `cu` have: which
-// of the sequence's tiles it is, and the sequence's spans in both offset arrays;
-// false past the last. By whole waves; the result is uniform. Each lane loads a
+// of the sequence's tiles it is, the sequence's spans in both offset arrays, and
+// which sequence; false past the last. By whole waves; the result is uniform. Each lane loads a
 // sequence's four offsets at once: what follows waits for one load.
 __device__ __forceinline__ bool find_tile(const int32_t *cu, int n, const int32_t *other,
                                           int n_other, int n_seqs, int rows, int tile, Span &mine,
-                                          Span &its, int &part) {
+                                          Span &its, int &part, int *seq = nullptr) {
   const int lane = lane_id();
   for (int base = 0; base < n_seqs; base += OPA_WAVE) {
     const int b = base + lane < n_seqs ? base + lane : n_seqs - 1;
@@ -304,6 +304,7 @@ __device__ __forceinline__ bool find_tile(const int32_t *cu, int n, const int32_
       mine = {from(x.first), from(x.count)};
       its = {from(y.first), from(y.count)};
       part = tile - from(inc - tiles);
+      if (seq) *seq = base + w;
       return true;
     }
     tile -= __builtin_amdgcn_readlane(inc, OPA_WAVE - 1);

@@ -31,18 +31,31 @@ constexpr int kStep(int dp) { return dp <= 64 ? 64 : 32; }
 // Weights and their gradients are rounded to 16 bits for the products. For
 // float16 both are scaled by powers of two first: the weights by 2^kWeight, and
 // ds by 2^e with |ds| <= 2 |dout_i| |v_j|, so that its largest stays below
-// 2^15 and small ones keep their bits.
+// 2^15 and small ones keep their bits. The largest are those of one sequence, of
+// the n query heads from `head` on and key head hk: what is large, or not finite,
+// in one sequence says nothing of another, and dq's of one head nothing of the next.
 template <class E>
 struct Scales {
   static constexpr float kWeight = 0.f;
-  static __device__ __forceinline__ float ds(const uint32_t *, int) { return 1.f; }
+  static __device__ __forceinline__ float ds(const PromptArgs &, int, int, int, int) {
+    return 1.f;
+  }
 };
 template <>
 struct Scales<F16> {
   static constexpr float kWeight = 10.f;
-  static __device__ __forceinline__ float ds(const uint32_t *norms, int hk) {
-    const float most = sqrtf(__uint_as_float(norms[2 * hk])) *
-                       sqrtf(__uint_as_float(norms[2 * hk + 1]));
+  static __device__ __forceinline__ float ds(const PromptArgs &a, int seq, int head, int n,
+                                             int hk) {
+    const uint32_t *norms = a.norms + (int64_t)seq * (a.n_heads + a.n_kv);
+    uint32_t dout = norms[head];
+    if (n > 1) {
+      for (int i = lane_id(); i < n; i += OPA_WAVE) dout = max(dout, norms[head + i]);
+#pragma unroll
+      for (int d = 32; d >= 1; d >>= 1) dout = max(dout, (uint32_t)__shfl_xor((int)dout, d));
+      dout = (uint32_t)uniform((int)dout);
+    }
+    const float most = sqrtf(__uint_as_float(dout)) *
+                       sqrtf(__uint_as_float(norms[a.n_heads + hk]));
     if (!(most > 0.f) || !(most < 1e30f)) return 1.f;
     int e;
     frexpf(most, &e);  // most < 2^e
@@ -50,34 +63,26 @@ struct Scales<F16> {
   }
 };
 
-// float16: the largest squared norms of dout's and v's rows (the bits of
-// non-negative floats order as integers, so the maximum is the same in any
-// order), of the rows from the lowest offset to the highest: what lies beside the
-// sequences has no part in the scale. A block takes kNormRows rows of one head:
-// blockIdx.y is a query head, and past those a key head. 4 lanes a row.
+// float16: the largest squared norms of dout's and v's rows, of each sequence and
+// head (the bits of non-negative floats order as integers, so the maximum is the same
+// in any order). A block takes kNormRows rows of a sequence and one head: blockIdx.y
+// is a query head, and past those a key head. 4 lanes a row.
 constexpr int kNormRows = 512;
 __global__ __launch_bounds__(256) void k_attn_norms(PromptArgs a) {
   __shared__ float most[4];
-  __shared__ int low, high;
   const int sub = threadIdx.x & 3;
   const bool q = (int)blockIdx.y < a.n_heads;
   const int head = q ? blockIdx.y : blockIdx.y - a.n_heads;
   const int n = q ? a.n_q : a.n_k;
   const Rows x = q ? a.dout : a.v;
   const int32_t *cu = q ? a.cu_q : a.cu_k;
-  if (threadIdx.x == 0) low = n, high = 0;
-  __syncthreads();
-  for (int b = threadIdx.x; b <= a.n_seqs; b += blockDim.x) {
-    const int at = clamp_to(cu[b], 0, n);
-    atomicMin(&low, at);
-    atomicMax(&high, at);
-  }
-  __syncthreads();
+  Span s, same;
+  int part, seq;
+  if (!find_tile(cu, n, cu, n, a.n_seqs, kNormRows, blockIdx.x, s, same, part, &seq)) return;
   float top = 0.f;
-  for (int64_t t = (int64_t)blockIdx.x * kNormRows + (threadIdx.x >> 2);
-       t < high && t < ((int64_t)blockIdx.x + 1) * kNormRows; t += 64) {
-    if (t < low) continue;
-    const uint16_t *px = x.p + t * x.ts + (int64_t)head * x.hs;
+  for (int t = part * kNormRows + (threadIdx.x >> 2); t < s.count && t < (part + 1) * kNormRows;
+       t += 64) {
+    const uint16_t *px = x.p + (int64_t)(s.first + t) * x.ts + (int64_t)head * x.hs;
     float norm = 0.f;
     for (int c = sub * 8; c < a.head_dim; c += 32) {
       const s16x8 u = *reinterpret_cast<const s16x8 *>(px + c);
@@ -96,7 +101,7 @@ __global__ __launch_bounds__(256) void k_attn_norms(PromptArgs a) {
   if (lane_id() == 0) most[wave_id()] = top;
   __syncthreads();
   if (threadIdx.x == 0)
-    atomicMax(&a.norms[2 * (q ? head / a.group : head) + !q],
+    atomicMax(&a.norms[(int64_t)seq * (a.n_heads + a.n_kv) + blockIdx.y],
               __float_as_uint(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]))));
 }
 
@@ -138,8 +143,8 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
     check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
   }
   Span sq, sk;
-  int part;
-  if (!find_tile(a.cu_q, a.n_q, a.cu_k, a.n_k, a.n_seqs, kHeld, id / a.group, sq, sk, part))
+  int part, seq;
+  if (!find_tile(a.cu_q, a.n_q, a.cu_k, a.n_k, a.n_seqs, kHeld, id / a.group, sq, sk, part, &seq))
     return;
   const int q0 = ((sq.count + kHeld - 1) / kHeld - 1 - part) * kHeld;
   const int lead = sk.count - sq.count;
@@ -184,7 +189,7 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
   const uint16_t *k0p = a.k.p + (int64_t)sk.first * a.k.ts + (int64_t)hk * a.k.hs;
   const uint16_t *v0p = a.v.p + (int64_t)sk.first * a.v.ts + (int64_t)hk * a.v.hs;
   const float c = a.scale * kLog2e;
-  const float up = Scales<E>::ds(a.norms, hk);
+  const float up = Scales<E>::ds(a, seq, head, 1, hk);
   const float fw = exp2_fast(-Scales<E>::kWeight), upw = up * fw;
   const int nat0 = nat_place<DP>(), tr0 = tr_place<DP>();
   f32x16 dq[DB], kp[DB];
@@ -360,8 +365,8 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   id /= a.n_kv;
   const int split = id % a.splits;
   Span sq, sk;
-  int part;
-  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, id / a.splits, sk, sq, part))
+  int part, seq;
+  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, id / a.splits, sk, sq, part, &seq))
     return;
   const int lead = sk.count - sq.count;
   const int key0 = part * kHeld + wave * 32, key = key0 + r;
@@ -394,7 +399,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
     }
   }
   const float c = a.scale * kLog2e;
-  const float up = Scales<E>::ds(a.norms, hk);
+  const float up = Scales<E>::ds(a, seq, hk * a.group, a.group, hk);
   const float fv = exp2_fast(-Scales<E>::kWeight), upw = up * fv;
   const int nat0 = nat_place<DP>(), tr0 = tr_place<DP>();
   f32x16 dk[DB], dv[DB];
@@ -555,10 +560,10 @@ static void launch(const PromptArgs &a, hipStream_t s) {
 template <class E>
 static void grad(const PromptArgs &a, hipStream_t s) {
   if (a.norms) {
-    hipLaunchKernelGGL(k_attn_zero, dim3((2 * a.n_kv + 63) / 64), dim3(64), 0, s, a.norms,
-                       2 * a.n_kv);
+    const int n = a.n_seqs * (a.n_heads + a.n_kv);
+    hipLaunchKernelGGL(k_attn_zero, dim3((n + 63) / 64), dim3(64), 0, s, a.norms, n);
     const int most = a.n_k > a.n_q ? a.n_k : a.n_q;
-    const dim3 grid((most + kNormRows - 1) / kNormRows, a.n_heads + a.n_kv);
+    const dim3 grid(most / kNormRows + a.n_seqs, a.n_heads + a.n_kv);
     if (most > 0) hipLaunchKernelGGL(k_attn_norms, grid, dim3(256), 0, s, a);
   }
   if (a.head_dim <= 64)

@@ -21,7 +21,7 @@ struct PromptArgs {
   float scale;
   opattr_diag *diag;
   // the gradient's workspace: pairs (lse in binary digits, D)
-  // [heads][n_q]; two bounds a key head (float16); the splits' dk and dv
+  // [heads][n_q]; bounds [n_seqs][n_heads + n_kv] (float16); the splits' dk and dv
   float *rows, *part;
   uint32_t *norms;
   int splits, split_steps;

@@ -731,3 +731,36 @@ def test_prompt_grad_hidden_finite_values(lens, d):
     s["vh"], s["doh"] = _host(s["v"]), _host(s["do"])
     assert not torch.isfinite(s["do"][:row, 0].float() @ s["v"][row, 0].float()).any()
     _check_prompt(s)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_grad_float16_sequences_of_other_sizes(d):
+    """A sequence's gradient keeps its bits beside one whose gradient is 10^8 times
+    larger, and beside one that is not finite."""
+    torch = _torch()
+    s = _prompt([70, 600, 61], [70, 600, 61], 4, 2, d, True, "float16")
+    s["do"] = s["do"].clone()
+    large = s["do"][69] * 1e4
+    s["do"] *= 1e-4
+    s["do"][69] = large
+    s["doh"] = _host(s["do"])
+    _check_prompt(s)
+    out, lse = attn.opattr_attn_prompt(s["q"], s["k"], s["v"], s["cu_q"], scale=s["scale"])
+    want = O.packed(s["qh"], s["kh"], s["vh"], s["hq"], s["hk"], s["scale"], True, "float16",
+                    s["doh"], _host(out))
+    s["do"][3] = float("inf")
+    got = attn.opattr_attn_prompt_grad(s["do"], s["q"], s["k"], s["v"], out, lse, s["cu_q"],
+                                       scale=s["scale"])
+    for name, t in zip(("dq", "dk", "dv"), got):
+        _within(t[70:], tuple(w[70:] for w in want[name]), name)
+
+
+def test_prompt_grad_float16_heads_of_other_sizes():
+    """So does a query head's beside another of its key head, in its own dq."""
+    s = _prompt([70, 61], [70, 61], 4, 2, 64, True, "float16")
+    s["do"] = s["do"].clone()
+    large = s["do"][69, ::2] * 1e4
+    s["do"] *= 1e-4
+    s["do"][69, ::2] = large
+    s["doh"] = _host(s["do"])
+    _check_prompt(s)
