@@ -596,6 +596,7 @@ GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_
 
 void run_prompt_grad(const PromptArgs &a, int dtype, hipStream_t s) {
   if (a.n_seqs == 0) return;
+  if (a.n_q == 0) run_check(a, s);
   if (dtype == OPATTR_BF16)
     grad<BF16>(a, s);
   else

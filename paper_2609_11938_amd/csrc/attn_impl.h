@@ -80,6 +80,7 @@ size_t paged_workspace(int n_seqs, int n_kv, int n_heads, int slots);
 void run_append(const AppendArgs &a, hipStream_t s);
 void run_fork(const PagesArgs &a, hipStream_t s);
 void run_compact(const PagesArgs &a, hipStream_t s);
+void run_check(const PromptArgs &a, hipStream_t s);
 void run_prompt(const PromptArgs &a, int dtype, hipStream_t s);
 void run_prompt_grad(const PromptArgs &a, int dtype, hipStream_t s);
 

@@ -266,8 +266,22 @@ static void launch(const PromptArgs &a, hipStream_t s) {
                        dim3(kWaves * OPA_WAVE), 0, s, a);
 }
 
+// The offsets alone, for calls whose kernels have no queries to start from.
+__global__ __launch_bounds__(256) void k_attn_check(PromptArgs a) {
+  check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag);
+  check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
+}
+
+void run_check(const PromptArgs &a, hipStream_t s) {
+  if (a.diag) hipLaunchKernelGGL(k_attn_check, dim3(1), dim3(256), 0, s, a);
+}
+
 void run_prompt(const PromptArgs &a, int dtype, hipStream_t s) {
-  if (a.n_q == 0 || a.n_seqs == 0) return;
+  if (a.n_seqs == 0) return;
+  if (a.n_q == 0) {
+    run_check(a, s);
+    return;
+  }
   if (dtype == OPATTR_BF16)
     a.head_dim <= 64 ? launch<BF16, 64>(a, s) : launch<BF16, 128>(a, s);
   else

@@ -764,3 +764,20 @@ def test_prompt_grad_float16_heads_of_other_sizes():
     s["do"][69, ::2] = large
     s["doh"] = _host(s["do"])
     _check_prompt(s)
+
+
+def test_prompt_offsets_are_checked_without_queries():
+    torch = _torch()
+    q = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device=DEV)
+    k = torch.ones(10, 1, 64, dtype=torch.bfloat16, device=DEV)
+    for cu_q, cu_k, status in (([0, 0], [0, 99], DATA), ([0, 0], [-1, 10], DATA),
+                               ([0, 3], [0, 10], DATA), ([0, 0, 0], [0, 7, 10], 0)):
+        diag = attn.new_diag(DEV)
+        out, lse = attn.opattr_attn_prompt(q, k, k, _ints(cu_q), _ints(cu_k), diag=diag)
+        assert opattr.read_diag(diag)["status"] == status, (cu_q, cu_k)
+        diag = attn.new_diag(DEV)
+        _, dk, dv = attn.opattr_attn_prompt_grad(q, q, k, k, out, lse, _ints(cu_q), _ints(cu_k),
+                                                 diag=diag)
+        assert opattr.read_diag(diag)["status"] == status, (cu_q, cu_k)
+        if not status:
+            assert (dk == 0).all() and (dv == 0).all()
