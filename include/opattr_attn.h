@@ -29,7 +29,8 @@
  * side. Pointers are 16-byte aligned, strides multiples of 8, the token stride
  * in [head_dim, 2^22], the head stride in [0, 2^40]: a slice of a packed
  * projection, or [heads, tokens, head_dim], is passed as it is. Outputs must
- * not overlap inputs or each other.
+ * not overlap inputs or each other; outputs, caches that are appended to, and pools of
+ * pages that have one place for two of their own rows or pages are refused.
  *
  * A query that sees no key (an empty sequence, or a causal mask that hides all
  * of them) has output 0, row statistic -inf, and gives and takes no gradient.

@@ -1,6 +1,8 @@
 // C entry points of the attention operators: argument checks, workspace.
 #include <math.h>
 
+#include <algorithm>
+
 #include "attn_impl.h"
 
 namespace opa {
@@ -27,6 +29,47 @@ static bool ok_rows(const opattr_rows *r, int64_t n, int head_dim) {
          r->head_stride % 8 == 0 && r->token_stride >= head_dim &&
          r->token_stride <= kMaxTokenStride && r->head_stride >= 0 &&
          r->head_stride <= kMaxHeadStride;
+}
+
+struct Steps {
+  int64_t n, stride;  // the stride not negative
+};
+// Whether two of the pieces of `each` values at i x + j y + k z (strides; i, j, k below
+// their counts) share a value.
+static bool overlap(Steps x, Steps y, Steps z, int64_t each) {
+  typedef __int128 wide;
+  if (x.n < 1 || y.n < 1 || z.n < 1) return false;
+  Steps d[3] = {x, y, z};
+  std::sort(d, d + 3, [](const Steps &a, const Steps &b) { return a.stride < b.stride; });
+  // each dimension's step past all of those below it: any order of a dense tensor's
+  // dimensions, and slices of it
+  wide extent = each;
+  bool nested = true;
+  for (const Steps &s : d) {
+    if (s.n > 1 && s.stride < each) return true;
+    nested = nested && (s.n == 1 || s.stride >= extent);
+    extent += (wide)(s.n - 1) * s.stride;
+  }
+  if (nested) return false;
+  // a difference nearer to 0 than `each`: for all of two dimensions, the nearest two
+  // of the longest
+  std::sort(d, d + 3, [](const Steps &a, const Steps &b) { return a.n < b.n; });
+  const wide step = d[2].stride, most = d[2].n - 1;
+  for (int64_t i = 0; i < d[0].n; ++i)
+    for (int64_t j = 1 - d[1].n; j < d[1].n; ++j) {
+      const wide at = (wide)i * d[0].stride + (wide)j * d[1].stride;
+      const wide to = at < 0 ? -at : at;
+      const wide k = to / step < most ? to / step : most;
+      if (((i || j || k) && to - k * step < each) || (k < most && (k + 1) * step - to < each))
+        return true;
+    }
+  return false;
+}
+
+// Rows that are written.
+static bool ok_out(const opattr_rows *r, int64_t n, int heads, int head_dim) {
+  return ok_rows(r, n, head_dim) &&
+         !overlap({n, r->token_stride}, {heads, r->head_stride}, {1, 0}, head_dim);
 }
 
 static Rows rows(const opattr_rows *r) {
@@ -87,6 +130,12 @@ static bool ok_pages(const opattr_kv_pages *c) {
          c->head_stride >= 0 && c->head_stride <= most;
 }
 
+// Pages that are written.
+static bool ok_pages_out(const opattr_kv_pages *c) {
+  return ok_pages(c) && !overlap({c->n_pages, c->page_stride}, {c->page_size, c->token_stride},
+                                 {c->n_kv_heads, c->head_stride}, c->head_dim);
+}
+
 static int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
 
 constexpr int kMaxPages = 1 << 24;
@@ -97,7 +146,9 @@ static bool ok_pool(const opattr_page_pool *p) {
     return false;
   if (p->n_planes == 0 || p->n_pages == 0 || p->page_bytes == 0) return true;
   return p->data && ((uintptr_t)p->data & 15) == 0 && p->plane_stride % 16 == 0 &&
-         p->page_stride % 16 == 0 && p->plane_stride >= 0 && p->page_stride >= p->page_bytes;
+         p->page_stride % 16 == 0 && p->plane_stride >= 0 && p->page_stride >= p->page_bytes &&
+         !overlap({p->n_pages, p->page_stride}, {p->n_planes, p->plane_stride}, {1, 0},
+                  p->page_bytes);
 }
 
 // rows x width entries of a page table
@@ -143,7 +194,7 @@ int opattr_attn_prompt(const opattr_attn_shape *a, const opattr_rows *q, const o
                        const opattr_rows *v, const opattr_rows *out, float *lse,
                        opattr_diag *diag, void *stream) {
   if (!ok_shape(a) || !ok_rows(q, a->n_q, a->head_dim) || !ok_rows(k, a->n_k, a->head_dim) ||
-      !ok_rows(v, a->n_k, a->head_dim) || !ok_rows(out, a->n_q, a->head_dim))
+      !ok_rows(v, a->n_k, a->head_dim) || !ok_out(out, a->n_q, a->n_heads, a->head_dim))
     return OPATTR_ERR_INVALID_ARG;
   PromptArgs p = prompt_args(a, diag);
   p.q = rows(q);
@@ -170,9 +221,9 @@ int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
                             void *ws, size_t ws_bytes, void *stream) {
   if (!ok_shape(a) || !ok_rows(dout, a->n_q, a->head_dim) || !ok_rows(q, a->n_q, a->head_dim) ||
       !ok_rows(k, a->n_k, a->head_dim) || !ok_rows(v, a->n_k, a->head_dim) ||
-      !ok_rows(out, a->n_q, a->head_dim) || !ok_rows(dq, a->n_q, a->head_dim) ||
-      !ok_rows(dk, a->n_k, a->head_dim) || !ok_rows(dv, a->n_k, a->head_dim) ||
-      (a->n_q > 0 && !lse))
+      !ok_rows(out, a->n_q, a->head_dim) || !ok_out(dq, a->n_q, a->n_heads, a->head_dim) ||
+      !ok_out(dk, a->n_k, a->n_kv_heads, a->head_dim) ||
+      !ok_out(dv, a->n_k, a->n_kv_heads, a->head_dim) || (a->n_q > 0 && !lse))
     return OPATTR_ERR_INVALID_ARG;
   if (!ok_ws(ws, ws_bytes, opattr_attn_prompt_grad_workspace_bytes(a)))
     return OPATTR_ERR_WORKSPACE;
@@ -208,7 +259,7 @@ int opattr_attn_paged(const opattr_kv_pages *c, int32_t n_heads, const opattr_ro
                       opattr_diag *diag, void *ws, size_t ws_bytes, void *stream) {
   if (!ok_pages(c) || !ok_heads(n_heads, c->n_kv_heads, c->head_dim) ||
       n_heads / c->n_kv_heads > 16 || !isfinite(scale) ||
-      !ok_rows(q, c->n_seqs, c->head_dim) || !ok_rows(out, c->n_seqs, c->head_dim) ||
+      !ok_rows(q, c->n_seqs, c->head_dim) || !ok_out(out, c->n_seqs, n_heads, c->head_dim) ||
       (c->n_seqs > 0 && !lens) || (int64_t)c->n_seqs * n_heads > kMaxGrid / 2)
     return OPATTR_ERR_INVALID_ARG;
   if (!ok_ws(ws, ws_bytes, opattr_attn_paged_workspace_bytes(c, n_heads)))
@@ -243,7 +294,7 @@ int opattr_attn_paged(const opattr_kv_pages *c, int32_t n_heads, const opattr_ro
 int opattr_kv_append(const opattr_kv_pages *c, int64_t n_new, const int32_t *cu,
                      const opattr_rows *k_new, const opattr_rows *v_new, const int32_t *lens,
                      int32_t *lens_out, opattr_diag *diag, void *stream) {
-  if (!ok_pages(c) || n_new < 0 || n_new > kMaxGrid * 4 ||
+  if (!ok_pages_out(c) || n_new < 0 || n_new > kMaxGrid * 4 ||
       !ok_rows(k_new, n_new, c->head_dim) || !ok_rows(v_new, n_new, c->head_dim) ||
       (c->n_seqs > 0 && (!cu || !lens)) || (lens_out && lens_out == lens))
     return OPATTR_ERR_INVALID_ARG;

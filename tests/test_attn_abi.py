@@ -280,3 +280,83 @@ def test_calls_past_one_launch_are_refused(lib):
     assert lib.opattr_attn_paged(c, 32, r, FAKE, 0.1, r, FAKE, None, FAKE, 1 << 30,
                                  None) == INVALID
     assert lib.opattr_kv_append(_pages(), 1 << 27, FAKE, r, r, FAKE, None, None, None) == INVALID
+
+
+OVERLAPS = [dict(hs=0), dict(hs=56), dict(ts=504), dict(ts=64, hs=64), dict(ts=128, hs=320),
+            dict(ts=3584, hs=512)]
+
+
+@pytest.mark.parametrize("bad", OVERLAPS, ids=str)
+def test_outputs_that_overlap_themselves_are_refused(lib, bad):
+    """8 heads of 64, 100 tokens: two rows of the output in one place."""
+    r, x = _rows(), _rows(**bad)
+    a = _shape(n_heads=8, n_kv_heads=8)
+    assert lib.opattr_attn_prompt(a, r, r, r, x, FAKE, None, None) == INVALID
+    for at in (6, 7, 8):
+        args = [r, r, r, r, r, FAKE, r, r, r]
+        args[at] = x
+        assert lib.opattr_attn_prompt_grad(a, *args, None, FAKE, 1 << 40, None) == INVALID, at
+    c = _pages(n_seqs=100, table_stride=1)
+    assert lib.opattr_attn_paged(c, 8, r, FAKE, 0.1, x, FAKE, None, FAKE, 1 << 30,
+                                 None) == INVALID
+
+
+@pytest.mark.parametrize("good", [dict(), dict(hs=6400, ts=64), dict(ts=1024, hs=120),
+                                  dict(ts=192, hs=64 * 3 * 100), dict(ts=128, hs=64 + 128 * 100),
+                                  dict(ts=3200, hs=320)], ids=str)
+def test_outputs_of_other_orders_pass(lib, good):
+    """Heads before tokens, gaps, heads between tokens: taken (the call ends at its
+    missing workspace)."""
+    r, x = _rows(), _rows(**good)
+    a = _shape(n_heads=8, n_kv_heads=8)
+    args = [r, r, r, r, r, FAKE, x, x, x]
+    assert lib.opattr_attn_prompt_grad(a, *args, None, None, 0, None) == WORKSPACE
+
+
+def test_caches_and_pools_that_overlap_themselves_are_refused(lib):
+    r = _rows()
+    for bad in (dict(page_stride=0), dict(token_stride=0), dict(head_stride=0),
+                dict(token_stride=64), dict(page_stride=2040), dict(page_stride=128 * 15)):
+        assert lib.opattr_kv_append(_pages(**bad), 3, FAKE, r, r, FAKE, None, None,
+                                    None) == INVALID, bad
+    for bad in (dict(plane_stride=0), dict(plane_stride=4096 * 99), dict(plane_stride=2048)):
+        p = _pool(**bad)
+        assert lib.opattr_pages_fork(p, FAKE, FAKE, 4, 5, FAKE, FAKE, 6, 2 * FAKE, 3 * FAKE, None,
+                                     None, FAKE, 1 << 30, None) == INVALID, bad
+        assert lib.opattr_pages_compact(p, FAKE, 4, 5, 2 * FAKE, FAKE, None, None, FAKE, 1 << 30,
+                                        None) == INVALID, bad
+    # planes between the pages: taken (the call ends at its missing workspace)
+    p = _pool(plane_stride=4096, page_stride=4 * 4096)
+    assert lib.opattr_pages_compact(p, FAKE, 4, 5, 2 * FAKE, FAKE, None, None, None, 0,
+                                    None) == WORKSPACE
+
+
+def test_overlap_rule_against_places(lib):
+    """The rule for every pair of strides of a small output, against its places."""
+    r = _rows()
+    n, heads, d = 5, 3, 16
+    a = _shape(n_q=n, n_k=n, n_heads=heads, n_kv_heads=heads, head_dim=d)
+    for ts in range(16, 96, 8):
+        for hs in range(0, 136, 8):
+            at = [t * ts + h * hs + e for t in range(n) for h in range(heads) for e in range(d)]
+            x = _rows(ts=ts, hs=hs)
+            want = INVALID if len(set(at)) < len(at) else WORKSPACE
+            assert lib.opattr_attn_prompt_grad(a, r, r, r, r, r, FAKE, x, x, x, None, None, 0,
+                                               None) == want, (ts, hs)
+
+
+def test_overlap_rule_of_caches_against_places(lib):
+    """So for caches, of which the overlapping ones only: the others would go on."""
+    r = _rows()
+    pages, size, heads, d = 3, 2, 3, 8
+    for ps in range(0, 120, 8):
+        for ts in range(0, 72, 8):
+            for hs in range(0, 72, 8):
+                at = [x * ps + t * ts + h * hs + e for x in range(pages) for t in range(size)
+                      for h in range(heads) for e in range(d)]
+                if len(set(at)) == len(at):
+                    continue
+                c = _pages(n_pages=pages, page_size=size, n_kv_heads=heads, head_dim=d,
+                           page_stride=ps, token_stride=ts, head_stride=hs)
+                assert lib.opattr_kv_append(c, 3, FAKE, r, r, FAKE, None, None,
+                                            None) == INVALID, (ps, ts, hs)
