@@ -155,8 +155,8 @@ typedef struct {
    When the free pages run out the remaining entries are -1, LIMIT is flagged,
    and a row whose copy got no page ends at its full pages. A parent out of
    range reads as -1, a kept entry out of range becomes -1, a length or room
-   past what the table can name is cut; all flagged DATA. table and table_out are [rows][width]; they, lens and lens_out do not
-   overlap. */
+   past what the table can name is cut; all flagged DATA. table and table_out are
+   [rows][width]; they, lens, lens_out, refs and held do not overlap. */
 size_t opattr_pages_fork_workspace_bytes(int32_t n_rows, int32_t n_out, int32_t width,
                                          int32_t n_pages);
 int opattr_pages_fork(const opattr_page_pool *p, const int32_t *table, const int32_t *lens,
@@ -169,7 +169,7 @@ int opattr_pages_fork(const opattr_page_pool *p, const int32_t *table, const int
    in order, take the free places below m in order. table_out[i] = the new place
    of table[i]'s page (-1 stays; an entry out of range becomes -1, flagged DATA);
    moved[n_pages] the new place of each page, -1 for free ones; live (or NULL)
-   receives m. table_out may be table itself. */
+   receives m. table_out may be table itself; moved does not overlap held. */
 size_t opattr_pages_compact_workspace_bytes(int32_t n_pages);
 int opattr_pages_compact(const opattr_page_pool *p, const int32_t *table, int32_t n_rows,
                          int32_t width, int32_t *table_out, int32_t *moved, int32_t *live,

@@ -337,7 +337,8 @@ int opattr_pages_fork(const opattr_page_pool *p, const int32_t *table, const int
   if (!ok_pool(p) || !ok_table(n_rows, width) || !ok_table(n_out, width) ||
       (n_rows > 0 && (!lens || (width > 0 && !table))) ||
       (n_out > 0 && (!parent || !lens_out || (width > 0 && !table_out))) ||
-      (table_out && table_out == table) || (lens_out && lens_out == lens))
+      (table_out && table_out == table) || (lens_out && lens_out == lens) ||
+      (refs && refs == p->held))
     return OPATTR_ERR_INVALID_ARG;
   if (!ok_ws(ws, ws_bytes, opattr_pages_fork_workspace_bytes(n_rows, n_out, width, p->n_pages)))
     return OPATTR_ERR_WORKSPACE;
@@ -369,7 +370,8 @@ int opattr_pages_compact(const opattr_page_pool *p, const int32_t *table, int32_
                          int32_t width, int32_t *table_out, int32_t *moved, int32_t *live,
                          opattr_diag *diag, void *ws, size_t ws_bytes, void *stream) {
   if (!ok_pool(p) || !ok_table(n_rows, width) ||
-      ((int64_t)n_rows * width > 0 && (!table || !table_out)) || (p->n_pages > 0 && !moved))
+      ((int64_t)n_rows * width > 0 && (!table || !table_out)) || (p->n_pages > 0 && !moved) ||
+      (moved && moved == p->held))
     return OPATTR_ERR_INVALID_ARG;
   if (!ok_ws(ws, ws_bytes, opattr_pages_compact_workspace_bytes(p->n_pages)))
     return OPATTR_ERR_WORKSPACE;

@@ -360,3 +360,12 @@ def test_overlap_rule_of_caches_against_places(lib):
                            page_stride=ps, token_stride=ts, head_stride=hs)
                 assert lib.opattr_kv_append(c, 3, FAKE, r, r, FAKE, None, None,
                                             None) == INVALID, (ps, ts, hs)
+
+
+def test_counts_written_where_they_are_read_are_refused(lib):
+    """Every block reads held while the first ones to be done write refs or moved."""
+    p, big = _pool(held=5 * FAKE), 1 << 30
+    assert lib.opattr_pages_fork(p, FAKE, FAKE, 4, 5, FAKE, FAKE, 6, 2 * FAKE, 3 * FAKE, 5 * FAKE,
+                                 None, FAKE, big, None) == INVALID
+    assert lib.opattr_pages_compact(p, FAKE, 4, 5, 2 * FAKE, 5 * FAKE, None, None, FAKE, big,
+                                    None) == INVALID
