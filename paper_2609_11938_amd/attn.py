@@ -9,7 +9,9 @@ Tensors of queries, keys, values, outputs and gradients are [tokens, heads,
 head_dim] in bfloat16 or float16, any strides with the last one 1 (multiples of
 8 elements, 16-byte aligned). Lengths, offsets and page tables are contiguous
 int32 tensors. Data errors go to the ``diag`` record, if one is given
-(``new_diag``; read it with ``opattr.read_diag``).
+(``new_diag``; read it with ``opattr.read_diag``). Autograd does not see the
+calls: with it on, queries, keys and values that require a gradient are refused;
+``opattr_attn_prompt_grad`` takes them and is the gradient.
 """
 from __future__ import annotations
 

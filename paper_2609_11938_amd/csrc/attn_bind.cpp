@@ -11,9 +11,11 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 
 #include <cmath>
+#include <initializer_list>
 #include <stdexcept>
 #include <string>
 
@@ -39,6 +41,17 @@ const at::Tensor &tensor(PyObject *o, const char *name) {
   const at::Tensor &t = THPVariable_Unpack(o);
   if (!t.is_cuda()) throw TypeError(std::string(name) + ": device tensors are taken");
   return t;
+}
+
+// Autograd does not see the calls: with it on, inputs that require a gradient would
+// lose it without a word.
+void no_gradient(std::initializer_list<PyObject *> inputs, const char *name) {
+  if (!c10::GradMode::is_enabled()) return;
+  for (PyObject *o : inputs)
+    if (tensor(o, name).requires_grad())
+      throw std::runtime_error(std::string(name) +
+                               ": an input requires a gradient, which the call does not record; "
+                               "detach it or call under torch.no_grad()");
 }
 
 int dtype_of(const at::Tensor &t) {
@@ -172,6 +185,7 @@ PyObject *attn_prompt(PyObject *const *o) {
   const opattr_rows rq = rows(o[0], q, a.n_q, h, d, "q"), rk = rows(o[1], q, a.n_k, g, d, "k"),
                     rv = rows(o[2], q, a.n_k, g, d, "v"),
                     ro = rows(o[7], q, a.n_q, h, d, "out");
+  no_gradient({o[0], o[1], o[2]}, "opattr_attn_prompt");
   return done(opattr_attn_prompt(&a, &rq, &rk, &rv, &ro, floats(o[8], q, {h, a.n_q}, "lse"),
                                  diag_of(o[9], q), stream_of(q)),
               "opattr_attn_prompt");
@@ -234,6 +248,7 @@ PyObject *attn_paged(PyObject *const *o) {
   alike(q, THPVariable_Unpack(o[1]), "q");
   const int64_t b = c.n_seqs, h = q.size(1), d = c.head_dim;
   const opattr_rows rq = rows(o[0], q, b, h, d, "q"), ro = rows(o[6], q, b, h, d, "out");
+  no_gradient({o[0], o[1], o[2]}, "opattr_attn_paged");
   const int32_t *lens = ints(o[4], q, {b}, "lens");
   float *lse = floats(o[7], q, {h, b}, "lse");
   const Work ws(o[8], q);
@@ -252,6 +267,7 @@ PyObject *kv_append(PyObject *const *o) {
   const int64_t b = c.n_seqs, n = k.dim() ? k.size(0) : 0;
   const opattr_rows rk = rows(o[0], cache, n, c.n_kv_heads, c.head_dim, "k_new"),
                     rv = rows(o[1], cache, n, c.n_kv_heads, c.head_dim, "v_new");
+  no_gradient({o[0], o[1]}, "opattr_kv_append");
   return done(opattr_kv_append(&c, n, ints(o[2], cache, {b + 1}, "cu"), &rk, &rv,
                                ints(o[6], cache, {b}, "lens"),
                                ints(o[7], cache, {b}, "lens_out"), diag_of(o[8], cache),

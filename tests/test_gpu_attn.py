@@ -781,3 +781,35 @@ def test_prompt_offsets_are_checked_without_queries():
         assert opattr.read_diag(diag)["status"] == status, (cu_q, cu_k)
         if not status:
             assert (dk == 0).all() and (dv == 0).all()
+
+
+def test_calls_that_would_lose_a_gradient_are_refused():
+    """The calls record nothing for autograd: with it on, inputs that require a
+    gradient are refused, as torch refuses them with out=. The gradient itself
+    takes them."""
+    torch = _torch()
+    s = _prompt([20], [20], 2, 1, 64, True, "bfloat16")
+    cu, table = s["cu_q"], _ints([[0, 1]])
+    pages = torch.zeros(2, 2, 16, 1, 64, dtype=torch.bfloat16, device=DEV)
+    want, lse = attn.opattr_attn_prompt(s["q"], s["k"], s["v"], cu)
+    grads = attn.opattr_attn_prompt_grad(s["do"], s["q"], s["k"], s["v"], want, lse, cu)
+    for at in "qkv":
+        args = {n: s[n].clone() for n in "qkv"}
+        args[at].requires_grad_()
+        calls = [lambda: attn.opattr_attn_prompt(args["q"], args["k"], args["v"], cu)]
+        if at == "q":
+            calls.append(lambda: attn.opattr_attn_paged(args["q"][:1], pages[0], pages[1], table,
+                                                        _ints([3])))
+        else:
+            calls.append(lambda: attn.opattr_kv_append(args["k"], args["v"], cu, pages[0],
+                                                       pages[1], table, _ints([0])))
+        for call in calls:
+            with pytest.raises(RuntimeError, match="grad"):
+                call()
+            with torch.no_grad():
+                call()
+        with torch.no_grad():
+            out, _ = attn.opattr_attn_prompt(args["q"], args["k"], args["v"], cu)
+        assert torch.equal(out, want)
+        got = attn.opattr_attn_prompt_grad(s["do"], args["q"], args["k"], args["v"], out, lse, cu)
+        assert all(torch.equal(t, u) for t, u in zip(got, grads))
