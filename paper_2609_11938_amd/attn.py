@@ -109,8 +109,15 @@ def binding():
 
 
 def new_diag(device="cuda:0", stream=None):
-    """A cleared diag record on the device."""
-    return opattr._new_diag(device, stream)
+    """A cleared diag record on the device, of the stream's own memory (None: the
+    device's current stream)."""
+    before = torch.cuda.current_stream(device)
+    if stream is None:
+        stream = before
+    with torch.cuda.stream(stream):
+        diag = opattr._new_diag(device, stream)
+    diag.record_stream(before)
+    return diag
 
 
 def _on(stream, call, *args, ws=None, **kw):

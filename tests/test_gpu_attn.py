@@ -813,3 +813,17 @@ def test_calls_that_would_lose_a_gradient_are_refused():
         assert torch.equal(out, want)
         got = attn.opattr_attn_prompt_grad(s["do"], args["q"], args["k"], args["v"], out, lse, cu)
         assert all(torch.equal(t, u) for t, u in zip(got, grads))
+
+
+def test_diag_records_of_another_stream_are_its_own():
+    """As the calls': a record for another stream is allocated there."""
+    torch = _torch()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    gone = [attn.new_diag(DEV) for _ in range(4)]
+    places = {t.data_ptr() for t in gone}
+    del gone
+    diag = attn.new_diag(DEV, side)
+    assert diag.data_ptr() not in places
+    torch.cuda.synchronize()
+    assert opattr.read_diag(diag)["status"] == 0
