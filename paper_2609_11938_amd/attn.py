@@ -9,7 +9,8 @@ Tensors of queries, keys, values, outputs and gradients are [tokens, heads,
 head_dim] in bfloat16 or float16, any strides with the last one 1 (multiples of
 8 elements, 16-byte aligned). Lengths, offsets and page tables are contiguous
 int32 tensors. Data errors go to the ``diag`` record, if one is given
-(``new_diag``; read it with ``opattr.read_diag``). Autograd does not see the
+(``new_diag``; read it with ``opattr.read_diag``). A ``Workspace`` serves one
+call at a time: calls that may overlap on two streams need one each. Autograd does not see the
 calls: with it on, queries, keys and values that require a gradient are refused;
 ``opattr_attn_prompt_grad`` takes them and is the gradient.
 """
@@ -132,7 +133,7 @@ def _on(stream, call, *args, ws=None, **kw):
         result = call(*args, **kw)
     made = [result] if torch.is_tensor(result) else \
         list(result.values() if isinstance(result, dict) else result)
-    for t in (*args, *kw.values(), *made, ws and ws.buf):
+    for t in (*args, *kw.values(), *made):
         if torch.is_tensor(t):
             t.record_stream(stream)
     for t in made:

@@ -12,6 +12,7 @@
 
 #include <c10/core/DeviceGuard.h>
 #include <c10/core/GradMode.h>
+#include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 
 #include <cmath>
@@ -132,6 +133,9 @@ PyObject *done(int rc, const char *name) {
                            std::to_string(rc) + ")");
 }
 
+// A workspace. One that a call on another stream allocated is that stream's memory:
+// let go, it stays until the current stream has passed this call too (on its own
+// stream the allocator notes nothing).
 struct Work {
   void *p = nullptr;
   size_t bytes = 0;
@@ -142,6 +146,8 @@ struct Work {
       throw TypeError("ws: a contiguous tensor on the others' device is wanted");
     p = t.data_ptr();
     bytes = t.nbytes();
+    c10::hip::HIPCachingAllocator::recordStream(
+        t.storage().data_ptr(), c10::hip::getCurrentHIPStream(like.get_device()));
   }
 };
 

@@ -827,3 +827,30 @@ def test_diag_records_of_another_stream_are_its_own():
     assert diag.data_ptr() not in places
     torch.cuda.synchronize()
     assert opattr.read_diag(diag)["status"] == 0
+
+
+def test_workspace_of_another_stream_is_kept_until_its_use_is_over():
+    """A workspace that a call on another stream made larger, used on the present
+    stream and let go: its memory is not given out while that use is pending."""
+    torch = _torch()
+    s = _prompt([300, 200], [300, 200], 4, 2, 64, True, "bfloat16")
+    q, k, v, cu = s["q"], s["k"], s["v"], s["cu_q"]
+    out, lse = attn.opattr_attn_prompt(q, k, v, cu)
+    a = torch.randn(4096, 4096, device=DEV)
+    b = a @ a
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    ws = attn.Workspace(DEV)
+    attn.opattr_attn_prompt_grad(s["do"], q, k, v, out, lse, cu, ws=ws, stream=side)
+    torch.cuda.synchronize()
+    place, size = ws.buf.data_ptr(), ws.buf.numel()
+    for _ in range(40):
+        torch.mm(a, a, out=b)
+    attn.opattr_attn_prompt_grad(s["do"], q, k, v, out, lse, cu, ws=ws)
+    ws = None
+    with torch.cuda.stream(side):
+        others = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(64)]
+    pending = not torch.cuda.current_stream().query()
+    torch.cuda.synchronize()
+    assert pending
+    assert not any(place - size < t.data_ptr() < place + size for t in others)
