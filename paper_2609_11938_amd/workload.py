@@ -8,12 +8,14 @@ this GPU next to the synthetic ones of ``tracegen``.
 forks, drops and compacts sequences as a scheduler does; ``train`` runs the
 forward pass and its gradient over packed documents. Rows of random numbers
 stand for the projections' outputs. Every call is recorded by a ``Recorder``
-(device time by events, bytes from its sizes) inside the operator range that
+(device time by events; bytes as the call has to move them, computed from its
+sizes and results, not counted in the memory) inside the operator range that
 issued it; ``profile`` attributes the trace and builds the profile document.
 """
 from __future__ import annotations
 
 import contextlib
+import functools
 import math
 import sys
 
@@ -59,10 +61,12 @@ class Recorder:
         self.ranges[at][2] = len(self.launches)
 
     def launch(self, name, read, written, call, *args, **kw):
-        """call(*args, **kw), recorded as one launch."""
+        """call(*args, **kw), recorded as one launch, whatever kernels it takes. Bytes
+        that depend on the data are functions of the result, called by trace()."""
         begin = self._event()
         result = call(*args, **kw)
-        self.launches.append((self._id(self.names, name), begin, self._event(), read, written))
+        moved = [functools.partial(n, result) if callable(n) else n for n in (read, written)]
+        self.launches.append((self._id(self.names, name), begin, self._event(), *moved))
         return result
 
     def trace(self) -> dict:
@@ -79,7 +83,8 @@ class Recorder:
             s = max(last, round(self.base.elapsed_time(begin) * 1e6))
             d = max(1, round(begin.elapsed_time(end) * 1e6))
             start[i], dur[i], last = s, d, s + d
-            counters[i, [TIME, READ, WRITTEN]] = d, read, written
+            counters[i, [TIME, READ, WRITTEN]] = d, *(n() if callable(n) else n
+                                                       for n in (read, written))
         ranges = [(o, a, b) for o, a, b in self.ranges if b > a]
         first, final = (np.array([r[k] for r in ranges], np.int64) for k in (1, 2))
         name = np.array([n for n, *_ in self.launches], np.uint32)
@@ -133,16 +138,35 @@ class Cache:
         room[i] tokens; pages in use move to the front of the pool."""
         table, lens = self._next
         ints = dict(dtype=torch.int32, device=self.table.device)
-        page = self.pool[0, 0].numel() * self.pool.element_size()
+        rows, pages, entries = len(parent), self.pool.shape[1], table.numel()
+        # a page in every plane, read and written
+        each = self.pool.shape[0] * self.pool[0, 0].numel() * self.pool.element_size()
+        lens_in, lens_out = self.lens.clone(), torch.empty_like(lens)
+
+        def copied():
+            """Bytes of the part-filled pages that the fork copied: those of rows
+            that are not their parent's first, where the copy got a page."""
+            had, has = lens_in.tolist(), lens_out.tolist()
+            return each * sum(p >= 0 and p in parent[:i] and had[p] % self.page_size > 0
+                              and has[i] == had[p] for i, p in enumerate(parent))
+
+        def moved(out):
+            to = out["moved"]
+            return each * int(((to >= 0) & (to != torch.arange(pages, **ints))).sum())
+
         with rec.op("cache::turn"):
-            tables = 2 * 4 * table.numel()
-            rec.launch("pages_fork", tables, tables, attn.opattr_pages_fork, self.pool,
-                       self.page_size, self.table, self.lens, torch.tensor(parent, **ints),
-                       torch.tensor(room, **ints), table_out=table, lens_out=lens, ws=self.ws)
+            rec.launch("pages_fork", lambda out: 4 * (entries + 3 * rows) + copied(),
+                       lambda out: 4 * (entries + rows + pages) + copied(),
+                       attn.opattr_pages_fork, self.pool, self.page_size, self.table, self.lens,
+                       torch.tensor(parent, **ints), torch.tensor(room, **ints),
+                       table_out=table, lens_out=lens, ws=self.ws)
+            lens_out.copy_(lens)  # which later steps write again
             self._next = self.table, self.lens
             self.table, self.lens = table, lens
-            out = rec.launch("pages_compact", page, page, attn.opattr_pages_compact, self.pool,
-                             table, table_out=table, ws=self.ws)
+            out = rec.launch("pages_compact", lambda out: 4 * entries + moved(out),
+                             lambda out: 4 * (entries + pages + 1) + moved(out),
+                             attn.opattr_pages_compact, self.pool, table, table_out=table,
+                             ws=self.ws)
         return out["live"]
 
     def append(self, rec, layer, k, v, cu, lens_out):
@@ -203,7 +227,9 @@ def serve(rec, lens=(100, 37, 64), steps=8, layers=2, heads=8, kv_heads=4, head_
                     cache.append(rec, layer, k, v, one, after)
                     with rec.op("aten::attention"):
                         out, _ = rec.launch(
-                            "attn_paged", 2 * sum(sizes) * kv_heads * each, rows * heads * each,
+                            "attn_paged",
+                            (2 * (sum(sizes) + rows) * kv_heads + rows * heads) * each,
+                            rows * heads * each,
                             attn.opattr_attn_paged, q, cache.data[layer, 0],
                             cache.data[layer, 1], cache.table, after, scale=scale, ws=cache.ws)
                     for b in range(rows):

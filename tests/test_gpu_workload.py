@@ -67,3 +67,32 @@ def test_profile_of_the_workload(tmp_path):
     assert calls["aten::attention_backward"] == [(1, {"attn_prompt_grad"})]
     kernels = sum(len(e["kernels"]) for e in doc["operators"])
     assert kernels == len(rec.launches)
+
+
+def test_turn_bytes_are_what_is_copied_and_moved():
+    """The records of a turn hold the pages that it copied and moved, in every
+    plane, and its tables."""
+    import torch
+
+    from paper_2609_11938_amd import workload
+
+    page, pages, rows, width, layers = 8, 24, 3, 4, 2
+    cache = workload.Cache(layers, pages, page, 1, 64, rows, width)
+    table = np.array([[20, 3, 21, -1], [9, 1, -1, -1], [5, 22, -1, -1]])
+    lens = [20, 16, 11]
+    cache.table.copy_(torch.tensor(table, dtype=torch.int32))
+    cache.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    parent, room = [0, 0, 2], [24, 25, 11]
+    rec = workload.Recorder()
+    cache.turn(rec, parent, room)
+    at = rec.trace()
+    read, written = (at["counters"][:, c] for c in (workload.READ, workload.WRITTEN))
+    forked, _, _, copies, short = O.fork(page, pages, table, lens, parent, room)
+    _, _, live, moves = O.compact(pages, forked)
+    assert not short and len(copies) == 1 and len(moves) > 1
+    each = 2 * layers * page * 64 * 2
+    tables = 4 * (2 * rows * width + 4 * rows + 3 * pages)
+    for moved, n in ((read, copies), (written, copies)):
+        assert len(n) * each < moved[0] <= len(n) * each + tables
+    for moved in (read, written):
+        assert len(moves) * each < moved[1] <= len(moves) * each + tables
