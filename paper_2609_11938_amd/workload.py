@@ -8,7 +8,7 @@ this GPU next to the synthetic ones of ``tracegen``.
 forks, drops and compacts sequences as a scheduler does; ``train`` runs the
 forward pass and its gradient over packed documents. Rows of random numbers
 stand for the projections' outputs. Every call is recorded by a ``Recorder``
-(device time by events; bytes as the call has to move them, computed from its
+(device time by events, with the host kept ahead; bytes as the call has to move them, computed from its
 sizes and results, not counted in the memory) inside the operator range that
 issued it; ``profile`` attributes the trace and builds the profile document.
 """
@@ -30,19 +30,41 @@ TIME, READ, WRITTEN = 0, 1, 2
 ABSENT = ((1 << opattr.NUM_COUNTERS) - 1) & ~(1 << TIME | 1 << READ | 1 << WRITTEN)
 
 
+# Clock cycles that the device waits before a recorded call, so that the host is done
+# with the call before the device begins: about 0.2 ms, for calls that cost the host
+# 4 to 20 us.
+AHEAD = 500_000
+
+
 class Recorder:
-    """Launch records and operator ranges of calls on the current stream."""
+    """Launch records and operator ranges of calls on the current stream. ``late``
+    counts the calls that the device began before the host was done with them:
+    their times hold some of the host's."""
 
     def __init__(self):
         self.names, self.ops = [], []
         self.launches, self.ranges, self.open = [], [], []
+        self.late = 0
         self.base = self._event()
+        self.idle = 0.0  # ms between two events with nothing in between
+        nothing = [self._timed(lambda: None)[1:] for _ in range(15)]
+        torch.cuda.synchronize()
+        self.idle = sorted(a.elapsed_time(b) for a, b in nothing)[7]
+        self.late = 0
 
     @staticmethod
     def _event():
         e = torch.cuda.Event(enable_timing=True)
         e.record()
         return e
+
+    def _timed(self, call, *args, **kw):
+        torch.cuda._sleep(AHEAD)
+        begin = self._event()
+        result = call(*args, **kw)
+        end = self._event()
+        self.late += begin.query()
+        return result, begin, end
 
     @staticmethod
     def _id(names, name):
@@ -63,10 +85,9 @@ class Recorder:
     def launch(self, name, read, written, call, *args, **kw):
         """call(*args, **kw), recorded as one launch, whatever kernels it takes. Bytes
         that depend on the data are functions of the result, called by trace()."""
-        begin = self._event()
-        result = call(*args, **kw)
+        result, begin, end = self._timed(call, *args, **kw)
         moved = [functools.partial(n, result) if callable(n) else n for n in (read, written)]
-        self.launches.append((self._id(self.names, name), begin, self._event(), *moved))
+        self.launches.append((self._id(self.names, name), begin, end, *moved))
         return result
 
     def trace(self) -> dict:
@@ -81,7 +102,7 @@ class Recorder:
             # events have their own resolution: a launch starts at or after the
             # end of the one before it
             s = max(last, round(self.base.elapsed_time(begin) * 1e6))
-            d = max(1, round(begin.elapsed_time(end) * 1e6))
+            d = max(1, round((begin.elapsed_time(end) - self.idle) * 1e6))
             start[i], dur[i], last = s, d, s + d
             counters[i, [TIME, READ, WRITTEN]] = d, *(n() if callable(n) else n
                                                        for n in (read, written))
@@ -112,7 +133,8 @@ def profile(rec: Recorder, **metadata) -> dict:
     return profile_doc.build(tr, out["match"].cpu().numpy(), tier, op, np.zeros_like(tier),
                              disp["row"].cpu().numpy(), disp.table_host(),
                              op_names=rec.ops, kernel_names=rec.names,
-                             metadata={"model_name": "attention workload", **metadata},
+                             metadata={"model_name": "attention workload",
+                                       "late_launches": rec.late, **metadata},
                              absent_mask=ABSENT)
 
 

@@ -96,3 +96,28 @@ def test_turn_bytes_are_what_is_copied_and_moved():
         assert len(n) * each < moved[0] <= len(n) * each + tables
     for moved in (read, written):
         assert len(moves) * each < moved[1] <= len(moves) * each + tables
+
+
+def test_launches_are_timed_on_the_device():
+    """What the host does inside a recorded call is not its device time."""
+    import time
+
+    import torch
+
+    from paper_2609_11938_amd import workload
+
+    x = torch.zeros(1000, device="cuda:0")
+
+    def call(wait):
+        time.sleep(wait)
+        x.add_(1)
+
+    call(0)
+    rec = workload.Recorder()
+    for _ in range(20):
+        rec.launch("add", 4000, 4000, call, 100e-6)
+    dur = rec.trace()["dur_ns"]
+    assert np.median(dur) < 50_000, dur
+    rec.late = 0
+    rec.launch("add", 4000, 4000, call, 20e-3)  # past what the device waits
+    assert rec.late == 1
