@@ -3,7 +3,6 @@ binding with the host compiler (in-tree, under _build/)."""
 from __future__ import annotations
 
 import glob
-import importlib.util
 import os
 import subprocess
 import sysconfig
@@ -36,25 +35,33 @@ def _run(cmd, out, verbose):
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source into one shared library, then the binding that
-    calls it (always recompiles)."""
-    os.makedirs(OUT_DIR, exist_ok=True)
-    include = os.path.join(HERE, "..", "include")
-    _run(["hipcc", *FLAGS, "-I", include, "-o", LIB + ".tmp", *sources()], LIB, verbose)
+    """The library, then the binding that calls it (always recompiles)."""
+    build_library(verbose)
     build_binding(verbose)
     return LIB
 
 
+def build_library(verbose: bool = False) -> str:
+    """Compile every HIP source into one shared library; needs nothing of torch."""
+    os.makedirs(OUT_DIR, exist_ok=True)
+    include = os.path.join(HERE, "..", "include")
+    _run(["hipcc", *FLAGS, "-I", include, "-o", LIB + ".tmp", *sources()], LIB, verbose)
+    return LIB
+
+
 def build_binding(verbose: bool = False) -> str:
-    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    """Compile the attention operators' binding against the installed torch."""
+    import torch
+
+    home = os.path.dirname(torch.__file__)
     _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
-          "-DUSE_ROCM=1", "-D_GLIBCXX_USE_CXX11_ABI=1",
-          *[f for d in (os.path.join(torch, "include"),
-                        os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+          "-DUSE_ROCM=1", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+          *[f for d in (os.path.join(home, "include"),
+                        os.path.join(home, "include", "torch", "csrc", "api", "include"),
                         os.path.join(ROCM, "include"), sysconfig.get_paths()["include"])
             for f in ("-isystem", d)],
           os.path.join(CSRC, "attn_bind.cpp"), "-o", BIND + ".tmp",
-          "-L", os.path.join(torch, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu",
+          "-L", os.path.join(home, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu",
           "-ltorch_python", "-L", OUT_DIR, "-lopattr", "-Wl,-rpath,$ORIGIN"], BIND, verbose)
     return BIND
 
