@@ -31,9 +31,11 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 struct BF16 {
   typedef __bf16 v8 __attribute__((ext_vector_type(8)));
   typedef __bf16 v2 __attribute__((ext_vector_type(2)));
-  // weights are exp2(x + kShift): float16 loses bits below 2^-14, bfloat16 has
-  // float32's range
-  static constexpr float kShift = 0.f;
+  // Weights are exp2(x + kShift). float16 loses bits below 2^-14. bfloat16 values go
+  // to float32's ends: weights of at most 2^(8 - 16) keep their sum in range while
+  // |v| times the keys is below 2^136, and values of 2^-124 still have their bits
+  // (with -24: of 2^-116).
+  static constexpr float kShift = -16.f;
   static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a),
                                                    __builtin_bit_cast(v8, b), c, 0, 0, 0);
@@ -88,6 +90,13 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The logarithm to base 2 of a weights' sum, without kShift (an exact product first:
+// no bits are lost to a difference).
+template <class E>
+__device__ __forceinline__ float log2_sum(float l) {
+  return log2f(l * exp2_fast(-E::kShift));
+}
 
 // Maximum and sum over a lane and its partner in the other half of the wave.
 __device__ __forceinline__ float half_max(float x) {

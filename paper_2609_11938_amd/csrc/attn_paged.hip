@@ -101,7 +101,7 @@ __device__ __forceinline__ void paged_store(const PagedArgs &a, int seq, int hea
     *reinterpret_cast<u32x2 *>(a.out.p + seq * a.out.ts + (int64_t)head * a.out.hs + d) = w;
   if (d == 0 && a.lse)
     a.lse[(int64_t)head * a.n_seqs + seq] =
-        l == 0.f ? -INFINITY : (top + log2f(l) - E::kShift) * kLn2;
+        l == 0.f ? -INFINITY : (top + log2_sum<E>(l)) * kLn2;
 }
 
 // Results of a share: [items][n_heads][DP + 4]: values, then reference and sum of

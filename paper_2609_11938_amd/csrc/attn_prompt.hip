@@ -252,7 +252,7 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
                     a.out.ts, sq.count - q0 - wave * 32, a.head_dim);
   if (a.lse && live && h == 0)
     a.lse[(int64_t)head * a.n_q + sq.first + qrow] =
-        l == 0.f ? -INFINITY : (m * c + log2f(l) - E::kShift) * kLn2;
+        l == 0.f ? -INFINITY : (m * c + log2_sum<E>(l)) * kLn2;
 }
 
 template <class E, int DP>

@@ -854,3 +854,29 @@ def test_workspace_of_another_stream_is_kept_until_its_use_is_over():
     torch.cuda.synchronize()
     assert pending
     assert not any(place - size < t.data_ptr() < place + size for t in others)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [200, 900])
+def test_prompt_values_near_the_largest(n, d):
+    """bfloat16 values whose weighted sum is in range, but not times the weights'
+    sum before its division."""
+    s = _prompt([n], [n], 2, 1, d, True, "bfloat16")
+    s["v"] = s["v"].abs() * 2.0 ** 124
+    s["vh"] = _host(s["v"])
+    _check_prompt(s, grad=False)
+
+
+def test_paged_values_near_the_largest():
+    rng = np.random.default_rng(8)
+    lens, g, d = [1100, 200], 2, 64
+    cache, table, kv = _cache(rng, lens, g, d, 16, "bfloat16")
+    cache[1] = cache[1].abs() * 2.0 ** 124
+    q, qh = _rand(rng, (2, 4, d), "bfloat16")
+    out, lse = attn.opattr_attn_paged(q, cache[0], cache[1], _ints(table), _ints(lens))
+    for b in range(2):
+        for j in range(4):
+            one = O.head(qh[b:b + 1, j], kv[b][0][:, j // 2], np.abs(kv[b][1][:, j // 2]) * 2.0 ** 124,
+                         0.125, False, "bfloat16")
+            _within(out[b:b + 1, j], one["out"], f"out[{b}, {j}]")
+            _within(lse[j, b:b + 1], one["lse"], f"lse[{j}, {b}]")
