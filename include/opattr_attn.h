@@ -38,7 +38,12 @@
  * beside a sequence, tokens past a length, keys and values that the causal mask
  * hides, NaN and infinities among them. The gradient is defined for finite
  * inputs: in a sequence that holds others, also rows that do not see them may
- * become NaN.
+ * become NaN. bfloat16 values of up to 2^136 over the number of keys keep the sum
+ * before its division by the weights' in float32's range.
+ *
+ * float16 gradients: ds is rounded after a power of two by the largest |dout| and |v|
+ * of its sequence and head, so neither another sequence nor, for dq, another query
+ * head costs it bits.
  */
 #ifndef OPATTR_ATTN_H
 #define OPATTR_ATTN_H

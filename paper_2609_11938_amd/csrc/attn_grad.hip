@@ -13,10 +13,13 @@
 // whose order changes the result; and sum_j p_j k_j, which takes the rounding of
 // `out` out of dq, is one more.
 //
-// Bound by issue, as the forward pass: 12 documents of up to 4001 tokens, 16 heads on
-// 4 of 128: dq 336 us, dk and dv 339, their sums 39, the matrix units busy 58% and 52%
-// of the first two; with the forward pass 879 us. 8 sequences of 512, 8 heads of 64:
-// 16 and 18 us, one round of blocks.
+// Products, exponentials and fragment reads follow one another in a wave, as in the
+// forward pass: 12 documents of up to 4001 tokens, 16 heads on 4 of 128: dq 346 us, dk
+// and dv 346, their sums 39, the matrix units busy 54% and 52% of the first two; with
+// the forward pass 887 us, in float16 (two launches more, which read dout and v once
+// more: 25 us) 961. 8 sequences of 512, 8 heads of 64: 16 and 18 us, one round of
+// blocks; a training pass 43 us, in float16 53. head_dim 72 to 120 costs nearly what 128
+// does.
 #include "attn_dev.h"
 #include "attn_impl.h"
 
@@ -118,9 +121,9 @@ constexpr int kFewBlocks = 256, kManyKeys = 768;
 // dS^T then is the B operand of dq^T = K^T dS^T. The pass goes by D' = dout . out,
 // which out's 16 bits make inexact; D - D' = sum_j p_j (dp_j - D') is summed beside
 // it, and with kp = sum_j p_j k_j, dq = sum_j p_j (dp_j - D') k_j - (D - D') kp puts
-// that right (a product more; dq's error against 64 bits, of values rounded to 16
-// bits once: 1.65 times that without, 1.4 with). The exact D goes to the second
-// pass with the scaled lse.
+// that right (a product more; the error of a training pass against 64 bits, in that of
+// the plain form rounded to 16 bits once: 1.65 without, 1.4 to 1.5 with). The exact D
+// goes to the second pass with the scaled lse.
 template <class E, int DP, int G>
 __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
@@ -330,8 +333,8 @@ __device__ __forceinline__ Span tile_queries(const PromptArgs &a, const Span &sq
   const int first = begin / kStep(DP), end = (sq.count + kStep(DP) - 1) / kStep(DP);
   return {first, end - first};
 }
-// Blocks that share the tile: at least a.split_steps steps of 32 queries each, at
-// most a.splits.
+// Blocks that share the tile: as many as bring each to a.split_steps steps of 32
+// queries or fewer, at most a.splits.
 template <int DP>
 __device__ __forceinline__ int tile_splits(const PromptArgs &a, const Span &sq, const Span &sk,
                                            int part) {
@@ -581,6 +584,9 @@ static void grad(const PromptArgs &a, hipStream_t s) {
 // block, a block takes fewer steps (4 sequences of 512, 8 heads on 4 of 128, 64 tiles
 // of up to 32 steps: a training pass of 85 us unsplit, 69 us by 8 steps, of which the
 // sums take 10; of 20 steps 48 and 47: not below 24).
+// The mean is what a batch of like sequences wants; a long one beside many short ones
+// is split less than alone: 4000 tokens, 8 heads on 2 of 128, a training pass of 268
+// us, with 30 sequences of one token beside it 797.
 constexpr int kSplitSteps = 24, kFewSteps = 8, kFewTiles = 192;
 GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv) {
   GradSplits x{1, kSplitSteps};

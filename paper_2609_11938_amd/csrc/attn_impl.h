@@ -28,7 +28,7 @@ struct PromptArgs {
 };
 
 // Blocks that share a key tile of the gradient at most, and the steps of 32 queries
-// that each has at least.
+// that each is to have, or fewer.
 struct GradSplits {
   int most, steps;
 };

@@ -11,7 +11,7 @@
 // Bound by the cache's bytes, each read once, with the next tile's keys and values in
 // registers and its pages a tile further: 2 sequences of 131000 tokens, 32 heads on 8
 // of 128: 192 us, 5.6 TB/s; 96 of up to 9001: 111 us, 4.9 TB/s, and 8 us for the join.
-// 4 of 150, 12 heads of 64: 5.5 us, the chain of length, table, keys and values.
+// 4 of 150, 12 heads of 64: 5.7 us, the chain of length, table, keys and values.
 #include <limits.h>
 
 #include "attn_dev.h"

@@ -8,12 +8,13 @@
 // lane's own but for one exchange between the halves, and the weights are where the
 // second product takes them.
 //
-// Bound by the issue of two waves a SIMD: 24 prompts of up to 4099 tokens, 32 heads on
-// 8 of 128: 363 us, 855 TFLOP/s counted (what is seen), the matrix units busy 52% of
-// the time; one of 16384, 16 heads on 4: 1082 us, 1.02 PFLOP/s, of which the products
-// alone take 680 us (softmax left out), the softmax 140, the reads of fragments from
-// LDS 260. 64 queries a wave, with half those reads, leave one wave a SIMD: twice the
-// time.
+// 24 prompts of up to 4099 tokens, 32 heads on 8 of 128: 358 us, 867 TFLOP/s counted
+// (what is seen), the matrix units busy 52% of the time; one of 16384, 16 heads on 4:
+// 1071 us, 1.03 PFLOP/s. In a wave the phases of a tile follow one another, and two
+// waves a SIMD hide little of that: products alone (softmax left out) 680 us, softmax
+// 140 and the reads of fragments from LDS 260 add up to the whole. 64 queries a wave,
+// with half those reads, leave one wave a SIMD: twice the time. head_dim 72 to 120
+// costs nearly what 128 does (24 prompts of 80: 313 us, of 96: 323).
 #include "attn_dev.h"
 #include "attn_impl.h"
 

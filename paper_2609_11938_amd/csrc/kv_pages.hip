@@ -9,7 +9,8 @@ namespace opa {
 
 // --------------------------------------------------------------------------
 // append: one wave a token, 16 bytes a lane. 40 sequences' 55k tokens, 8 heads of
-// 128: 90 us, 5.0 TB/s read and written; a few tokens: the launch
+// 128: 90 us, 5.0 TB/s read and written; a few tokens: the launch. Narrow tokens leave
+// lanes without a piece: 2 heads of 64 17 us, 3.3 TB/s, one head 16 us, 1.7 TB/s
 // --------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   const int lane = lane_id();
@@ -73,7 +74,7 @@ void run_append(const AppendArgs &a, hipStream_t s) {
 // and copies, each block for itself. The rest of a call is how the bits come
 // about (kHow):
 //   kSelf   every block sets them in LDS from the table: one launch, for small
-//           tables (8 sequences, 176 entries: a fork of 10 us where five
+//           tables (8 sequences, 176 entries: a fork of 8 us where five
 //           launches took 20 and their gaps; a table of 160 sequences, 41k
 //           entries, would be 166 KB for every block to read)
 //   kWords  a launch before sets them in memory, each block sums them in LDS
@@ -439,7 +440,7 @@ __global__ __launch_bounds__(kThreads) void k_compact_mark(PagesArgs a) {
 // m pages are in use. The j-th of those at or above m takes the j-th free place
 // below m; there are as many of one as of the other.
 // Bound by the copies: 160 sequences of up to 4096 tokens, 8 planes of 8192 pages of 32
-// KB: 205 us of a turn's 237 (1.04 GB read and written in all).
+// KB: 206 us of a turn's 239 (1.04 GB read and written in all).
 template <int kHow>
 __global__ __launch_bounds__(kThreads) void k_compact(PagesArgs a) {
   constexpr int kMost = kHow == kSelf ? kSelfPages : kLdsPages;
