@@ -8,6 +8,12 @@
  *   opattr_attn_paged        attention of one new token a sequence over a paged
  *                            cache, split over the cache's length and joined
  *   opattr_kv_append         new tokens' keys and values into their pages
+ *   opattr_attn_prompt_window, opattr_attn_prompt_window_grad,
+ *   opattr_attn_paged_window the same through a sliding window, with a few first
+ *                            tokens that stay visible
+ *   opattr_kv_append_scaled, opattr_attn_paged_scaled
+ *                            a paged cache of 8 bits a value, and the attention
+ *                            that reads it
  *   opattr_pages_fork        the next page table from the present one: sequences
  *                            dropped, continued, forked, and given room
  *   opattr_pages_compact     the pages in use moved to the front of the pool
@@ -99,6 +105,25 @@ int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
                             const opattr_rows *dk, const opattr_rows *dv, opattr_diag *diag,
                             void *ws, size_t ws_bytes, void *stream);
 
+/* Both through a sliding window with sinks. a->causal is 1, and query i, which stands
+   at p = i + (keys - queries), sees key j of its sequence when
+     j <= p and (j > p - window or j < sinks):
+   the last `window` keys up to its own, and the first `sinks`. window is 1 or more,
+   sinks 0 or more; a window as long as the sequence is the causal mask. Times go by
+   the keys that are seen. Everything else is as above: what the window hides takes no
+   part in an output, whatever its bits, and a query that sees no key has output 0. */
+int opattr_attn_prompt_window(const opattr_attn_shape *a, int32_t window, int32_t sinks,
+                              const opattr_rows *q, const opattr_rows *k, const opattr_rows *v,
+                              const opattr_rows *out, float *lse, opattr_diag *diag, void *stream);
+size_t opattr_attn_prompt_window_grad_workspace_bytes(const opattr_attn_shape *a, int32_t window,
+                                                      int32_t sinks);
+int opattr_attn_prompt_window_grad(const opattr_attn_shape *a, int32_t window, int32_t sinks,
+                                   const opattr_rows *dout, const opattr_rows *q,
+                                   const opattr_rows *k, const opattr_rows *v,
+                                   const opattr_rows *out, const float *lse, const opattr_rows *dq,
+                                   const opattr_rows *dk, const opattr_rows *dv, opattr_diag *diag,
+                                   void *ws, size_t ws_bytes, void *stream);
+
 /* One layer's paged cache: key (value) head g of token t of page x is at
    k (v) + x page_stride + t token_stride + g head_stride (elements, the same
    for both; 16-byte aligned, multiples of 8). page_size is a power of two
@@ -125,6 +150,16 @@ int opattr_attn_paged(const opattr_kv_pages *c, int32_t n_heads, const opattr_ro
                       const int32_t *lens, float scale, const opattr_rows *out, float *lse,
                       opattr_diag *diag, void *ws, size_t ws_bytes, void *stream);
 
+/* The same through a sliding window with sinks: of its n = lens[b] tokens sequence b's
+   query sees those with j >= n - window or j < sinks. Pages of which no token is seen
+   are not looked up: their table entries may be anything. */
+size_t opattr_attn_paged_window_workspace_bytes(const opattr_kv_pages *c, int32_t n_heads,
+                                                int32_t window, int32_t sinks);
+int opattr_attn_paged_window(const opattr_kv_pages *c, int32_t n_heads, int32_t window,
+                             int32_t sinks, const opattr_rows *q, const int32_t *lens, float scale,
+                             const opattr_rows *out, float *lse, opattr_diag *diag, void *ws,
+                             size_t ws_bytes, void *stream);
+
 /* Rows cu[b] .. cu[b+1]) of k_new and v_new (n_new rows, fewer than 2^26 - 4) become tokens lens[b],
    lens[b] + 1, ... of sequence b. lens_out (or NULL; not lens itself) receives
    lens[b] + (cu[b+1] - cu[b]). Tokens past the table's width or on a page
@@ -133,6 +168,54 @@ int opattr_attn_paged(const opattr_kv_pages *c, int32_t n_heads, const opattr_ro
 int opattr_kv_append(const opattr_kv_pages *c, int64_t n_new, const int32_t *cu,
                      const opattr_rows *k_new, const opattr_rows *v_new, const int32_t *lens,
                      int32_t *lens_out, opattr_diag *diag, void *stream);
+
+/* One layer's paged cache of 8 bits: a value is code * 2^(s - 127), its code an e4m3
+   number (4 bits of exponent, 3 of mantissa, largest 448, 0x7f and 0xff NaN), and s one
+   byte for block_size tokens of one head (255: NaN). Code d of key (value) head g of
+   token t of page x is the byte at k (v) + x page_stride + t token_stride + g
+   head_stride + d, and the scale of its block at k_scale (v_scale) + x scale_page_stride
+   + (t / block_size) scale_block_stride + g scale_head_stride: strides in BYTES, the
+   same for keys and values; k and v 16-byte aligned, their strides multiples of 16,
+   head_dim a multiple of 16. block_size is a power of two, at most page_size. The
+   scales may lie behind the codes in a page's own bytes: opattr_pages_fork and
+   opattr_pages_compact then take both along. dtype is that of the new rows, the queries
+   and the outputs; the rest is as in opattr_kv_pages. */
+typedef struct {
+  void *k, *v;
+  int64_t page_stride, token_stride, head_stride;
+  uint8_t *k_scale, *v_scale;
+  int64_t scale_page_stride, scale_block_stride, scale_head_stride;
+  int32_t n_pages, page_size, block_size;
+  const int32_t *table; /* [n_seqs][table_stride] */
+  int32_t n_seqs, table_stride;
+  int32_t n_kv_heads, head_dim;
+  int32_t dtype;
+} opattr_kv_scaled;
+
+/* opattr_kv_append into a cache of 8 bits. For each block and head that gets new
+   tokens let e be the least exponent of [-127, 127] with |x| <= 448 * 2^e for their
+   finite values (-127 if all are 0), or the block's present one if that is larger and
+   the block already holds tokens of the sequence. The new codes are x / 2^e rounded to
+   nearest, ties to even (what is not finite: NaN), the scale is e + 127, and where e has
+   grown the codes of the tokens already there are rounded again in the same way: powers
+   of two, so they change only where bits fall below e4m3's smallest, 2^-9. Other tokens'
+   codes and other blocks' scales stay as they are. Two sequences may not append into
+   one block. n_new, the blocks and the heads together are limited by one launch: (least
+   of n_new and n_new / block_size + 2 n_seqs) n_kv_heads is below 2^25. */
+int opattr_kv_append_scaled(const opattr_kv_scaled *c, int64_t n_new, const int32_t *cu,
+                            const opattr_rows *k_new, const opattr_rows *v_new,
+                            const int32_t *lens, int32_t *lens_out, opattr_diag *diag,
+                            void *stream);
+
+/* opattr_attn_paged_window over a cache of 8 bits (a window of 2^30 sees every token).
+   The codes are exact in the products; scores and values are scaled in float32, and
+   weights are rounded to 16 bits with the value's scale in them. */
+size_t opattr_attn_paged_scaled_workspace_bytes(const opattr_kv_scaled *c, int32_t n_heads,
+                                                int32_t window, int32_t sinks);
+int opattr_attn_paged_scaled(const opattr_kv_scaled *c, int32_t n_heads, int32_t window,
+                             int32_t sinks, const opattr_rows *q, const int32_t *lens, float scale,
+                             const opattr_rows *out, float *lse, opattr_diag *diag, void *ws,
+                             size_t ws_bytes, void *stream);
 
 /* A pool of pages: n_planes arrays (keys and values of each layer) of n_pages
    pages that share one page table. Page x of plane l is the page_bytes bytes

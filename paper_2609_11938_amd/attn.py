@@ -47,6 +47,16 @@ class opattr_kv_pages(C.Structure):
                 ("dtype", C.c_int32)]
 
 
+class opattr_kv_scaled(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("scale_page_stride", C.c_int64),
+                ("scale_block_stride", C.c_int64), ("scale_head_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("block_size", C.c_int32),
+                ("table", C.c_void_p), ("n_seqs", C.c_int32), ("table_stride", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
 class opattr_page_pool(C.Structure):
     _fields_ = [("data", C.c_void_p), ("plane_stride", C.c_int64), ("page_stride", C.c_int64),
                 ("n_planes", C.c_int32), ("n_pages", C.c_int32), ("page_bytes", C.c_int32),
@@ -55,7 +65,12 @@ class opattr_page_pool(C.Structure):
 
 EXPORTS = ("opattr_attn_prompt", "opattr_attn_prompt_grad",
            "opattr_attn_prompt_grad_workspace_bytes", "opattr_attn_paged",
-           "opattr_attn_paged_workspace_bytes", "opattr_kv_append", "opattr_pages_fork",
+           "opattr_attn_paged_workspace_bytes", "opattr_kv_append",
+           "opattr_attn_prompt_window", "opattr_attn_prompt_window_grad",
+           "opattr_attn_prompt_window_grad_workspace_bytes", "opattr_attn_paged_window",
+           "opattr_attn_paged_window_workspace_bytes", "opattr_kv_append_scaled",
+           "opattr_attn_paged_scaled", "opattr_attn_paged_scaled_workspace_bytes",
+           "opattr_pages_fork",
            "opattr_pages_fork_workspace_bytes", "opattr_pages_compact",
            "opattr_pages_compact_workspace_bytes")
 
@@ -82,6 +97,18 @@ def library():
     L.opattr_attn_paged.argtypes = [P(opattr_kv_pages), i32, rows, vp, C.c_float, rows, vp, vp,
                                     vp, sz, vp]
     L.opattr_kv_append.argtypes = [P(opattr_kv_pages), i64, vp, rows, rows, vp, vp, vp, vp]
+    L.opattr_attn_prompt_window.argtypes = [P(opattr_attn_shape), i32, i32, rows, rows, rows, rows,
+                                            vp, vp, vp]
+    L.opattr_attn_prompt_window_grad_workspace_bytes.argtypes = [P(opattr_attn_shape), i32, i32]
+    L.opattr_attn_prompt_window_grad.argtypes = [P(opattr_attn_shape), i32, i32, rows, rows, rows,
+                                                 rows, rows, vp, rows, rows, rows, vp, vp, sz, vp]
+    L.opattr_attn_paged_window_workspace_bytes.argtypes = [P(opattr_kv_pages), i32, i32, i32]
+    L.opattr_attn_paged_window.argtypes = [P(opattr_kv_pages), i32, i32, i32, rows, vp, C.c_float,
+                                           rows, vp, vp, vp, sz, vp]
+    L.opattr_kv_append_scaled.argtypes = [P(opattr_kv_scaled), i64, vp, rows, rows, vp, vp, vp, vp]
+    L.opattr_attn_paged_scaled_workspace_bytes.argtypes = [P(opattr_kv_scaled), i32, i32, i32]
+    L.opattr_attn_paged_scaled.argtypes = [P(opattr_kv_scaled), i32, i32, i32, rows, vp, C.c_float,
+                                           rows, vp, vp, vp, sz, vp]
     L.opattr_pages_fork_workspace_bytes.argtypes = [i32, i32, i32, i32]
     L.opattr_pages_fork.argtypes = [P(opattr_page_pool), vp, vp, i32, i32, vp, vp, i32, vp, vp,
                                     vp, vp, vp, sz, vp]
@@ -212,6 +239,97 @@ def opattr_kv_append(k_new, v_new, cu, k_pages, v_pages, table, lens, lens_out=N
     (_bind or binding()).kv_append(k_new, v_new, cu, k_pages, v_pages, table, lens, lens_out,
                                    diag)
     return lens_out
+
+
+def opattr_attn_prompt_window(q, k, v, cu_q, window, sinks=0, cu_k=None, scale=None, out=None,
+                              lse=None, diag=None, stream=None):
+    """Causal attention over packed prompts through a sliding window: (out, lse). A
+    query sees the last ``window`` keys up to its own place, and the first ``sinks``
+    of its sequence; the rest as in opattr_attn_prompt."""
+    if stream is not None:
+        return _on(stream, opattr_attn_prompt_window, q, k, v, cu_q, window, sinks, cu_k, scale,
+                   out, lse, diag=diag)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty(q.shape[1::-1], dtype=torch.float32, device=q.device)
+    (_bind or binding()).attn_prompt_window(q, k, v, cu_q, cu_k, window, sinks, scale, out, lse,
+                                            diag)
+    return out, lse
+
+
+def opattr_attn_prompt_window_grad(dout, q, k, v, out, lse, cu_q, window, sinks=0, cu_k=None,
+                                   scale=None, dq=None, dk=None, dv=None,
+                                   ws: Workspace | None = None, diag=None, stream=None):
+    """Gradients of sum(out * dout): (dq, dk, dv). out and lse are
+    opattr_attn_prompt_window's for the same inputs."""
+    if stream is not None:
+        return _on(stream, opattr_attn_prompt_window_grad, dout, q, k, v, out, lse, cu_q, window,
+                   sinks, cu_k, scale, dq, dk, dv, ws=ws, diag=diag)
+    if dq is None:
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if dk is None:
+        dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    if dv is None:
+        dv = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    _with_workspace((_bind or binding()).attn_prompt_window_grad, ws, q.device,
+                    (dout, q, k, v, out, lse, cu_q, cu_k, window, sinks, scale, dq, dk, dv), diag)
+    return dq, dk, dv
+
+
+def opattr_attn_paged_window(q, k_pages, v_pages, table, lens, window, sinks=0, scale=None,
+                             out=None, lse=None, ws: Workspace | None = None, diag=None,
+                             stream=None):
+    """Attention of one token a sequence over the last ``window`` and the first
+    ``sinks`` of its lens[b] tokens: (out, lse [heads, sequences]). Pages of which no
+    token is seen are not looked up."""
+    if stream is not None:
+        return _on(stream, opattr_attn_paged_window, q, k_pages, v_pages, table, lens, window,
+                   sinks, scale, out, lse, ws=ws, diag=diag)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty(q.shape[1::-1], dtype=torch.float32, device=q.device)
+    _with_workspace((_bind or binding()).attn_paged_window, ws, q.device,
+                    (q, k_pages, v_pages, table, lens, window, sinks, scale, out, lse), diag)
+    return out, lse
+
+
+def opattr_kv_append_scaled(k_new, v_new, cu, k_pages, v_pages, k_scales, v_scales, table, lens,
+                            lens_out=None, diag=None, stream=None):
+    """opattr_kv_append into a cache of 8 bits: codes k_pages and v_pages [pages,
+    page_size, kv_heads, head_dim] (float8_e4m3fn or uint8), and an exponent's byte for
+    each block of tokens and head, k_scales and v_scales [pages, blocks, kv_heads]
+    (float8_e8m0fnu or uint8): page_size / blocks tokens a block. A block's exponent
+    grows with its tokens, and what it holds is rounded to it again. Returns the new
+    lengths."""
+    if stream is not None:
+        return _on(stream, opattr_kv_append_scaled, k_new, v_new, cu, k_pages, v_pages, k_scales,
+                   v_scales, table, lens, lens_out, diag=diag)
+    if lens_out is None:
+        lens_out = torch.empty(lens.shape, dtype=torch.int32, device=k_pages.device)
+    (_bind or binding()).kv_append_scaled(k_new, v_new, cu, k_pages, v_pages, k_scales, v_scales,
+                                          table, lens, lens_out, diag)
+    return lens_out
+
+
+def opattr_attn_paged_scaled(q, k_pages, v_pages, k_scales, v_scales, table, lens, window=None,
+                             sinks=0, scale=None, out=None, lse=None,
+                             ws: Workspace | None = None, diag=None, stream=None):
+    """Attention of one token a sequence over a cache of 8 bits (see
+    opattr_kv_append_scaled): (out, lse [heads, sequences]). window None: all of the
+    lens[b] tokens; else the last ``window`` and the first ``sinks``."""
+    if stream is not None:
+        return _on(stream, opattr_attn_paged_scaled, q, k_pages, v_pages, k_scales, v_scales,
+                   table, lens, window, sinks, scale, out, lse, ws=ws, diag=diag)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty(q.shape[1::-1], dtype=torch.float32, device=q.device)
+    _with_workspace((_bind or binding()).attn_paged_scaled, ws, q.device,
+                    (q, k_pages, v_pages, k_scales, v_scales, table, lens, window, sinks, scale,
+                     out, lse), diag)
+    return out, lse
 
 
 def opattr_pages_fork(pool, page_size, table, lens, parent, room=None, held=None, table_out=None,

@@ -87,7 +87,14 @@ static bool ok_shape(const opattr_attn_shape *a) {
   return ((a->n_q > a->n_k ? a->n_q : a->n_k) / 128 + a->n_seqs) * a->n_heads <= kMaxGrid;
 }
 
-static PromptArgs prompt_args(const opattr_attn_shape *a, opattr_diag *diag) {
+// A window of a causal mask. No sequence has 2^30 tokens: what is past them says
+// nothing, and sums of the two stay in 32 bits.
+constexpr int32_t kMostWindow = (1 << 30) - 1;
+static bool ok_window(int32_t window, int32_t sinks) { return window >= 1 && sinks >= 0; }
+static int32_t at_most(int32_t x) { return std::min(x, kMostWindow); }
+
+static PromptArgs prompt_args(const opattr_attn_shape *a, int32_t window, int32_t sinks,
+                              opattr_diag *diag) {
   PromptArgs p{};
   p.cu_q = a->cu_q;
   p.cu_k = a->cu_k;
@@ -99,6 +106,8 @@ static PromptArgs prompt_args(const opattr_attn_shape *a, opattr_diag *diag) {
   p.group = a->n_heads / a->n_kv_heads;
   p.head_dim = a->head_dim;
   p.causal = a->causal;
+  p.window = at_most(window);
+  p.sinks = at_most(sinks);
   p.scale = a->scale;
   p.diag = diag;
   return p;
@@ -136,7 +145,73 @@ static bool ok_pages_out(const opattr_kv_pages *c) {
                                  {c->n_kv_heads, c->head_stride}, c->head_dim);
 }
 
+// Tokens of a sequence that its query sees, at most.
+template <class Cache>
+static int most_seen(const Cache *c, int32_t window, int32_t sinks) {
+  const int slots = c->table_stride * c->page_size;
+  return window ? std::min(slots, at_most(window) + at_most(sinks)) : slots;
+}
+
+// The cache of 8 bits: as above, in bytes.
+static bool ok_scaled(const opattr_kv_scaled *c) {
+  if (!c || c->n_pages < 0 || c->n_seqs < 0 || c->n_seqs >= 1 << 20 || c->table_stride < 0 ||
+      c->page_size < 1 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)) ||
+      c->block_size < 1 || c->block_size > c->page_size || (c->block_size & (c->block_size - 1)) ||
+      !ok_type(c->dtype) || !ok_heads(c->n_kv_heads, c->n_kv_heads, c->head_dim) ||
+      c->head_dim % 16)
+    return false;
+  if (c->n_seqs > 0 && c->table_stride > 0 && !c->table) return false;
+  if ((int64_t)c->table_stride * c->page_size >= (int64_t)1 << 30) return false;
+  if (c->n_pages == 0) return true;
+  if (!c->k || !c->v || (((uintptr_t)c->k | (uintptr_t)c->v) & 15) != 0 || !c->k_scale ||
+      !c->v_scale || (c->page_stride | c->token_stride | c->head_stride) % 16 != 0)
+    return false;
+  const int64_t most = (int64_t)1 << 40;
+  for (int64_t s : {c->page_stride, c->token_stride, c->head_stride, c->scale_page_stride,
+                    c->scale_block_stride, c->scale_head_stride})
+    if (s < 0 || s > most) return false;
+  return true;
+}
+static bool ok_scaled_out(const opattr_kv_scaled *c) {
+  return ok_scaled(c) &&
+         !overlap({c->n_pages, c->page_stride}, {c->page_size, c->token_stride},
+                  {c->n_kv_heads, c->head_stride}, c->head_dim) &&
+         !overlap({c->n_pages, c->scale_page_stride},
+                  {c->page_size / c->block_size, c->scale_block_stride},
+                  {c->n_kv_heads, c->scale_head_stride}, 1);
+}
+
 static int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
+
+// What the attention of one token a sequence takes of a cache, of either kind.
+template <class Cache>
+static void paged_args(PagedArgs &a, const Cache *c, int32_t n_heads, int32_t window,
+                       int32_t sinks, const opattr_rows *q, const int32_t *lens, float scale,
+                       const opattr_rows *out, float *lse, opattr_diag *diag, void *ws) {
+  a.ps = c->page_stride;
+  a.ts = c->token_stride;
+  a.hs = c->head_stride;
+  a.n_pages = c->n_pages;
+  a.shift = log2_of(c->page_size);
+  a.slots = c->table_stride * c->page_size;
+  a.window = at_most(window);
+  a.sinks = at_most(sinks);
+  a.most = most_seen(c, window, sinks);
+  a.table = c->table;
+  a.n_seqs = c->n_seqs;
+  a.width = c->table_stride;
+  a.n_kv = c->n_kv_heads;
+  a.group = n_heads / c->n_kv_heads;
+  a.n_heads = n_heads;
+  a.head_dim = c->head_dim;
+  a.q = rows(q);
+  a.out = rows(out);
+  a.lens = lens;
+  a.scale = scale;
+  a.lse = lse;
+  a.part = static_cast<float *>(ws);
+  a.diag = diag;
+}
 
 constexpr int kMaxPages = 1 << 24;
 
@@ -184,19 +259,14 @@ static int32_t *take(char *&at, size_t n) {
 
 static int launched() { return hipGetLastError() == hipSuccess ? OPATTR_OK : OPATTR_ERR_HIP; }
 
-}  // namespace opa
-
-using namespace opa;
-
-extern "C" {
-
-int opattr_attn_prompt(const opattr_attn_shape *a, const opattr_rows *q, const opattr_rows *k,
-                       const opattr_rows *v, const opattr_rows *out, float *lse,
-                       opattr_diag *diag, void *stream) {
+// The forward pass and the gradient; window 0: none.
+static int prompt(const opattr_attn_shape *a, int32_t window, int32_t sinks, const opattr_rows *q,
+                  const opattr_rows *k, const opattr_rows *v, const opattr_rows *out, float *lse,
+                  opattr_diag *diag, void *stream) {
   if (!ok_shape(a) || !ok_rows(q, a->n_q, a->head_dim) || !ok_rows(k, a->n_k, a->head_dim) ||
       !ok_rows(v, a->n_k, a->head_dim) || !ok_out(out, a->n_q, a->n_heads, a->head_dim))
     return OPATTR_ERR_INVALID_ARG;
-  PromptArgs p = prompt_args(a, diag);
+  PromptArgs p = prompt_args(a, window, sinks, diag);
   p.q = rows(q);
   p.k = rows(k);
   p.v = rows(v);
@@ -206,28 +276,29 @@ int opattr_attn_prompt(const opattr_attn_shape *a, const opattr_rows *q, const o
   return launched();
 }
 
-size_t opattr_attn_prompt_grad_workspace_bytes(const opattr_attn_shape *a) {
+static size_t grad_workspace(const opattr_attn_shape *a, int32_t window, int32_t sinks) {
   if (!ok_shape(a)) return 0;
   const size_t dp = a->head_dim <= 64 ? 64 : 128;
-  const int n = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads).most;
+  const int n = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads, at_most(window),
+                            at_most(sinks))
+                    .most;
   return align256((size_t)a->n_q * a->n_heads * 8) + norms_bytes(a) +
          (n > 1 ? (size_t)n * (a->n_k / 128 + a->n_seqs) * 128 * a->n_kv_heads * 2 * dp * 4 : 0);
 }
 
-int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
-                            const opattr_rows *q, const opattr_rows *k, const opattr_rows *v,
-                            const opattr_rows *out, const float *lse, const opattr_rows *dq,
-                            const opattr_rows *dk, const opattr_rows *dv, opattr_diag *diag,
-                            void *ws, size_t ws_bytes, void *stream) {
+static int prompt_grad(const opattr_attn_shape *a, int32_t window, int32_t sinks,
+                       const opattr_rows *dout, const opattr_rows *q, const opattr_rows *k,
+                       const opattr_rows *v, const opattr_rows *out, const float *lse,
+                       const opattr_rows *dq, const opattr_rows *dk, const opattr_rows *dv,
+                       opattr_diag *diag, void *ws, size_t ws_bytes, void *stream) {
   if (!ok_shape(a) || !ok_rows(dout, a->n_q, a->head_dim) || !ok_rows(q, a->n_q, a->head_dim) ||
       !ok_rows(k, a->n_k, a->head_dim) || !ok_rows(v, a->n_k, a->head_dim) ||
       !ok_rows(out, a->n_q, a->head_dim) || !ok_out(dq, a->n_q, a->n_heads, a->head_dim) ||
       !ok_out(dk, a->n_k, a->n_kv_heads, a->head_dim) ||
       !ok_out(dv, a->n_k, a->n_kv_heads, a->head_dim) || (a->n_q > 0 && !lse))
     return OPATTR_ERR_INVALID_ARG;
-  if (!ok_ws(ws, ws_bytes, opattr_attn_prompt_grad_workspace_bytes(a)))
-    return OPATTR_ERR_WORKSPACE;
-  PromptArgs p = prompt_args(a, diag);
+  if (!ok_ws(ws, ws_bytes, grad_workspace(a, window, sinks))) return OPATTR_ERR_WORKSPACE;
+  PromptArgs p = prompt_args(a, window, sinks, diag);
   p.dout = rows(dout);
   p.q = rows(q);
   p.k = rows(k);
@@ -242,52 +313,184 @@ int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
   at += align256((size_t)a->n_q * a->n_heads * 8);
   if (a->dtype == OPATTR_F16) p.norms = reinterpret_cast<uint32_t *>(at);
   p.part = reinterpret_cast<float *>(at + norms_bytes(a));
-  const GradSplits x = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads);
+  const GradSplits x = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads, p.window,
+                                   p.sinks);
   p.splits = x.most;
   p.split_steps = x.steps;
   run_prompt_grad(p, a->dtype, (hipStream_t)stream);
   return launched();
 }
 
-size_t opattr_attn_paged_workspace_bytes(const opattr_kv_pages *c, int32_t n_heads) {
+static size_t paged_bytes(const opattr_kv_pages *c, int32_t n_heads, int32_t window,
+                          int32_t sinks) {
   if (!ok_pages(c) || !ok_heads(n_heads, c->n_kv_heads, c->head_dim)) return 0;
-  return paged_workspace(c->n_seqs, c->n_kv_heads, n_heads, c->table_stride * c->page_size);
+  return paged_workspace(c->n_seqs, c->n_kv_heads, n_heads, most_seen(c, window, sinks));
+}
+
+template <class Cache>
+static bool ok_paged_call(const Cache *c, int32_t n_heads, const opattr_rows *q,
+                          const int32_t *lens, float scale, const opattr_rows *out) {
+  return ok_heads(n_heads, c->n_kv_heads, c->head_dim) && n_heads / c->n_kv_heads <= 16 &&
+         isfinite(scale) && ok_rows(q, c->n_seqs, c->head_dim) &&
+         ok_out(out, c->n_seqs, n_heads, c->head_dim) && (c->n_seqs == 0 || lens) &&
+         (int64_t)c->n_seqs * n_heads <= kMaxGrid / 2;
+}
+
+static int paged(const opattr_kv_pages *c, int32_t n_heads, int32_t window, int32_t sinks,
+                 const opattr_rows *q, const int32_t *lens, float scale, const opattr_rows *out,
+                 float *lse, opattr_diag *diag, void *ws, size_t ws_bytes, void *stream) {
+  if (!ok_pages(c) || !ok_paged_call(c, n_heads, q, lens, scale, out))
+    return OPATTR_ERR_INVALID_ARG;
+  if (!ok_ws(ws, ws_bytes, paged_bytes(c, n_heads, window, sinks))) return OPATTR_ERR_WORKSPACE;
+  PagedArgs a{};
+  paged_args(a, c, n_heads, window, sinks, q, lens, scale, out, lse, diag, ws);
+  a.k = static_cast<const uint16_t *>(c->k);
+  a.v = static_cast<const uint16_t *>(c->v);
+  run_paged(a, c->dtype, (hipStream_t)stream);
+  return launched();
+}
+
+}  // namespace opa
+
+using namespace opa;
+
+extern "C" {
+
+int opattr_attn_prompt(const opattr_attn_shape *a, const opattr_rows *q, const opattr_rows *k,
+                       const opattr_rows *v, const opattr_rows *out, float *lse,
+                       opattr_diag *diag, void *stream) {
+  return prompt(a, 0, 0, q, k, v, out, lse, diag, stream);
+}
+
+int opattr_attn_prompt_window(const opattr_attn_shape *a, int32_t window, int32_t sinks,
+                              const opattr_rows *q, const opattr_rows *k, const opattr_rows *v,
+                              const opattr_rows *out, float *lse, opattr_diag *diag,
+                              void *stream) {
+  if (!a || !a->causal || !ok_window(window, sinks)) return OPATTR_ERR_INVALID_ARG;
+  return prompt(a, window, sinks, q, k, v, out, lse, diag, stream);
+}
+
+size_t opattr_attn_prompt_grad_workspace_bytes(const opattr_attn_shape *a) {
+  return grad_workspace(a, 0, 0);
+}
+
+size_t opattr_attn_prompt_window_grad_workspace_bytes(const opattr_attn_shape *a, int32_t window,
+                                                      int32_t sinks) {
+  if (!a || !a->causal || !ok_window(window, sinks)) return 0;
+  return grad_workspace(a, window, sinks);
+}
+
+int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
+                            const opattr_rows *q, const opattr_rows *k, const opattr_rows *v,
+                            const opattr_rows *out, const float *lse, const opattr_rows *dq,
+                            const opattr_rows *dk, const opattr_rows *dv, opattr_diag *diag,
+                            void *ws, size_t ws_bytes, void *stream) {
+  return prompt_grad(a, 0, 0, dout, q, k, v, out, lse, dq, dk, dv, diag, ws, ws_bytes, stream);
+}
+
+int opattr_attn_prompt_window_grad(const opattr_attn_shape *a, int32_t window, int32_t sinks,
+                                   const opattr_rows *dout, const opattr_rows *q,
+                                   const opattr_rows *k, const opattr_rows *v,
+                                   const opattr_rows *out, const float *lse,
+                                   const opattr_rows *dq, const opattr_rows *dk,
+                                   const opattr_rows *dv, opattr_diag *diag, void *ws,
+                                   size_t ws_bytes, void *stream) {
+  if (!a || !a->causal || !ok_window(window, sinks)) return OPATTR_ERR_INVALID_ARG;
+  return prompt_grad(a, window, sinks, dout, q, k, v, out, lse, dq, dk, dv, diag, ws, ws_bytes,
+                     stream);
+}
+
+size_t opattr_attn_paged_workspace_bytes(const opattr_kv_pages *c, int32_t n_heads) {
+  return paged_bytes(c, n_heads, 0, 0);
+}
+
+size_t opattr_attn_paged_window_workspace_bytes(const opattr_kv_pages *c, int32_t n_heads,
+                                                int32_t window, int32_t sinks) {
+  return ok_window(window, sinks) ? paged_bytes(c, n_heads, window, sinks) : 0;
 }
 
 int opattr_attn_paged(const opattr_kv_pages *c, int32_t n_heads, const opattr_rows *q,
                       const int32_t *lens, float scale, const opattr_rows *out, float *lse,
                       opattr_diag *diag, void *ws, size_t ws_bytes, void *stream) {
-  if (!ok_pages(c) || !ok_heads(n_heads, c->n_kv_heads, c->head_dim) ||
-      n_heads / c->n_kv_heads > 16 || !isfinite(scale) ||
-      !ok_rows(q, c->n_seqs, c->head_dim) || !ok_out(out, c->n_seqs, n_heads, c->head_dim) ||
-      (c->n_seqs > 0 && !lens) || (int64_t)c->n_seqs * n_heads > kMaxGrid / 2)
+  return paged(c, n_heads, 0, 0, q, lens, scale, out, lse, diag, ws, ws_bytes, stream);
+}
+
+int opattr_attn_paged_window(const opattr_kv_pages *c, int32_t n_heads, int32_t window,
+                             int32_t sinks, const opattr_rows *q, const int32_t *lens, float scale,
+                             const opattr_rows *out, float *lse, opattr_diag *diag, void *ws,
+                             size_t ws_bytes, void *stream) {
+  if (!ok_window(window, sinks)) return OPATTR_ERR_INVALID_ARG;
+  return paged(c, n_heads, window, sinks, q, lens, scale, out, lse, diag, ws, ws_bytes, stream);
+}
+
+size_t opattr_attn_paged_scaled_workspace_bytes(const opattr_kv_scaled *c, int32_t n_heads,
+                                                int32_t window, int32_t sinks) {
+  if (!ok_scaled(c) || !ok_heads(n_heads, c->n_kv_heads, c->head_dim) ||
+      !ok_window(window, sinks))
+    return 0;
+  return paged_workspace(c->n_seqs, c->n_kv_heads, n_heads, most_seen(c, window, sinks));
+}
+
+int opattr_attn_paged_scaled(const opattr_kv_scaled *c, int32_t n_heads, int32_t window,
+                             int32_t sinks, const opattr_rows *q, const int32_t *lens, float scale,
+                             const opattr_rows *out, float *lse, opattr_diag *diag, void *ws,
+                             size_t ws_bytes, void *stream) {
+  if (!ok_window(window, sinks) || !ok_scaled(c) ||
+      !ok_paged_call(c, n_heads, q, lens, scale, out))
     return OPATTR_ERR_INVALID_ARG;
-  if (!ok_ws(ws, ws_bytes, opattr_attn_paged_workspace_bytes(c, n_heads)))
+  if (!ok_ws(ws, ws_bytes, opattr_attn_paged_scaled_workspace_bytes(c, n_heads, window, sinks)))
     return OPATTR_ERR_WORKSPACE;
-  PagedArgs a{};
-  a.k = static_cast<const uint16_t *>(c->k);
-  a.v = static_cast<const uint16_t *>(c->v);
+  ScaledArgs a{};
+  paged_args(a, c, n_heads, window, sinks, q, lens, scale, out, lse, diag, ws);
+  a.k_codes = static_cast<const uint8_t *>(c->k);
+  a.v_codes = static_cast<const uint8_t *>(c->v);
+  a.k_scale = c->k_scale;
+  a.v_scale = c->v_scale;
+  a.sps = c->scale_page_stride;
+  a.sbs = c->scale_block_stride;
+  a.shs = c->scale_head_stride;
+  a.block_shift = log2_of(c->block_size);
+  run_paged_scaled(a, c->dtype, (hipStream_t)stream);
+  return launched();
+}
+
+int opattr_kv_append_scaled(const opattr_kv_scaled *c, int64_t n_new, const int32_t *cu,
+                            const opattr_rows *k_new, const opattr_rows *v_new,
+                            const int32_t *lens, int32_t *lens_out, opattr_diag *diag,
+                            void *stream) {
+  if (!ok_scaled_out(c) || n_new < 0 || n_new > kMaxGrid * 4 ||
+      !ok_rows(k_new, n_new, c->head_dim) || !ok_rows(v_new, n_new, c->head_dim) ||
+      (c->n_seqs > 0 && (!cu || !lens)) || (lens_out && lens_out == lens) ||
+      append_units(n_new, c->n_seqs, log2_of(c->block_size)) * c->n_kv_heads * 2 > kMaxGrid * 4)
+    return OPATTR_ERR_INVALID_ARG;
+  AppendScaledArgs a{};
+  a.k = static_cast<uint8_t *>(c->k);
+  a.v = static_cast<uint8_t *>(c->v);
+  a.k_scale = c->k_scale;
+  a.v_scale = c->v_scale;
   a.ps = c->page_stride;
   a.ts = c->token_stride;
   a.hs = c->head_stride;
+  a.sps = c->scale_page_stride;
+  a.sbs = c->scale_block_stride;
+  a.shs = c->scale_head_stride;
   a.n_pages = c->n_pages;
   a.shift = log2_of(c->page_size);
   a.slots = c->table_stride * c->page_size;
+  a.block_shift = log2_of(c->block_size);
   a.table = c->table;
   a.n_seqs = c->n_seqs;
   a.width = c->table_stride;
   a.n_kv = c->n_kv_heads;
-  a.group = n_heads / c->n_kv_heads;
-  a.n_heads = n_heads;
   a.head_dim = c->head_dim;
-  a.q = rows(q);
-  a.out = rows(out);
+  a.n_new = (int)n_new;
+  a.cu = cu;
   a.lens = lens;
-  a.scale = scale;
-  a.lse = lse;
-  a.part = static_cast<float *>(ws);
+  a.kn = rows(k_new);
+  a.vn = rows(v_new);
+  a.lens_out = lens_out;
   a.diag = diag;
-  run_paged(a, c->dtype, (hipStream_t)stream);
+  run_append_scaled(a, c->dtype, (hipStream_t)stream);
   return launched();
 }
 

@@ -15,6 +15,7 @@
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 #include <stdexcept>
@@ -182,6 +183,17 @@ opattr_attn_shape shape(const at::Tensor &q, PyObject *ko, PyObject *cu_q, PyObj
   return a;
 }
 
+// A window's length and its sinks, which a query may see any number of.
+struct Window {
+  int32_t length, sinks;
+};
+Window window_of(PyObject *length, PyObject *sinks) {
+  const auto cut = [](int64_t x) {
+    return static_cast<int32_t>(std::min<int64_t>(std::max<int64_t>(x, -1), 1 << 30));
+  };
+  return {length == Py_None ? 1 << 30 : cut(integer(length)), cut(integer(sinks))};
+}
+
 // q k v cu_q cu_k causal scale out lse diag
 PyObject *attn_prompt(PyObject *const *o) {
   const at::Tensor &q = tensor(o[0], "q");
@@ -216,6 +228,46 @@ PyObject *attn_prompt_grad(PyObject *const *o) {
   return done(opattr_attn_prompt_grad(&a, &rd, &rq, &rk, &rv, &ro, lse, &sq, &sk, &sv,
                                       diag_of(o[14], q), ws.p, ws.bytes, stream_of(q)),
               "opattr_attn_prompt_grad");
+}
+
+// q k v cu_q cu_k window sinks scale out lse diag
+PyObject *attn_prompt_window(PyObject *const *o) {
+  const at::Tensor &q = tensor(o[0], "q");
+  const c10::DeviceGuard on(q.device());
+  const opattr_attn_shape a = shape(q, o[1], o[3], o[4], Py_True, o[7]);
+  const Window w = window_of(o[5], o[6]);
+  const int64_t h = a.n_heads, g = a.n_kv_heads, d = a.head_dim;
+  const opattr_rows rq = rows(o[0], q, a.n_q, h, d, "q"), rk = rows(o[1], q, a.n_k, g, d, "k"),
+                    rv = rows(o[2], q, a.n_k, g, d, "v"),
+                    ro = rows(o[8], q, a.n_q, h, d, "out");
+  no_gradient({o[0], o[1], o[2]}, "opattr_attn_prompt_window");
+  return done(opattr_attn_prompt_window(&a, w.length, w.sinks, &rq, &rk, &rv, &ro,
+                                        floats(o[9], q, {h, a.n_q}, "lse"), diag_of(o[10], q),
+                                        stream_of(q)),
+              "opattr_attn_prompt_window");
+}
+
+// dout q k v out lse cu_q cu_k window sinks scale dq dk dv ws diag
+PyObject *attn_prompt_window_grad(PyObject *const *o) {
+  const at::Tensor &q = tensor(o[1], "q");
+  const c10::DeviceGuard on(q.device());
+  const opattr_attn_shape a = shape(q, o[2], o[6], o[7], Py_True, o[10]);
+  const Window w = window_of(o[8], o[9]);
+  const int64_t h = a.n_heads, g = a.n_kv_heads, d = a.head_dim;
+  const opattr_rows rd = rows(o[0], q, a.n_q, h, d, "dout"), rq = rows(o[1], q, a.n_q, h, d, "q"),
+                    rk = rows(o[2], q, a.n_k, g, d, "k"), rv = rows(o[3], q, a.n_k, g, d, "v"),
+                    ro = rows(o[4], q, a.n_q, h, d, "out"),
+                    sq = rows(o[11], q, a.n_q, h, d, "dq"),
+                    sk = rows(o[12], q, a.n_k, g, d, "dk"),
+                    sv = rows(o[13], q, a.n_k, g, d, "dv");
+  const float *lse = floats(o[5], q, {h, a.n_q}, "lse");
+  const Work ws(o[14], q);
+  const size_t need = opattr_attn_prompt_window_grad_workspace_bytes(&a, w.length, w.sinks);
+  if (need > ws.bytes) return PyLong_FromSize_t(need);
+  return done(opattr_attn_prompt_window_grad(&a, w.length, w.sinks, &rd, &rq, &rk, &rv, &ro, lse,
+                                             &sq, &sk, &sv, diag_of(o[15], q), ws.p, ws.bytes,
+                                             stream_of(q)),
+              "opattr_attn_prompt_window_grad");
 }
 
 opattr_kv_pages kv_pages(PyObject *ko, PyObject *vo, PyObject *to) {
@@ -263,6 +315,115 @@ PyObject *attn_paged(PyObject *const *o) {
   return done(opattr_attn_paged(&c, small(h), &rq, lens, scale_of(o[5], d), &ro, lse,
                                 diag_of(o[9], q), ws.p, ws.bytes, stream_of(q)),
               "opattr_attn_paged");
+}
+
+// q k_pages v_pages table lens window sinks scale out lse ws diag
+PyObject *attn_paged_window(PyObject *const *o) {
+  const at::Tensor &q = tensor(o[0], "q");
+  const c10::DeviceGuard on(q.device());
+  const opattr_kv_pages c = kv_pages(o[1], o[2], o[3]);
+  if (q.dim() != 3) throw ValueError("q is [sequences, heads, head_dim]");
+  alike(q, THPVariable_Unpack(o[1]), "q");
+  const Window w = window_of(o[5], o[6]);
+  const int64_t b = c.n_seqs, h = q.size(1), d = c.head_dim;
+  const opattr_rows rq = rows(o[0], q, b, h, d, "q"), ro = rows(o[8], q, b, h, d, "out");
+  no_gradient({o[0], o[1], o[2]}, "opattr_attn_paged_window");
+  const int32_t *lens = ints(o[4], q, {b}, "lens");
+  float *lse = floats(o[9], q, {h, b}, "lse");
+  const Work ws(o[10], q);
+  const size_t need = opattr_attn_paged_window_workspace_bytes(&c, small(h), w.length, w.sinks);
+  if (need > ws.bytes) return PyLong_FromSize_t(need);
+  return done(opattr_attn_paged_window(&c, small(h), w.length, w.sinks, &rq, lens,
+                                       scale_of(o[7], d), &ro, lse, diag_of(o[11], q), ws.p,
+                                       ws.bytes, stream_of(q)),
+              "opattr_attn_paged_window");
+}
+
+// A cache of 8 bits for rows of like's type and device.
+opattr_kv_scaled kv_scaled(PyObject *ko, PyObject *vo, PyObject *kso, PyObject *vso, PyObject *to,
+                           const at::Tensor &like) {
+  const at::Tensor &k = tensor(ko, "k_pages"), &v = tensor(vo, "v_pages"),
+                   &ks = tensor(kso, "k_scales"), &vs = tensor(vso, "v_scales"),
+                   &t = tensor(to, "table");
+  for (const at::Tensor *x : {&k, &v})
+    if (x->scalar_type() != at::kFloat8_e4m3fn && x->scalar_type() != at::kByte)
+      throw TypeError("k_pages and v_pages: float8_e4m3fn or uint8 codes are taken");
+  for (const at::Tensor *x : {&ks, &vs})
+    if (x->scalar_type() != at::kFloat8_e8m0fnu && x->scalar_type() != at::kByte)
+      throw TypeError("k_scales and v_scales: float8_e8m0fnu or uint8 exponents are taken");
+  for (const at::Tensor *x : {&k, &v, &ks, &vs})
+    if (x->get_device() != like.get_device())
+      throw TypeError("the cache: not on the others' device");
+  if (k.dim() != 4 || k.sizes() != v.sizes() || k.strides() != v.strides())
+    throw ValueError("k_pages and v_pages are [pages, page_size, kv_heads, head_dim], alike in "
+                     "shape and strides");
+  if (k.stride(3) != 1 && k.size(3) > 1)
+    throw ValueError("k_pages: the last dimension's values must lie side by side");
+  if (ks.dim() != 3 || ks.sizes() != vs.sizes() || ks.strides() != vs.strides() ||
+      ks.size(0) != k.size(0) || ks.size(2) != k.size(2) || ks.size(1) < 1 ||
+      k.size(1) % ks.size(1) != 0)
+    throw ValueError("k_scales and v_scales are [pages, blocks, kv_heads], alike in shape and "
+                     "strides, their blocks a divisor of the page size");
+  if (t.dim() != 2) throw ValueError("table is [sequences, entries]");
+  opattr_kv_scaled c{};
+  c.k = k.data_ptr();
+  c.v = v.data_ptr();
+  c.page_stride = k.size(0) > 1 ? k.stride(0) : 0;
+  c.token_stride = k.size(1) > 1 ? k.stride(1) : 0;
+  c.head_stride = k.size(2) > 1 ? k.stride(2) : 0;
+  c.k_scale = static_cast<uint8_t *>(ks.data_ptr());
+  c.v_scale = static_cast<uint8_t *>(vs.data_ptr());
+  c.scale_page_stride = ks.size(0) > 1 ? ks.stride(0) : 0;
+  c.scale_block_stride = ks.size(1) > 1 ? ks.stride(1) : 0;
+  c.scale_head_stride = ks.size(2) > 1 ? ks.stride(2) : 0;
+  c.n_pages = small(k.size(0));
+  c.page_size = small(k.size(1));
+  c.block_size = small(k.size(1) / ks.size(1));
+  c.table = ints(to, k, {t.size(0), t.size(1)}, "table");
+  c.n_seqs = small(t.size(0));
+  c.table_stride = small(t.size(1));
+  c.n_kv_heads = small(k.size(2));
+  c.head_dim = small(k.size(3));
+  c.dtype = dtype_of(like);
+  return c;
+}
+
+// k_new v_new cu k_pages v_pages k_scales v_scales table lens lens_out diag
+PyObject *kv_append_scaled(PyObject *const *o) {
+  const at::Tensor &k = tensor(o[0], "k_new"), &cache = tensor(o[3], "k_pages");
+  const c10::DeviceGuard on(cache.device());
+  if (k.get_device() != cache.get_device()) throw TypeError("k_new: not on the others' device");
+  const opattr_kv_scaled c = kv_scaled(o[3], o[4], o[5], o[6], o[7], k);
+  const int64_t b = c.n_seqs, n = k.dim() ? k.size(0) : 0;
+  const opattr_rows rk = rows(o[0], k, n, c.n_kv_heads, c.head_dim, "k_new"),
+                    rv = rows(o[1], k, n, c.n_kv_heads, c.head_dim, "v_new");
+  no_gradient({o[0], o[1]}, "opattr_kv_append_scaled");
+  return done(opattr_kv_append_scaled(&c, n, ints(o[2], cache, {b + 1}, "cu"), &rk, &rv,
+                                      ints(o[8], cache, {b}, "lens"),
+                                      ints(o[9], cache, {b}, "lens_out"), diag_of(o[10], cache),
+                                      stream_of(cache)),
+              "opattr_kv_append_scaled");
+}
+
+// q k_pages v_pages k_scales v_scales table lens window sinks scale out lse ws diag
+PyObject *attn_paged_scaled(PyObject *const *o) {
+  const at::Tensor &q = tensor(o[0], "q");
+  const c10::DeviceGuard on(q.device());
+  const opattr_kv_scaled c = kv_scaled(o[1], o[2], o[3], o[4], o[5], q);
+  if (q.dim() != 3) throw ValueError("q is [sequences, heads, head_dim]");
+  const Window w = window_of(o[7], o[8]);
+  const int64_t b = c.n_seqs, h = q.size(1), d = c.head_dim;
+  const opattr_rows rq = rows(o[0], q, b, h, d, "q"), ro = rows(o[10], q, b, h, d, "out");
+  no_gradient({o[0]}, "opattr_attn_paged_scaled");
+  const int32_t *lens = ints(o[6], q, {b}, "lens");
+  float *lse = floats(o[11], q, {h, b}, "lse");
+  const Work ws(o[12], q);
+  const size_t need = opattr_attn_paged_scaled_workspace_bytes(&c, small(h), w.length, w.sinks);
+  if (need > ws.bytes) return PyLong_FromSize_t(need);
+  return done(opattr_attn_paged_scaled(&c, small(h), w.length, w.sinks, &rq, lens,
+                                       scale_of(o[9], d), &ro, lse, diag_of(o[13], q), ws.p,
+                                       ws.bytes, stream_of(q)),
+              "opattr_attn_paged_scaled");
 }
 
 // k_new v_new cu k_pages v_pages table lens lens_out diag
@@ -376,6 +537,11 @@ PyMethodDef methods[] = {method<attn_prompt, 10>("attn_prompt"),
                          method<attn_prompt_grad, 15>("attn_prompt_grad"),
                          method<attn_paged, 10>("attn_paged"),
                          method<kv_append, 9>("kv_append"),
+                         method<attn_prompt_window, 11>("attn_prompt_window"),
+                         method<attn_prompt_window_grad, 16>("attn_prompt_window_grad"),
+                         method<attn_paged_window, 12>("attn_paged_window"),
+                         method<kv_append_scaled, 11>("kv_append_scaled"),
+                         method<attn_paged_scaled, 14>("attn_paged_scaled"),
                          method<pages_fork, 12>("pages_fork"),
                          method<pages_compact, 8>("pages_compact"),
                          {nullptr, nullptr, 0, nullptr}};

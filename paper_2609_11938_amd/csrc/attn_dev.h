@@ -321,6 +321,22 @@ __device__ __forceinline__ bool find_tile(const int32_t *cu, int n, const int32_
   return false;
 }
 
+// The key tiles of ROWS keys that a block of queries walks through a window with
+// sinks: the first `sinks`, those of the sinks, then `skip` left out, `count` in all.
+// keys: as many as its last query sees without the window; place: how many keys
+// stand before its first query's own.
+struct Tiles {
+  int count, sinks, skip;
+};
+template <int ROWS>
+__device__ __forceinline__ Tiles window_tiles(int keys, int place, int window, int sinks) {
+  const int end = (keys + ROWS - 1) / ROWS;
+  const int first = clamp_to(place + 1 - window, 0, keys) / ROWS;
+  const int kept = ((sinks < keys ? sinks : keys) + ROWS - 1) / ROWS;
+  const int skip = first > kept ? first - kept : 0;
+  return {end - skip, kept, skip};
+}
+
 // Errors found in the data, into the record's flags, status and bad_records.
 __device__ inline void report(opattr_diag *diag, uint32_t flag, int bad) {
   if (!diag || bad <= 0) return;

@@ -124,7 +124,8 @@ constexpr int kFewBlocks = 256, kManyKeys = 768;
 // that right (a product more; the error of a training pass against 64 bits, in that of
 // the plain form rounded to 16 bits once: 1.65 without, 1.4 to 1.5 with). The exact D
 // goes to the second pass with the scaled lse.
-template <class E, int DP, int G>
+// W: through a window with sinks, as in the forward pass.
+template <class E, int DP, int G, bool W>
 __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
   constexpr int kStepK = kStep(DP), kTile = kStepK * DP;
@@ -155,9 +156,17 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
   const bool live = qrow < sq.count;
   const int last = (q0 + kHeld < sq.count ? q0 + kHeld : sq.count) - 1;
   const int keys = a.causal ? clamp_to(last + lead + 1, 0, sk.count) : sk.count;
-  const int tiles = (keys + kStepK - 1) / kStepK;
+  const Tiles walk = W ? window_tiles<kStepK>(keys, q0 + lead, a.window, a.sinks)
+                       : Tiles{(keys + kStepK - 1) / kStepK, 0, 0};
+  const int tiles = walk.count;
   const int whole = a.causal ? clamp_to(q0 + wave * 32 + lead + 1, 0, sk.count) : sk.count;
   const int seen = live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) : sk.count) : 0;
+  // this query's first key in the window, and the last one of the wave's queries
+  const int late = W ? qrow + lead + 1 - a.window : 0;
+  const int latest = W ? q0 + wave * 32 + 31 + lead + 1 - a.window : 0;
+  const auto place = [&](int t) __attribute__((always_inline)) {
+    return (W && t >= walk.sinks ? t + walk.skip : t) * kStepK;
+  };
   s16x8 qf[KS], df[kHeldHere ? KS : 1];
   float L = INFINITY, D = 0.f, off = 0.f;
   {
@@ -207,7 +216,8 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
   };
   const auto step = [&](const uint16_t *k, const uint16_t *v, int k0)
                         __attribute__((always_inline)) {
-    const bool cut = k0 + kStepK > whole;
+    const bool cut =
+        k0 + kStepK > whole || (W && k0 < latest && k0 + kStepK > a.sinks);
     const int nat = fresh(nat0), tr = fresh(tr0);
 #pragma unroll
     for (int kb = 0; kb < kStepK / 32; ++kb) {
@@ -225,8 +235,10 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
       }
       if (cut) {  // both: of a hidden key either may be past float32
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (k0 + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3) >= seen) x[e] = y[e] = 0.f;
+        for (int e = 0; e < 16; ++e) {
+          const int key = k0 + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3);
+          if (key >= seen || (W && key < late && key >= a.sinks)) x[e] = y[e] = 0.f;
+        }
       }
 #pragma unroll
       for (int e = 0; e < 16; e += 4) off += (y[e] + y[e + 1]) + (y[e + 2] + y[e + 3]);
@@ -252,11 +264,11 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
       (tiles + G - 1) / G,
       [&](auto i, int t) __attribute__((always_inline)) {
         load(i == 0 ? tk0[group] : tk1[group], i == 0 ? tv0[group] : tv1[group],
-             (t * G + group) * kStepK);
+             place(t * G + group));
       },
       [&](auto i, int t) __attribute__((always_inline)) {
         step(i == 0 ? tk0[group] : tk1[group], i == 0 ? tv0[group] : tv1[group],
-             (t * G + group) * kStepK);
+             place(t * G + group));
       });
   off = half_sum(off);
   const int t = threadIdx.x % (kGradWaves * OPA_WAVE);
@@ -303,11 +315,11 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
   block_sync();  // the tiles' last readers are done
   if (group) return;
   constexpr int kFit = G * kTile / (32 * DP);  // waves' rows in one tile's place
-  uint16_t *const place = wave / kFit == 0 ? tk0[0]
-                          : wave / kFit == 1 ? tk1[0]
-                          : wave / kFit == 2 ? tv0[0]
-                                             : tv1[0];
-  store_rows<E, DP>(place + wave % kFit * 32 * DP, dq, 1.f,
+  uint16_t *const room = wave / kFit == 0 ? tk0[0]
+                         : wave / kFit == 1 ? tk1[0]
+                         : wave / kFit == 2 ? tv0[0]
+                                            : tv1[0];
+  store_rows<E, DP>(room + wave % kFit * 32 * DP, dq, 1.f,
                     a.dq.p + (int64_t)(sq.first + q0 + wave * 32) * a.dq.ts +
                         (int64_t)head * a.dq.hs,
                     a.dq.ts, sq.count - q0 - wave * 32, a.head_dim);
@@ -325,20 +337,25 @@ __device__ __forceinline__ void row_load(float *to, const float *p, int left) {
 }
 
 // Tiles of queries that key tile `part` of a sequence meets: the first, and how many.
-template <int DP>
+template <int DP, bool W>
 __device__ __forceinline__ Span tile_queries(const PromptArgs &a, const Span &sq, const Span &sk,
                                              int part) {
-  const int begin =
-      a.causal ? clamp_to(part * kHeld - (sk.count - sq.count), 0, sq.count) : 0;
-  const int first = begin / kStep(DP), end = (sq.count + kStep(DP) - 1) / kStep(DP);
+  const int lead = sk.count - sq.count;
+  const int begin = a.causal ? clamp_to(part * kHeld - lead, 0, sq.count) : 0;
+  int past = sq.count;  // the last query that sees one, and one more
+  if (W && part * kHeld >= a.sinks) {
+    const int last = (part * kHeld + kHeld < sk.count ? part * kHeld + kHeld : sk.count) - 1;
+    past = clamp_to(last - lead + a.window, begin, sq.count);
+  }
+  const int first = begin / kStep(DP), end = (past + kStep(DP) - 1) / kStep(DP);
   return {first, end - first};
 }
 // Blocks that share the tile: as many as bring each to a.split_steps steps of 32
 // queries or fewer, at most a.splits.
-template <int DP>
+template <int DP, bool W>
 __device__ __forceinline__ int tile_splits(const PromptArgs &a, const Span &sq, const Span &sk,
                                            int part) {
-  const int steps = tile_queries<DP>(a, sq, sk, part).count * a.group * (kStep(DP) / 32);
+  const int steps = tile_queries<DP, W>(a, sq, sk, part).count * a.group * (kStep(DP) / 32);
   return clamp_to((steps + a.split_steps - 1) / a.split_steps, 1, a.splits);
 }
 
@@ -355,7 +372,7 @@ __device__ __forceinline__ f32x4 *part_of(const PromptArgs &a, int split, int ti
 // dk and dv of 32 keys a wave: S = Q K^T with the wave's keys as columns, so
 // that a lane holds one key; P and dS then are the B operands of
 // dv^T = dout^T P and dk^T = q^T dS.
-template <class E, int DP>
+template <class E, int DP, bool W>
 __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
   constexpr int kStepQ = kStep(DP), kTile = kStepQ * DP, kQB = kStepQ / 32;
@@ -379,10 +396,15 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   const int whole = key0 + 32 > sk.count ? sq.count
                                          : a.causal ? clamp_to(key0 + 31 - lead, 0, sq.count) : 0;
   const int from = live ? (a.causal ? clamp_to(key - lead, 0, sq.count) : 0) : sq.count;
-  const Span met = tile_queries<DP>(a, sq, sk, part);
+  // W: the last query that sees this lane's key, and the first that has left one of
+  // this wave's behind, both and one more
+  const int to = W && key >= a.sinks ? key - lead + a.window : sq.count;
+  const int plain = key0 > a.sinks ? key0 : a.sinks;  // the wave's first key that is no sink
+  const int left_from = W && plain < key0 + 32 ? plain - lead + a.window : sq.count;
+  const Span met = tile_queries<DP, W>(a, sq, sk, part);
   const int t0 = met.first, per = met.count;
   // this block's steps of the tile's: a head's queries, then the next head's
-  const int splits = tile_splits<DP>(a, sq, sk, part), all = per * a.group;
+  const int splits = tile_splits<DP, W>(a, sq, sk, part), all = per * a.group;
   if (split >= splits) return;
   const int first = (int)((int64_t)all * split / splits);
   const int steps = (int)((int64_t)all * (split + 1) / splits);
@@ -450,10 +472,12 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
           x[e] = p;
         }
       }
-      if (q0 < whole) {
+      if (q0 < whole || (W && q0 + kStepQ > left_from)) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (q0 + 32 * qb + 8 * (e >> 2) + 4 * h + (e & 3) < from) x[e] = y[e] = 0.f;
+        for (int e = 0; e < 16; ++e) {
+          const int row = q0 + 32 * qb + 8 * (e >> 2) + 4 * h + (e & 3);
+          if (row < from || (W && row >= to)) x[e] = y[e] = 0.f;
+        }
       }
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -513,7 +537,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
 
 // A key tile's dk and dv from those of its blocks, added in order; a tile of one
 // block is done already. A wave takes dk or dv of 32 keys.
-template <class E, int DP>
+template <class E, int DP, bool W>
 __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArgs a) {
   constexpr int DB = DP / 32;
   __shared__ __align__(16) uint16_t rows[2 * kGradWaves][32 * DP];
@@ -522,7 +546,7 @@ __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArg
   Span sq, sk;
   int part;
   if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part)) return;
-  const int splits = tile_splits<DP>(a, sq, sk, part);
+  const int splits = tile_splits<DP, W>(a, sq, sk, part);
   const int key0 = part * kHeld + wave * 32;
   if (splits == 1 || key0 >= sk.count) return;
   f32x16 sum[DB];
@@ -543,20 +567,22 @@ __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArg
                     sk.count - key0, a.head_dim);
 }
 
-template <class E, int DP>
+template <class E, int DP, bool W>
 static void launch(const PromptArgs &a, hipStream_t s) {
   const int64_t kt = (int64_t)a.n_k / kHeld + a.n_seqs, qt = (int64_t)a.n_q / kHeld + a.n_seqs;
   const dim3 block(kGradWaves * OPA_WAVE);
   const dim3 rows((uint32_t)(qt * a.n_heads));
-  if (a.n_q > 0 && qt * a.n_heads <= kFewBlocks && a.n_k >= (int64_t)kManyKeys * a.n_seqs)
-    hipLaunchKernelGGL((k_attn_dq<E, DP, 2>), rows, dim3(2 * kGradWaves * OPA_WAVE), 0, s, a);
+  const bool many = a.n_k >= (int64_t)kManyKeys * a.n_seqs &&
+                    (!W || (int64_t)a.window + a.sinks >= kManyKeys);
+  if (a.n_q > 0 && qt * a.n_heads <= kFewBlocks && many)
+    hipLaunchKernelGGL((k_attn_dq<E, DP, 2, W>), rows, dim3(2 * kGradWaves * OPA_WAVE), 0, s, a);
   else if (a.n_q > 0)
-    hipLaunchKernelGGL((k_attn_dq<E, DP, 1>), rows, block, 0, s, a);
+    hipLaunchKernelGGL((k_attn_dq<E, DP, 1, W>), rows, block, 0, s, a);
   if (a.n_k == 0) return;
-  hipLaunchKernelGGL((k_attn_dkv<E, DP>), dim3((uint32_t)(kt * a.n_kv * a.splits)), block, 0, s,
+  hipLaunchKernelGGL((k_attn_dkv<E, DP, W>), dim3((uint32_t)(kt * a.n_kv * a.splits)), block, 0, s,
                      a);
   if (a.splits > 1)
-    hipLaunchKernelGGL((k_dkv_sum<E, DP>), dim3((uint32_t)(kt * a.n_kv)),
+    hipLaunchKernelGGL((k_dkv_sum<E, DP, W>), dim3((uint32_t)(kt * a.n_kv)),
                        dim3(2 * kGradWaves * OPA_WAVE), 0, s, a);
 }
 
@@ -569,10 +595,10 @@ static void grad(const PromptArgs &a, hipStream_t s) {
     const dim3 grid(most / kNormRows + a.n_seqs, a.n_heads + a.n_kv);
     if (most > 0) hipLaunchKernelGGL(k_attn_norms, grid, dim3(256), 0, s, a);
   }
-  if (a.head_dim <= 64)
-    launch<E, 64>(a, s);
+  if (a.window)
+    a.head_dim <= 64 ? launch<E, 64, true>(a, s) : launch<E, 128, true>(a, s);
   else
-    launch<E, 128>(a, s);
+    a.head_dim <= 64 ? launch<E, 64, false>(a, s) : launch<E, 128, false>(a, s);
 }
 
 // Blocks of a key tile at most. A tile's steps go one after another, and a causal
@@ -588,11 +614,16 @@ static void grad(const PromptArgs &a, hipStream_t s) {
 // is split less than alone: 4000 tokens, 8 heads on 2 of 128, a training pass of 268
 // us, with 30 sequences of one token beside it 797.
 constexpr int kSplitSteps = 24, kFewSteps = 8, kFewTiles = 192;
-GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv) {
+GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv, int window,
+                       int sinks) {
   GradSplits x{1, kSplitSteps};
   if (n_seqs == 0 || n_k == 0) return x;
   const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
-  const int64_t steps = n_q * (n_heads / n_kv) / 32 / n_seqs;
+  // queries of a key tile, at most: a sink's tile meets every one
+  int64_t rows = n_q;
+  if (window && !sinks && (int64_t)n_seqs * (window + (int64_t)kHeld) < rows)
+    rows = (int64_t)n_seqs * (window + (int64_t)kHeld);
+  const int64_t steps = rows * (n_heads / n_kv) / 32 / n_seqs;
   if (blocks <= kFewTiles && steps >= kSplitSteps) x.steps = kFewSteps;
   int64_t n = (2048 + blocks - 1) / blocks;
   if (n > steps / x.steps) n = steps / x.steps;

@@ -25,6 +25,7 @@ struct PromptArgs {
   float *rows, *part;
   uint32_t *norms;
   int splits, split_steps;
+  int window, sinks;  // window 0: none
 };
 
 // Blocks that share a key tile of the gradient at most, and the steps of 32 queries
@@ -32,7 +33,8 @@ struct PromptArgs {
 struct GradSplits {
   int most, steps;
 };
-GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv);
+GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv, int window,
+                       int sinks);
 
 struct PagedArgs {
   const uint16_t *k, *v;
@@ -45,6 +47,27 @@ struct PagedArgs {
   float scale;
   float *lse;
   float *part;  // partial results
+  opattr_diag *diag;
+  int window, sinks;  // window 0: none
+  int most;           // tokens of a sequence that its query can see
+};
+
+// The cache of 8 bits; strides (those of PagedArgs too) in bytes.
+struct ScaledArgs : PagedArgs {
+  const uint8_t *k_codes, *v_codes, *k_scale, *v_scale;
+  int64_t sps, sbs, shs;  // the scales' page, block and head strides
+  int block_shift;        // log2 of the tokens with one scale
+};
+
+struct AppendScaledArgs {
+  uint8_t *k, *v, *k_scale, *v_scale;
+  int64_t ps, ts, hs, sps, sbs, shs;
+  int n_pages, shift, slots, block_shift;
+  const int32_t *table;
+  int n_seqs, width, n_kv, head_dim, n_new;
+  const int32_t *cu, *lens;
+  Rows kn, vn;
+  int32_t *lens_out;
   opattr_diag *diag;
 };
 
@@ -76,7 +99,11 @@ struct PagesArgs {
 };
 
 void run_paged(const PagedArgs &a, int dtype, hipStream_t s);
-size_t paged_workspace(int n_seqs, int n_kv, int n_heads, int slots);
+size_t paged_workspace(int n_seqs, int n_kv, int n_heads, int most);
+void run_paged_scaled(const ScaledArgs &a, int dtype, hipStream_t s);
+void run_append_scaled(const AppendScaledArgs &a, int dtype, hipStream_t s);
+// blocks of tokens that n_new new ones of n_seqs sequences touch, at most
+int64_t append_units(int64_t n_new, int n_seqs, int block_shift);
 void run_append(const AppendArgs &a, hipStream_t s);
 void run_fork(const PagesArgs &a, hipStream_t s);
 void run_compact(const PagesArgs &a, hipStream_t s);

@@ -12,84 +12,9 @@
 // registers and its pages a tile further: 2 sequences of 131000 tokens, 32 heads on 8
 // of 128: 192 us, 5.6 TB/s; 96 of up to 9001: 111 us, 4.9 TB/s, and 8 us for the join.
 // 4 of 150, 12 heads of 64: 5.7 us, the chain of length, table, keys and values.
-#include <limits.h>
-
-#include "attn_dev.h"
-#include "attn_impl.h"
+#include "attn_paged_dev.h"
 
 namespace opa {
-
-constexpr int kPagedWaves = 4;
-constexpr int kTile = 32;        // tokens a wave takes at a time
-constexpr int kMinShare = 256;   // tokens of the smallest share
-constexpr int kBlocks = 1024;
-
-// Tokens of sequence b, as many as its table can name.
-__device__ __forceinline__ int paged_len(const PagedArgs &a, int b) {
-  return b < a.n_seqs ? clamp_to(a.lens[b], 0, a.slots) : 0;
-}
-
-__device__ __forceinline__ int shares_of(int len, int c) { return len > c ? (len + c - 1) / c : 1; }
-
-// Sequences one to a lane; past 64, loops of as many.
-struct Share {
-  int size;   // tokens of every share but a sequence's last
-  int seq, part, len;
-  int first;  // the sequence's first share, as the shares are counted
-};
-
-// Tokens of a share, from every sequence's length: as many as make kBlocks shares
-// of the work of all key heads. mine: this lane's sequence's length.
-__device__ __forceinline__ int share_size(const PagedArgs &a, int mine) {
-  if (a.slots <= kMinShare) return kMinShare;
-  int64_t sum = mine;
-  for (int b = OPA_WAVE + lane_id(); b < a.n_seqs; b += OPA_WAVE) sum += paged_len(a, b);
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-  const int64_t each = (sum * a.n_kv + kBlocks - 1) / kBlocks;
-  const int64_t c = (each + kTile * kPagedWaves - 1) / (kTile * kPagedWaves) *
-                    (kTile * kPagedWaves);
-  return uniform((int)(c < kMinShare ? kMinShare : c < 1 << 30 ? c : 1 << 30));
-}
-
-// Share `item` of all the sequences' shares; false past the last. By whole waves.
-__device__ __forceinline__ bool find_share(const PagedArgs &a, int item, Share &s) {
-  const int lane = lane_id();
-  const int mine = paged_len(a, lane);
-  s.size = share_size(a, mine);
-  int done = 0;
-  for (int base = 0; base < a.n_seqs; base += OPA_WAVE) {
-    const int b = base + lane;
-    const int len = base ? paged_len(a, b) : mine;
-    const int n = b < a.n_seqs ? shares_of(len, s.size) : 0;
-    const int inc = wave_sums(n);
-    const uint64_t m = __ballot(done + inc > item);
-    if (m) {
-      const int w = __ffsll((unsigned long long)m) - 1;
-      s.seq = base + w;
-      s.first = done + __builtin_amdgcn_readlane(inc - n, w);
-      s.part = item - s.first;
-      s.len = __builtin_amdgcn_readlane(len, w);
-      return true;
-    }
-    done += __builtin_amdgcn_readlane(inc, OPA_WAVE - 1);
-  }
-  return false;
-}
-
-// The shares of sequence seq. By whole waves.
-__device__ __forceinline__ Share shares_at(const PagedArgs &a, int seq) {
-  const int lane = lane_id();
-  Share s{};
-  const int mine = paged_len(a, lane);
-  s.size = share_size(a, mine);
-  s.seq = seq;
-  s.len = uniform(paged_len(a, seq));
-  int sum = lane < seq ? shares_of(mine, s.size) : 0;
-  for (int b = OPA_WAVE + lane; b < seq; b += OPA_WAVE) sum += shares_of(paged_len(a, b), s.size);
-  s.first = __builtin_amdgcn_readlane(wave_sums(sum), OPA_WAVE - 1);
-  return s;
-}
 
 // A row's result from its values' sum, its weights' sum and reference.
 template <class E>
@@ -105,8 +30,9 @@ __device__ __forceinline__ void paged_store(const PagedArgs &a, int seq, int hea
 }
 
 // Results of a share: [items][n_heads][DP + 4]: values, then reference and sum of
-// the weights.
-template <class E, int DP>
+// the weights. W: through a window with sinks; the tokens that the query sees are
+// counted through, and what lies between them is never looked at.
+template <class E, int DP, bool W>
 __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedArgs a) {
   constexpr int KS = DP / 32, DB = DP / 16, C = DP / 8, N = kTile * C / OPA_WAVE;
   // each wave's tile of values; at the end the waves' sums
@@ -123,7 +49,8 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedA
   const int seq = s.seq, len = s.len;
   const int t0 = s.part * s.size, t1 = len < t0 + s.size ? len : t0 + s.size;
   const int32_t *table = a.table + (int64_t)seq * a.width;
-  if (a.diag && threadIdx.x == 0 && s.part == 0 && hk == 0 && a.lens[seq] != len)
+  const int tokens = W ? uniform(paged_tokens(a, seq)) : len, skip = tokens - len;
+  if (a.diag && threadIdx.x == 0 && s.part == 0 && hk == 0 && a.lens[seq] != tokens)
     report(a.diag, OPATTR_F_DATA, 1);
 
   const uint16_t *qrow = a.q.p + seq * a.q.ts + (int64_t)hk * a.group * a.q.hs;
@@ -148,12 +75,14 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedA
   constexpr int kNone = INT_MIN;
   const auto page_of = [&](int k0) __attribute__((always_inline)) {
     const int tok = k0 + (lane & 31);
-    return tok < t1 ? table[tok >> a.shift] : kNone;
+    return tok < t1 ? table[(W && tok >= a.sinks ? tok + skip : tok) >> a.shift] : kNone;
   };
   const auto place = [&](int page, int k0) __attribute__((always_inline)) {
     const bool ok = page >= 0 && page < a.n_pages;
     bad += page != kNone && !ok && lane < 32;
-    const int64_t at = page * a.ps + ((k0 + (lane & 31)) & mask) * a.ts + (int64_t)hk * a.hs;
+    const int tok = k0 + (lane & 31);
+    const int64_t at = page * a.ps + ((W && tok >= a.sinks ? tok + skip : tok) & mask) * a.ts +
+                       (int64_t)hk * a.hs;
     return ok ? at : (int64_t)-1;
   };
   // A tile's values (a row's chunks side by side) and keys (as A operands).
@@ -348,25 +277,20 @@ __global__ __launch_bounds__(kJoin * DP / 4) void k_paged_join(PagedArgs a) {
   paged_store<E>(a, seq, head, d, v, top, l);
 }
 
-// Shares at most: sum of ceil(len / c) with c >= kMinShare and c >= sum / (kBlocks
-// / n_kv).
-static int64_t most_items(int n_seqs, int n_kv, int slots) {
-  const int64_t a = (int64_t)kBlocks / n_kv + 1 + n_seqs;
-  const int64_t b = (int64_t)n_seqs * (slots > kMinShare ? (slots + kMinShare - 1) / kMinShare : 1);
-  return a < b ? a : b;
-}
-
-size_t paged_workspace(int n_seqs, int n_kv, int n_heads, int slots) {
-  if (slots <= kMinShare) return 0;  // no sequence has two shares
-  return (size_t)most_items(n_seqs, n_kv, slots) * n_heads * (128 + 4) * sizeof(float);
+size_t paged_workspace(int n_seqs, int n_kv, int n_heads, int most) {
+  if (most <= kMinShare) return 0;  // no sequence has two shares
+  return (size_t)most_items(n_seqs, n_kv, most) * n_heads * (128 + 4) * sizeof(float);
 }
 
 template <class E, int DP>
 static void launch(const PagedArgs &a, hipStream_t s) {
-  const int64_t items = most_items(a.n_seqs, a.n_kv, a.slots);
-  hipLaunchKernelGGL((k_attn_paged<E, DP>), dim3((uint32_t)(items * a.n_kv)),
-                     dim3(kPagedWaves * OPA_WAVE), 0, s, a);
-  if (a.slots > kMinShare)
+  const int64_t items = most_items(a.n_seqs, a.n_kv, a.most);
+  const dim3 grid((uint32_t)(items * a.n_kv)), block(kPagedWaves * OPA_WAVE);
+  if (a.window)
+    hipLaunchKernelGGL((k_attn_paged<E, DP, true>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((k_attn_paged<E, DP, false>), grid, block, 0, s, a);
+  if (a.most > kMinShare)
     hipLaunchKernelGGL((k_paged_join<E, DP>), dim3((uint32_t)(a.n_seqs * a.n_heads)),
                        dim3(kJoin * DP / 4), 0, s, a);
 }

@@ -1,0 +1,96 @@
+// Shares of the sequences' tokens, for the attention of one new token a sequence
+// over a paged cache (16 bits and 8).
+#pragma once
+#include <limits.h>
+
+#include "attn_dev.h"
+#include "attn_impl.h"
+
+namespace opa {
+
+constexpr int kPagedWaves = 4;
+constexpr int kTile = 32;        // tokens a wave takes at a time
+constexpr int kMinShare = 256;   // tokens of the smallest share
+constexpr int kBlocks = 1024;
+
+// Tokens of sequence b, as many as its table can name; of these, as many as its
+// query sees: the first and the last ones, through a window with sinks.
+__device__ __forceinline__ int paged_tokens(const PagedArgs &a, int b) {
+  return b < a.n_seqs ? clamp_to(a.lens[b], 0, a.slots) : 0;
+}
+__device__ __forceinline__ int paged_len(const PagedArgs &a, int b) {
+  const int n = paged_tokens(a, b);
+  return n < a.most ? n : a.most;
+}
+
+__device__ __forceinline__ int shares_of(int len, int c) { return len > c ? (len + c - 1) / c : 1; }
+
+// Sequences one to a lane; past 64, loops of as many.
+struct Share {
+  int size;   // tokens of every share but a sequence's last
+  int seq, part, len;
+  int first;  // the sequence's first share, as the shares are counted
+};
+
+// Tokens of a share, from every sequence's length: as many as make kBlocks shares
+// of the work of all key heads. mine: this lane's sequence's length.
+__device__ __forceinline__ int share_size(const PagedArgs &a, int mine) {
+  if (a.most <= kMinShare) return kMinShare;
+  int64_t sum = mine;
+  for (int b = OPA_WAVE + lane_id(); b < a.n_seqs; b += OPA_WAVE) sum += paged_len(a, b);
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+  const int64_t each = (sum * a.n_kv + kBlocks - 1) / kBlocks;
+  const int64_t c = (each + kTile * kPagedWaves - 1) / (kTile * kPagedWaves) *
+                    (kTile * kPagedWaves);
+  return uniform((int)(c < kMinShare ? kMinShare : c < 1 << 30 ? c : 1 << 30));
+}
+
+// Share `item` of all the sequences' shares; false past the last. By whole waves.
+__device__ __forceinline__ bool find_share(const PagedArgs &a, int item, Share &s) {
+  const int lane = lane_id();
+  const int mine = paged_len(a, lane);
+  s.size = share_size(a, mine);
+  int done = 0;
+  for (int base = 0; base < a.n_seqs; base += OPA_WAVE) {
+    const int b = base + lane;
+    const int len = base ? paged_len(a, b) : mine;
+    const int n = b < a.n_seqs ? shares_of(len, s.size) : 0;
+    const int inc = wave_sums(n);
+    const uint64_t m = __ballot(done + inc > item);
+    if (m) {
+      const int w = __ffsll((unsigned long long)m) - 1;
+      s.seq = base + w;
+      s.first = done + __builtin_amdgcn_readlane(inc - n, w);
+      s.part = item - s.first;
+      s.len = __builtin_amdgcn_readlane(len, w);
+      return true;
+    }
+    done += __builtin_amdgcn_readlane(inc, OPA_WAVE - 1);
+  }
+  return false;
+}
+
+// The shares of sequence seq. By whole waves.
+__device__ __forceinline__ Share shares_at(const PagedArgs &a, int seq) {
+  const int lane = lane_id();
+  Share s{};
+  const int mine = paged_len(a, lane);
+  s.size = share_size(a, mine);
+  s.seq = seq;
+  s.len = uniform(paged_len(a, seq));
+  int sum = lane < seq ? shares_of(mine, s.size) : 0;
+  for (int b = OPA_WAVE + lane; b < seq; b += OPA_WAVE) sum += shares_of(paged_len(a, b), s.size);
+  s.first = __builtin_amdgcn_readlane(wave_sums(sum), OPA_WAVE - 1);
+  return s;
+}
+
+// Shares at most: sum of ceil(len / c) with c >= kMinShare and c >= sum / (kBlocks
+// / n_kv).
+inline int64_t most_items(int n_seqs, int n_kv, int most) {
+  const int64_t a = (int64_t)kBlocks / n_kv + 1 + n_seqs;
+  const int64_t b = (int64_t)n_seqs * (most > kMinShare ? (most + kMinShare - 1) / kMinShare : 1);
+  return a < b ? a : b;
+}
+
+}  // namespace opa

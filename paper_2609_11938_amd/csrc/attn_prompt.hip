@@ -31,7 +31,10 @@ constexpr int kFewBlocks = 384, kManyKeys = 768;
 
 // G groups of kWaves waves take the key tiles in turn and join their sums at the
 // end: the waves that a few rows would leave a compute unit without.
-template <class E, int DP, int G>
+// W: through a window with sinks. A block's tiles are those of the sinks and those
+// from its first query's window on; in a tile that a query of the wave does not see
+// whole, the hidden scores are -inf as the causal mask's are.
+template <class E, int DP, int G, bool W>
 __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
   constexpr int kTile = kRowsK * DP;
@@ -59,10 +62,21 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
   const bool live = qrow < sq.count;
   const int last = (q0 + kRowsQ < sq.count ? q0 + kRowsQ : sq.count) - 1;
   const int keys = a.causal ? clamp_to(last + lead + 1, 0, sk.count) : sk.count;
-  const int tiles = (keys + kRowsK - 1) / kRowsK;
+  const Tiles walk = W ? window_tiles<kRowsK>(keys, q0 + lead, a.window, a.sinks)
+                       : Tiles{(keys + kRowsK - 1) / kRowsK, 0, 0};
+  const int tiles = walk.count;
   // keys below `whole` are seen by every query of this wave
   const int whole = a.causal ? clamp_to(q0 + wave * 32 + lead + 1, 0, sk.count) : sk.count;
   const int seen = live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) : sk.count) : 0;
+  // this query's first key in the window, and the last one of the wave's queries
+  const int late = W ? qrow + lead + 1 - a.window : 0;
+  const int latest = W ? q0 + wave * 32 + 31 + lead + 1 - a.window : 0;
+  const auto hidden = [&](int key) __attribute__((always_inline)) {
+    return key >= seen || (W && key < late && key >= a.sinks);
+  };
+  const auto place = [&](int t) __attribute__((always_inline)) {
+    return (W && t >= walk.sinks ? t + walk.skip : t) * kRowsK;
+  };
 
   // scores in units of 1 / c, c > 0: a negative scale turns the queries round
   const float c = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-120f);
@@ -99,13 +113,14 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
         x[kb] = E::mfma(nat_frag<DP>(k, nat, 32 * kb, s), qf[s], x[kb]);
-    const bool cut = k0 + kRowsK > whole;
+    const bool cut =
+        k0 + kRowsK > whole || (W && k0 < latest && k0 + kRowsK > a.sinks);
     if (cut) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (k0 + 32 * kb + 8 * (i >> 2) + 4 * h + (i & 3) >= seen) x[kb][i] = -INFINITY;
+          if (hidden(k0 + 32 * kb + 8 * (i >> 2) + 4 * h + (i & 3))) x[kb][i] = -INFINITY;
     }
     float top = m;
 #pragma unroll
@@ -152,7 +167,7 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             only[i] = h == n >> 3 && i == (n & 7) >> 1 ? (n & 1 ? 0xffff0000u : 0xffffu) : 0u;
-          const bool sees = k0 + 16 * s + 8 * ((n & 7) >> 2) + 4 * (n >> 3) + (n & 3) < seen;
+          const bool sees = !hidden(k0 + 16 * s + 8 * ((n & 7) >> 2) + 4 * (n >> 3) + (n & 3));
           const s16x8 pn = __builtin_bit_cast(s16x8, __builtin_bit_cast(u32x4, pf[s]) & only);
 #pragma unroll
           for (int d = 0; d < DB; ++d) {
@@ -215,11 +230,11 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
       (tiles + G - 1) / G,
       [&](auto i, int t) __attribute__((always_inline)) {
         load(i == 0 ? tk0[group] : tk1[group], i == 0 ? tv0[group] : tv1[group],
-             (t * G + group) * kRowsK);
+             place(t * G + group));
       },
       [&](auto i, int t) __attribute__((always_inline)) {
         step(std::false_type{}, i == 0 ? tk0[group] : tk1[group],
-             i == 0 ? tv0[group] : tv1[group], (t * G + group) * kRowsK);
+             i == 0 ? tv0[group] : tv1[group], place(t * G + group));
       });
   if constexpr (G > 1) join();
   // A weight of 0 times a value that is not finite is no 0: where a sum is not
@@ -233,7 +248,8 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
       for (int i = 0; i < 16; ++i) zero = fmaf(o[d][i], 0.f, zero);
     if (__syncthreads_or(group == 0 && !(zero == 0.f))) {
       start();
-      for (int k0 = group * kRowsK; k0 < tiles * kRowsK + group * kRowsK; k0 += G * kRowsK) {
+      for (int t = group; t < tiles + group; t += G) {
+        const int k0 = place(t);
         load(tk0[group], tv0[group], k0);
         wait_loads();
         block_sync();
@@ -256,15 +272,22 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
         l == 0.f ? -INFINITY : (m * c + log2_sum<E>(l)) * kLn2;
 }
 
-template <class E, int DP>
-static void launch(const PromptArgs &a, hipStream_t s) {
+template <class E, int DP, bool W>
+static void launch_as(const PromptArgs &a, hipStream_t s) {
   const int64_t blocks = ((int64_t)a.n_q / kRowsQ + a.n_seqs) * a.n_heads;
-  if (blocks <= kFewBlocks && a.n_k >= (int64_t)kManyKeys * a.n_seqs)
-    hipLaunchKernelGGL((k_attn_prompt<E, DP, 2>), dim3((uint32_t)blocks),
+  const bool many = a.n_k >= (int64_t)kManyKeys * a.n_seqs &&
+                    (!W || (int64_t)a.window + a.sinks >= kManyKeys);
+  if (blocks <= kFewBlocks && many)
+    hipLaunchKernelGGL((k_attn_prompt<E, DP, 2, W>), dim3((uint32_t)blocks),
                        dim3(2 * kWaves * OPA_WAVE), 0, s, a);
   else
-    hipLaunchKernelGGL((k_attn_prompt<E, DP, 1>), dim3((uint32_t)blocks),
+    hipLaunchKernelGGL((k_attn_prompt<E, DP, 1, W>), dim3((uint32_t)blocks),
                        dim3(kWaves * OPA_WAVE), 0, s, a);
+}
+
+template <class E, int DP>
+static void launch(const PromptArgs &a, hipStream_t s) {
+  a.window ? launch_as<E, DP, true>(a, s) : launch_as<E, DP, false>(a, s);
 }
 
 // The offsets alone, for calls whose kernels have no queries to start from.
