@@ -108,6 +108,7 @@ static PromptArgs prompt_args(const opattr_attn_shape *a, int32_t window, int32_
   p.causal = a->causal;
   p.window = at_most(window);
   p.sinks = at_most(sinks);
+  p.head_shift = window ? window_heads(p.group) : 0;
   p.scale = a->scale;
   p.diag = diag;
   return p;

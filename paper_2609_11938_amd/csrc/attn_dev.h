@@ -297,14 +297,22 @@ __device__ __forceinline__ int wave_sums(int x) {
 // of the sequence's tiles it is, the sequence's spans in both offset arrays, and
 // which sequence; false past the last. By whole waves; the result is uniform. Each lane loads a
 // sequence's four offsets at once: what follows waits for one load.
+__device__ __forceinline__ int tiles_of(int count, int rows) { return (count + rows - 1) / rows; }
+struct RowsLog2 {
+  int n;  // 2^n rows
+};
+__device__ __forceinline__ int tiles_of(int count, RowsLog2 rows) {
+  return (count + (1 << rows.n) - 1) >> rows.n;
+}
+template <class R>
 __device__ __forceinline__ bool find_tile(const int32_t *cu, int n, const int32_t *other,
-                                          int n_other, int n_seqs, int rows, int tile, Span &mine,
+                                          int n_other, int n_seqs, R rows, int tile, Span &mine,
                                           Span &its, int &part, int *seq = nullptr) {
   const int lane = lane_id();
   for (int base = 0; base < n_seqs; base += OPA_WAVE) {
     const int b = base + lane < n_seqs ? base + lane : n_seqs - 1;
     const Span x = span_of(cu, b, n), y = span_of(other, b, n_other);
-    const int tiles = base + lane < n_seqs ? (x.count + rows - 1) / rows : 0;
+    const int tiles = base + lane < n_seqs ? tiles_of(x.count, rows) : 0;
     const int inc = wave_sums(tiles);
     const uint64_t m = __ballot(inc > tile);
     if (m) {
@@ -321,20 +329,42 @@ __device__ __forceinline__ bool find_tile(const int32_t *cu, int n, const int32_
   return false;
 }
 
-// The key tiles of ROWS keys that a block of queries walks through a window with
-// sinks: the first `sinks`, those of the sinks, then `skip` left out, `count` in all.
-// keys: as many as its last query sees without the window; place: how many keys
-// stand before its first query's own.
-struct Tiles {
-  int count, sinks, skip;
-};
-template <int ROWS>
-__device__ __forceinline__ Tiles window_tiles(int keys, int place, int window, int sinks) {
-  const int end = (keys + ROWS - 1) / ROWS;
-  const int first = clamp_to(place + 1 - window, 0, keys) / ROWS;
-  const int kept = ((sinks < keys ? sinks : keys) + ROWS - 1) / ROWS;
-  const int skip = first > kept ? first - kept : 0;
-  return {end - skip, kept, skip};
+// Through a window with sinks a block of queries counts its keys without those that
+// lie between the sinks and its first query's window: key j is place j, or past the
+// sinks place j - window_skip. place: how many keys stand before its first query's.
+__device__ __forceinline__ int window_skip(int place, int window, int sinks) {
+  const int first = place + 1 - window;
+  return first > sinks ? first - sinks : 0;
+}
+// tile_load of the places from k0 on; `left` places exist from there. The tile that
+// the last sink is in has rows of both: each lane asks one of two ranges.
+template <int DP, int ROWS, int NW>
+__device__ __forceinline__ void window_tile_load(uint16_t *tile, const uint16_t *src, int64_t ts,
+                                                 int k0, int left, int sinks, int skip,
+                                                 int head_dim, int wave) {
+  if (skip == 0 || k0 >= sinks) {
+    tile_load<DP, ROWS, NW>(tile, src + (int64_t)(k0 + skip) * ts, ts, left, head_dim, wave);
+    return;
+  }
+  constexpr int C = DP / 8, N = ROWS * C / (NW * OPA_WAVE);
+  const auto near = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint16_t *>(uniform(src + (int64_t)(k0 + skip) * ts)), (short)0,
+      uniform((int)(clamp_to(left, 0, ROWS) * ts * 2)), 0x00027000);
+  const auto front = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint16_t *>(uniform(src + (int64_t)k0 * ts)), (short)0,
+      uniform((int)(clamp_to(sinks - k0, 0, ROWS) * ts * 2)), 0x00027000);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int first = (i * NW + wave) * OPA_WAVE;
+    const int id = first + lane_id(), row = id / C, chunk = (id % C) ^ swz<DP>(row);
+    const uint32_t off = chunk * 8 < head_dim ? (uint32_t)(row * (int)ts * 2 + chunk * 16)
+                                              : 0xfffffff0u;
+    const auto to = (__attribute__((address_space(3))) void *)(tile + first * 8);
+    if (k0 + row < sinks)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(front, to, 16, (int)off, 0, 0, 0);
+    else
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(near, to, 16, (int)off, 0, 0, 0);
+  }
 }
 
 // Errors found in the data, into the record's flags, status and bad_records.

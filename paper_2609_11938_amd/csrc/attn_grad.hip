@@ -124,7 +124,7 @@ constexpr int kFewBlocks = 256, kManyKeys = 768;
 // that right (a product more; the error of a training pass against 64 bits, in that of
 // the plain form rounded to 16 bits once: 1.65 without, 1.4 to 1.5 with). The exact D
 // goes to the second pass with the scaled lse.
-// W: through a window with sinks, as in the forward pass.
+// W: through a window with sinks, with heads and keys as in the forward pass.
 template <class E, int DP, int G, bool W>
 __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
@@ -141,32 +141,39 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
   int id = blockIdx.x;
   const int hk = id % a.n_kv;
   id /= a.n_kv;
-  const int head = hk * a.group + id % a.group;
+  const int hs = W ? a.head_shift : 0, heads = a.group >> hs;
+  const int head = hk * a.group + (id % heads << hs) + (wave & ((1 << hs) - 1));
+  const int rows = kHeld >> hs, from = (wave >> hs) * 32;  // the block's, the wave's first
   if (blockIdx.x == 0) {
     check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag);
     check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
   }
   Span sq, sk;
   int part, seq;
-  if (!find_tile(a.cu_q, a.n_q, a.cu_k, a.n_k, a.n_seqs, kHeld, id / a.group, sq, sk, part, &seq))
-    return;
-  const int q0 = ((sq.count + kHeld - 1) / kHeld - 1 - part) * kHeld;
+  if constexpr (W) {
+    if (!find_tile(a.cu_q, a.n_q, a.cu_k, a.n_k, a.n_seqs, RowsLog2{7 - hs}, id / heads, sq, sk,
+                   part, &seq))
+      return;
+  } else {
+    if (!find_tile(a.cu_q, a.n_q, a.cu_k, a.n_k, a.n_seqs, kHeld, id / heads, sq, sk, part, &seq))
+      return;
+  }
+  const int q0 = W ? (tiles_of(sq.count, RowsLog2{7 - hs}) - 1 - part) * rows
+                   : ((sq.count + kHeld - 1) / kHeld - 1 - part) * kHeld;
   const int lead = sk.count - sq.count;
-  const int qrow = q0 + wave * 32 + r;
+  const int qrow = q0 + from + r;
   const bool live = qrow < sq.count;
-  const int last = (q0 + kHeld < sq.count ? q0 + kHeld : sq.count) - 1;
-  const int keys = a.causal ? clamp_to(last + lead + 1, 0, sk.count) : sk.count;
-  const Tiles walk = W ? window_tiles<kStepK>(keys, q0 + lead, a.window, a.sinks)
-                       : Tiles{(keys + kStepK - 1) / kStepK, 0, 0};
-  const int tiles = walk.count;
-  const int whole = a.causal ? clamp_to(q0 + wave * 32 + lead + 1, 0, sk.count) : sk.count;
-  const int seen = live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) : sk.count) : 0;
+  const int last = (q0 + rows < sq.count ? q0 + rows : sq.count) - 1;
+  const int skip = W ? window_skip(q0 + lead, a.window, a.sinks) : 0;
+  const int there = sk.count - skip;  // keys, without those skipped
+  const int keys = a.causal ? clamp_to(last + lead + 1, 0, sk.count) - skip : sk.count;
+  const int tiles = (keys + kStepK - 1) / kStepK;
+  const int whole = a.causal ? clamp_to(q0 + from + lead + 1, 0, sk.count) - skip : sk.count;
+  const int seen =
+      live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) - skip : sk.count) : 0;
   // this query's first key in the window, and the last one of the wave's queries
-  const int late = W ? qrow + lead + 1 - a.window : 0;
-  const int latest = W ? q0 + wave * 32 + 31 + lead + 1 - a.window : 0;
-  const auto place = [&](int t) __attribute__((always_inline)) {
-    return (W && t >= walk.sinks ? t + walk.skip : t) * kStepK;
-  };
+  const int late = W ? qrow + lead + 1 - a.window - skip : 0;
+  const int latest = W ? q0 + from + 31 + lead + 1 - a.window - skip : 0;
   s16x8 qf[KS], df[kHeldHere ? KS : 1];
   float L = INFINITY, D = 0.f, off = 0.f;
   {
@@ -209,10 +216,17 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
   for (int d = 0; d < DB; ++d) dq[d] = kp[d] = (f32x16)(0.f);
 
   const auto load = [&](uint16_t *k, uint16_t *v, int k0) __attribute__((always_inline)) {
-    tile_load<DP, kStepK, kGradWaves>(k, k0p + k0 * a.k.ts, a.k.ts, sk.count - k0, a.head_dim,
-                                     wave);
-    tile_load<DP, kStepK, kGradWaves>(v, v0p + k0 * a.v.ts, a.v.ts, sk.count - k0, a.head_dim,
-                                     wave);
+    if constexpr (W) {
+      window_tile_load<DP, kStepK, kGradWaves>(k, k0p, a.k.ts, k0, there - k0, a.sinks, skip,
+                                               a.head_dim, wave);
+      window_tile_load<DP, kStepK, kGradWaves>(v, v0p, a.v.ts, k0, there - k0, a.sinks, skip,
+                                               a.head_dim, wave);
+    } else {
+      tile_load<DP, kStepK, kGradWaves>(k, k0p + k0 * a.k.ts, a.k.ts, there - k0, a.head_dim,
+                                       wave);
+      tile_load<DP, kStepK, kGradWaves>(v, v0p + k0 * a.v.ts, a.v.ts, there - k0, a.head_dim,
+                                       wave);
+    }
   };
   const auto step = [&](const uint16_t *k, const uint16_t *v, int k0)
                         __attribute__((always_inline)) {
@@ -264,11 +278,11 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
       (tiles + G - 1) / G,
       [&](auto i, int t) __attribute__((always_inline)) {
         load(i == 0 ? tk0[group] : tk1[group], i == 0 ? tv0[group] : tv1[group],
-             place(t * G + group));
+             (t * G + group) * kStepK);
       },
       [&](auto i, int t) __attribute__((always_inline)) {
         step(i == 0 ? tk0[group] : tk1[group], i == 0 ? tv0[group] : tv1[group],
-             place(t * G + group));
+             (t * G + group) * kStepK);
       });
   off = half_sum(off);
   const int t = threadIdx.x % (kGradWaves * OPA_WAVE);
@@ -320,9 +334,8 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
                          : wave / kFit == 2 ? tv0[0]
                                             : tv1[0];
   store_rows<E, DP>(room + wave % kFit * 32 * DP, dq, 1.f,
-                    a.dq.p + (int64_t)(sq.first + q0 + wave * 32) * a.dq.ts +
-                        (int64_t)head * a.dq.hs,
-                    a.dq.ts, sq.count - q0 - wave * 32, a.head_dim);
+                    a.dq.p + (int64_t)(sq.first + q0 + from) * a.dq.ts + (int64_t)head * a.dq.hs,
+                    a.dq.ts, sq.count - q0 - from, a.head_dim);
 }
 
 // 32 pairs (lse, D) from p to LDS, past `left` of them zero; by a whole wave.
@@ -569,12 +582,14 @@ __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArg
 
 template <class E, int DP, bool W>
 static void launch(const PromptArgs &a, hipStream_t s) {
-  const int64_t kt = (int64_t)a.n_k / kHeld + a.n_seqs, qt = (int64_t)a.n_q / kHeld + a.n_seqs;
+  const int hs = W ? a.head_shift : 0;
+  const int64_t kt = (int64_t)a.n_k / kHeld + a.n_seqs;
+  const int64_t qt = ((int64_t)a.n_q / (kHeld >> hs) + a.n_seqs) * (a.n_heads >> hs);
   const dim3 block(kGradWaves * OPA_WAVE);
-  const dim3 rows((uint32_t)(qt * a.n_heads));
+  const dim3 rows((uint32_t)qt);
   const bool many = a.n_k >= (int64_t)kManyKeys * a.n_seqs &&
                     (!W || (int64_t)a.window + a.sinks >= kManyKeys);
-  if (a.n_q > 0 && qt * a.n_heads <= kFewBlocks && many)
+  if (a.n_q > 0 && qt <= kFewBlocks && many)
     hipLaunchKernelGGL((k_attn_dq<E, DP, 2, W>), rows, dim3(2 * kGradWaves * OPA_WAVE), 0, s, a);
   else if (a.n_q > 0)
     hipLaunchKernelGGL((k_attn_dq<E, DP, 1, W>), rows, block, 0, s, a);

@@ -26,7 +26,12 @@ struct PromptArgs {
   uint32_t *norms;
   int splits, split_steps;
   int window, sinks;  // window 0: none
+  int head_shift;     // a window's: log2 of the query heads that a block takes
 };
+
+// Query heads of a key head that a block takes, as a power of two: of a window's keys
+// a block reads those of all its rows, so that fewer rows of more heads waste fewer.
+inline int window_heads(int group) { return group % 4 == 0 ? 2 : group % 2 == 0 ? 1 : 0; }
 
 // Blocks that share a key tile of the gradient at most, and the steps of 32 queries
 // that each is to have, or fewer.

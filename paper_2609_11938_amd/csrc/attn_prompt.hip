@@ -31,9 +31,10 @@ constexpr int kFewBlocks = 384, kManyKeys = 768;
 
 // G groups of kWaves waves take the key tiles in turn and join their sums at the
 // end: the waves that a few rows would leave a compute unit without.
-// W: through a window with sinks. A block's tiles are those of the sinks and those
-// from its first query's window on; in a tile that a query of the wave does not see
-// whole, the hidden scores are -inf as the causal mask's are.
+// W: through a window with sinks. A block's keys are the sinks and those from its
+// first query's window on, counted through (window_skip); in a tile that a query of the
+// wave does not see whole, the hidden scores are -inf as the causal mask's are. Its
+// waves are 2^head_shift heads of fewer rows.
 template <class E, int DP, int G, bool W>
 __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
@@ -46,36 +47,43 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
   int id = blockIdx.x;
   const int hk = id % a.n_kv;
   id /= a.n_kv;
-  const int head = hk * a.group + id % a.group;
+  const int hs = W ? a.head_shift : 0, heads = a.group >> hs;
+  const int head = hk * a.group + (id % heads << hs) + (wave & ((1 << hs) - 1));
+  const int rows = kRowsQ >> hs, from = (wave >> hs) * 32;  // the block's, the wave's first
   if (blockIdx.x == 0) {
     check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag);
     check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
   }
   Span sq, sk;
   int part;
-  if (!find_tile(a.cu_q, a.n_q, a.cu_k, a.n_k, a.n_seqs, kRowsQ, id / a.group, sq, sk, part))
-    return;
+  if constexpr (W) {
+    if (!find_tile(a.cu_q, a.n_q, a.cu_k, a.n_k, a.n_seqs, RowsLog2{7 - hs}, id / heads, sq, sk,
+                   part))
+      return;
+  } else {
+    if (!find_tile(a.cu_q, a.n_q, a.cu_k, a.n_k, a.n_seqs, kRowsQ, id / heads, sq, sk, part))
+      return;
+  }
   // the sequence's last queries, which see the most keys, first
-  const int q0 = ((sq.count + kRowsQ - 1) / kRowsQ - 1 - part) * kRowsQ;
+  const int q0 = W ? (tiles_of(sq.count, RowsLog2{7 - hs}) - 1 - part) * rows
+                   : ((sq.count + kRowsQ - 1) / kRowsQ - 1 - part) * kRowsQ;
   const int lead = sk.count - sq.count;
-  const int qrow = q0 + wave * 32 + r;  // this lane's query
+  const int qrow = q0 + from + r;  // this lane's query
   const bool live = qrow < sq.count;
-  const int last = (q0 + kRowsQ < sq.count ? q0 + kRowsQ : sq.count) - 1;
-  const int keys = a.causal ? clamp_to(last + lead + 1, 0, sk.count) : sk.count;
-  const Tiles walk = W ? window_tiles<kRowsK>(keys, q0 + lead, a.window, a.sinks)
-                       : Tiles{(keys + kRowsK - 1) / kRowsK, 0, 0};
-  const int tiles = walk.count;
+  const int last = (q0 + rows < sq.count ? q0 + rows : sq.count) - 1;
+  const int skip = W ? window_skip(q0 + lead, a.window, a.sinks) : 0;
+  const int there = sk.count - skip;  // keys, without those skipped
+  const int keys = a.causal ? clamp_to(last + lead + 1, 0, sk.count) - skip : sk.count;
+  const int tiles = (keys + kRowsK - 1) / kRowsK;
   // keys below `whole` are seen by every query of this wave
-  const int whole = a.causal ? clamp_to(q0 + wave * 32 + lead + 1, 0, sk.count) : sk.count;
-  const int seen = live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) : sk.count) : 0;
+  const int whole = a.causal ? clamp_to(q0 + from + lead + 1, 0, sk.count) - skip : sk.count;
+  const int seen =
+      live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) - skip : sk.count) : 0;
   // this query's first key in the window, and the last one of the wave's queries
-  const int late = W ? qrow + lead + 1 - a.window : 0;
-  const int latest = W ? q0 + wave * 32 + 31 + lead + 1 - a.window : 0;
+  const int late = W ? qrow + lead + 1 - a.window - skip : 0;
+  const int latest = W ? q0 + from + 31 + lead + 1 - a.window - skip : 0;
   const auto hidden = [&](int key) __attribute__((always_inline)) {
     return key >= seen || (W && key < late && key >= a.sinks);
-  };
-  const auto place = [&](int t) __attribute__((always_inline)) {
-    return (W && t >= walk.sinks ? t + walk.skip : t) * kRowsK;
   };
 
   // scores in units of 1 / c, c > 0: a negative scale turns the queries round
@@ -100,8 +108,15 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
   const int nat0 = nat_place<DP>(), tr0 = tr_place<DP>();
 
   const auto load = [&](uint16_t *k, uint16_t *v, int k0) __attribute__((always_inline)) {
-    tile_load<DP, kRowsK, kWaves>(k, kp + k0 * a.k.ts, a.k.ts, sk.count - k0, a.head_dim, wave);
-    tile_load<DP, kRowsK, kWaves>(v, vp + k0 * a.v.ts, a.v.ts, sk.count - k0, a.head_dim, wave);
+    if constexpr (W) {
+      window_tile_load<DP, kRowsK, kWaves>(k, kp, a.k.ts, k0, there - k0, a.sinks, skip,
+                                           a.head_dim, wave);
+      window_tile_load<DP, kRowsK, kWaves>(v, vp, a.v.ts, k0, there - k0, a.sinks, skip,
+                                           a.head_dim, wave);
+    } else {
+      tile_load<DP, kRowsK, kWaves>(k, kp + k0 * a.k.ts, a.k.ts, there - k0, a.head_dim, wave);
+      tile_load<DP, kRowsK, kWaves>(v, vp + k0 * a.v.ts, a.v.ts, there - k0, a.head_dim, wave);
+    }
   };
   const auto step = [&](auto careful, const uint16_t *k, const uint16_t *v,
                         int k0) __attribute__((always_inline)) {
@@ -230,11 +245,11 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
       (tiles + G - 1) / G,
       [&](auto i, int t) __attribute__((always_inline)) {
         load(i == 0 ? tk0[group] : tk1[group], i == 0 ? tv0[group] : tv1[group],
-             place(t * G + group));
+             (t * G + group) * kRowsK);
       },
       [&](auto i, int t) __attribute__((always_inline)) {
         step(std::false_type{}, i == 0 ? tk0[group] : tk1[group],
-             i == 0 ? tv0[group] : tv1[group], place(t * G + group));
+             i == 0 ? tv0[group] : tv1[group], (t * G + group) * kRowsK);
       });
   if constexpr (G > 1) join();
   // A weight of 0 times a value that is not finite is no 0: where a sum is not
@@ -248,8 +263,7 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
       for (int i = 0; i < 16; ++i) zero = fmaf(o[d][i], 0.f, zero);
     if (__syncthreads_or(group == 0 && !(zero == 0.f))) {
       start();
-      for (int t = group; t < tiles + group; t += G) {
-        const int k0 = place(t);
+      for (int k0 = group * kRowsK; k0 < tiles * kRowsK + group * kRowsK; k0 += G * kRowsK) {
         load(tk0[group], tv0[group], k0);
         wait_loads();
         block_sync();
@@ -264,9 +278,9 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
   if (group) return;
   store_rows<E, DP>((wave < 2 ? tk0[0] : tk1[0]) + wave % 2 * (kTile / 2), o,
                     l == 0.f ? 0.f : 1.f / l,
-                    a.out.p + (int64_t)(sq.first + q0 + wave * 32) * a.out.ts +
+                    a.out.p + (int64_t)(sq.first + q0 + from) * a.out.ts +
                         (int64_t)head * a.out.hs,
-                    a.out.ts, sq.count - q0 - wave * 32, a.head_dim);
+                    a.out.ts, sq.count - q0 - from, a.head_dim);
   if (a.lse && live && h == 0)
     a.lse[(int64_t)head * a.n_q + sq.first + qrow] =
         l == 0.f ? -INFINITY : (m * c + log2_sum<E>(l)) * kLn2;
@@ -274,7 +288,8 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
 
 template <class E, int DP, bool W>
 static void launch_as(const PromptArgs &a, hipStream_t s) {
-  const int64_t blocks = ((int64_t)a.n_q / kRowsQ + a.n_seqs) * a.n_heads;
+  const int hs = W ? a.head_shift : 0;
+  const int64_t blocks = ((int64_t)a.n_q / (kRowsQ >> hs) + a.n_seqs) * (a.n_heads >> hs);
   const bool many = a.n_k >= (int64_t)kManyKeys * a.n_seqs &&
                     (!W || (int64_t)a.window + a.sinks >= kManyKeys);
   if (blocks <= kFewBlocks && many)
