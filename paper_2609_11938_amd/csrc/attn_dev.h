@@ -11,6 +11,7 @@
 // A is loaded in that order (tr_frag).
 #pragma once
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 
 #include <type_traits>
@@ -330,40 +331,59 @@ __device__ __forceinline__ bool find_tile(const int32_t *cu, int n, const int32_
 }
 
 // Through a window with sinks a block of queries counts its keys without those that
-// lie between the sinks and its first query's window: key j is place j, or past the
-// sinks place j - window_skip. place: how many keys stand before its first query's.
-__device__ __forceinline__ int window_skip(int place, int window, int sinks) {
+// lie between the first `front` (the sinks, and up to a multiple of 8) and its first
+// query's window: key j is place j, or past the front place j - window_skip. place: how
+// many keys stand before its first query's.
+__device__ __forceinline__ int window_front(int sinks) { return (sinks + 7) & ~7; }
+__device__ __forceinline__ int window_skip(int place, int window, int front) {
   const int first = place + 1 - window;
-  return first > sinks ? first - sinks : 0;
+  return first > front ? first - front : 0;
 }
-// tile_load of the places from k0 on; `left` places exist from there. The tile that
-// the last sink is in has rows of both: each lane asks one of two ranges.
+// tile_load of the places from k0 on; `left` places exist from there. A load's rows are
+// 8 or fewer, all of the front or none.
 template <int DP, int ROWS, int NW>
 __device__ __forceinline__ void window_tile_load(uint16_t *tile, const uint16_t *src, int64_t ts,
-                                                 int k0, int left, int sinks, int skip,
+                                                 int k0, int left, int front, int skip,
                                                  int head_dim, int wave) {
-  if (skip == 0 || k0 >= sinks) {
+  if (skip == 0 || k0 >= front) {
     tile_load<DP, ROWS, NW>(tile, src + (int64_t)(k0 + skip) * ts, ts, left, head_dim, wave);
     return;
   }
-  constexpr int C = DP / 8, N = ROWS * C / (NW * OPA_WAVE);
-  const auto near = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint16_t *>(uniform(src + (int64_t)(k0 + skip) * ts)), (short)0,
-      uniform((int)(clamp_to(left, 0, ROWS) * ts * 2)), 0x00027000);
-  const auto front = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint16_t *>(uniform(src + (int64_t)k0 * ts)), (short)0,
-      uniform((int)(clamp_to(sinks - k0, 0, ROWS) * ts * 2)), 0x00027000);
+  constexpr int C = DP / 8, N = ROWS * C / (NW * OPA_WAVE), R = OPA_WAVE / C;
+  static_assert(R <= 8 && 8 % R == 0, "a load's rows");
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int first = (i * NW + wave) * OPA_WAVE;
-    const int id = first + lane_id(), row = id / C, chunk = (id % C) ^ swz<DP>(row);
+    const int first = (i * NW + wave) * OPA_WAVE, row0 = first / C;
+    const int rows = clamp_to(left - row0, 0, R);
+    const int key = k0 + row0 < front ? k0 + row0 : k0 + row0 + skip;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint16_t *>(uniform(src + (int64_t)key * ts)), (short)0,
+        uniform((int)(rows * ts * 2)), 0x00027000);
+    const int row = lane_id() / C, chunk = (lane_id() % C) ^ swz<DP>(row0 + row);
     const uint32_t off = chunk * 8 < head_dim ? (uint32_t)(row * (int)ts * 2 + chunk * 16)
                                               : 0xfffffff0u;
-    const auto to = (__attribute__((address_space(3))) void *)(tile + first * 8);
-    if (k0 + row < sinks)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(front, to, 16, (int)off, 0, 0, 0);
-    else
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(near, to, 16, (int)off, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rsrc, (__attribute__((address_space(3))) void *)(tile + first * 8), 16, (int)off, 0, 0,
+        0);
+  }
+}
+
+// Where a query of the wave does not see all of 32 keys that begin at place c0, hide(e)
+// for each of this lane's elements e that it does not see: it sees those of the window
+// that ends before place `seen`, and the sinks before that. All queries see the places
+// below `whole`, and those from `latest` on.
+template <class Hide>
+__device__ __forceinline__ void hide_keys(int c0, int whole, int seen, int latest, int window,
+                                          int sinks, const Hide &hide) {
+  if (c0 + 32 <= whole && (c0 >= latest || c0 + 32 <= sinks)) return;
+  // how far the lane's first element is past the window's begin: one comparison of
+  // numbers without a sign for both ends
+  const int past = c0 + ((lane_id() >> 5) << 2) - seen + window;
+  const int kept = c0 < sinks ? (sinks < seen ? sinks : seen) - seen + window : INT_MIN;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int at = past + 8 * (e >> 2) + (e & 3);
+    if ((uint32_t)at >= (uint32_t)window && at >= kept) hide(e);
   }
 }
 

@@ -164,15 +164,15 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
   const int qrow = q0 + from + r;
   const bool live = qrow < sq.count;
   const int last = (q0 + rows < sq.count ? q0 + rows : sq.count) - 1;
-  const int skip = W ? window_skip(q0 + lead, a.window, a.sinks) : 0;
+  const int front = W ? window_front(a.sinks) : 0;
+  const int skip = W ? window_skip(q0 + lead, a.window, front) : 0;
   const int there = sk.count - skip;  // keys, without those skipped
   const int keys = a.causal ? clamp_to(last + lead + 1, 0, sk.count) - skip : sk.count;
   const int tiles = (keys + kStepK - 1) / kStepK;
   const int whole = a.causal ? clamp_to(q0 + from + lead + 1, 0, sk.count) - skip : sk.count;
   const int seen =
       live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) - skip : sk.count) : 0;
-  // this query's first key in the window, and the last one of the wave's queries
-  const int late = W ? qrow + lead + 1 - a.window - skip : 0;
+  // where the window of the wave's last query begins
   const int latest = W ? q0 + from + 31 + lead + 1 - a.window - skip : 0;
   s16x8 qf[KS], df[kHeldHere ? KS : 1];
   float L = INFINITY, D = 0.f, off = 0.f;
@@ -217,9 +217,9 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
 
   const auto load = [&](uint16_t *k, uint16_t *v, int k0) __attribute__((always_inline)) {
     if constexpr (W) {
-      window_tile_load<DP, kStepK, kGradWaves>(k, k0p, a.k.ts, k0, there - k0, a.sinks, skip,
+      window_tile_load<DP, kStepK, kGradWaves>(k, k0p, a.k.ts, k0, there - k0, front, skip,
                                                a.head_dim, wave);
-      window_tile_load<DP, kStepK, kGradWaves>(v, v0p, a.v.ts, k0, there - k0, a.sinks, skip,
+      window_tile_load<DP, kStepK, kGradWaves>(v, v0p, a.v.ts, k0, there - k0, front, skip,
                                                a.head_dim, wave);
     } else {
       tile_load<DP, kStepK, kGradWaves>(k, k0p + k0 * a.k.ts, a.k.ts, there - k0, a.head_dim,
@@ -230,8 +230,7 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
   };
   const auto step = [&](const uint16_t *k, const uint16_t *v, int k0)
                         __attribute__((always_inline)) {
-    const bool cut =
-        k0 + kStepK > whole || (W && k0 < latest && k0 + kStepK > a.sinks);
+    const bool cut = k0 + kStepK > whole;
     const int nat = fresh(nat0), tr = fresh(tr0);
 #pragma unroll
     for (int kb = 0; kb < kStepK / 32; ++kb) {
@@ -247,12 +246,14 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
         x[e] = exp2_fast(fmaf(x[e], c, -L));
         y[e] = x[e] * (y[e] - D) * upw;
       }
-      if (cut) {  // both: of a hidden key either may be past float32
+      // both: of a hidden key either may be past float32
+      if constexpr (W) {
+        hide_keys(k0 + 32 * kb, whole, fresh(seen), latest, a.window, a.sinks,
+                  [&](int e) __attribute__((always_inline)) { x[e] = y[e] = 0.f; });
+      } else if (cut) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = k0 + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3);
-          if (key >= seen || (W && key < late && key >= a.sinks)) x[e] = y[e] = 0.f;
-        }
+        for (int e = 0; e < 16; ++e)
+          if (k0 + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3) >= seen) x[e] = y[e] = 0.f;
       }
 #pragma unroll
       for (int e = 0; e < 16; e += 4) off += (y[e] + y[e + 1]) + (y[e + 2] + y[e + 3]);
@@ -408,12 +409,16 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   // this lane's
   const int whole = key0 + 32 > sk.count ? sq.count
                                          : a.causal ? clamp_to(key0 + 31 - lead, 0, sq.count) : 0;
-  const int from = live ? (a.causal ? clamp_to(key - lead, 0, sq.count) : 0) : sq.count;
-  // W: the last query that sees this lane's key, and the first that has left one of
-  // this wave's behind, both and one more
-  const int to = W && key >= a.sinks ? key - lead + a.window : sq.count;
+  // (W: the query whose own key it is, or what no query is)
+  const int from = W      ? (live ? key - lead : 1 << 30)
+                   : live ? (a.causal ? clamp_to(key - lead, 0, sq.count) : 0)
+                          : sq.count;
+  // W: the first query that has left one of this wave's keys behind
   const int plain = key0 > a.sinks ? key0 : a.sinks;  // the wave's first key that is no sink
   const int left_from = W && plain < key0 + 32 ? plain - lead + a.window : sq.count;
+  // and the first that sees one of this wave's, and the last, and one more
+  const int first_met = W ? clamp_to(key0 - lead, 0, sq.count) : 0;
+  const int last_met = !W || key0 < a.sinks ? sq.count : key0 + 31 - lead + a.window;
   const Span met = tile_queries<DP, W>(a, sq, sk, part);
   const int t0 = met.first, per = met.count;
   // this block's steps of the tile's: a head's queries, then the next head's
@@ -464,6 +469,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   const auto step = [&](const uint16_t *q, const uint16_t *dout, const float *rows, int t)
                         __attribute__((always_inline)) {
     const int q0 = (t0 + t % per) * kStepQ;
+    if (W && (q0 >= last_met || q0 + kStepQ <= first_met || key0 >= sk.count)) return;
     const int nat = fresh(nat0), tr = fresh(tr0);
 #pragma unroll
     for (int qb = 0; qb < kQB; ++qb) {
@@ -485,12 +491,19 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
           x[e] = p;
         }
       }
-      if (q0 < whole || (W && q0 + kStepQ > left_from)) {
+      if constexpr (W) {  // as hide_keys, of the queries
+        const int at = q0 + 32 * qb;
+        if (at < whole || at + 32 > left_from) {
+          const int past = at + 4 * h - fresh(from);
+          const uint32_t span = key0 + r < a.sinks ? INT_MAX : a.window;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int row = q0 + 32 * qb + 8 * (e >> 2) + 4 * h + (e & 3);
-          if (row < from || (W && row >= to)) x[e] = y[e] = 0.f;
+          for (int e = 0; e < 16; ++e)
+            if ((uint32_t)(past + 8 * (e >> 2) + (e & 3)) >= span) x[e] = y[e] = 0.f;
         }
+      } else if (q0 < whole) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (q0 + 32 * qb + 8 * (e >> 2) + 4 * h + (e & 3) < from) x[e] = y[e] = 0.f;
       }
 #pragma unroll
       for (int s = 0; s < 2; ++s) {

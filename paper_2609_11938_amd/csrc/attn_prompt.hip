@@ -71,7 +71,8 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
   const int qrow = q0 + from + r;  // this lane's query
   const bool live = qrow < sq.count;
   const int last = (q0 + rows < sq.count ? q0 + rows : sq.count) - 1;
-  const int skip = W ? window_skip(q0 + lead, a.window, a.sinks) : 0;
+  const int front = W ? window_front(a.sinks) : 0;
+  const int skip = W ? window_skip(q0 + lead, a.window, front) : 0;
   const int there = sk.count - skip;  // keys, without those skipped
   const int keys = a.causal ? clamp_to(last + lead + 1, 0, sk.count) - skip : sk.count;
   const int tiles = (keys + kRowsK - 1) / kRowsK;
@@ -79,11 +80,10 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
   const int whole = a.causal ? clamp_to(q0 + from + lead + 1, 0, sk.count) - skip : sk.count;
   const int seen =
       live ? (a.causal ? clamp_to(qrow + lead + 1, 0, sk.count) - skip : sk.count) : 0;
-  // this query's first key in the window, and the last one of the wave's queries
-  const int late = W ? qrow + lead + 1 - a.window - skip : 0;
+  // where the window of the wave's last query begins
   const int latest = W ? q0 + from + 31 + lead + 1 - a.window - skip : 0;
   const auto hidden = [&](int key) __attribute__((always_inline)) {
-    return key >= seen || (W && key < late && key >= a.sinks);
+    return key >= seen || (W && key < seen - a.window && key >= a.sinks);
   };
 
   // scores in units of 1 / c, c > 0: a negative scale turns the queries round
@@ -109,9 +109,9 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
 
   const auto load = [&](uint16_t *k, uint16_t *v, int k0) __attribute__((always_inline)) {
     if constexpr (W) {
-      window_tile_load<DP, kRowsK, kWaves>(k, kp, a.k.ts, k0, there - k0, a.sinks, skip,
+      window_tile_load<DP, kRowsK, kWaves>(k, kp, a.k.ts, k0, there - k0, front, skip,
                                            a.head_dim, wave);
-      window_tile_load<DP, kRowsK, kWaves>(v, vp, a.v.ts, k0, there - k0, a.sinks, skip,
+      window_tile_load<DP, kRowsK, kWaves>(v, vp, a.v.ts, k0, there - k0, front, skip,
                                            a.head_dim, wave);
     } else {
       tile_load<DP, kRowsK, kWaves>(k, kp + k0 * a.k.ts, a.k.ts, there - k0, a.head_dim, wave);
@@ -130,7 +130,12 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
         x[kb] = E::mfma(nat_frag<DP>(k, nat, 32 * kb, s), qf[s], x[kb]);
     const bool cut =
         k0 + kRowsK > whole || (W && k0 < latest && k0 + kRowsK > a.sinks);
-    if (cut) {
+    if constexpr (W) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+        hide_keys(k0 + 32 * kb, whole, fresh(seen), latest, a.window, a.sinks,
+                  [&](int i) __attribute__((always_inline)) { x[kb][i] = -INFINITY; });
+    } else if (cut) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
