@@ -280,11 +280,10 @@ static int prompt(const opattr_attn_shape *a, int32_t window, int32_t sinks, con
 static size_t grad_workspace(const opattr_attn_shape *a, int32_t window, int32_t sinks) {
   if (!ok_shape(a)) return 0;
   const size_t dp = a->head_dim <= 64 ? 64 : 128;
-  const int n = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads, at_most(window),
-                            at_most(sinks))
-                    .most;
+  const GradSplits x = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads,
+                                   at_most(window), at_most(sinks));
   return align256((size_t)a->n_q * a->n_heads * 8) + norms_bytes(a) +
-         (n > 1 ? (size_t)n * (a->n_k / 128 + a->n_seqs) * 128 * a->n_kv_heads * 2 * dp * 4 : 0);
+         (size_t)grad_parts(x, a->n_k, a->n_seqs) * 128 * a->n_kv_heads * 2 * dp * 4;
 }
 
 static int prompt_grad(const opattr_attn_shape *a, int32_t window, int32_t sinks,
@@ -318,6 +317,8 @@ static int prompt_grad(const opattr_attn_shape *a, int32_t window, int32_t sinks
                                    p.sinks);
   p.splits = x.most;
   p.split_steps = x.steps;
+  p.sink_tiles = x.sink_tiles;
+  p.sink_splits = x.sink_most;
   run_prompt_grad(p, a->dtype, (hipStream_t)stream);
   return launched();
 }

@@ -339,15 +339,19 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
                     a.dq.ts, sq.count - q0 - from, a.head_dim);
 }
 
-// 32 pairs (lse, D) from p to LDS, past `left` of them zero; by a whole wave.
-__device__ __forceinline__ void row_load(float *to, const float *p, int left) {
+// 32 pairs (lse, D) from p to LDS, to + at, past `left` of them zero; by a whole wave.
+__device__ __forceinline__ void row_load(float *to, int at, const float *p, int left) {
   const int n = left < 0 ? 0 : left > 32 ? 32 : left;
   const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<float *>(reinterpret_cast<const float *>(
           uniform(reinterpret_cast<const uint16_t *>(p)))),
       (short)0, uniform(n * 8), 0x00027000);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)to, 4,
-                                           lane_id() * 4, 0, 0, 0);
+  // (`at` once it is LDS: of a constant place past an array's first this compiler makes
+  // a comparison that it cannot encode)
+  __attribute__((address_space(3))) float *const lds =
+      (__attribute__((address_space(3))) float *)to;
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(
+      rsrc, (__attribute__((address_space(3))) void *)(lds + at), 4, lane_id() * 4, 0, 0, 0);
 }
 
 // Tiles of queries that key tile `part` of a sequence meets: the first, and how many.
@@ -370,17 +374,38 @@ template <int DP, bool W>
 __device__ __forceinline__ int tile_splits(const PromptArgs &a, const Span &sq, const Span &sk,
                                            int part) {
   const int steps = tile_queries<DP, W>(a, sq, sk, part).count * a.group * (kStep(DP) / 32);
-  return clamp_to((steps + a.split_steps - 1) / a.split_steps, 1, a.splits);
+  const int most = W && part < a.sink_tiles ? a.splits + a.sink_splits : a.splits;
+  return clamp_to((steps + a.split_steps - 1) / a.split_steps, 1, most);
 }
 
 // Where a wave of one of a tile's blocks leaves its dk and dv, as its registers hold
-// them: [splits][tiles][n_kv][waves][dk, dv][DP / 8][64 lanes] of four values.
-template <int DP>
-__device__ __forceinline__ f32x4 *part_of(const PromptArgs &a, int split, int tile, int hk,
-                                          int wave) {
+// them: [parts][n_kv][waves][dk, dv][DP / 8][64 lanes] of four values, the parts
+// [splits][tiles], none where splits is 1 and the tile has no sinks, and then
+// [sink_splits][sequences][sink_tiles]. Where the tiles are not split, a sink's tile
+// has the first of its parts in the place of the first sequence's.
+template <int DP, bool W>
+__device__ __forceinline__ f32x4 *part_of(const PromptArgs &a, int split, int tile, int seq,
+                                          int part, int hk, int wave) {
   const int64_t tiles = a.n_k / kHeld + a.n_seqs;
-  const int64_t at = ((split * tiles + tile) * a.n_kv + hk) * kGradWaves + wave;
+  int64_t at = split * tiles + tile;
+  if constexpr (W) {
+    const int64_t sinks = (int64_t)a.n_seqs * a.sink_tiles;
+    const int64_t mine = (int64_t)seq * a.sink_tiles + part;
+    if (a.splits == 1)
+      at = split * sinks + mine;
+    else if (split >= a.splits)
+      at = a.splits * tiles + (split - a.splits) * sinks + mine;
+  }
+  at = (at * a.n_kv + hk) * kGradWaves + wave;
   return reinterpret_cast<f32x4 *>(a.part) + at * (2 * DP / 8 * OPA_WAVE) + lane_id();
+}
+
+// Sequence `seq`'s key tile `part` without a search; false if it has none.
+__device__ __forceinline__ bool sink_tile(const PromptArgs &a, int seq, int part, Span &sk,
+                                          Span &sq) {
+  sk = span_of(a.cu_k, seq, a.n_k);
+  sq = span_of(a.cu_q, seq, a.n_q);
+  return part * kHeld < sk.count;
 }
 
 // dk and dv of 32 keys a wave: S = Q K^T with the wave's keys as columns, so
@@ -397,11 +422,24 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   int id = blockIdx.x;
   const int hk = id % a.n_kv;
   id /= a.n_kv;
-  const int split = id % a.splits;
   Span sq, sk;
-  int part, seq;
-  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, id / a.splits, sk, sq, part, &seq))
-    return;
+  int part, seq, split;
+  // W: before the blocks of every tile those that the sinks' tiles have besides
+  const int more = W ? a.n_seqs * a.sink_tiles * a.sink_splits : 0;
+  bool found;
+  if (id < more) {
+    const int x = id / a.sink_splits;
+    split = a.splits + id % a.sink_splits;
+    part = x % a.sink_tiles;
+    seq = x / a.sink_tiles;
+    found = sink_tile(a, seq, part, sk, sq);
+  } else {
+    id -= more;
+    split = id % a.splits;
+    found = find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, id / a.splits, sk, sq, part,
+                      &seq);
+  }
+  if (!found) return;
   const int lead = sk.count - sq.count;
   const int key0 = part * kHeld + wave * 32, key = key0 + r;
   const bool live = key < sk.count;
@@ -464,7 +502,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
 #pragma unroll
     for (int b = 0; b < kQB; ++b)
       if (wave == b)
-        row_load(rows + 64 * b, a.rows + ((int64_t)head * a.n_q + tok + 32 * b) * 2, left - 32 * b);
+        row_load(rows, 64 * b, a.rows + ((int64_t)head * a.n_q + tok + 32 * b) * 2, left - 32 * b);
   };
   const auto step = [&](const uint16_t *q, const uint16_t *dout, const float *rows, int t)
                         __attribute__((always_inline)) {
@@ -532,7 +570,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
       });
   const float fk = a.scale / up;
   if (splits > 1) {
-    f32x4 *p = part_of<DP>(a, split, id / a.splits, hk, wave);
+    f32x4 *p = part_of<DP, W>(a, split, id / a.splits, seq, part, hk, wave);
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -570,8 +608,16 @@ __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArg
   const int hk = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv;
   const int all = uniform(wave_id()), wave = all / 2, which = all % 2;
   Span sq, sk;
-  int part;
-  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part)) return;
+  int part, seq = 0;
+  bool found;
+  if (W && a.splits == 1) {  // the sinks' tiles alone
+    part = tile % a.sink_tiles;
+    seq = tile / a.sink_tiles;
+    found = sink_tile(a, seq, part, sk, sq);
+  } else {
+    found = find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part, &seq);
+  }
+  if (!found) return;
   const int splits = tile_splits<DP, W>(a, sq, sk, part);
   const int key0 = part * kHeld + wave * 32;
   if (splits == 1 || key0 >= sk.count) return;
@@ -579,7 +625,7 @@ __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArg
 #pragma unroll
   for (int d = 0; d < DB; ++d) sum[d] = (f32x16)(0.f);
   for (int k = 0; k < splits; ++k) {
-    const f32x4 *p = part_of<DP>(a, k, tile, hk, wave) + which * 4 * DB * OPA_WAVE;
+    const f32x4 *p = part_of<DP, W>(a, k, tile, seq, part, hk, wave) + which * 4 * DB * OPA_WAVE;
 #pragma unroll
     for (int i = 0; i < 4 * DB; ++i) {
       const f32x4 v = p[i * OPA_WAVE];
@@ -607,10 +653,12 @@ static void launch(const PromptArgs &a, hipStream_t s) {
   else if (a.n_q > 0)
     hipLaunchKernelGGL((k_attn_dq<E, DP, 1, W>), rows, block, 0, s, a);
   if (a.n_k == 0) return;
-  hipLaunchKernelGGL((k_attn_dkv<E, DP, W>), dim3((uint32_t)(kt * a.n_kv * a.splits)), block, 0, s,
-                     a);
-  if (a.splits > 1)
-    hipLaunchKernelGGL((k_dkv_sum<E, DP, W>), dim3((uint32_t)(kt * a.n_kv)),
+  const int64_t sinks = (int64_t)a.n_seqs * a.sink_tiles;
+  const int64_t parts = kt * a.splits + sinks * a.sink_splits;
+  const int64_t sums = a.splits > 1 ? kt : a.sink_splits > 0 ? sinks : 0;
+  hipLaunchKernelGGL((k_attn_dkv<E, DP, W>), dim3((uint32_t)(parts * a.n_kv)), block, 0, s, a);
+  if (sums > 0)
+    hipLaunchKernelGGL((k_dkv_sum<E, DP, W>), dim3((uint32_t)(sums * a.n_kv)),
                        dim3(2 * kGradWaves * OPA_WAVE), 0, s, a);
 }
 
@@ -642,16 +690,49 @@ static void grad(const PromptArgs &a, hipStream_t s) {
 // is split less than alone: 4000 tokens, 8 heads on 2 of 128, a training pass of 268
 // us, with 30 sequences of one token beside it 797.
 constexpr int kSplitSteps = 24, kFewSteps = 8, kFewTiles = 192;
+
+// Through a window a key tile meets as many queries as any other, and partial sums cost
+// more than they gain where the tiles fill the chip: they are split only to come to
+// kRound blocks. The sinks' tiles, which meet every query, have blocks of as many steps
+// as the others, kMostSinks at most besides.
+constexpr int kRound = 512, kMostSinks = 15, kSinkBlocks = 1024;
+static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group, int64_t blocks,
+                                int window, int sinks) {
+  GradSplits x{1, kSplitSteps, 0, 0};
+  const int64_t mean = n_q / n_seqs;
+  const int64_t met = mean < (int64_t)window + kHeld ? mean : (int64_t)window + kHeld;
+  const int64_t steps = (met * group + 31) / 32;
+  int64_t n = kRound / blocks;
+  if (n > steps / kFewSteps) n = steps / kFewSteps;
+  x.most = n < 1 ? 1 : n > 16 ? 16 : (int)n;
+  x.steps = (int)((steps + x.most - 1) / x.most);
+  if (x.steps < kSplitSteps) x.steps = x.most > 1 && x.steps > kFewSteps ? x.steps : kSplitSteps;
+  if (sinks) {
+    const int64_t tiles = ((sinks < n_k ? sinks : n_k) + kHeld - 1) / kHeld;
+    int64_t more = (n_q * group / 32 + x.steps - 1) / x.steps - x.most;
+    const int64_t room = kSinkBlocks / (n_seqs * tiles);
+    if (more > room) more = room;
+    if (more > 0) {
+      x.sink_tiles = (int)tiles;
+      x.sink_most = more > kMostSinks ? kMostSinks : (int)more;
+    }
+  }
+  return x;
+}
+
+int64_t grad_parts(const GradSplits &x, int64_t n_k, int n_seqs) {
+  const int64_t tiles = n_k / kHeld + n_seqs, sinks = (int64_t)n_seqs * x.sink_tiles;
+  // with sinks alone, their tiles' first parts too
+  return (x.most > 1 ? x.most * tiles : x.sink_most > 0 ? sinks : 0) + sinks * x.sink_most;
+}
+
 GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv, int window,
                        int sinks) {
-  GradSplits x{1, kSplitSteps};
+  GradSplits x{1, kSplitSteps, 0, 0};
   if (n_seqs == 0 || n_k == 0) return x;
   const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
-  // queries of a key tile, at most: a sink's tile meets every one
-  int64_t rows = n_q;
-  if (window && !sinks && (int64_t)n_seqs * (window + (int64_t)kHeld) < rows)
-    rows = (int64_t)n_seqs * (window + (int64_t)kHeld);
-  const int64_t steps = rows * (n_heads / n_kv) / 32 / n_seqs;
+  if (window) return window_splits(n_q, n_k, n_seqs, n_heads / n_kv, blocks, window, sinks);
+  const int64_t steps = n_q * (n_heads / n_kv) / 32 / n_seqs;
   if (blocks <= kFewTiles && steps >= kSplitSteps) x.steps = kFewSteps;
   int64_t n = (2048 + blocks - 1) / blocks;
   if (n > steps / x.steps) n = steps / x.steps;

@@ -27,6 +27,7 @@ struct PromptArgs {
   int splits, split_steps;
   int window, sinks;  // window 0: none
   int head_shift;     // a window's: log2 of the query heads that a block takes
+  int sink_tiles, sink_splits;  // key tiles with sinks; blocks for each beyond `splits`
 };
 
 // Query heads of a key head that a block takes, as a power of two: of a window's keys
@@ -34,12 +35,15 @@ struct PromptArgs {
 inline int window_heads(int group) { return group % 4 == 0 ? 2 : group % 2 == 0 ? 1 : 0; }
 
 // Blocks that share a key tile of the gradient at most, and the steps of 32 queries
-// that each is to have, or fewer.
+// that each is to have, or fewer; through a window, the key tiles of a sequence that
+// hold sinks, and as many blocks more for each.
 struct GradSplits {
-  int most, steps;
+  int most, steps, sink_tiles, sink_most;
 };
 GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv, int window,
                        int sinks);
+// Key tiles' parts that the blocks leave for the sums: of 128 keys of a key head, at most.
+int64_t grad_parts(const GradSplits &x, int64_t n_k, int n_seqs);
 
 struct PagedArgs {
   const uint16_t *k, *v;
