@@ -368,14 +368,16 @@ __device__ __forceinline__ Span tile_queries(const PromptArgs &a, const Span &sq
   const int first = begin / kStep(DP), end = (past + kStep(DP) - 1) / kStep(DP);
   return {first, end - first};
 }
+constexpr int kSinkSteps = 32;
 // Blocks that share the tile: as many as bring each to a.split_steps steps of 32
 // queries or fewer, at most a.splits.
 template <int DP, bool W>
 __device__ __forceinline__ int tile_splits(const PromptArgs &a, const Span &sq, const Span &sk,
                                            int part) {
   const int steps = tile_queries<DP, W>(a, sq, sk, part).count * a.group * (kStep(DP) / 32);
-  const int most = W && part < a.sink_tiles ? a.splits + a.sink_splits : a.splits;
-  return clamp_to((steps + a.split_steps - 1) / a.split_steps, 1, most);
+  if (W && part < a.sink_tiles)
+    return clamp_to((steps + kSinkSteps - 1) / kSinkSteps, a.splits, a.splits + a.sink_splits);
+  return clamp_to((steps + a.split_steps - 1) / a.split_steps, 1, a.splits);
 }
 
 // Where a wave of one of a tile's blocks leaves its dk and dv, as its registers hold
@@ -424,17 +426,16 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   id /= a.n_kv;
   Span sq, sk;
   int part, seq, split;
-  // W: before the blocks of every tile those that the sinks' tiles have besides
-  const int more = W ? a.n_seqs * a.sink_tiles * a.sink_splits : 0;
+  // W: past the blocks of every tile those that the sinks' tiles have besides
+  const int64_t more = W ? id - (a.n_k / kHeld + (int64_t)a.n_seqs) * a.splits : -1;
   bool found;
-  if (id < more) {
-    const int x = id / a.sink_splits;
-    split = a.splits + id % a.sink_splits;
+  if (more >= 0) {
+    const int x = (int)more / a.sink_splits;
+    split = a.splits + (int)more % a.sink_splits;
     part = x % a.sink_tiles;
     seq = x / a.sink_tiles;
     found = sink_tile(a, seq, part, sk, sq);
   } else {
-    id -= more;
     split = id % a.splits;
     found = find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, id / a.splits, sk, sq, part,
                       &seq);
@@ -695,7 +696,7 @@ constexpr int kSplitSteps = 24, kFewSteps = 8, kFewTiles = 192;
 // more than they gain where the tiles fill the chip: they are split only to come to
 // kRound blocks. The sinks' tiles, which meet every query, have blocks of as many steps
 // as the others, kMostSinks at most besides.
-constexpr int kRound = 512, kMostSinks = 15, kSinkBlocks = 1024;
+constexpr int kRound = 512, kMostSinks = 31, kSinkBlocks = 1024;
 static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group, int64_t blocks,
                                 int window, int sinks) {
   GradSplits x{1, kSplitSteps, 0, 0};
@@ -709,7 +710,7 @@ static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group,
   if (x.steps < kSplitSteps) x.steps = x.most > 1 && x.steps > kFewSteps ? x.steps : kSplitSteps;
   if (sinks) {
     const int64_t tiles = ((sinks < n_k ? sinks : n_k) + kHeld - 1) / kHeld;
-    int64_t more = (n_q * group / 32 + x.steps - 1) / x.steps - x.most;
+    int64_t more = (n_q * group / 32 + kSinkSteps - 1) / kSinkSteps - x.most;
     const int64_t room = kSinkBlocks / (n_seqs * tiles);
     if (more > room) more = room;
     if (more > 0) {
