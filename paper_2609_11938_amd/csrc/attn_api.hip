@@ -146,11 +146,16 @@ static bool ok_pages_out(const opattr_kv_pages *c) {
                                  {c->n_kv_heads, c->head_stride}, c->head_dim);
 }
 
-// Tokens of a sequence that its query sees, at most.
-template <class Cache>
-static int most_seen(const Cache *c, int32_t window, int32_t sinks) {
+// Tokens of a sequence that its query sees, at most; of the cache of 8 bits by whole runs
+// of 16 at the sinks' end and the window's begin.
+static int most_seen(const opattr_kv_pages *c, int32_t window, int32_t sinks) {
   const int slots = c->table_stride * c->page_size;
   return window ? std::min(slots, at_most(window) + at_most(sinks)) : slots;
+}
+static int most_seen(const opattr_kv_scaled *c, int32_t window, int32_t sinks) {
+  const int64_t slots = (int64_t)c->table_stride * c->page_size;
+  const int64_t seen = (int64_t)at_most(window) + 15 + (at_most(sinks) + 15) / 16 * 16;
+  return (int)std::min(slots, seen);
 }
 
 // The cache of 8 bits: as above, in bytes.

@@ -65,6 +65,7 @@ struct PagedArgs {
 struct ScaledArgs : PagedArgs {
   const uint8_t *k_codes, *v_codes, *k_scale, *v_scale;
   int64_t sps, sbs, shs;  // the scales' page, block and head strides
+  // (most: places, as they are counted through by runs of 16)
   int block_shift;        // log2 of the tokens with one scale
 };
 

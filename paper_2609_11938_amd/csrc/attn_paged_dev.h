@@ -25,6 +25,27 @@ __device__ __forceinline__ int paged_len(const PagedArgs &a, int b) {
 
 __device__ __forceinline__ int shares_of(int len, int c) { return len > c ? (len + c - 1) / c : 1; }
 
+// Over the cache of 8 bits a query's tokens are counted through by runs of 16, which
+// lie on one page each where pages have as many: the sinks' last and the window's first
+// may hold tokens that are not seen. Token j is place j, or past the sinks' runs place
+// j - skip; places [hide, shown) are not seen.
+struct Seen {
+  int front, skip, hide, shown;
+};
+__device__ __forceinline__ Seen seen_of(const ScaledArgs &a, int tokens) {
+  Seen s{(a.sinks + 15) & ~15, 0, 0, 0};
+  const int first = tokens - a.window;
+  if (first <= a.sinks) return s;
+  if (first > s.front) s.skip = (first & ~15) - s.front;
+  s.hide = a.sinks;
+  s.shown = first - s.skip;
+  return s;
+}
+__device__ __forceinline__ int paged_len(const ScaledArgs &a, int b) {
+  const int n = paged_tokens(a, b);
+  return n - seen_of(a, n).skip;
+}
+
 // Sequences one to a lane; past 64, loops of as many.
 struct Share {
   int size;   // tokens of every share but a sequence's last
@@ -34,7 +55,8 @@ struct Share {
 
 // Tokens of a share, from every sequence's length: as many as make kBlocks shares
 // of the work of all key heads. mine: this lane's sequence's length.
-__device__ __forceinline__ int share_size(const PagedArgs &a, int mine) {
+template <class Args>
+__device__ __forceinline__ int share_size(const Args &a, int mine) {
   if (a.most <= kMinShare) return kMinShare;
   int64_t sum = mine;
   for (int b = OPA_WAVE + lane_id(); b < a.n_seqs; b += OPA_WAVE) sum += paged_len(a, b);
@@ -47,7 +69,8 @@ __device__ __forceinline__ int share_size(const PagedArgs &a, int mine) {
 }
 
 // Share `item` of all the sequences' shares; false past the last. By whole waves.
-__device__ __forceinline__ bool find_share(const PagedArgs &a, int item, Share &s) {
+template <class Args>
+__device__ __forceinline__ bool find_share(const Args &a, int item, Share &s) {
   const int lane = lane_id();
   const int mine = paged_len(a, lane);
   s.size = share_size(a, mine);
@@ -72,7 +95,8 @@ __device__ __forceinline__ bool find_share(const PagedArgs &a, int item, Share &
 }
 
 // The shares of sequence seq. By whole waves.
-__device__ __forceinline__ Share shares_at(const PagedArgs &a, int seq) {
+template <class Args>
+__device__ __forceinline__ Share shares_at(const Args &a, int seq) {
   const int lane = lane_id();
   Share s{};
   const int mine = paged_len(a, lane);

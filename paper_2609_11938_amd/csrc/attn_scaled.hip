@@ -216,15 +216,39 @@ __device__ __forceinline__ void scaled_store(const PagedArgs &a, int seq, int he
         l == 0.f ? -INFINITY : (top + log2_sum<E>(l)) * kLn2;
 }
 
-// As k_attn_paged, which see; a share's results end in m', m and l. W: a window.
-template <class E, int DP>
-__global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_scaled(ScaledArgs a) {
+// Largest over the lanes that hold the same column: 16 and 32 lanes apart.
+__device__ __forceinline__ float column_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return half_max(fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])));
+}
+
+// Values' codes of a tile in LDS: rows of DP bytes in chunks of 16, chunk c at place
+// c ^ code_swz(row), so that the 32 lanes of a read, 16 rows' pieces of one chunk, meet
+// each bank once.
+template <int DP>
+__device__ __forceinline__ int code_swz(int row) {
+  return DP == 128 ? ((row >> 1) & 3) | ((row >> 4) & 1) << 2
+                   : ((row >> 2) & 1) | ((row >> 4) & 1) << 1;
+}
+
+// As k_attn_paged, which see; a share's results end in m', m and l. Keys' codes come to
+// registers, values' straight to LDS, from where the transposing read gives a lane the
+// codes of one column of the 8 tokens whose weights it holds: they become 16-bit values
+// only as operands. The references follow the maxima only when those have passed them
+// by 8 binary digits: until then weights are at most 2^(8 + kShift).
+//
+// R: pages and blocks of 16 tokens or more. A run of 16 then has one page and one scale:
+// its addresses are scalars and a lane's own offsets, its exponents scalars. Otherwise
+// each token has its own (ts of any size too).
+template <class E, int DP, bool R>
+__global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 128 ? 3 : 4) void k_attn_scaled(ScaledArgs a) {
   constexpr int KS = DP / 32, DB = DP / 16, C = DP / 16, N = kTile * C / OPA_WAVE;
-  __shared__ __align__(16) union {
-    uint16_t v[kPagedWaves][kTile * DP];
-    float o[kPagedWaves][16][DP + 4];
-  } t;
-  __shared__ __align__(16) int se[kPagedWaves][kTile];  // a tile's exponents, k and v
+  constexpr int kBytes = kTile * DP;  // a wave's tile
+  // the tiles of the waves, two in turn; at the end the waves' sums, two waves' in each
+  __shared__ __align__(16) uint8_t v0[kPagedWaves * kBytes], v1[kPagedWaves * kBytes];
+  static_assert(kPagedWaves * kBytes == 2 * 16 * DP * 4, "sums of two waves");
+  __shared__ __align__(16) int se[R ? 1 : kPagedWaves][kTile];  // a tile's exponents, k and v
   __shared__ float sm[kPagedWaves][16], sv[kPagedWaves][16], sl[kPagedWaves][16];
   const int lane = lane_id(), wave = uniform(wave_id());
   const int r = lane & 15, g = lane >> 4;
@@ -234,13 +258,13 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_scaled(Scale
   const int seq = s.seq, len = s.len;
   const int t0 = s.part * s.size, t1 = len < t0 + s.size ? len : t0 + s.size;
   const int32_t *table = a.table + (int64_t)seq * a.width;
-  const int tokens = uniform(paged_tokens(a, seq)), skip = tokens - len;
+  const int tokens = uniform(paged_tokens(a, seq));
+  const Seen seen = seen_of(a, tokens);
   if (a.diag && threadIdx.x == 0 && s.part == 0 && hk == 0 && a.lens[seq] != tokens)
     report(a.diag, OPATTR_F_DATA, 1);
 
   // Queries as the keys' chunks of 16 come: chunk 4 e + g, its first 8 and its last.
   const uint16_t *qrow = a.q.p + seq * a.q.ts + (int64_t)hk * a.group * a.q.hs;
-  const uint8_t *nothing = reinterpret_cast<const uint8_t *>(qrow);
   s16x8 qf[KS];
 #pragma unroll
   for (int e = 0; e < KS; ++e) {
@@ -258,106 +282,192 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_scaled(Scale
   int bad = 0;
 
   constexpr int kNone = INT_MIN;
-  const auto token_of = [&](int k0) __attribute__((always_inline)) {
-    const int tok = k0 + (lane & 31);
-    return tok >= a.sinks ? tok + skip : tok;
+  const auto token_at = [&](int place) __attribute__((always_inline)) {
+    return place >= seen.front ? place + seen.skip : place;
   };
+  const auto is_seen = [&](int place) __attribute__((always_inline)) {
+    return place < t1 && !(place >= seen.hide && place < seen.shown);
+  };
+  // This lane's place of a tile: of a token, or the first of its run.
+  const int mine = R ? lane & 16 : lane & 31;
   const auto page_of = [&](int k0) __attribute__((always_inline)) {
-    return k0 + (lane & 31) < t1 ? table[token_of(k0) >> a.shift] : kNone;
+    return (R ? k0 + mine < t1 : is_seen(k0 + mine)) ? table[token_at(k0 + mine) >> a.shift]
+                                                     : kNone;
   };
-  // Where the token's codes lie (-1: nowhere), and its two exponents' bytes.
-  u32x4 vr[N], kr[KS];
-  int ek, ev;
-  const auto load = [&](int page, int k0) __attribute__((always_inline)) {
-    const bool ok = page >= 0 && page < a.n_pages;
-    bad += page != kNone && !ok && lane < 32;
-    const int slot = token_of(k0) & mask;
-    const int64_t to = page * a.ps + slot * a.ts + (int64_t)hk * a.hs;
-    const int64_t at = ok ? to : (int64_t)-1;
-    const int64_t es =
-        page * a.sps + (slot >> a.block_shift) * a.sbs + (int64_t)hk * a.shs;
+  // The loads of the tile at k0: keys to registers, values to `to`, the bytes of the
+  // exponents. `here`: this lane's token (run) is there; what is not there leaves what
+  // was in its place.
+  u32x4 kr[KS] = {};
+  int ek = 0, ev = 0;  // R: ev's byte is in the lanes' other half
+  bool here = false;
+  // R: a lane's part of the addresses; rows 8 i of a run besides, where a load has 8
+  // (fresh: kept as the offsets that they are, not as addresses)
+  int k_off[KS / 2], v_off[2];
+  if constexpr (R) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int id = i * OPA_WAVE + lane, ch = id % C < last ? id % C : last;
-      const int64_t p = __shfl(at, id / C);
-      vr[i] = *reinterpret_cast<const u32x4 *>((p >= 0 ? a.v_codes + p : nothing) + ch * 16);
-    }
+    for (int e = 0; e < KS / 2; ++e)
+      k_off[e] = r * (int)a.ts + (4 * e + g < last ? 4 * e + g : last) * 16;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int64_t p = __shfl(at, 16 * u + r);
-      const uint8_t *kp = p >= 0 ? a.k_codes + p : nothing;
-#pragma unroll
-      for (int e = 0; e < KS / 2; ++e) {
-        const int ch = 4 * e + g < last ? 4 * e + g : last;
-        kr[u * (KS / 2) + e] = *reinterpret_cast<const u32x4 *>(kp + ch * 16);
-      }
+      const int row = lane / C, ch = (lane % C) ^ code_swz<DP>(16 * u + row);
+      v_off[u] = row * (int)a.ts + (ch < last ? ch : last) * 16;
     }
-    ek = *(ok ? a.k_scale + es : nothing);
-    ev = *(ok ? a.v_scale + es : nothing);
-    return at;
+  }
+  const auto load = [&](uint8_t *to, int page, int k0) __attribute__((always_inline)) {
+    here = page >= 0 && page < a.n_pages;
+    if constexpr (R) {
+      if (page != kNone && !here && lane < 32)
+        for (int i = 0; lane == mine && i < 16; ++i) bad += is_seen(k0 + mine + i);
+      const int slot = token_at(k0 + mine) & mask;
+      if (here) {
+        const int64_t es =
+            page * a.sps + (slot >> a.block_shift) * a.sbs + (int64_t)hk * a.shs;
+        ek = (lane < 32 ? a.k_scale : a.v_scale)[es];
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int p = __builtin_amdgcn_readlane(page, 16 * u);
+        if (p < 0 || p >= a.n_pages) continue;
+        const int64_t base = p * a.ps + (token_at(k0 + 16 * u) & mask) * a.ts + (int64_t)hk * a.hs;
+        const uint8_t *kb = a.k_codes + base, *vb = a.v_codes + base;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i)  // (8 rows on, the swizzle is the same)
+          __builtin_amdgcn_global_load_lds(
+              (const __attribute__((address_space(1))) void *)(vb + i * 8 * a.ts +
+                                                               (uint32_t)fresh(v_off[u])),
+              (__attribute__((address_space(3))) void *)(to + wave * kBytes +
+                                                         (u * (N / 2) + i) * OPA_WAVE * 16),
+              16, 0, 0);
+#pragma unroll
+        for (int e = 0; e < KS / 2; ++e)
+          kr[u * (KS / 2) + e] = 
+              *reinterpret_cast<const u32x4 *>(kb + (uint32_t)fresh(k_off[e]));
+      }
+    } else {
+      bad += page != kNone && !here && lane < 32;
+      const int slot = token_at(k0 + mine) & mask;
+      const uint8_t *nothing = reinterpret_cast<const uint8_t *>(qrow);
+      const int64_t at =
+          here ? page * a.ps + slot * a.ts + (int64_t)hk * a.hs : (int64_t)-1;
+      const int64_t es = page * a.sps + (slot >> a.block_shift) * a.sbs + (int64_t)hk * a.shs;
+      const uint32_t id = fresh(lane);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int row = (i * OPA_WAVE + id) / C, ch = (id % C) ^ code_swz<DP>(row);
+        const int64_t p = __shfl(at, row);
+        __builtin_amdgcn_global_load_lds(
+            (const __attribute__((address_space(1))) void *)((p >= 0 ? a.v_codes + p : nothing) +
+                                                             (ch < last ? ch : last) * 16),
+            (__attribute__((address_space(3))) void *)(to + wave * kBytes + i * OPA_WAVE * 16),
+            16, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int64_t p = __shfl(at, 16 * u + (id & 15));
+        const uint8_t *kp = p >= 0 ? a.k_codes + p : nothing;
+#pragma unroll
+        for (int e = 0; e < KS / 2; ++e) {
+          const int ch = 4 * e + (int)(id >> 4);
+          kr[u * (KS / 2) + e] =
+              *reinterpret_cast<const u32x4 *>(kp + (ch < last ? ch : last) * 16);
+        }
+      }
+      ek = *(here ? a.k_scale + es : nothing);
+      ev = *(here ? a.v_scale + es : nothing);
+    }
   };
 
-  int k0 = t0 + wave * kTile;
-  int64_t at = -1;
-  int next = kNone;
-  if (k0 < t1) {
-    at = load(page_of(k0), k0);
-    next = page_of(k0 + kTile * kPagedWaves);
-  }
-  for (; k0 < t1; k0 += kTile * kPagedWaves) {
-    const uint64_t there = __ballot(at >= 0);  // the tokens, in both halves
-    const uint64_t nan_k = __ballot(ek == 255), nan_v = __ballot(ev == 255);
-    if (lane < 32) se[wave][lane] = ek | ev << 8;
+  // The transposing read: of 16 lanes, lanes 2 k and 2 k + 1 name the two halves of a
+  // chunk of row k, and lane i gets column i of the 8 rows, here the tokens of its weights.
+  // The chunks differ in bits that the swizzle leaves to an exclusive or.
+  const int k = r >> 1, row = k < 4 ? 4 * g + k : 12 + 4 * g + k;
+  const int place = row * DP + (code_swz<DP>(row) << 4) + (r & 1) * 8;
+  constexpr int kNext = kTile * kPagedWaves;
+  int k0 = t0 + wave * kTile, next = kNone;
+  // One tile, from `v`, with the next one's loads on their way to `after`.
+  const auto step = [&](uint8_t *v, uint8_t *after) __attribute__((always_inline)) {
+    // the tokens that are seen, in both halves
+    uint64_t there = ~0ull, nan_k = 0, nan_v = 0;
+    int xk[2], xv[2];
+    if constexpr (R) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int id = i * OPA_WAVE + lane, row = id / C, ch = id % C;
-      if (!((there >> row) & 1) || ch > last) vr[i] = (u32x4)(0u);
-      uint16_t *p = &t.v[wave][row * DP];
-      *reinterpret_cast<s16x8 *>(p + (((2 * ch) ^ swz<DP>(row)) << 3)) =
-          eight_values<E>(vr[i][0], vr[i][1]);
-      *reinterpret_cast<s16x8 *>(p + (((2 * ch + 1) ^ swz<DP>(row)) << 3)) =
-          eight_values<E>(vr[i][2], vr[i][3]);
+      for (int u = 0; u < 2; ++u) {
+        xk[u] = __builtin_amdgcn_readlane(ek, 16 * u);
+        xv[u] = __builtin_amdgcn_readlane(ek, 16 * u + 32);
+      }
+      const uint64_t runs = __ballot(here);
+      if (runs != ~0ull || k0 + kTile > t1 || (k0 < seen.shown && k0 + kTile > seen.hide))
+        there = __ballot(here && is_seen(k0 + (lane & 31)));
+      if (xk[0] == 255 || xk[1] == 255 || xv[0] == 255 || xv[1] == 255) {
+        const uint64_t run[2] = {0xffffull, 0xffff0000ull};
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if (xk[u] == 255) nan_k |= run[u] & there;
+          if (xv[u] == 255) nan_v |= run[u] & there;
+        }
+      }
+    } else {
+      there = __ballot(here);
+      nan_k = __ballot(here && ek == 255);
+      nan_v = __ballot(here && ev == 255);
+      if (lane < 32) se[wave][lane] = ek | ev << 8;
     }
-    f32x4 x[2];
+    if (there != ~0ull) {  // a weight of 0 times what is not finite is no 0
+      const uint32_t id = fresh(lane);
+      const u32x4 zero = {(uint32_t)fresh(0), 0u, 0u, 0u};
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (!((there >> ((i * OPA_WAVE + id) / C)) & 1))
+          *reinterpret_cast<u32x4 *>(v + wave * kBytes + (i * OPA_WAVE + id) * 16) = zero;
+    }
+    if (a.head_dim < DP) {
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+        if (4 * (i % (KS / 2)) + g > last) kr[i] = (u32x4)(0u);
+    }
+    f32x4 x[2], y[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       x[u] = (f32x4)(0.f);
 #pragma unroll
       for (int e = 0; e < KS / 2; ++e) {
-        u32x4 w = kr[u * (KS / 2) + e];
-        if (4 * e + g > last) w = (u32x4)(0u);
+        const u32x4 w = kr[u * (KS / 2) + e];
         x[u] = E::mfma16(eight_values<E>(w[0], w[1]), qf[2 * e], x[u]);
         x[u] = E::mfma16(eight_values<E>(w[2], w[3]), qf[2 * e + 1], x[u]);
       }
     }
-    typedef int i32x4 __attribute__((ext_vector_type(4)));
-    const i32x4 ex[2] = {*reinterpret_cast<const i32x4 *>(&se[wave][4 * g]),
-                         *reinterpret_cast<const i32x4 *>(&se[wave][16 + 4 * g])};
     // the next tile's loads, before this one's softmax; pages one tile further
-    if (k0 + kTile * kPagedWaves < t1) {
-      at = load(next, k0 + kTile * kPagedWaves);
-      next = page_of(k0 + 2 * kTile * kPagedWaves);
+    if (k0 + kNext < t1) {
+      load(after, next, k0 + kNext);
+      next = page_of(k0 + 2 * kNext);
     }
-    float top = -INFINITY, vtop = -INFINITY;
-    f32x4 y[2];
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) {
+      i32x4 ex;
+      if constexpr (!R) ex = *reinterpret_cast<const i32x4 *>(&se[wave][16 * u + 4 * g]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool ok = (there >> (16 * u + 4 * g + i)) & 1;
-        x[u][i] = ok ? ldexpf(x[u][i] * c, (ex[u][i] & 255) - 127) : -INFINITY;
-        y[u][i] = x[u][i] + (float)((ex[u][i] >> 8) - 127);
+        const int sk = R ? xk[u] : ex[i] & 255, sv8 = R ? xv[u] : ex[i] >> 8;
+        x[u][i] = __builtin_amdgcn_ldexpf(x[u][i] * c, sk - 127);
+        y[u][i] = x[u][i] + (float)(sv8 - 127);
       }
-    if ((nan_k | nan_v) & there) {
+    }
+    if (there != ~0ull || (nan_k | nan_v)) {
+      const int shift = 4 * (fresh(lane) >> 4 & 3);
+      const uint32_t seen4 = (uint32_t)there >> shift, nk = (uint32_t)nan_k >> shift,
+                     nv = (uint32_t)nan_v >> shift;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int tok = 16 * u + 4 * g + i;
-          if ((nan_k & there) >> tok & 1) x[u][i] = y[u][i] = __builtin_nanf("");
-          if ((nan_v & there) >> tok & 1) y[u][i] = __builtin_nanf("");
+          const uint32_t bit = 1u << (16 * u + i);
+          if (nk & bit) x[u][i] = y[u][i] = __builtin_nanf("");
+          if (nv & bit) y[u][i] = __builtin_nanf("");
+          if (!(seen4 & bit)) x[u][i] = y[u][i] = -INFINITY;
         }
     }
+    float top = -INFINITY, vtop = -INFINITY;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -365,49 +475,64 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_scaled(Scale
         top = fmaxf(top, x[u][i]);
         vtop = fmaxf(vtop, y[u][i]);
       }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    vtop = fmaxf(vtop, __shfl_xor(vtop, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    vtop = fmaxf(vtop, __shfl_xor(vtop, 32));
-    const float mn = fmaxf(m, top), mvn = fmaxf(mv, vtop);
-    const float ref = mn == -INFINITY ? 0.f : mn, vref = mvn == -INFINITY ? 0.f : mvn;
-    const float old = exp2_fast(m - ref), vold = exp2_fast(mv - vref);
-    m = mn;
-    mv = mvn;
+    if (__any(top > m + 8.f || vtop > mv + 8.f)) {
+      const float mn = fmaxf(m, column_max(top)), mvn = fmaxf(mv, column_max(vtop));
+      l *= mn == -INFINITY ? 1.f : exp2_fast(m - mn);
+      const float by = mvn == -INFINITY ? 1.f : exp2_fast(mv - mvn);
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[d][e] *= by;
+      m = mn;
+      mv = mvn;
+    }
+    const float ref = E::kShift - (m == -INFINITY ? 0.f : m);
+    const float vref = E::kShift - (mv == -INFINITY ? 0.f : mv);
     float sum = 0.f;
     u32x4 w;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        sum += exp2_fast(x[u][2 * i] - ref + E::kShift) +
-               exp2_fast(x[u][2 * i + 1] - ref + E::kShift);
-        w[2 * u + i] = E::pack(exp2_fast(y[u][2 * i] - vref + E::kShift),
-                               exp2_fast(y[u][2 * i + 1] - vref + E::kShift));
+        sum += exp2_fast(x[u][2 * i] + ref) + exp2_fast(x[u][2 * i + 1] + ref);
+        w[2 * u + i] =
+            E::pack(exp2_fast(y[u][2 * i] + vref), exp2_fast(y[u][2 * i + 1] + vref));
       }
-    l = l * old + sum;
+    l += sum;
     const s16x8 pf = __builtin_bit_cast(s16x8, w);
+    const int at = fresh(place);
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-      typedef s16x4 __attribute__((address_space(3))) * lds4;
-      const int i = lane & 15, row = 4 * g + (i >> 2), col = 16 * d + 4 * (i & 3);
-      const uint16_t *p0 = &t.v[wave][row * DP + (((col >> 3) ^ swz<DP>(row)) << 3) + (col & 4)];
-      const uint16_t *p1 = p0 + 16 * DP;  // swz repeats every 16 rows
-      const s16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p0);
-      const s16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p1);
-      const s16x8 vf = __builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[d][e] *= vold;
-      o[d] = E::mfma16(vf, pf, o[d]);
+      typedef int i32x2 __attribute__((ext_vector_type(2)));
+      typedef i32x2 __attribute__((address_space(3))) * lds8;
+      const i32x2 codes =
+          __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds8)(v + wave * kBytes + (at ^ (d << 4))));
+      o[d] = E::mfma16(eight_values<E>((uint32_t)codes[0], (uint32_t)codes[1]), pf, o[d]);
     }
+    k0 += kNext;
+  };
+  if (k0 < t1) {
+    load(v0, page_of(k0), k0);
+    next = page_of(k0 + kNext);
+  }
+  while (k0 < t1) {
+    wait_loads();
+    step(v0, v1);
+    if (k0 >= t1) break;
+    wait_loads();
+    step(v1, v0);
   }
   if (hk == 0 && bad) report(a.diag, OPATTR_F_DATA, bad);
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   __syncthreads();
+  // a wave's row r of sums, piece p of four values at place p ^ r
+  const auto sums = [&](int w, int row, int p) __attribute__((always_inline)) {
+    return reinterpret_cast<f32x4 *>(w < 2 ? v0 : v1) +
+           (((w & 1) * 16 + row) * (DP / 4) + (p ^ row));
+  };
 #pragma unroll
-  for (int d = 0; d < DB; ++d)
-    *reinterpret_cast<f32x4 *>(&t.o[wave][r][16 * d + 4 * g]) = o[d];
+  for (int d = 0; d < DB; ++d) *sums(wave, r, 4 * d + g) = o[d];
   if (g == 0) {
     sm[wave][r] = m;
     sv[wave][r] = mv;
@@ -416,7 +541,7 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_scaled(Scale
   __syncthreads();
   const bool whole = shares_of(len, s.size) == 1;
   for (int i = threadIdx.x; i < a.group * (DP / 4); i += kPagedWaves * OPA_WAVE) {
-    const int row = i / (DP / 4), d = i % (DP / 4) * 4, head = hk * a.group + row;
+    const int row = i / (DP / 4), p = i % (DP / 4), head = hk * a.group + row;
     float top = -INFINITY, vtop = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kPagedWaves; ++w) {
@@ -428,15 +553,15 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_scaled(Scale
     float ls = 0.f;
 #pragma unroll
     for (int w = 0; w < kPagedWaves; ++w) {
-      v += *reinterpret_cast<const f32x4 *>(&t.o[w][row][d]) * exp2_fast(sv[w][row] - vref);
+      v += *sums(w, row, p) * exp2_fast(sv[w][row] - vref);
       ls = fmaf(sl[w][row], exp2_fast(sm[w][row] - ref), ls);
     }
     if (whole) {
-      scaled_store<E>(a, seq, head, d, v, vtop, top, ls);
+      scaled_store<E>(a, seq, head, 4 * p, v, vtop, top, ls);
     } else {
-      float *p = a.part + ((int64_t)item * a.n_heads + head) * (DP + 4);
-      *reinterpret_cast<f32x4 *>(p + d) = v;
-      if (d == 0) *reinterpret_cast<f32x4 *>(p + DP) = f32x4{vtop, top, ls, 0.f};
+      float *to = a.part + ((int64_t)item * a.n_heads + head) * (DP + 4);
+      *reinterpret_cast<f32x4 *>(to + 4 * p) = v;
+      if (p == 0) *reinterpret_cast<f32x4 *>(to + DP) = f32x4{vtop, top, ls, 0.f};
     }
   }
 }
@@ -500,11 +625,16 @@ __global__ __launch_bounds__(kJoin * DP / 4) void k_scaled_join(ScaledArgs a) {
   scaled_store<E>(a, seq, head, d, v, vtop, top, l);
 }
 
+constexpr int64_t kMaxRunStride = 1 << 26;  // 16 tokens within 2^31 bytes
+
 template <class E, int DP>
 static void launch(const ScaledArgs &a, hipStream_t s) {
   const int64_t items = most_items(a.n_seqs, a.n_kv, a.most);
-  hipLaunchKernelGGL((k_attn_scaled<E, DP>), dim3((uint32_t)(items * a.n_kv)),
-                     dim3(kPagedWaves * OPA_WAVE), 0, s, a);
+  const dim3 grid((uint32_t)(items * a.n_kv)), block(kPagedWaves * OPA_WAVE);
+  if (a.shift >= 4 && a.block_shift >= 4 && a.ts <= kMaxRunStride)
+    hipLaunchKernelGGL((k_attn_scaled<E, DP, true>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((k_attn_scaled<E, DP, false>), grid, block, 0, s, a);
   if (a.most > kMinShare)
     hipLaunchKernelGGL((k_scaled_join<E, DP>), dim3((uint32_t)(a.n_seqs * a.n_heads)),
                        dim3(kJoin * DP / 4), 0, s, a);
