@@ -252,7 +252,7 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 128 ? 3 : 4) void k_a
   __shared__ float sm[kPagedWaves][16], sv[kPagedWaves][16], sl[kPagedWaves][16];
   const int lane = lane_id(), wave = uniform(wave_id());
   const int r = lane & 15, g = lane >> 4;
-  const int hk = blockIdx.x % a.n_kv, item = blockIdx.x / a.n_kv;
+  const int hk = blockIdx.x / 8 % a.n_kv, item = blockIdx.x % 8 + blockIdx.x / 8 / a.n_kv * 8;
   Share s;
   if (!find_share(a, item, s)) return;
   const int seq = s.seq, len = s.len;
@@ -629,7 +629,7 @@ constexpr int64_t kMaxRunStride = 1 << 26;  // 16 tokens within 2^31 bytes
 
 template <class E, int DP>
 static void launch(const ScaledArgs &a, hipStream_t s) {
-  const int64_t items = most_items(a.n_seqs, a.n_kv, a.most);
+  const int64_t items = (most_items(a.n_seqs, a.n_kv, a.most) + 7) / 8 * 8;
   const dim3 grid((uint32_t)(items * a.n_kv)), block(kPagedWaves * OPA_WAVE);
   if (a.shift >= 4 && a.block_shift >= 4 && a.ts <= kMaxRunStride)
     hipLaunchKernelGGL((k_attn_scaled<E, DP, true>), grid, block, 0, s, a);
