@@ -189,6 +189,20 @@ static bool ok_scaled_out(const opattr_kv_scaled *c) {
 
 static int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
 
+// The partial results of the attention of one token a sequence, and with what their join
+// has to know.
+static size_t parts_of(const opattr_kv_pages *c, int32_t n_heads, int most) {
+  return align256(paged_parts(c->n_seqs, c->n_kv_heads, n_heads, most));
+}
+static size_t parts_of(const opattr_kv_scaled *c, int32_t n_heads, int most) {
+  return align256(scaled_parts(c->n_seqs, c->n_kv_heads, n_heads, most));
+}
+template <class Cache>
+static size_t parts_and_shares(const Cache *c, int32_t n_heads, int most) {
+  const size_t parts = parts_of(c, n_heads, most);
+  return parts ? parts + align256((size_t)c->n_seqs * 8) : 0;
+}
+
 // What the attention of one token a sequence takes of a cache, of either kind.
 template <class Cache>
 static void paged_args(PagedArgs &a, const Cache *c, int32_t n_heads, int32_t window,
@@ -215,8 +229,11 @@ static void paged_args(PagedArgs &a, const Cache *c, int32_t n_heads, int32_t wi
   a.lens = lens;
   a.scale = scale;
   a.lse = lse;
-  a.part = static_cast<float *>(ws);
   a.diag = diag;
+  const size_t parts = parts_of(c, n_heads, a.most);
+  if (parts == 0) return;
+  a.part = static_cast<float *>(ws);
+  a.shares = reinterpret_cast<int32_t *>(static_cast<char *>(ws) + parts);
 }
 
 constexpr int kMaxPages = 1 << 24;
@@ -331,7 +348,7 @@ static int prompt_grad(const opattr_attn_shape *a, int32_t window, int32_t sinks
 static size_t paged_bytes(const opattr_kv_pages *c, int32_t n_heads, int32_t window,
                           int32_t sinks) {
   if (!ok_pages(c) || !ok_heads(n_heads, c->n_kv_heads, c->head_dim)) return 0;
-  return paged_workspace(c->n_seqs, c->n_kv_heads, n_heads, most_seen(c, window, sinks));
+  return parts_and_shares(c, n_heads, most_seen(c, window, sinks));
 }
 
 template <class Cache>
@@ -435,7 +452,7 @@ size_t opattr_attn_paged_scaled_workspace_bytes(const opattr_kv_scaled *c, int32
   if (!ok_scaled(c) || !ok_heads(n_heads, c->n_kv_heads, c->head_dim) ||
       !ok_window(window, sinks))
     return 0;
-  return paged_workspace(c->n_seqs, c->n_kv_heads, n_heads, most_seen(c, window, sinks));
+  return parts_and_shares(c, n_heads, most_seen(c, window, sinks));
 }
 
 int opattr_attn_paged_scaled(const opattr_kv_scaled *c, int32_t n_heads, int32_t window,

@@ -59,6 +59,7 @@ struct PagedArgs {
   opattr_diag *diag;
   int window, sinks;  // window 0: none
   int most;           // tokens of a sequence that its query can see
+  int32_t *shares;    // [n_seqs][2] behind the partial results, for their join
 };
 
 // The cache of 8 bits; strides (those of PagedArgs too) in bytes.
@@ -109,7 +110,9 @@ struct PagesArgs {
 };
 
 void run_paged(const PagedArgs &a, int dtype, hipStream_t s);
-size_t paged_workspace(int n_seqs, int n_kv, int n_heads, int most);
+// Bytes of the partial results; the sequences' shares come behind them.
+size_t paged_parts(int n_seqs, int n_kv, int n_heads, int most);
+size_t scaled_parts(int n_seqs, int n_kv, int n_heads, int most);
 void run_paged_scaled(const ScaledArgs &a, int dtype, hipStream_t s);
 void run_append_scaled(const AppendScaledArgs &a, int dtype, hipStream_t s);
 // blocks of tokens that n_new new ones of n_seqs sequences touch, at most

@@ -46,6 +46,7 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, 2) void k_attn_paged(PagedA
   const int hk = blockIdx.x % a.n_kv, item = blockIdx.x / a.n_kv;
   Share s;
   if (!find_share(a, item, s)) return;
+  if (hk == 0) note_shares(a, s);
   const int seq = s.seq, len = s.len;
   const int t0 = s.part * s.size, t1 = len < t0 + s.size ? len : t0 + s.size;
   const int32_t *table = a.table + (int64_t)seq * a.width;
@@ -239,11 +240,11 @@ __global__ __launch_bounds__(kJoin * DP / 4) void k_paged_join(PagedArgs a) {
   __shared__ __align__(16) f32x4 sums[kJoin][DP / 4];
   __shared__ float wave_top[kThreads / OPA_WAVE], run_l[kJoin];
   const int head = blockIdx.x % a.n_heads, seq = blockIdx.x / a.n_heads;
-  const Share s = shares_at(a, seq);
-  const int n = shares_of(s.len, s.size);
+  const int2 mine = *reinterpret_cast<const int2 *>(a.shares + 2 * seq);
+  const int n = mine.y;
   if (n == 1) return;
   const int64_t step = (int64_t)a.n_heads * (DP + 4);
-  const float *p = a.part + ((int64_t)s.first * a.n_heads + head) * (DP + 4);
+  const float *p = a.part + ((int64_t)mine.x * a.n_heads + head) * (DP + 4);
   float top = -INFINITY;
   for (int k = threadIdx.x; k < n; k += kThreads) {
     f[k] = p[k * step + DP];
@@ -277,14 +278,21 @@ __global__ __launch_bounds__(kJoin * DP / 4) void k_paged_join(PagedArgs a) {
   paged_store<E>(a, seq, head, d, v, top, l);
 }
 
-size_t paged_workspace(int n_seqs, int n_kv, int n_heads, int most) {
+static size_t parts(int n_seqs, int n_kv, int n_heads, int most, int blocks) {
   if (most <= kMinShare) return 0;  // no sequence has two shares
-  return (size_t)most_items(n_seqs, n_kv, most) * n_heads * (128 + 4) * sizeof(float);
+  return (size_t)most_items(n_seqs, n_kv, most, blocks) * n_heads * (128 + 4) * sizeof(float);
+}
+
+size_t paged_parts(int n_seqs, int n_kv, int n_heads, int most) {
+  return parts(n_seqs, n_kv, n_heads, most, kBlocks);
+}
+size_t scaled_parts(int n_seqs, int n_kv, int n_heads, int most) {
+  return parts(n_seqs, n_kv, n_heads, most, kScaledBlocks);
 }
 
 template <class E, int DP>
 static void launch(const PagedArgs &a, hipStream_t s) {
-  const int64_t items = most_items(a.n_seqs, a.n_kv, a.most);
+  const int64_t items = most_items(a.n_seqs, a.n_kv, a.most, kBlocks);
   const dim3 grid((uint32_t)(items * a.n_kv)), block(kPagedWaves * OPA_WAVE);
   if (a.window)
     hipLaunchKernelGGL((k_attn_paged<E, DP, true>), grid, block, 0, s, a);

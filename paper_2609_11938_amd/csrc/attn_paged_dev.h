@@ -11,7 +11,7 @@ namespace opa {
 constexpr int kPagedWaves = 4;
 constexpr int kTile = 32;        // tokens a wave takes at a time
 constexpr int kMinShare = 256;   // tokens of the smallest share
-constexpr int kBlocks = 1024;
+constexpr int kBlocks = 1024, kScaledBlocks = 2048;
 
 // Tokens of sequence b, as many as its table can name; of these, as many as its
 // query sees: the first and the last ones, through a window with sinks.
@@ -53,16 +53,24 @@ struct Share {
   int first;  // the sequence's first share, as the shares are counted
 };
 
-// Tokens of a share, from every sequence's length: as many as make kBlocks shares
+// Blocks that the shares come to.
+__host__ __device__ constexpr int blocks_of(const PagedArgs &) { return kBlocks; }
+__host__ __device__ constexpr int blocks_of(const ScaledArgs &) { return kScaledBlocks; }
+
+// Tokens of a share, from every sequence's length: as many as make blocks_of shares
 // of the work of all key heads. mine: this lane's sequence's length.
 template <class Args>
 __device__ __forceinline__ int share_size(const Args &a, int mine) {
   if (a.most <= kMinShare) return kMinShare;
   int64_t sum = mine;
   for (int b = OPA_WAVE + lane_id(); b < a.n_seqs; b += OPA_WAVE) sum += paged_len(a, b);
+  if (__all(sum < 1 << 25)) {
+    sum = __builtin_amdgcn_readlane(wave_sums((int)sum), OPA_WAVE - 1);
+  } else {
 #pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-  const int64_t each = (sum * a.n_kv + kBlocks - 1) / kBlocks;
+    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+  }
+  const int64_t each = (sum * a.n_kv + blocks_of(a) - 1) / blocks_of(a);
   const int64_t c = (each + kTile * kPagedWaves - 1) / (kTile * kPagedWaves) *
                     (kTile * kPagedWaves);
   return uniform((int)(c < kMinShare ? kMinShare : c < 1 << 30 ? c : 1 << 30));
@@ -94,25 +102,16 @@ __device__ __forceinline__ bool find_share(const Args &a, int item, Share &s) {
   return false;
 }
 
-// The shares of sequence seq. By whole waves.
-template <class Args>
-__device__ __forceinline__ Share shares_at(const Args &a, int seq) {
-  const int lane = lane_id();
-  Share s{};
-  const int mine = paged_len(a, lane);
-  s.size = share_size(a, mine);
-  s.seq = seq;
-  s.len = uniform(paged_len(a, seq));
-  int sum = lane < seq ? shares_of(mine, s.size) : 0;
-  for (int b = OPA_WAVE + lane; b < seq; b += OPA_WAVE) sum += shares_of(paged_len(a, b), s.size);
-  s.first = __builtin_amdgcn_readlane(wave_sums(sum), OPA_WAVE - 1);
-  return s;
+// What the join wants to know of a sequence: its first share, and how many.
+__device__ __forceinline__ void note_shares(const PagedArgs &a, const Share &s) {
+  if (a.shares && s.part == 0 && threadIdx.x == 0)
+    *reinterpret_cast<int2 *>(a.shares + 2 * s.seq) = int2{s.first, shares_of(s.len, s.size)};
 }
 
-// Shares at most: sum of ceil(len / c) with c >= kMinShare and c >= sum / (kBlocks
+// Shares at most: sum of ceil(len / c) with c >= kMinShare and c >= sum / (blocks
 // / n_kv).
-inline int64_t most_items(int n_seqs, int n_kv, int most) {
-  const int64_t a = (int64_t)kBlocks / n_kv + 1 + n_seqs;
+inline int64_t most_items(int n_seqs, int n_kv, int most, int blocks) {
+  const int64_t a = (int64_t)blocks / n_kv + 1 + n_seqs;
   const int64_t b = (int64_t)n_seqs * (most > kMinShare ? (most + kMinShare - 1) / kMinShare : 1);
   return a < b ? a : b;
 }

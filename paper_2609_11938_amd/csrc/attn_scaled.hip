@@ -255,6 +255,7 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 128 ? 3 : 4) void k_a
   const int hk = blockIdx.x / 8 % a.n_kv, item = blockIdx.x % 8 + blockIdx.x / 8 / a.n_kv * 8;
   Share s;
   if (!find_share(a, item, s)) return;
+  if (hk == 0) note_shares(a, s);
   const int seq = s.seq, len = s.len;
   const int t0 = s.part * s.size, t1 = len < t0 + s.size ? len : t0 + s.size;
   const int32_t *table = a.table + (int64_t)seq * a.width;
@@ -572,15 +573,15 @@ constexpr int kJoin = 8;
 template <class E, int DP>
 __global__ __launch_bounds__(kJoin * DP / 4) void k_scaled_join(ScaledArgs a) {
   constexpr int kThreads = kJoin * DP / 4;
-  __shared__ float f[kBlocks + 64], fv[kBlocks + 64];  // the most shares of a sequence
+  __shared__ float f[kScaledBlocks + 64], fv[kScaledBlocks + 64];  // the most shares of a sequence
   __shared__ __align__(16) f32x4 sums[kJoin][DP / 4];
   __shared__ float wave_top[kThreads / OPA_WAVE][2], run_l[kJoin];
   const int head = blockIdx.x % a.n_heads, seq = blockIdx.x / a.n_heads;
-  const Share s = shares_at(a, seq);
-  const int n = shares_of(s.len, s.size);
+  const int2 mine = *reinterpret_cast<const int2 *>(a.shares + 2 * seq);
+  const int n = mine.y;
   if (n == 1) return;
   const int64_t step = (int64_t)a.n_heads * (DP + 4);
-  const float *p = a.part + ((int64_t)s.first * a.n_heads + head) * (DP + 4);
+  const float *p = a.part + ((int64_t)mine.x * a.n_heads + head) * (DP + 4);
   float top = -INFINITY, vtop = -INFINITY;
   for (int k = threadIdx.x; k < n; k += kThreads) {
     fv[k] = p[k * step + DP];
@@ -629,7 +630,7 @@ constexpr int64_t kMaxRunStride = 1 << 26;  // 16 tokens within 2^31 bytes
 
 template <class E, int DP>
 static void launch(const ScaledArgs &a, hipStream_t s) {
-  const int64_t items = (most_items(a.n_seqs, a.n_kv, a.most) + 7) / 8 * 8;
+  const int64_t items = (most_items(a.n_seqs, a.n_kv, a.most, kScaledBlocks) + 7) / 8 * 8;
   const dim3 grid((uint32_t)(items * a.n_kv)), block(kPagedWaves * OPA_WAVE);
   if (a.shift >= 4 && a.block_shift >= 4 && a.ts <= kMaxRunStride)
     hipLaunchKernelGGL((k_attn_scaled<E, DP, true>), grid, block, 0, s, a);

@@ -88,10 +88,14 @@ def test_window_workspaces(lib):  # noqa: F811
         for ws, n in ((None, need), (FAKE, need - 1), (FAKE + 16, need)):
             assert _grad(lib, a, w, [r] * 8, ws=ws, n=n) == WORKSPACE
         assert _grad(lib, a, w, [r] * 8, lse=None) == INVALID
-    # a window that no share is larger than needs no room for partial results
-    for c, need in ((_pages(table_stride=500), lib.opattr_attn_paged_window_workspace_bytes),
-                    (_scaled(table_stride=500), lib.opattr_attn_paged_scaled_workspace_bytes)):
-        assert need(c, 8, 200, 56) == 0 < need(c, 8, 200, 57) <= need(c, 8, 2 ** 31 - 1, 5)
+    # a window that no share is larger than needs no room for partial results; the cache
+    # of 8 bits counts it by whole runs of 16 tokens
+    for c, need, none, some in (
+            (_pages(table_stride=500), lib.opattr_attn_paged_window_workspace_bytes, (200, 56),
+             (200, 57)),
+            (_scaled(table_stride=500), lib.opattr_attn_paged_scaled_workspace_bytes, (193, 33),
+             (194, 33))):
+        assert need(c, 8, *none) == 0 < need(c, 8, *some) <= need(c, 8, 2 ** 31 - 1, 5)
     for c, call, need in (
             (_pages(table_stride=500), lib.opattr_attn_paged_window,
              lib.opattr_attn_paged_window_workspace_bytes),
