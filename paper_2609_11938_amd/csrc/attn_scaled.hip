@@ -242,7 +242,7 @@ __device__ __forceinline__ int code_swz(int row) {
 // its addresses are scalars and a lane's own offsets, its exponents scalars. Otherwise
 // each token has its own (ts of any size too).
 template <class E, int DP, bool R>
-__global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 128 ? 3 : 4) void k_attn_scaled(ScaledArgs a) {
+__global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 64 ? 4 : 3) void k_attn_scaled(ScaledArgs a) {
   constexpr int KS = DP / 32, DB = DP / 16, C = DP / 16, N = kTile * C / OPA_WAVE;
   constexpr int kBytes = kTile * DP;  // a wave's tile
   // the tiles of the waves, two in turn; at the end the waves' sums, two waves' in each
@@ -301,19 +301,6 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 128 ? 3 : 4) void k_a
   u32x4 kr[KS] = {};
   int ek = 0, ev = 0;  // R: ev's byte is in the lanes' other half
   bool here = false;
-  // R: a lane's part of the addresses; rows 8 i of a run besides, where a load has 8
-  // (fresh: kept as the offsets that they are, not as addresses)
-  int k_off[KS / 2], v_off[2];
-  if constexpr (R) {
-#pragma unroll
-    for (int e = 0; e < KS / 2; ++e)
-      k_off[e] = r * (int)a.ts + (4 * e + g < last ? 4 * e + g : last) * 16;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int row = lane / C, ch = (lane % C) ^ code_swz<DP>(16 * u + row);
-      v_off[u] = row * (int)a.ts + (ch < last ? ch : last) * 16;
-    }
-  }
   const auto load = [&](uint8_t *to, int page, int k0) __attribute__((always_inline)) {
     here = page >= 0 && page < a.n_pages;
     if constexpr (R) {
@@ -323,26 +310,34 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 128 ? 3 : 4) void k_a
       if (here) {
         const int64_t es =
             page * a.sps + (slot >> a.block_shift) * a.sbs + (int64_t)hk * a.shs;
-        ek = (lane < 32 ? a.k_scale : a.v_scale)[es];
+        ek = (fresh(lane) < 32 ? a.k_scale : a.v_scale)[es];
       }
+      // A lane's part of the addresses, rows 8 i of a run besides where a load has 8:
+      // again each time (held over the loop, or kept as addresses, they take more
+      // registers than four waves a SIMD have).
+      const uint32_t id = fresh(lane), ts = (uint32_t)a.ts;
+      const uint32_t k_row = (id & 15) * ts, v_row = id / C * ts;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int p = __builtin_amdgcn_readlane(page, 16 * u);
         if (p < 0 || p >= a.n_pages) continue;
         const int64_t base = p * a.ps + (token_at(k0 + 16 * u) & mask) * a.ts + (int64_t)hk * a.hs;
         const uint8_t *kb = a.k_codes + base, *vb = a.v_codes + base;
+        const int vc = (int)(id % C) ^ code_swz<DP>(16 * u + (int)(id / C));
+        const uint32_t v_at = v_row + (vc < last ? vc : last) * 16;
 #pragma unroll
         for (int i = 0; i < N / 2; ++i)  // (8 rows on, the swizzle is the same)
           __builtin_amdgcn_global_load_lds(
-              (const __attribute__((address_space(1))) void *)(vb + i * 8 * a.ts +
-                                                               (uint32_t)fresh(v_off[u])),
+              (const __attribute__((address_space(1))) void *)(vb + i * 8 * a.ts + v_at),
               (__attribute__((address_space(3))) void *)(to + wave * kBytes +
                                                          (u * (N / 2) + i) * OPA_WAVE * 16),
               16, 0, 0);
 #pragma unroll
-        for (int e = 0; e < KS / 2; ++e)
-          kr[u * (KS / 2) + e] = 
-              *reinterpret_cast<const u32x4 *>(kb + (uint32_t)fresh(k_off[e]));
+        for (int e = 0; e < KS / 2; ++e) {
+          const int ch = 4 * e + (int)(id >> 4);
+          kr[u * (KS / 2) + e] = *reinterpret_cast<const u32x4 *>(
+              kb + (k_row + (uint32_t)(ch < last ? ch : last) * 16));
+        }
       }
     } else {
       bad += page != kNone && !here && lane < 32;
@@ -389,22 +384,23 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 128 ? 3 : 4) void k_a
   const auto step = [&](uint8_t *v, uint8_t *after) __attribute__((always_inline)) {
     // the tokens that are seen, in both halves
     uint64_t there = ~0ull, nan_k = 0, nan_v = 0;
-    int xk[2], xv[2];
+    int xk[2];
+    float xv[2];  // R: the exponent of the run's values
     if constexpr (R) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         xk[u] = __builtin_amdgcn_readlane(ek, 16 * u);
-        xv[u] = __builtin_amdgcn_readlane(ek, 16 * u + 32);
+        xv[u] = (float)(__builtin_amdgcn_readlane(ek, 16 * u + 32) - 127);
       }
       const uint64_t runs = __ballot(here);
       if (runs != ~0ull || k0 + kTile > t1 || (k0 < seen.shown && k0 + kTile > seen.hide))
         there = __ballot(here && is_seen(k0 + (lane & 31)));
-      if (xk[0] == 255 || xk[1] == 255 || xv[0] == 255 || xv[1] == 255) {
+      if (xk[0] == 255 || xk[1] == 255 || xv[0] == 128.f || xv[1] == 128.f) {
         const uint64_t run[2] = {0xffffull, 0xffff0000ull};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           if (xk[u] == 255) nan_k |= run[u] & there;
-          if (xv[u] == 255) nan_v |= run[u] & there;
+          if (xv[u] == 128.f) xv[u] = run[u] & there ? __builtin_nanf("") : 0.f;
         }
       }
     } else {
@@ -426,7 +422,7 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 128 ? 3 : 4) void k_a
       for (int i = 0; i < KS; ++i)
         if (4 * (i % (KS / 2)) + g > last) kr[i] = (u32x4)(0u);
     }
-    f32x4 x[2], y[2];
+    f32x4 x[2], y[R ? 1 : 2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       x[u] = (f32x4)(0.f);
@@ -449,9 +445,8 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 128 ? 3 : 4) void k_a
       if constexpr (!R) ex = *reinterpret_cast<const i32x4 *>(&se[wave][16 * u + 4 * g]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int sk = R ? xk[u] : ex[i] & 255, sv8 = R ? xv[u] : ex[i] >> 8;
-        x[u][i] = __builtin_amdgcn_ldexpf(x[u][i] * c, sk - 127);
-        y[u][i] = x[u][i] + (float)(sv8 - 127);
+        x[u][i] = __builtin_amdgcn_ldexpf(x[u][i] * c, (R ? xk[u] : ex[i] & 255) - 127);
+        if constexpr (!R) y[u][i] = x[u][i] + (float)((ex[i] >> 8) - 127);
       }
     }
     if (there != ~0ull || (nan_k | nan_v)) {
@@ -463,19 +458,29 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 128 ? 3 : 4) void k_a
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t bit = 1u << (16 * u + i);
-          if (nk & bit) x[u][i] = y[u][i] = __builtin_nanf("");
-          if (nv & bit) y[u][i] = __builtin_nanf("");
-          if (!(seen4 & bit)) x[u][i] = y[u][i] = -INFINITY;
+          if (nk & bit) x[u][i] = __builtin_nanf("");
+          if (!(seen4 & bit)) x[u][i] = -INFINITY;
+          if constexpr (!R) {
+            if ((nk | nv) & bit) y[u][i] = __builtin_nanf("");
+            if (!(seen4 & bit)) y[u][i] = -INFINITY;
+          }
         }
     }
+    const auto with_value = [&](int u, int i) __attribute__((always_inline)) {
+      return R ? x[u][i] + xv[u] : y[R ? 0 : u][i];
+    };
     float top = -INFINITY, vtop = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) {
+      float t = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        top = fmaxf(top, x[u][i]);
-        vtop = fmaxf(vtop, y[u][i]);
+        t = fmaxf(t, x[u][i]);
+        if (!R) vtop = fmaxf(vtop, with_value(u, i));
       }
+      top = fmaxf(top, t);
+      if (R) vtop = fmaxf(vtop, t + xv[u]);
+    }
     if (__any(top > m + 8.f || vtop > mv + 8.f)) {
       const float mn = fmaxf(m, column_max(top)), mvn = fmaxf(mv, column_max(vtop));
       l *= mn == -INFINITY ? 1.f : exp2_fast(m - mn);
@@ -496,8 +501,8 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 128 ? 3 : 4) void k_a
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         sum += exp2_fast(x[u][2 * i] + ref) + exp2_fast(x[u][2 * i + 1] + ref);
-        w[2 * u + i] =
-            E::pack(exp2_fast(y[u][2 * i] + vref), exp2_fast(y[u][2 * i + 1] + vref));
+        w[2 * u + i] = E::pack(exp2_fast(with_value(u, 2 * i) + vref),
+                               exp2_fast(with_value(u, 2 * i + 1) + vref));
       }
     l += sum;
     const s16x8 pf = __builtin_bit_cast(s16x8, w);
