@@ -12,9 +12,9 @@ namespace opa {
 // append: a wave a block of tokens, head, and keys or values
 // --------------------------------------------------------------------------
 constexpr int kAppendWaves = 4;
-constexpr int kHeldPieces = 8;  // pieces of 8 values that a lane keeps from one read
 
-__device__ __forceinline__ int scale_word(const u32x4 &x, uint32_t most, uint32_t top) {
+// The largest magnitude below `most` of 8 values, as their type's bits, and `top`.
+__device__ __forceinline__ uint32_t largest(const u32x4 &x, uint32_t most, uint32_t top) {
   uint32_t m = top;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -22,7 +22,7 @@ __device__ __forceinline__ int scale_word(const u32x4 &x, uint32_t most, uint32_
     if (lo < most && lo > m) m = lo;
     if (hi < most && hi > m) m = hi;
   }
-  return (int)m;
+  return m;
 }
 
 // 8 values as codes.
@@ -38,7 +38,9 @@ __device__ __forceinline__ u32x2 codes_of(const u32x4 &x, float by) {
   return c;
 }
 
-template <class E>
+// kHeld: pieces of 8 values that a lane keeps from their first read; what a block has
+// beyond is read again.
+template <class E, int kHeld>
 __global__ __launch_bounds__(kAppendWaves * OPA_WAVE) void k_append_scaled(AppendScaledArgs a) {
   const int lane = lane_id();
   if (blockIdx.x == 0) {
@@ -88,23 +90,26 @@ __global__ __launch_bounds__(kAppendWaves * OPA_WAVE) void k_append_scaled(Appen
   const int kept = from - begin;
   row += from - lo;
   const Rows &x = which ? a.vn : a.kn;
-  const uint16_t *src = x.p + (int64_t)row * x.ts + (int64_t)head * x.hs;
-  const int per = a.head_dim / 8, pieces = (past - from) * per;
-  const auto piece = [&](int i) __attribute__((always_inline)) {
-    const int t = i / per;
-    return *reinterpret_cast<const u32x4 *>(src + t * x.ts + (i - t * per) * 8);
-  };
-  u32x4 held[kHeldPieces];
+  // pieces of 8 values, a row's side by side on 2^ls lanes, rows `apart` on in each pass
+  const int per = a.head_dim / 8, ls = per > 8 ? 4 : per > 4 ? 3 : per > 2 ? 2 : 1;
+  const int n = past - from, apart = OPA_WAVE >> ls, t = lane >> ls;
+  const int col = (lane & ((1 << ls) - 1)) * 8;
+  const int rows = col < a.head_dim ? n : 0;  // this lane's: none where a row has no piece
+  const uint16_t *src = x.p + (int64_t)(row + t) * x.ts + (int64_t)head * x.hs + col;
+  u32x4 held[kHeld];
 #pragma unroll
-  for (int j = 0; j < kHeldPieces; ++j)
-    if (j * OPA_WAVE + lane < pieces) held[j] = piece(j * OPA_WAVE + lane);
+  for (int j = 0; j < kHeld; ++j) {
+    held[j] = (u32x4)(0u);
+    if (j * apart < n && t + j * apart < rows)
+      held[j] = *reinterpret_cast<const u32x4 *>(src + j * apart * x.ts);
+  }
   const int page = a.table[(int64_t)seq * a.width + (begin >> a.shift)];
   if (page < 0 || page >= a.n_pages) {
-    if (lane == 0 && which == 0 && head == 0) report(a.diag, OPATTR_F_DATA, past - from);
+    if (lane == 0 && which == 0 && head == 0) report(a.diag, OPATTR_F_DATA, n);
     return;
   }
   const int slot = begin & ((1 << a.shift) - 1);
-  uint8_t *to = (which ? a.v : a.k) + page * a.ps + slot * a.ts + (int64_t)head * a.hs;
+  uint8_t *to = (which ? a.v : a.k) + page * a.ps + (slot + t) * a.ts + (int64_t)head * a.hs + col;
   uint8_t *scale = (which ? a.v_scale : a.k_scale) + page * a.sps +
                    (slot >> a.block_shift) * a.sbs + (int64_t)head * a.shs;
   const int had = kept > 0 ? *scale : 0;
@@ -112,10 +117,9 @@ __global__ __launch_bounds__(kAppendWaves * OPA_WAVE) void k_append_scaled(Appen
   constexpr uint32_t kInf = std::is_same<E, BF16>::value ? 0x7f80u : 0x7c00u;
   uint32_t top = 0;
 #pragma unroll
-  for (int j = 0; j < kHeldPieces; ++j)
-    if (j * OPA_WAVE + lane < pieces) top = scale_word(held[j], kInf, top);
-  for (int i = kHeldPieces * OPA_WAVE + lane; i < pieces; i += OPA_WAVE)
-    top = scale_word(piece(i), kInf, top);
+  for (int j = 0; j < kHeld; ++j) top = largest(held[j], kInf, top);
+  for (int i = kHeld * apart; i < n; i += apart)
+    if (t + i < rows) top = largest(*reinterpret_cast<const u32x4 *>(src + i * x.ts), kInf, top);
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
   const float most = E::widen((uint16_t)uniform((int)top));
@@ -128,20 +132,20 @@ __global__ __launch_bounds__(kAppendWaves * OPA_WAVE) void k_append_scaled(Appen
   if (had > e) e = had;
   const float by = ldexpf(1.f, 127 - e);
   uint8_t *put = to + kept * a.ts;
-  const auto write = [&](int i, const u32x4 &v) __attribute__((always_inline)) {
-    const int t = i / per;
-    *reinterpret_cast<u32x2 *>(put + t * a.ts + (i - t * per) * 8) = codes_of<E>(v, by);
-  };
 #pragma unroll
-  for (int j = 0; j < kHeldPieces; ++j)
-    if (j * OPA_WAVE + lane < pieces) write(j * OPA_WAVE + lane, held[j]);
-  for (int i = kHeldPieces * OPA_WAVE + lane; i < pieces; i += OPA_WAVE) write(i, piece(i));
+  for (int j = 0; j < kHeld; ++j)
+    if (j * apart < n && t + j * apart < rows)
+      *reinterpret_cast<u32x2 *>(put + j * apart * a.ts) = codes_of<E>(held[j], by);
+  for (int i = kHeld * apart; i < n; i += apart)
+    if (t + i < rows)
+      *reinterpret_cast<u32x2 *>(put + i * a.ts) =
+          codes_of<E>(*reinterpret_cast<const u32x4 *>(src + i * x.ts), by);
   if (kept > 0 && e > had) {
     // below 2^-126 everything has become 0 long before
     const float down = ldexpf(1.f, had - e > -126 ? had - e : -126);
-    for (int i = lane; i < kept * per; i += OPA_WAVE) {
-      const int t = i / per;
-      u32x2 *p = reinterpret_cast<u32x2 *>(to + t * a.ts + (i - t * per) * 8);
+    for (int i = 0; i < kept; i += apart) {
+      if (t + i >= kept || col >= a.head_dim) continue;
+      u32x2 *p = reinterpret_cast<u32x2 *>(to + i * a.ts);
       u32x2 c = *p;
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
@@ -166,10 +170,18 @@ void run_append_scaled(const AppendScaledArgs &a, int dtype, hipStream_t s) {
   if (a.n_seqs == 0) return;
   const int64_t waves = append_units(a.n_new, a.n_seqs, a.block_shift) * a.n_kv * 2;
   const dim3 grid((uint32_t)(waves > 0 ? (waves + kAppendWaves - 1) / kAppendWaves : 1));
-  if (dtype == OPATTR_BF16)
-    hipLaunchKernelGGL(k_append_scaled<BF16>, grid, dim3(kAppendWaves * OPA_WAVE), 0, s, a);
+  const dim3 block(kAppendWaves * OPA_WAVE);
+  // rows that the lanes take at once: 4 of 128 values, 8 of 64
+  const int at_once = a.head_dim > 64 ? 4 : a.head_dim > 32 ? 8 : a.head_dim > 16 ? 16 : 32;
+  const bool few = 1 << a.block_shift <= 4 * at_once;
+  if (dtype == OPATTR_BF16 && few)
+    hipLaunchKernelGGL((k_append_scaled<BF16, 4>), grid, block, 0, s, a);
+  else if (dtype == OPATTR_BF16)
+    hipLaunchKernelGGL((k_append_scaled<BF16, 16>), grid, block, 0, s, a);
+  else if (few)
+    hipLaunchKernelGGL((k_append_scaled<F16, 4>), grid, block, 0, s, a);
   else
-    hipLaunchKernelGGL(k_append_scaled<F16>, grid, dim3(kAppendWaves * OPA_WAVE), 0, s, a);
+    hipLaunchKernelGGL((k_append_scaled<F16, 16>), grid, block, 0, s, a);
 }
 
 // --------------------------------------------------------------------------
