@@ -376,8 +376,36 @@ __device__ __forceinline__ int tile_splits(const PromptArgs &a, const Span &sq, 
                                            int part) {
   const int steps = tile_queries<DP, W>(a, sq, sk, part).count * a.group * (kStep(DP) / 32);
   if (W && part < a.sink_tiles)
-    return clamp_to((steps + kSinkSteps - 1) / kSinkSteps, a.splits, a.splits + a.sink_splits);
+    return clamp_to((steps + kSinkSteps - 1) / kSinkSteps, 1, a.splits + a.sink_splits);
   return clamp_to((steps + a.split_steps - 1) / a.split_steps, 1, a.splits);
+}
+
+// A split's steps of a tile: a head's tiles of queries, then the next head's.
+struct Steps {
+  int first, past;
+};
+__device__ __forceinline__ Steps split_steps(int all, int split, int splits) {
+  return {(int)((int64_t)all * split / splits), (int)((int64_t)all * (split + 1) / splits)};
+}
+
+// The queries that see a key of the 32 from key0 on, through a window.
+struct Met {
+  int first, past;
+  __device__ __forceinline__ Met(const PromptArgs &a, const Span &sq, int lead, int key0)
+      : first(clamp_to(key0 - lead, 0, sq.count)),
+        past(key0 < a.sinks ? sq.count : key0 + 31 - lead + a.window) {}
+};
+// Whether a split has one: a wave without leaves no part.
+template <int DP>
+__device__ __forceinline__ bool split_meets(const Met &m, const Span &tiles, const Steps &s) {
+  const int lo = m.first / kStep(DP) - tiles.first;
+  const int hi = (m.past + kStep(DP) - 1) / kStep(DP) - tiles.first;
+  for (int g = s.first / tiles.count; g * tiles.count < s.past; ++g) {
+    const int from = g * tiles.count + (lo > 0 ? lo : 0);
+    const int to = g * tiles.count + (hi < tiles.count ? hi : tiles.count);
+    if ((from > s.first ? from : s.first) < (to < s.past ? to : s.past)) return true;
+  }
+  return false;
 }
 
 // Where a wave of one of a tile's blocks leaves its dk and dv, as its registers hold
@@ -455,16 +483,13 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   // W: the first query that has left one of this wave's keys behind
   const int plain = key0 > a.sinks ? key0 : a.sinks;  // the wave's first key that is no sink
   const int left_from = W && plain < key0 + 32 ? plain - lead + a.window : sq.count;
-  // and the first that sees one of this wave's, and the last, and one more
-  const int first_met = W ? clamp_to(key0 - lead, 0, sq.count) : 0;
-  const int last_met = !W || key0 < a.sinks ? sq.count : key0 + 31 - lead + a.window;
+  const Met mine(a, sq, lead, key0);
   const Span met = tile_queries<DP, W>(a, sq, sk, part);
   const int t0 = met.first, per = met.count;
-  // this block's steps of the tile's: a head's queries, then the next head's
   const int splits = tile_splits<DP, W>(a, sq, sk, part), all = per * a.group;
   if (split >= splits) return;
-  const int first = (int)((int64_t)all * split / splits);
-  const int steps = (int)((int64_t)all * (split + 1) / splits);
+  const Steps part_steps = split_steps(all, split, splits);
+  const int first = part_steps.first, steps = part_steps.past;
   s16x8 kf[KS], vf[KS];
   {
     const int64_t tok = sk.first + (live ? key : 0);
@@ -508,7 +533,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   const auto step = [&](const uint16_t *q, const uint16_t *dout, const float *rows, int t)
                         __attribute__((always_inline)) {
     const int q0 = (t0 + t % per) * kStepQ;
-    if (W && (q0 >= last_met || q0 + kStepQ <= first_met || key0 >= sk.count)) return;
+    if (W && (q0 >= mine.past || q0 + kStepQ <= mine.first || key0 >= sk.count)) return;
     const int nat = fresh(nat0), tr = fresh(tr0);
 #pragma unroll
     for (int qb = 0; qb < kQB; ++qb) {
@@ -571,6 +596,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
       });
   const float fk = a.scale / up;
   if (splits > 1) {
+    if (W && !split_meets<DP>(mine, met, part_steps)) return;
     f32x4 *p = part_of<DP, W>(a, split, id / a.splits, seq, part, hk, wave);
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -609,23 +635,18 @@ __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArg
   const int hk = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv;
   const int all = uniform(wave_id()), wave = all / 2, which = all % 2;
   Span sq, sk;
-  int part, seq = 0;
-  bool found;
-  if (W && a.splits == 1) {  // the sinks' tiles alone
-    part = tile % a.sink_tiles;
-    seq = tile / a.sink_tiles;
-    found = sink_tile(a, seq, part, sk, sq);
-  } else {
-    found = find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part, &seq);
-  }
-  if (!found) return;
+  int part, seq;
+  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part, &seq)) return;
   const int splits = tile_splits<DP, W>(a, sq, sk, part);
   const int key0 = part * kHeld + wave * 32;
   if (splits == 1 || key0 >= sk.count) return;
   f32x16 sum[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) sum[d] = (f32x16)(0.f);
+  const Met mine(a, sq, sk.count - sq.count, key0);
+  const Span met = tile_queries<DP, W>(a, sq, sk, part);
   for (int k = 0; k < splits; ++k) {
+    if (W && !split_meets<DP>(mine, met, split_steps(met.count * a.group, k, splits))) continue;
     const f32x4 *p = part_of<DP, W>(a, k, tile, seq, part, hk, wave) + which * 4 * DB * OPA_WAVE;
 #pragma unroll
     for (int i = 0; i < 4 * DB; ++i) {
@@ -638,6 +659,56 @@ __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArg
   store_rows<E, DP>(rows[all], sum, 1.f,
                     o.p + (int64_t)(sk.first + key0) * o.ts + (int64_t)hk * o.hs, o.ts,
                     sk.count - key0, a.head_dim);
+}
+
+// The same of the sinks' tiles alone, which have many parts and are few: a wave takes 32
+// columns of dk or dv of 32 keys, with several parts' loads on their way.
+template <class E, int DP>
+__global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_sink_sum(PromptArgs a) {
+  constexpr int DB = DP / 32;
+  int id = blockIdx.x;
+  const int hk = id % a.n_kv;
+  id /= a.n_kv;
+  const int d = id % DB, tile = id / DB, lane = lane_id(), r = lane & 31, h = lane >> 5;
+  const int all = uniform(wave_id()), wave = all / 2, which = all % 2;
+  const int seq = tile / a.sink_tiles, part = tile % a.sink_tiles, key0 = part * kHeld + wave * 32;
+  Span sq, sk;
+  if (!sink_tile(a, seq, part, sk, sq)) return;
+  const int splits = tile_splits<DP, true>(a, sq, sk, part);
+  if (splits == 1 || key0 >= sk.count) return;
+  const Met mine(a, sq, sk.count - sq.count, key0);
+  const Span met = tile_queries<DP, true>(a, sq, sk, part);
+  f32x4 sum[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] = (f32x4)(0.f);
+  constexpr int kAhead = 4;
+  for (int k0 = 0; k0 < splits; k0 += kAhead) {
+    f32x4 v[kAhead][4];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const bool there =
+          k0 + k < splits &&
+          split_meets<DP>(mine, met, split_steps(met.count * a.group, k0 + k, splits));
+      const f32x4 *p = part_of<DP, true>(a, k0 + k, 0, seq, part, hk, wave) +
+                       (which * 4 * DB + 4 * d) * OPA_WAVE;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[k][i] = there ? p[i * OPA_WAVE] : (f32x4)(0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += v[k][i];
+  }
+  const Rows &o = which ? a.dv : a.dk;
+  uint16_t *row = o.p + (int64_t)(sk.first + key0 + r) * o.ts + (int64_t)hk * o.hs;
+  if (key0 + r >= sk.count) return;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int col = 32 * d + 8 * g + 4 * h;
+    if (col < a.head_dim)
+      *reinterpret_cast<u32x2 *>(row + col) =
+          u32x2{E::pack(sum[g][0], sum[g][1]), E::pack(sum[g][2], sum[g][3])};
+  }
 }
 
 template <class E, int DP, bool W>
@@ -656,11 +727,13 @@ static void launch(const PromptArgs &a, hipStream_t s) {
   if (a.n_k == 0) return;
   const int64_t sinks = (int64_t)a.n_seqs * a.sink_tiles;
   const int64_t parts = kt * a.splits + sinks * a.sink_splits;
-  const int64_t sums = a.splits > 1 ? kt : a.sink_splits > 0 ? sinks : 0;
   hipLaunchKernelGGL((k_attn_dkv<E, DP, W>), dim3((uint32_t)(parts * a.n_kv)), block, 0, s, a);
-  if (sums > 0)
-    hipLaunchKernelGGL((k_dkv_sum<E, DP, W>), dim3((uint32_t)(sums * a.n_kv)),
-                       dim3(2 * kGradWaves * OPA_WAVE), 0, s, a);
+  const dim3 twice(2 * kGradWaves * OPA_WAVE);
+  if (a.splits > 1)
+    hipLaunchKernelGGL((k_dkv_sum<E, DP, W>), dim3((uint32_t)(kt * a.n_kv)), twice, 0, s, a);
+  else if (W && a.sink_splits > 0)
+    hipLaunchKernelGGL((k_sink_sum<E, DP>), dim3((uint32_t)(sinks * DP / 32 * a.n_kv)), twice, 0,
+                       s, a);
 }
 
 template <class E>
