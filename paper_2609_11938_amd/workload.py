@@ -2,11 +2,12 @@
 ``attn`` and profiled with the attribution join of ``opattr``: a real trace of
 this GPU next to the synthetic ones of ``tracegen``.
 
-    python -m paper_2609_11938_amd.workload profile.json
+    python -m paper_2609_11938_amd.workload profile.json [--window N] [--sinks N] [--scaled]
 
 ``serve`` takes prompts into a paged cache, generates tokens, and between them
 forks, drops and compacts sequences as a scheduler does; ``train`` runs the
-forward pass and its gradient over packed documents. Rows of random numbers
+forward pass and its gradient over packed documents. Both take a sliding window with
+sinks, and ``serve`` a cache of 8 bits. Rows of random numbers
 stand for the projections' outputs. Every call is recorded by a ``Recorder``
 (device time by events, with the host kept ahead; bytes as the call has to move them, computed from its
 sizes and results, not counted in the memory) inside the operator range that
@@ -14,6 +15,7 @@ issued it; ``profile`` attributes the trace and builds the profile document.
 """
 from __future__ import annotations
 
+import argparse
 import contextlib
 import functools
 import math
@@ -140,15 +142,27 @@ def profile(rec: Recorder, **metadata) -> dict:
 
 class Cache:
     """A paged cache of several layers: one pool [layers, 2, pages, page_size,
-    kv_heads, head_dim], one page table, one length a sequence."""
+    kv_heads, head_dim], one page table, one length a sequence. scaled: of 8 bits, a
+    page's exponents (one for `block` tokens of a head) behind its codes, so that turns
+    take both along; `data` holds the codes and `scales` the exponents."""
 
     def __init__(self, layers, pages, page_size, kv_heads, head_dim, rows, width,
-                 dtype=torch.bfloat16, device="cuda:0"):
+                 dtype=torch.bfloat16, device="cuda:0", scaled=False, block=None):
         ints = dict(dtype=torch.int32, device=device)
         self.page_size, self.layers = page_size, layers
-        self.data = torch.zeros(layers, 2, pages, page_size, kv_heads, head_dim, dtype=dtype,
-                                device=device)
-        self.pool = self.data.flatten(0, 1)
+        shape = (layers, 2, pages, page_size, kv_heads, head_dim)
+        self.scales = None
+        if scaled:
+            each, blocks = math.prod(shape[3:]), page_size // (block or page_size)
+            room = -(-blocks * kv_heads // 16) * 16
+            pool = torch.zeros(layers, 2, pages, each + room, dtype=torch.uint8, device=device)
+            self.data = pool[..., :each].view(shape)
+            self.scales = pool[..., each:each + blocks * kv_heads].view(layers, 2, pages, blocks,
+                                                                        kv_heads)
+            self.pool = pool.flatten(0, 1)
+        else:
+            self.data = torch.zeros(shape, dtype=dtype, device=device)
+            self.pool = self.data.flatten(0, 1)
         self.table = torch.full((rows, width), -1, **ints)
         self.lens = torch.zeros(rows, **ints)
         self.ws = attn.Workspace(device)
@@ -194,9 +208,33 @@ class Cache:
     def append(self, rec, layer, k, v, cu, lens_out):
         size = 2 * k.numel() * k.element_size()
         with rec.op("cache::append"):
-            rec.launch("kv_append", size, size, attn.opattr_kv_append, k, v, cu,
-                       self.data[layer, 0], self.data[layer, 1], self.table, self.lens,
-                       lens_out=lens_out)
+            if self.scales is not None:
+                rec.launch("kv_append_scaled", size, 2 * k.numel(), attn.opattr_kv_append_scaled,
+                           k, v, cu, *self.data[layer], *self.scales[layer], self.table,
+                           self.lens, lens_out=lens_out)
+            else:
+                rec.launch("kv_append", size, size, attn.opattr_kv_append, k, v, cu,
+                           self.data[layer, 0], self.data[layer, 1], self.table, self.lens,
+                           lens_out=lens_out)
+
+    def attend(self, rec, layer, q, lens, sizes, scale, window=None, sinks=0):
+        """Attention of one token a sequence over the layer's cache, of the given
+        lengths (on the device, and as numbers): (out, lse)."""
+        seen = sum(n if window is None else min(n, window + min(sinks, max(0, n - window)))
+                   for n in sizes)
+        k, v = self.data[layer]
+        rows = q.numel() * q.element_size()
+        read = 2 * seen * k.shape[2] * k.shape[3] * k.element_size() + rows
+        kw = dict(scale=scale, ws=self.ws)
+        if self.scales is not None:
+            return rec.launch("attn_paged_scaled", read, rows, attn.opattr_attn_paged_scaled, q, k,
+                              v, *self.scales[layer], self.table, lens, window=window,
+                              sinks=sinks, **kw)
+        if window is not None:
+            return rec.launch("attn_paged_window", read, rows, attn.opattr_attn_paged_window, q, k,
+                              v, self.table, lens, window, sinks, **kw)
+        return rec.launch("attn_paged", read, rows, attn.opattr_attn_paged, q, k, v, self.table,
+                          lens, **kw)
 
 
 def _rows(n, heads, kv_heads, head_dim, gen, dtype):
@@ -212,17 +250,27 @@ def _starts(lens):
     return _ints([0, *np.cumsum(lens).tolist()])
 
 
+def _prompt(rec, read, q, k, v, cu, window, sinks, **kw):
+    written = q.numel() * q.element_size()
+    if window is None:
+        return rec.launch("attn_prompt", read, written, attn.opattr_attn_prompt, q, k, v, cu,
+                          causal=True, **kw)
+    return rec.launch("attn_prompt_window", read, written, attn.opattr_attn_prompt_window, q, k, v,
+                      cu, window, sinks, **kw)
+
+
 def serve(rec, lens=(100, 37, 64), steps=8, layers=2, heads=8, kv_heads=4, head_dim=64,
-          page_size=16, dtype=torch.bfloat16, seed=0):
+          page_size=16, dtype=torch.bfloat16, seed=0, window=None, sinks=0, scaled=False):
     """Prompts of the given lengths, `steps` tokens each, a turn in which the
-    first sequence is forked into the place of the second, and `steps` more.
-    Returns, for every sequence alive at the end, its layers' queries, keys,
+    first sequence is forked into the place of the second, and `steps` more; through a
+    window with sinks, if one is given, and from a cache of 8 bits, if scaled. Returns, for every sequence alive at the end, its layers' queries, keys,
     values and outputs, each [tokens, heads, head_dim]."""
     gen = torch.Generator(device="cuda:0")
     gen.manual_seed(seed)
     rows, most = len(lens), max(lens) + 2 * steps
     width = -(-most // page_size)
-    cache = Cache(layers, 2 * rows * width, page_size, kv_heads, head_dim, rows, width, dtype)
+    cache = Cache(layers, 2 * rows * width, page_size, kv_heads, head_dim, rows, width, dtype,
+                  scaled=scaled)
     cache.turn(rec, [-1] * rows, [n + steps for n in lens])
     history = [[[] for _ in range(layers)] for _ in range(rows)]
     sizes, cu, one = list(lens), _starts(lens), _starts([1] * rows)
@@ -232,9 +280,8 @@ def serve(rec, lens=(100, 37, 64), steps=8, layers=2, heads=8, kv_heads=4, head_
         for layer in range(layers):
             q, k, v = _rows(sum(lens), heads, kv_heads, head_dim, gen, dtype)
             with rec.op("aten::attention"):
-                out, _ = rec.launch("attn_prompt", (q.shape[0] * (heads + 2 * kv_heads)) * each,
-                                    q.shape[0] * heads * each, attn.opattr_attn_prompt, q, k, v,
-                                    cu, causal=True, scale=scale)
+                out, _ = _prompt(rec, (q.shape[0] * (heads + 2 * kv_heads)) * each, q, k, v, cu,
+                                 window, sinks, scale=scale)
             cache.append(rec, layer, k, v, cu, after)
             for b in range(rows):
                 s = slice(sum(lens[:b]), sum(lens[:b + 1]))
@@ -248,12 +295,8 @@ def serve(rec, lens=(100, 37, 64), steps=8, layers=2, heads=8, kv_heads=4, head_
                     q, k, v = _rows(rows, heads, kv_heads, head_dim, gen, dtype)
                     cache.append(rec, layer, k, v, one, after)
                     with rec.op("aten::attention"):
-                        out, _ = rec.launch(
-                            "attn_paged",
-                            (2 * (sum(sizes) + rows) * kv_heads + rows * heads) * each,
-                            rows * heads * each,
-                            attn.opattr_attn_paged, q, cache.data[layer, 0],
-                            cache.data[layer, 1], cache.table, after, scale=scale, ws=cache.ws)
+                        out, _ = cache.attend(rec, layer, q, after, [n + 1 for n in sizes], scale,
+                                              window, sinks)
                     for b in range(rows):
                         s = slice(b, b + 1)
                         history[b][layer].append((q[s], k[s], v[s], out[s]))
@@ -271,9 +314,10 @@ def serve(rec, lens=(100, 37, 64), steps=8, layers=2, heads=8, kv_heads=4, head_
 
 
 def train(rec, lens=(300, 120, 77), heads=8, kv_heads=4, head_dim=64, dtype=torch.bfloat16,
-          seed=0):
-    """One attention layer over packed documents, forward and backward. Returns
-    the output and the gradients of queries, keys and values."""
+          seed=0, window=None, sinks=0):
+    """One attention layer over packed documents, forward and backward, through a window
+    with sinks, if one is given. Returns the output and the gradients of queries, keys
+    and values."""
     gen = torch.Generator(device="cuda:0")
     gen.manual_seed(seed)
     cu, n = _starts(lens), sum(lens)
@@ -283,25 +327,32 @@ def train(rec, lens=(300, 120, 77), heads=8, kv_heads=4, head_dim=64, dtype=torc
     read = n * (heads + 2 * kv_heads) * each
     with rec.op("model::train"):
         with rec.op("aten::attention"):
-            out, lse = rec.launch("attn_prompt", read, n * heads * each, attn.opattr_attn_prompt,
-                                  q, k, v, cu)
+            out, lse = _prompt(rec, read, q, k, v, cu, window, sinks)
         with rec.op("aten::attention_backward"):
-            grads = rec.launch("attn_prompt_grad", read + 2 * n * heads * each, read,
-                               attn.opattr_attn_prompt_grad, dout, q, k, v, out, lse, cu)
+            if window is None:
+                grads = rec.launch("attn_prompt_grad", read + 2 * n * heads * each, read,
+                                   attn.opattr_attn_prompt_grad, dout, q, k, v, out, lse, cu)
+            else:
+                grads = rec.launch("attn_prompt_window_grad", read + 2 * n * heads * each, read,
+                                   attn.opattr_attn_prompt_window_grad, dout, q, k, v, out, lse,
+                                   cu, window, sinks)
     return (out, *grads)
 
 
 def main(argv):
-    if len(argv) != 2:
-        print(__doc__)
-        return 2
-    serve(Recorder())  # loads the kernels
-    train(Recorder())
-    rec = Recorder()
-    serve(rec)
-    train(rec)
+    parser = argparse.ArgumentParser(description=__doc__, prog="workload",
+                                     formatter_class=argparse.RawDescriptionHelpFormatter)
+    parser.add_argument("profile", help="the profile document that is written")
+    parser.add_argument("--window", type=int, help="tokens of a sliding window")
+    parser.add_argument("--sinks", type=int, default=0, help="first tokens that stay visible")
+    parser.add_argument("--scaled", action="store_true", help="a cache of 8 bits")
+    args = parser.parse_args(argv[1:])
+    window = dict(window=args.window, sinks=args.sinks)
+    for rec in (Recorder(), Recorder()):  # the first loads the kernels
+        serve(rec, scaled=args.scaled, **window)
+        train(rec, **window)
     doc = profile(rec)
-    profile_doc.write(argv[1], doc)
+    profile_doc.write(args.profile, doc)
     total = {}
     for entry in doc["operators"]:
         t = total.setdefault(entry["operator_name"], [0, 0, 0.0])
