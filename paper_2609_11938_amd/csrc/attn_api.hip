@@ -341,6 +341,7 @@ static int prompt_grad(const opattr_attn_shape *a, int32_t window, int32_t sinks
   p.split_steps = x.steps;
   p.sink_tiles = x.sink_tiles;
   p.sink_splits = x.sink_most;
+  p.sink_steps = x.sink_steps;
   run_prompt_grad(p, a->dtype, (hipStream_t)stream);
   return launched();
 }

@@ -368,7 +368,6 @@ __device__ __forceinline__ Span tile_queries(const PromptArgs &a, const Span &sq
   const int first = begin / kStep(DP), end = (past + kStep(DP) - 1) / kStep(DP);
   return {first, end - first};
 }
-constexpr int kSinkSteps = 32;
 // Blocks that share the tile: as many as bring each to a.split_steps steps of 32
 // queries or fewer, at most a.splits.
 template <int DP, bool W>
@@ -376,7 +375,7 @@ __device__ __forceinline__ int tile_splits(const PromptArgs &a, const Span &sq, 
                                            int part) {
   const int steps = tile_queries<DP, W>(a, sq, sk, part).count * a.group * (kStep(DP) / 32);
   if (W && part < a.sink_tiles)
-    return clamp_to((steps + kSinkSteps - 1) / kSinkSteps, 1, a.splits + a.sink_splits);
+    return clamp_to((steps + a.sink_steps - 1) / a.sink_steps, 1, a.splits + a.sink_splits);
   return clamp_to((steps + a.split_steps - 1) / a.split_steps, 1, a.splits);
 }
 
@@ -769,12 +768,12 @@ constexpr int kSplitSteps = 24, kFewSteps = 8, kFewTiles = 192;
 // more than they gain where the tiles fill the chip: they are split only to come to
 // kRound blocks. The sinks' tiles, which meet every query, have blocks of as many steps
 // as the others, kMostSinks at most besides.
-constexpr int kRound = 512, kMostSinks = 31, kSinkBlocks = 1024;
+constexpr int kRound = 512, kMostSinks = 31, kSinkBlocks = 1024, kSinkSteps = 32;
 static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group, int64_t blocks,
                                 int window, int sinks) {
-  GradSplits x{1, kSplitSteps, 0, 0};
-  const int64_t mean = n_q / n_seqs;
-  const int64_t met = mean < (int64_t)window + kHeld ? mean : (int64_t)window + kHeld;
+  GradSplits x{1, kSplitSteps, 0, 0, kSinkSteps};
+  // (of the longest sequence that there may be: a short one's tiles are split by their steps)
+  const int64_t met = n_q < (int64_t)window + kHeld ? n_q : (int64_t)window + kHeld;
   const int64_t steps = (met * group + 31) / 32;
   int64_t n = kRound / blocks;
   if (n > steps / kFewSteps) n = steps / kFewSteps;
@@ -783,7 +782,8 @@ static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group,
   if (x.steps < kSplitSteps) x.steps = x.most > 1 && x.steps > kFewSteps ? x.steps : kSplitSteps;
   if (sinks) {
     const int64_t tiles = ((sinks < n_k ? sinks : n_k) + kHeld - 1) / kHeld;
-    int64_t more = (n_q * group / 32 + kSinkSteps - 1) / kSinkSteps - x.most;
+    x.sink_steps = blocks <= kFewTiles ? kFewSteps : kSinkSteps;
+    int64_t more = (n_q * group / 32 + x.sink_steps - 1) / x.sink_steps - x.most;
     const int64_t room = kSinkBlocks / (n_seqs * tiles);
     if (more > room) more = room;
     if (more > 0) {
@@ -802,7 +802,7 @@ int64_t grad_parts(const GradSplits &x, int64_t n_k, int n_seqs) {
 
 GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv, int window,
                        int sinks) {
-  GradSplits x{1, kSplitSteps, 0, 0};
+  GradSplits x{1, kSplitSteps, 0, 0, kSinkSteps};
   if (n_seqs == 0 || n_k == 0) return x;
   const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
   if (window) return window_splits(n_q, n_k, n_seqs, n_heads / n_kv, blocks, window, sinks);

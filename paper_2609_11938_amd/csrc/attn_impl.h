@@ -27,7 +27,8 @@ struct PromptArgs {
   int splits, split_steps;
   int window, sinks;  // window 0: none
   int head_shift;     // a window's: log2 of the query heads that a block takes
-  int sink_tiles, sink_splits;  // key tiles with sinks; blocks for each beyond `splits`
+  // key tiles with sinks; blocks for each beyond `splits`, and their steps
+  int sink_tiles, sink_splits, sink_steps;
 };
 
 // Query heads of a key head that a block takes, as a power of two: of a window's keys
@@ -36,9 +37,9 @@ inline int window_heads(int group) { return group % 4 == 0 ? 2 : group % 2 == 0 
 
 // Blocks that share a key tile of the gradient at most, and the steps of 32 queries
 // that each is to have, or fewer; through a window, the key tiles of a sequence that
-// hold sinks, and as many blocks more for each.
+// hold sinks, as many blocks more for each, and the steps that each of those is to have.
 struct GradSplits {
-  int most, steps, sink_tiles, sink_most;
+  int most, steps, sink_tiles, sink_most, sink_steps;
 };
 GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv, int window,
                        int sinks);
