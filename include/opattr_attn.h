@@ -109,8 +109,8 @@ int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
    at p = i + (keys - queries), sees key j of its sequence when
      j <= p and (j > p - window or j < sinks):
    the last `window` keys up to its own, and the first `sinks`. window is 1 or more,
-   sinks 0 or more; a window as long as the sequence is the causal mask. Times go by
-   the keys that are seen. Everything else is as above: what the window hides takes no
+   sinks 0 or more; a window as long as the sequence is the causal mask. n_q and n_k are
+   below 2^29. Times go by the keys that are seen. Everything else is as above: what the window hides takes no
    part in an output, whatever its bits, and a query that sees no key has output 0. */
 int opattr_attn_prompt_window(const opattr_attn_shape *a, int32_t window, int32_t sinks,
                               const opattr_rows *q, const opattr_rows *k, const opattr_rows *v,
@@ -208,8 +208,9 @@ int opattr_kv_append_scaled(const opattr_kv_scaled *c, int64_t n_new, const int3
                             void *stream);
 
 /* opattr_attn_paged_window over a cache of 8 bits (a window of 2^30 sees every token).
-   The codes are exact in the products; scores and values are scaled in float32, and
-   weights are rounded to 16 bits with the value's scale in them. */
+   The codes are exact in the products, whose sums are q.code in float32; scores and
+   values are scaled there, and weights are rounded to 16 bits with the value's scale in
+   them. */
 size_t opattr_attn_paged_scaled_workspace_bytes(const opattr_kv_scaled *c, int32_t n_heads,
                                                 int32_t window, int32_t sinks);
 int opattr_attn_paged_scaled(const opattr_kv_scaled *c, int32_t n_heads, int32_t window,

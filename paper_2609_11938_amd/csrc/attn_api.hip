@@ -93,6 +93,14 @@ constexpr int32_t kMostWindow = (1 << 30) - 1;
 static bool ok_window(int32_t window, int32_t sinks) { return window >= 1 && sinks >= 0; }
 static int32_t at_most(int32_t x) { return std::min(x, kMostWindow); }
 
+// Of whole prompts: a token's place and a window past it stay in 32 bits. (A block of
+// several heads has as many fewer rows: one launch takes them where it takes ok_shape's.)
+constexpr int64_t kMostWindowTokens = (int64_t)1 << 29;
+static bool ok_window_shape(const opattr_attn_shape *a, int32_t window, int32_t sinks) {
+  return ok_shape(a) && a->causal && ok_window(window, sinks) && a->n_q < kMostWindowTokens &&
+         a->n_k < kMostWindowTokens;
+}
+
 static PromptArgs prompt_args(const opattr_attn_shape *a, int32_t window, int32_t sinks,
                               opattr_diag *diag) {
   PromptArgs p{};
@@ -106,7 +114,7 @@ static PromptArgs prompt_args(const opattr_attn_shape *a, int32_t window, int32_
   p.group = a->n_heads / a->n_kv_heads;
   p.head_dim = a->head_dim;
   p.causal = a->causal;
-  p.window = at_most(window);
+  p.window = (int)std::min<int64_t>(window, kMostWindowTokens);
   p.sinks = at_most(sinks);
   p.head_shift = window ? window_heads(p.group) : 0;
   p.scale = a->scale;
@@ -302,8 +310,9 @@ static int prompt(const opattr_attn_shape *a, int32_t window, int32_t sinks, con
 static size_t grad_workspace(const opattr_attn_shape *a, int32_t window, int32_t sinks) {
   if (!ok_shape(a)) return 0;
   const size_t dp = a->head_dim <= 64 ? 64 : 128;
-  const GradSplits x = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads,
-                                   at_most(window), at_most(sinks));
+  const PromptArgs p = prompt_args(a, window, sinks, nullptr);
+  const GradSplits x = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads, p.window,
+                                   p.sinks);
   return align256((size_t)a->n_q * a->n_heads * 8) + norms_bytes(a) +
          (size_t)grad_parts(x, a->n_k, a->n_seqs) * 128 * a->n_kv_heads * 2 * dp * 4;
 }
@@ -391,7 +400,7 @@ int opattr_attn_prompt_window(const opattr_attn_shape *a, int32_t window, int32_
                               const opattr_rows *q, const opattr_rows *k, const opattr_rows *v,
                               const opattr_rows *out, float *lse, opattr_diag *diag,
                               void *stream) {
-  if (!a || !a->causal || !ok_window(window, sinks)) return OPATTR_ERR_INVALID_ARG;
+  if (!ok_window_shape(a, window, sinks)) return OPATTR_ERR_INVALID_ARG;
   return prompt(a, window, sinks, q, k, v, out, lse, diag, stream);
 }
 
@@ -401,7 +410,7 @@ size_t opattr_attn_prompt_grad_workspace_bytes(const opattr_attn_shape *a) {
 
 size_t opattr_attn_prompt_window_grad_workspace_bytes(const opattr_attn_shape *a, int32_t window,
                                                       int32_t sinks) {
-  if (!a || !a->causal || !ok_window(window, sinks)) return 0;
+  if (!ok_window_shape(a, window, sinks)) return 0;
   return grad_workspace(a, window, sinks);
 }
 
@@ -420,7 +429,7 @@ int opattr_attn_prompt_window_grad(const opattr_attn_shape *a, int32_t window, i
                                    const opattr_rows *dq, const opattr_rows *dk,
                                    const opattr_rows *dv, opattr_diag *diag, void *ws,
                                    size_t ws_bytes, void *stream) {
-  if (!a || !a->causal || !ok_window(window, sinks)) return OPATTR_ERR_INVALID_ARG;
+  if (!ok_window_shape(a, window, sinks)) return OPATTR_ERR_INVALID_ARG;
   return prompt_grad(a, window, sinks, dout, q, k, v, out, lse, dq, dk, dv, diag, ws, ws_bytes,
                      stream);
 }

@@ -769,8 +769,10 @@ constexpr int kSplitSteps = 24, kFewSteps = 8, kFewTiles = 192;
 // kRound blocks. The sinks' tiles, which meet every query, have blocks of as many steps
 // as the others, kMostSinks at most besides.
 constexpr int kRound = 512, kMostSinks = 31, kSinkBlocks = 1024, kSinkSteps = 32;
-static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group, int64_t blocks,
+constexpr int64_t kManyBlocks = 1 << 16;  // past these a few blocks more say nothing
+static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group, int n_kv,
                                 int window, int sinks) {
+  const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
   GradSplits x{1, kSplitSteps, 0, 0, kSinkSteps};
   // (of the longest sequence that there may be: a short one's tiles are split by their steps)
   const int64_t met = n_q < (int64_t)window + kHeld ? n_q : (int64_t)window + kHeld;
@@ -780,7 +782,7 @@ static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group,
   x.most = n < 1 ? 1 : n > 16 ? 16 : (int)n;
   x.steps = (int)((steps + x.most - 1) / x.most);
   if (x.steps < kSplitSteps) x.steps = x.most > 1 && x.steps > kFewSteps ? x.steps : kSplitSteps;
-  if (sinks) {
+  if (sinks && blocks < kManyBlocks) {
     const int64_t tiles = ((sinks < n_k ? sinks : n_k) + kHeld - 1) / kHeld;
     x.sink_steps = blocks <= kFewTiles ? kFewSteps : kSinkSteps;
     int64_t more = (n_q * group / 32 + x.sink_steps - 1) / x.sink_steps - x.most;
@@ -805,7 +807,7 @@ GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_
   GradSplits x{1, kSplitSteps, 0, 0, kSinkSteps};
   if (n_seqs == 0 || n_k == 0) return x;
   const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
-  if (window) return window_splits(n_q, n_k, n_seqs, n_heads / n_kv, blocks, window, sinks);
+  if (window) return window_splits(n_q, n_k, n_seqs, n_heads / n_kv, n_kv, window, sinks);
   const int64_t steps = n_q * (n_heads / n_kv) / 32 / n_seqs;
   if (blocks <= kFewTiles && steps >= kSplitSteps) x.steps = kFewSteps;
   int64_t n = (2048 + blocks - 1) / blocks;

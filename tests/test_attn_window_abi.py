@@ -80,6 +80,19 @@ def test_window_outputs_that_overlap_themselves_are_refused(lib, bad):  # noqa: 
                                         None) == INVALID
 
 
+def test_window_calls_past_their_places_or_one_launch_are_refused(lib):  # noqa: F811
+    """Places and windows past them stay in 32 bits; a launch takes fewer than 2^32
+    threads."""
+    r = _rows()
+    for a in (_shape(n_q=1 << 29), _shape(n_k=1 << 29),
+              _shape(n_heads=64, n_kv_heads=64, n_seqs=1 << 19)):
+        assert _prompt(lib, a, (5, 1), [r] * 4) == INVALID
+        assert lib.opattr_attn_prompt_window_grad_workspace_bytes(a, 5, 1) == 0
+        assert _grad(lib, a, (5, 1), [r] * 8) == INVALID
+    assert lib.opattr_attn_prompt_window_grad_workspace_bytes(
+        _shape(n_q=(1 << 29) - 1, n_k=(1 << 29) - 1, n_heads=2), 2 ** 31 - 1, 2 ** 31 - 1) > 0
+
+
 def test_window_workspaces(lib):  # noqa: F811
     r, a = _rows(), _shape(n_q=5000, n_k=5000)
     for w in ((5, 0), (5, 1), (2 ** 31 - 1, 2 ** 31 - 1)):

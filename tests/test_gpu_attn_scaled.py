@@ -299,20 +299,53 @@ def test_scaled_many_sequences(n):
 
 @pytest.mark.parametrize("window,sinks", [(1, 0), (31, 1), (32, 0), (100, 4), (252, 4), (600, 300),
                                           (5, 1000)])
-@pytest.mark.parametrize("dtype,d", [("bfloat16", 64), ("float16", 128)])
-def test_scaled_window(window, sinks, dtype, d):
-    _case([5000, 3, 0, 700, 256, 257], 4, 1, d, 16, 8, dtype, window=window, sinks=sinks)
+@pytest.mark.parametrize("dtype,d,page,block", [("bfloat16", 64, 16, 8), ("float16", 128, 16, 8),
+                                                ("bfloat16", 128, 16, 16),
+                                                ("float16", 64, 64, 32)])
+def test_scaled_window(window, sinks, dtype, d, page, block):
+    _case([5000, 3, 0, 700, 256, 257], 4, 1, d, page, block, dtype, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("sinks", [0, 1, 15, 16, 17, 31, 33, 128, 130])
+@pytest.mark.parametrize("window", [1, 15, 16, 17, 100, 113])
+def test_scaled_window_edges(window, sinks):
+    """Sinks and windows that end and begin on, before and after a run of 16 tokens and a
+    tile of 32, for lengths on both sides of them."""
+    lens = [window + sinks + n for n in (-1, 0, 1, 14, 15, 16, 17, 31, 33, 300)]
+    _case(lens, 2, 1, 64, 32, 16, "bfloat16", window=window, sinks=sinks)
+
+
+def test_scaled_window_leaves_pages_behind():
+    """Entries of pages of which no token is seen say nothing, their codes neither."""
+    torch = _torch()
+    rng = np.random.default_rng(21)
+    lens, page, window, sinks = [500, 90, 1300], 16, 75, 20
+    codes, scales, table, _ = _filled(rng, lens, 2, 64, page, 16, "bfloat16")
+    q, _ = _rand(rng, (3, 4, 64), "bfloat16", 0.2)
+    want, wl = _check(codes, scales, table, lens, q, window, sinks)
+    for b, n in enumerate(lens):
+        for x in range(-(-n // page)):
+            if x * page >= sinks and (x + 1) * page <= n - window:
+                codes[:, table[b, x]] = 0x7f
+                scales[:, table[b, x]] = 255
+                table[b, x] = (-1, 1 << 30, table[b, x])[x % 3]
+    diag = attn.new_diag(DEV)
+    out, lse = attn.opattr_attn_paged_scaled(q, *codes, *scales, _ints(table), _ints(lens),
+                                             window=window, sinks=sinks, diag=diag)
+    assert torch.equal(out, want) and torch.equal(lse, wl)
+    assert opattr.read_diag(diag)["status"] == 0
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 @pytest.mark.parametrize("spread", [0.0, 5.0])
-def test_scaled_blocks_of_other_sizes(dtype, spread):
+@pytest.mark.parametrize("block", [4, 16])
+def test_scaled_blocks_of_other_sizes(dtype, spread, block):
     """Blocks whose scales differ by many powers of two, in one tile and over shares:
     the weights keep their bits where the scale is small and where it is large."""
     torch = _torch()
     rng = np.random.default_rng(11)
     lens, g, d = [900, 70], 2, 64
-    codes, scales, table, _ = _filled(rng, lens, g, d, 16, 4, dtype, spread=0.5)
+    codes, scales, table, _ = _filled(rng, lens, g, d, 16, block, dtype, spread=0.5)
     # a token's key and value scales, one against the other; large values with little weight
     shift = torch.from_numpy(np.round(spread * 4 * rng.normal(size=scales[1].shape)).clip(-40, 40)
                              ).to(DEV)
@@ -325,26 +358,28 @@ def test_scaled_blocks_of_other_sizes(dtype, spread):
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
-def test_scaled_largest_and_smallest_scales(dtype):
+@pytest.mark.parametrize("block", [8, 16])
+def test_scaled_largest_and_smallest_scales(dtype, block):
     """Values near the type's largest, and down to the smallest exponent."""
     torch = _torch()
     rng = np.random.default_rng(12)
     lens, g, d = [300, 40], 1, 64
     for e in (127 + (118 if dtype == "bfloat16" else 6), 20, 1, 0):
-        codes, scales, table, _ = _filled(rng, lens, g, d, 16, 16, dtype, spread=0.0)
+        codes, scales, table, _ = _filled(rng, lens, g, d, 16, block, dtype, spread=0.0)
         codes.bitwise_and_(0xf7)  # no NaN, at most 240
         scales[1].fill_(e)
         q, _ = _rand(rng, (2, 2, d), dtype)
         _check(codes, scales, table, lens, q)
 
 
-def test_scaled_nan_codes_and_scales():
+@pytest.mark.parametrize("block", [8, 16])
+def test_scaled_nan_codes_and_scales(block):
     """A NaN code or scale of a key makes its sequence's heads NaN, of a value the
     outputs that it meets; of a token that is not seen, nothing."""
     torch = _torch()
     rng = np.random.default_rng(13)
     lens, g, d, page = [100, 60], 2, 64, 16
-    codes, scales, table, _ = _filled(rng, lens, g, d, page, 8, "bfloat16")
+    codes, scales, table, _ = _filled(rng, lens, g, d, page, block, "bfloat16")
     q, _ = _rand(rng, (2, 4, d), "bfloat16")
     args = (_ints(table), _ints(lens))
     want, wl = attn.opattr_attn_paged_scaled(q, *codes, *scales, *args)
@@ -381,16 +416,17 @@ def test_scaled_nan_codes_and_scales():
         assert torch.isnan(out[0, :2]).all()
         assert torch.isnan(lse[:2, 0]).all() if i == 0 else torch.equal(lse, wl)
         others(out, lse, (0, 1))
-        out, lse = got(window=60, sinks=32)
+        out, lse = got(window=52, sinks=32)
         assert torch.isfinite(out).all()
         scales[i, x, 0, 0] = was
 
 
-def test_scaled_bad_table_and_lens():
+@pytest.mark.parametrize("block", [8, 16])
+def test_scaled_bad_table_and_lens(block):
     torch = _torch()
     rng = np.random.default_rng(5)
     lens, page = [50, 40], 16
-    codes, scales, table, _ = _filled(rng, lens, 2, 64, page, 8, "bfloat16")
+    codes, scales, table, _ = _filled(rng, lens, 2, 64, page, block, "bfloat16")
     q, _ = _rand(rng, (2, 4, 64), "bfloat16")
     for where, value in (((0, 1), 10_000), ((1, 0), -3)):
         bad = table.copy()
@@ -408,6 +444,20 @@ def test_scaled_bad_table_and_lens():
         o, s = W.head_scaled(_host(q)[b, 0], *k, *v, 0.125, seen, "bfloat16")
         _within(out[b, 0], o, "out")
         _within(lse[0, b], s, "lse")
+    for window, sinks in ((20, 4), (20, 18), (24, 4), (2, 50)):
+        bad = table.copy()  # tokens 16 to 31 of the first
+        bad[0, 1] = -1
+        diag = attn.new_diag(DEV)
+        out, lse = attn.opattr_attn_paged_scaled(q, *codes, *scales, _ints(bad), _ints(lens),
+                                                 window=window, sinks=sinks, diag=diag)
+        torch.cuda.synchronize()
+        seen = W.visible(1, lens[0], window, sinks)[0]
+        assert opattr.read_diag(diag)["bad_records"] == seen[16:32].sum() > 0
+        seen[16:32] = False
+        k, v = _tokens(codes, scales, table, 0, lens[0], 0)
+        o, s = W.head_scaled(_host(q)[0, 0], *k, *v, 0.125, seen, "bfloat16")
+        _within(out[0, 0], o, "out")
+        _within(lse[0, 0], s, "lse")
     codes.fill_(0x38)
     scales.fill_(127)
     full = _ints(rng.permutation(codes.shape[1])[:8].reshape(2, 4))
@@ -514,6 +564,24 @@ def test_scaled_other_stream():
     out, lse = attn.opattr_attn_paged_scaled(*args, window=300, sinks=2, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(out, want) and torch.equal(lse, wl)
+
+
+def test_append_other_stream():
+    torch = _torch()
+    rng = np.random.default_rng(20)
+    table, pages = _table(rng, [300, 41], 16)
+    rows = _rows(rng, 341, 2, 64, "bfloat16")
+    args = (_ints([0, 300, 341]), _ints(table), _ints([0, 0]))
+    done = []
+    side = torch.cuda.Stream()
+    for stream in (None, side):
+        codes, scales, _ = _empty(pages, 16, 16, 2, 64)
+        torch.cuda.synchronize()
+        after = attn.opattr_kv_append_scaled(*rows, args[0], *codes, *scales, *args[1:],
+                                             stream=stream)
+        torch.cuda.synchronize()
+        done.append((codes, scales, after))
+    assert all(torch.equal(x, y) for x, y in zip(*done))
 
 
 def test_scaled_cache_forks_and_compacts():

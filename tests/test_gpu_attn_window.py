@@ -199,26 +199,33 @@ def test_window_rows_beside_sequences():
     """Neither read nor written."""
     torch = _torch()
     s = _case([140], [140], 2, 1, 64, 30, 3, "float16")
-    out, lse, _ = _check(s, grad=False)
-    grads = attn.opattr_attn_prompt_window_grad(s["do"], s["q"], s["k"], s["v"], out, lse,
-                                                s["cu_q"], 30, 3, scale=s["scale"])
+    out, lse, want = _check(s, grad=False)
+    dq, _, _ = attn.opattr_attn_prompt_window_grad(s["do"], s["q"], s["k"], s["v"], out, lse,
+                                                   s["cu_q"], 30, 3, scale=s["scale"])
 
-    def wide(t):
-        w = torch.full((300,) + t.shape[1:], float("nan"), dtype=t.dtype, device=DEV)
+    def wide(t, beside):
+        w = torch.full((300,) + t.shape[1:], beside, dtype=t.dtype, device=DEV)
         w[100:240] = t
         return w
 
-    args = [wide(s[n]) for n in "qkv"]
-    cu = _ints([100, 240])
-    o2, l2 = torch.full_like(args[0], 7.0), torch.full((2, 300), 7.0, device=DEV)
-    attn.opattr_attn_prompt_window(*args, cu, 30, 3, scale=s["scale"], out=o2, lse=l2)
-    assert torch.equal(o2[100:240], out) and torch.equal(l2[:, 100:240], lse)
-    assert (o2[:100] == 7).all() and (o2[240:] == 7).all() and (l2[:, :100] == 7).all()
-    new = [torch.full_like(t, 7.0) for t in args]
-    attn.opattr_attn_prompt_window_grad(wide(s["do"]), *args, o2, l2, cu, 30, 3, scale=s["scale"],
-                                        dq=new[0], dk=new[1], dv=new[2])
-    for t, u in zip(new, grads):
-        assert torch.equal(t[100:240], u) and (t[:100] == 7).all() and (t[240:] == 7).all()
+    cu, first = _ints([100, 240]), None
+    for beside in (float("nan"), 3.0):
+        args = [wide(s[n], beside) for n in "qkv"]
+        o2, l2 = torch.full_like(args[0], 7.0), torch.full((2, 300), 7.0, device=DEV)
+        attn.opattr_attn_prompt_window(*args, cu, 30, 3, scale=s["scale"], out=o2, lse=l2)
+        assert torch.equal(o2[100:240], out) and torch.equal(l2[:, 100:240], lse)
+        assert (o2[:100] == 7).all() and (o2[240:] == 7).all() and (l2[:, :100] == 7).all()
+        new = [torch.full_like(t, 7.0) for t in args]
+        attn.opattr_attn_prompt_window_grad(wide(s["do"], beside), *args, o2, l2, cu, 30, 3,
+                                            scale=s["scale"], dq=new[0], dk=new[1], dv=new[2])
+        # a query's sum has one order; a sink's is split by the rows that the buffers have,
+        # 140 or 300, so its bits are those of buffers as large, its value the formula's
+        assert torch.equal(new[0][100:240], dq)
+        for name, t in zip(("dq", "dk", "dv"), new):
+            assert (t[:100] == 7).all() and (t[240:] == 7).all()
+            _within(t[100:240], want[name], name)
+        assert first is None or all(torch.equal(t, u) for t, u in zip(new, first))
+        first = new
 
 
 def test_window_grad_against_differences():
@@ -322,6 +329,22 @@ def test_window_other_stream():
     torch.cuda.synchronize()
     assert torch.equal(out, want) and torch.equal(lse, wl)
     assert all(torch.equal(t, u) for t, u in zip(got, grads))
+
+
+def test_paged_window_other_stream():
+    torch = _torch()
+    rng = np.random.default_rng(3)
+    lens = [900, 70]
+    cache, table, _ = _cache(rng, lens, 2, 64, 16, "bfloat16")
+    q, _ = _rand(rng, (2, 4, 64), "bfloat16")
+    args = (q, cache[0], cache[1], _ints(table), _ints(lens), 400, 5)
+    want, wl = attn.opattr_attn_paged_window(*args)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out, lse = attn.opattr_attn_paged_window(*args, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, wl)
 
 
 def test_window_binding_refuses():
