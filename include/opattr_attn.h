@@ -110,8 +110,9 @@ int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
      j <= p and (j > p - window or j < sinks):
    the last `window` keys up to its own, and the first `sinks`. window is 1 or more,
    sinks 0 or more; a window as long as the sequence is the causal mask. n_q and n_k are
-   below 2^29. Times go by the keys that are seen. Everything else is as above: what the window hides takes no
-   part in an output, whatever its bits, and a query that sees no key has output 0. */
+   below 2^29. Times go by the keys that are seen. Everything else is as above: what the
+   window hides takes no part in an output, whatever its bits, and a query that sees no
+   key has output 0. */
 int opattr_attn_prompt_window(const opattr_attn_shape *a, int32_t window, int32_t sinks,
                               const opattr_rows *q, const opattr_rows *k, const opattr_rows *v,
                               const opattr_rows *out, float *lse, opattr_diag *diag, void *stream);

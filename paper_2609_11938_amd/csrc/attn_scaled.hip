@@ -11,6 +11,16 @@ namespace opa {
 // --------------------------------------------------------------------------
 // append: a wave a block of tokens, head, and keys or values
 // --------------------------------------------------------------------------
+// e = the least exponent with max |x| <= 448 2^e: with max |x| = f 2^x, f in [1/2, 1),
+// x - 9 if f <= 7/8 (448 = 7/8 2^9), else x - 8. The maximum is of the values' own bits,
+// whose order is that of the magnitudes. One wave sees a whole block, so its scale needs
+// no second launch, no atomic and no memory; a block's rows are read once, kept in
+// registers until the scale is known, and written.
+//
+// Bound by the bytes: 55000 tokens of 8 heads of 128 in bfloat16, blocks of 16, 341 MB
+// read and written: 69 us, 4.9 TB/s, as a large copy has; in float16 79 us, of blocks of
+// 64 tokens 72 us. A wave finds its sequence, its page and its old scale before its
+// rows' maximum: one token for each of 96 sequences 5 us, for 4 of them 3 us.
 constexpr int kAppendWaves = 4;
 
 // The largest magnitude below `most` of 8 values, as their type's bits, and `top`.
@@ -39,7 +49,9 @@ __device__ __forceinline__ u32x2 codes_of(const u32x4 &x, float by) {
 }
 
 // kHeld: pieces of 8 values that a lane keeps from their first read; what a block has
-// beyond is read again.
+// beyond is read again. 4 where a block has no more, 16 else: with 16 for blocks of 16
+// tokens of 128 the 55000 take 92 us and not 69 (86 and not 79 in float16), as fewer
+// waves fit; with 4 for blocks of 32 they take 79 us and not 70, of 64 92 us and not 72.
 template <class E, int kHeld>
 __global__ __launch_bounds__(kAppendWaves * OPA_WAVE) void k_append_scaled(AppendScaledArgs a) {
   const int lane = lane_id();
@@ -191,6 +203,13 @@ void run_append_scaled(const AppendScaledArgs &a, int dtype, hipStream_t s) {
 // m' the largest x_j + e_j so far; those of the sum are 2^(x_j - m) as elsewhere. So
 // no scale, however large or small, takes a weight past the 16 bits of its product:
 // out = 2^(m' - m) sum_j 2^(x_j + e_j - m') c_j / sum_j 2^(x_j - m).
+//
+// Bound by the cache's bytes, half of those of 16 bits: 2 sequences of 131000 tokens, 32
+// heads on 8 of 128: 108 us, 537 MB at 5.0 TB/s, and 6 us to join the shares; 96 of up to
+// 9001, 275 MB: 65 us, 4.2 TB/s, and 5 us. At half the bytes a tile's conversions, softmax
+// and products are no longer hidden by themselves, so the work is what the loop looks
+// after: codes become 16-bit values only as operands, an exponent is added and not
+// multiplied, a run's addresses and exponents are scalars.
 
 // The two codes of half h of a word as 16-bit values (exact).
 template <class E>
@@ -252,7 +271,15 @@ __device__ __forceinline__ int code_swz(int row) {
 //
 // R: pages and blocks of 16 tokens or more. A run of 16 then has one page and one scale:
 // its addresses are scalars and a lane's own offsets, its exponents scalars. Otherwise
-// each token has its own (ts of any size too).
+// each token has its own (ts of any size too). 2 sequences of 131000 tokens: 108 us by
+// runs, 111 us otherwise; 96 of up to 9001: 65 and 68 us; 4 of 150, heads of 64: 5.5 and
+// 7.0 us.
+//
+// Three waves a SIMD for heads of 128: the registers of four hold a tile's loads no more
+// (2 of 131000: 115 us and not 108; 96 of up to 9001: 68 and not 64).
+//
+// Blocks go round the 8 chiplets: a share's key heads lie 8 blocks apart, on one chiplet,
+// so that a token's heads, side by side in memory, are read through one cache.
 template <class E, int DP, bool R>
 __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 64 ? 4 : 3) void k_attn_scaled(ScaledArgs a) {
   constexpr int KS = DP / 32, DB = DP / 16, C = DP / 16, N = kTile * C / OPA_WAVE;
@@ -325,8 +352,8 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 64 ? 4 : 3) void k_at
         ek = (fresh(lane) < 32 ? a.k_scale : a.v_scale)[es];
       }
       // A lane's part of the addresses, rows 8 i of a run besides where a load has 8:
-      // again each time (held over the loop, or kept as addresses, they take more
-      // registers than four waves a SIMD have).
+      // again each time (held over the loop, or kept as addresses, they take registers
+      // from the waves that a SIMD has).
       const uint32_t id = fresh(lane), ts = (uint32_t)a.ts;
       const uint32_t k_row = (id & 15) * ts, v_row = id / C * ts;
 #pragma unroll
