@@ -409,22 +409,16 @@ __device__ __forceinline__ bool split_meets(const Met &m, const Span &tiles, con
 
 // Where a wave of one of a tile's blocks leaves its dk and dv, as its registers hold
 // them: [parts][n_kv][waves][dk, dv][DP / 8][64 lanes] of four values, the parts
-// [splits][tiles], none where splits is 1 and the tile has no sinks, and then
-// [sink_splits][sequences][sink_tiles]. Where the tiles are not split, a sink's tile
-// has the first of its parts in the place of the first sequence's.
+// [splits][tiles], none where splits is 1, and then those of the sinks' tiles,
+// [splits + sink_splits][sequences][sink_tiles].
 template <int DP, bool W>
 __device__ __forceinline__ f32x4 *part_of(const PromptArgs &a, int split, int tile, int seq,
                                           int part, int hk, int wave) {
   const int64_t tiles = a.n_k / kHeld + a.n_seqs;
   int64_t at = split * tiles + tile;
-  if constexpr (W) {
-    const int64_t sinks = (int64_t)a.n_seqs * a.sink_tiles;
-    const int64_t mine = (int64_t)seq * a.sink_tiles + part;
-    if (a.splits == 1)
-      at = split * sinks + mine;
-    else if (split >= a.splits)
-      at = a.splits * tiles + (split - a.splits) * sinks + mine;
-  }
+  if (W && part < a.sink_tiles)
+    at = (a.splits > 1 ? a.splits * tiles : 0) +
+         ((int64_t)split * a.n_seqs + seq) * a.sink_tiles + part;
   at = (at * a.n_kv + hk) * kGradWaves + wave;
   return reinterpret_cast<f32x4 *>(a.part) + at * (2 * DP / 8 * OPA_WAVE) + lane_id();
 }
@@ -625,47 +619,12 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
                     sk.count - key0, a.head_dim);
 }
 
-// A key tile's dk and dv from those of its blocks, added in order; a tile of one
-// block is done already. A wave takes dk or dv of 32 keys.
-template <class E, int DP, bool W>
-__global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArgs a) {
-  constexpr int DB = DP / 32;
-  __shared__ __align__(16) uint16_t rows[2 * kGradWaves][32 * DP];
-  const int hk = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv;
-  const int all = uniform(wave_id()), wave = all / 2, which = all % 2;
-  Span sq, sk;
-  int part, seq;
-  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part, &seq)) return;
-  const int splits = tile_splits<DP, W>(a, sq, sk, part);
-  const int key0 = part * kHeld + wave * 32;
-  if (splits == 1 || key0 >= sk.count) return;
-  f32x16 sum[DB];
-#pragma unroll
-  for (int d = 0; d < DB; ++d) sum[d] = (f32x16)(0.f);
-  const Met mine(a, sq, sk.count - sq.count, key0);
-  const Span met = tile_queries<DP, W>(a, sq, sk, part);
-  for (int k = 0; k < splits; ++k) {
-    if (W && !split_meets<DP>(mine, met, split_steps(met.count * a.group, k, splits))) continue;
-    const f32x4 *p = part_of<DP, W>(a, k, tile, seq, part, hk, wave) + which * 4 * DB * OPA_WAVE;
-#pragma unroll
-    for (int i = 0; i < 4 * DB; ++i) {
-      const f32x4 v = p[i * OPA_WAVE];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[i / 4][i % 4 * 4 + e] += v[e];
-    }
-  }
-  const Rows &o = which ? a.dv : a.dk;
-  store_rows<E, DP>(rows[all], sum, 1.f,
-                    o.p + (int64_t)(sk.first + key0) * o.ts + (int64_t)hk * o.hs, o.ts,
-                    sk.count - key0, a.head_dim);
-}
-
-// The same of the sinks' tiles alone, which have many parts and are few: a wave takes 32
-// columns of dk or dv of 32 keys, with several parts' loads on their way.
+// dk and dv of a sinks' tile, of which there are few and of many parts: a wave takes 32
+// columns of dk or dv of 32 keys, with several parts' loads on their way (12 documents,
+// window 512, 4 sinks, parts of 16 heads on 4 of 128: 13 us, 25 by the tiles' way).
 template <class E, int DP>
-__global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_sink_sum(PromptArgs a) {
+__device__ __forceinline__ void sink_sum(const PromptArgs &a, int id) {
   constexpr int DB = DP / 32;
-  int id = blockIdx.x;
   const int hk = id % a.n_kv;
   id /= a.n_kv;
   const int d = id % DB, tile = id / DB, lane = lane_id(), r = lane & 31, h = lane >> 5;
@@ -710,6 +669,52 @@ __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_sink_sum(PromptAr
   }
 }
 
+// A key tile's dk and dv from those of its blocks, added in order; a tile of one
+// block is done already. A wave takes dk or dv of 32 keys. The sinks' tiles' blocks
+// are the first.
+template <class E, int DP, bool W>
+__global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArgs a) {
+  constexpr int DB = DP / 32;
+  __shared__ __align__(16) uint16_t rows[2 * kGradWaves][32 * DP];
+  int id = blockIdx.x;
+  if constexpr (W) {
+    const int first = a.n_seqs * a.sink_tiles * DB * a.n_kv;
+    if (id < first) {
+      sink_sum<E, DP>(a, id);
+      return;
+    }
+    id -= first;
+  }
+  const int hk = id % a.n_kv, tile = id / a.n_kv;
+  const int all = uniform(wave_id()), wave = all / 2, which = all % 2;
+  Span sq, sk;
+  int part, seq;
+  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part, &seq)) return;
+  if (W && part < a.sink_tiles) return;
+  const int splits = tile_splits<DP, W>(a, sq, sk, part);
+  const int key0 = part * kHeld + wave * 32;
+  if (splits == 1 || key0 >= sk.count) return;
+  f32x16 sum[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) sum[d] = (f32x16)(0.f);
+  const Met mine(a, sq, sk.count - sq.count, key0);
+  const Span met = tile_queries<DP, W>(a, sq, sk, part);
+  for (int k = 0; k < splits; ++k) {
+    if (W && !split_meets<DP>(mine, met, split_steps(met.count * a.group, k, splits))) continue;
+    const f32x4 *p = part_of<DP, W>(a, k, tile, seq, part, hk, wave) + which * 4 * DB * OPA_WAVE;
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) {
+      const f32x4 v = p[i * OPA_WAVE];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[i / 4][i % 4 * 4 + e] += v[e];
+    }
+  }
+  const Rows &o = which ? a.dv : a.dk;
+  store_rows<E, DP>(rows[all], sum, 1.f,
+                    o.p + (int64_t)(sk.first + key0) * o.ts + (int64_t)hk * o.hs, o.ts,
+                    sk.count - key0, a.head_dim);
+}
+
 template <class E, int DP, bool W>
 static void launch(const PromptArgs &a, hipStream_t s) {
   const int hs = W ? a.head_shift : 0;
@@ -728,11 +733,9 @@ static void launch(const PromptArgs &a, hipStream_t s) {
   const int64_t parts = kt * a.splits + sinks * a.sink_splits;
   hipLaunchKernelGGL((k_attn_dkv<E, DP, W>), dim3((uint32_t)(parts * a.n_kv)), block, 0, s, a);
   const dim3 twice(2 * kGradWaves * OPA_WAVE);
-  if (a.splits > 1)
-    hipLaunchKernelGGL((k_dkv_sum<E, DP, W>), dim3((uint32_t)(kt * a.n_kv)), twice, 0, s, a);
-  else if (W && a.sink_splits > 0)
-    hipLaunchKernelGGL((k_sink_sum<E, DP>), dim3((uint32_t)(sinks * DP / 32 * a.n_kv)), twice, 0,
-                       s, a);
+  const int64_t sums = ((a.splits > 1 ? kt : 0) + sinks * (DP / 32)) * a.n_kv;
+  if (sums > 0)
+    hipLaunchKernelGGL((k_dkv_sum<E, DP, W>), dim3((uint32_t)sums), twice, 0, s, a);
 }
 
 template <class E>
@@ -764,24 +767,45 @@ static void grad(const PromptArgs &a, hipStream_t s) {
 // us, with 30 sequences of one token beside it 797.
 constexpr int kSplitSteps = 24, kFewSteps = 8, kFewTiles = 192;
 
-// Through a window a key tile meets as many queries as any other, and partial sums cost
-// more than they gain where the tiles fill the chip: they are split only to come to
-// kRound blocks. The sinks' tiles, which meet every query, have blocks of as many steps
-// as the others, kMostSinks at most besides.
+static int most_splits(int64_t n) { return n < 1 ? 1 : n > 16 ? 16 : (int)n; }
+static GradSplits causal_splits(int64_t n_q, int64_t n_k, int n_seqs, int group, int n_kv) {
+  const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
+  GradSplits x{1, kSplitSteps, 0, 0, 0};
+  const int64_t steps = n_q * group / 32 / n_seqs;
+  if (blocks <= kFewTiles && steps >= kSplitSteps) x.steps = kFewSteps;
+  const int64_t n = (2048 + blocks - 1) / blocks;
+  x.most = most_splits(n < steps / x.steps ? n : steps / x.steps);
+  return x;
+}
+
+// Through a window shorter than the sequences a key tile meets as many queries as any
+// other, and partial sums cost more than they gain where the tiles fill the chip: they
+// are split only to come to kRound blocks, by the longest sequence that there may be (a
+// short one's tiles are split by their steps). A window as long as the mean sequence
+// leaves the first tiles the most, as the causal mask does. 12 documents of up to 4001,
+// 16 heads on 4 of 128, 608 blocks: through 1024 tokens dk and dv 278 us unsplit, 302 by
+// the causal rule, sums included; through 2048 449 and 370, through 4096 706 and 408; one
+// of 16000: through 4096 986 and 1018, through all 3315 and 2070.
+//
+// The sinks' tiles meet every query: they have blocks of sink_steps steps besides,
+// kMostSinks each and kSinkBlocks in all at most, which begin first. 12 documents, window
+// 512, 4 sinks, with the sums: 254 us with 64 steps, 233 with 32; one of 4000, whose tiles
+// are few, 100 us without the sums with 32 and 75 with 8.
 constexpr int kRound = 512, kMostSinks = 31, kSinkBlocks = 1024, kSinkSteps = 32;
 constexpr int64_t kManyBlocks = 1 << 16;  // past these a few blocks more say nothing
 static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group, int n_kv,
                                 int window, int sinks) {
   const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
-  GradSplits x{1, kSplitSteps, 0, 0, kSinkSteps};
-  // (of the longest sequence that there may be: a short one's tiles are split by their steps)
+  GradSplits x{1, kSplitSteps, 0, 0, 0};
   const int64_t met = n_q < (int64_t)window + kHeld ? n_q : (int64_t)window + kHeld;
   const int64_t steps = (met * group + 31) / 32;
-  int64_t n = kRound / blocks;
-  if (n > steps / kFewSteps) n = steps / kFewSteps;
-  x.most = n < 1 ? 1 : n > 16 ? 16 : (int)n;
-  x.steps = (int)((steps + x.most - 1) / x.most);
-  if (x.steps < kSplitSteps) x.steps = x.most > 1 && x.steps > kFewSteps ? x.steps : kSplitSteps;
+  x.most = most_splits(kRound / blocks < steps / kFewSteps ? kRound / blocks : steps / kFewSteps);
+  const int64_t each = (steps + x.most - 1) / x.most;
+  if (each >= kSplitSteps || (x.most > 1 && each > kFewSteps)) x.steps = (int)each;
+  if (window >= n_q / n_seqs) {  // the mean length
+    const GradSplits y = causal_splits(n_q, n_k, n_seqs, group, n_kv);
+    if (y.most > x.most) return y;  // (the sinks' tiles are then like the first ones)
+  }
   if (sinks && blocks < kManyBlocks) {
     const int64_t tiles = ((sinks < n_k ? sinks : n_k) + kHeld - 1) / kHeld;
     x.sink_steps = blocks <= kFewTiles ? kFewSteps : kSinkSteps;
@@ -798,22 +822,15 @@ static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group,
 
 int64_t grad_parts(const GradSplits &x, int64_t n_k, int n_seqs) {
   const int64_t tiles = n_k / kHeld + n_seqs, sinks = (int64_t)n_seqs * x.sink_tiles;
-  // with sinks alone, their tiles' first parts too
-  return (x.most > 1 ? x.most * tiles : x.sink_most > 0 ? sinks : 0) + sinks * x.sink_most;
+  return (x.most > 1 ? x.most * tiles : 0) + (x.sink_tiles ? sinks * (x.most + x.sink_most) : 0);
 }
 
 GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv, int window,
                        int sinks) {
-  GradSplits x{1, kSplitSteps, 0, 0, kSinkSteps};
-  if (n_seqs == 0 || n_k == 0) return x;
-  const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
-  if (window) return window_splits(n_q, n_k, n_seqs, n_heads / n_kv, n_kv, window, sinks);
-  const int64_t steps = n_q * (n_heads / n_kv) / 32 / n_seqs;
-  if (blocks <= kFewTiles && steps >= kSplitSteps) x.steps = kFewSteps;
-  int64_t n = (2048 + blocks - 1) / blocks;
-  if (n > steps / x.steps) n = steps / x.steps;
-  x.most = n < 1 ? 1 : n > 16 ? 16 : (int)n;
-  return x;
+  if (n_seqs == 0 || n_k == 0) return {1, kSplitSteps, 0, 0, 0};
+  const int group = n_heads / n_kv;
+  return window ? window_splits(n_q, n_k, n_seqs, group, n_kv, window, sinks)
+                : causal_splits(n_q, n_k, n_seqs, group, n_kv);
 }
 
 void run_prompt_grad(const PromptArgs &a, int dtype, hipStream_t s) {

@@ -111,6 +111,15 @@ def test_window_split_key_tiles(window, sinks, h, g):
     _check(s)
 
 
+@pytest.mark.parametrize("lens", [[1300, 40], [1, 900, 1, 1]], ids=str)
+@pytest.mark.parametrize("window,sinks", [(449, 0), (449, 3), (670, 3), (671, 3), (671, 200),
+                                          (5000, 140)])
+def test_window_near_the_mean_length(lens, window, sinks):
+    """Windows on both sides of the sequences' mean length, where the gradient's key tiles
+    begin to be split as the causal mask's are."""
+    _check(_case(lens, lens, 8, 2, 64, window, sinks, "bfloat16"))
+
+
 def test_window_as_long_as_the_sequences_is_the_causal_mask():
     """By the bounds of attention without a window: which of two products joins a sum by
     a fused operation is the compiler's choice in each kernel, so bits may differ."""
