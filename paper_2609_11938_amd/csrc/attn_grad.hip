@@ -124,7 +124,9 @@ constexpr int kFewBlocks = 256, kManyKeys = 768;
 // that right (a product more; the error of a training pass against 64 bits, in that of
 // the plain form rounded to 16 bits once: 1.65 without, 1.4 to 1.5 with). The exact D
 // goes to the second pass with the scaled lse.
-// W: through a window with sinks, with heads and keys as in the forward pass.
+// W: through a window with sinks, with heads and keys as in the forward pass: 12
+// documents of up to 4001 tokens, 16 heads on 4 of 128, window 512, 4 sinks, float16: 172
+// us, dk and dv 204 and the sinks' sums 13 (without a window 346, 346 and 39).
 template <class E, int DP, int G, bool W>
 __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;

@@ -31,8 +31,10 @@ struct PromptArgs {
   int sink_tiles, sink_splits, sink_steps;
 };
 
-// Query heads of a key head that a block takes, as a power of two: of a window's keys
-// a block reads those of all its rows, so that fewer rows of more heads waste fewer.
+// Query heads of a key head that a block takes, as a power of two: a block passes over
+// the keys that any of its rows sees, window + rows - 1 of them, so that fewer rows of
+// more heads waste fewer (24 prompts of up to 4099 tokens, 32 heads on 8 of 128, window
+// 512: 194 us by 128 rows of one head, 159 by 32 of four).
 inline int window_heads(int group) { return group % 4 == 0 ? 2 : group % 2 == 0 ? 1 : 0; }
 
 // Blocks that share a key tile of the gradient at most, and the steps of 32 queries
