@@ -28,6 +28,24 @@ constexpr int kRowsK = 64;      // keys a tile
 // 3 of 1500, 16 heads, 608 blocks: 48 and 55; 4 of 128, where there is a tile for
 // each group: 6.9 and 7.6)
 constexpr int kFewBlocks = 384, kManyKeys = 768;
+// Through a window, where a block of few rows passes over few keys as it is, the groups
+// pay from the fourth tile of 64 on (heads of 64: 4 sequences of 300, window 64, 4 sinks,
+// 199 keys: 10.8 and 9.7 us, without sinks, 191 keys, 9.0 and 9.6; 8 of 512, window 128:
+// 11.9 and 11.1; 4 of 600, window 512: 17.3 and 14.4), and of heads of 128, whose sums are
+// twice as long, from the seventh (one of 2000, 8 heads on 2, window 256, 287 keys: 14.4
+// and 15.2; window 512: 19.3 and 18.9). A compute unit takes one block of two groups:
+// more blocks than units are a second round (8 of 300, 12 heads of 64, 288 blocks: 14.0
+// with one group and 16.5 us; 5 of 1900, 8 heads on 2 of 128, window 1500, 300 blocks:
+// 62.6 and 70.4, but 4 heads of 64: 37.2 and 31.6).
+constexpr int kComputeUnits = 256;
+template <int DP>
+static bool window_groups(const PromptArgs &a, int rows) {
+  const int64_t keys = a.n_k / a.n_seqs, sinks = ((int64_t)a.sinks + 7) / 8 * 8;
+  const int64_t passed = a.window + sinks + rows - 1;
+  if ((keys < passed ? keys : passed) <= 3 * DP) return false;
+  const int64_t tiles = (a.n_q / a.n_seqs + rows - 1) / rows;  // of the mean sequence
+  return tiles * a.n_seqs * a.n_heads / (kRowsQ / rows) <= kComputeUnits;
+}
 
 // G groups of kWaves waves take the key tiles in turn and join their sums at the
 // end: the waves that a few rows would leave a compute unit without.
@@ -301,9 +319,9 @@ template <class E, int DP, bool W>
 static void launch_as(const PromptArgs &a, hipStream_t s) {
   const int hs = W ? a.head_shift : 0;
   const int64_t blocks = ((int64_t)a.n_q / (kRowsQ >> hs) + a.n_seqs) * (a.n_heads >> hs);
-  const bool many = a.n_k >= (int64_t)kManyKeys * a.n_seqs &&
-                    (!W || (int64_t)a.window + a.sinks >= kManyKeys);
-  if (blocks <= kFewBlocks && many)
+  const bool two = W ? window_groups<DP>(a, kRowsQ >> hs)
+                     : blocks <= kFewBlocks && a.n_k >= (int64_t)kManyKeys * a.n_seqs;
+  if (two)
     hipLaunchKernelGGL((k_attn_prompt<E, DP, 2, W>), dim3((uint32_t)blocks),
                        dim3(2 * kWaves * OPA_WAVE), 0, s, a);
   else
