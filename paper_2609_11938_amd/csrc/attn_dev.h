@@ -401,11 +401,13 @@ __device__ inline void report(opattr_diag *diag, uint32_t flag, int bad) {
   }
 }
 
-// Offsets outside [0, n] or decreasing, by one block.
-__device__ inline void check_spans(const int32_t *cu, int n_seqs, int n, opattr_diag *diag) {
+// Offsets outside [0, n] or decreasing, by one block of `threads`. (Asking the launch for
+// them makes a kernel's arguments 256 bytes longer: 0.2 us of a launch of 6.4.)
+__device__ inline void check_spans(const int32_t *cu, int n_seqs, int n, opattr_diag *diag,
+                                   int threads) {
   if (!diag) return;
   int bad = 0;
-  for (int b = threadIdx.x; b < n_seqs; b += blockDim.x)
+  for (int b = threadIdx.x; b < n_seqs; b += threads)
     bad += cu[b] < 0 || cu[b + 1] > n || cu[b + 1] < cu[b];
   if (bad) report(diag, OPATTR_F_DATA, bad);
 }

@@ -147,8 +147,8 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
   const int head = hk * a.group + (id % heads << hs) + (wave & ((1 << hs) - 1));
   const int rows = kHeld >> hs, from = (wave >> hs) * 32;  // the block's, the wave's first
   if (blockIdx.x == 0) {
-    check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag);
-    check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
+    check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag, G * kGradWaves * OPA_WAVE);
+    check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag, G * kGradWaves * OPA_WAVE);
   }
   Span sq, sk;
   int part, seq;

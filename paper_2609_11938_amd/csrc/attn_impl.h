@@ -14,19 +14,20 @@ struct Rows {
 };
 
 struct PromptArgs {
-  Rows q, k, v, out, dout, dq, dk, dv;
+  Rows q, k, v, out;
   float *lse;  // [heads][n_q]
   const int32_t *cu_q, *cu_k;
   int n_q, n_k, n_seqs, n_heads, n_kv, group, head_dim, causal;
   float scale;
+  int window, sinks;  // window 0: none
+  int head_shift;     // a window's: log2 of the query heads that a block takes
   opattr_diag *diag;
+  Rows dout, dq, dk, dv;
   // the gradient's workspace: pairs (lse in binary digits, D)
   // [heads][n_q]; bounds [n_seqs][n_heads + n_kv] (float16); the splits' dk and dv
   float *rows, *part;
   uint32_t *norms;
   int splits, split_steps;
-  int window, sinks;  // window 0: none
-  int head_shift;     // a window's: log2 of the query heads that a block takes
   // key tiles with sinks; blocks for each beyond `splits`, and their steps
   int sink_tiles, sink_splits, sink_steps;
 };

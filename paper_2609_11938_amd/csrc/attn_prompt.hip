@@ -75,8 +75,8 @@ __global__ __launch_bounds__(G * kWaves * OPA_WAVE, 2) void k_attn_prompt(Prompt
   const int head = hk * a.group + (id % heads << hs) + (wave & ((1 << hs) - 1));
   const int rows = kRowsQ >> hs, from = (wave >> hs) * 32;  // the block's, the wave's first
   if (blockIdx.x == 0) {
-    check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag);
-    check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
+    check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag, G * kWaves * OPA_WAVE);
+    check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag, G * kWaves * OPA_WAVE);
   }
   Span sq, sk;
   int part;
@@ -336,8 +336,8 @@ static void launch(const PromptArgs &a, hipStream_t s) {
 
 // The offsets alone, for calls whose kernels have no queries to start from.
 __global__ __launch_bounds__(256) void k_attn_check(PromptArgs a) {
-  check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag);
-  check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag);
+  check_spans(a.cu_q, a.n_seqs, a.n_q, a.diag, 256);
+  check_spans(a.cu_k, a.n_seqs, a.n_k, a.diag, 256);
 }
 
 void run_check(const PromptArgs &a, hipStream_t s) {

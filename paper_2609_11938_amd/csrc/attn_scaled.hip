@@ -56,9 +56,9 @@ template <class E, int kHeld>
 __global__ __launch_bounds__(kAppendWaves * OPA_WAVE) void k_append_scaled(AppendScaledArgs a) {
   const int lane = lane_id();
   if (blockIdx.x == 0) {
-    check_spans(a.cu, a.n_seqs, a.n_new, a.diag);
+    check_spans(a.cu, a.n_seqs, a.n_new, a.diag, kAppendWaves * OPA_WAVE);
     int bad = 0;  // tokens before 0 or past the table
-    for (int b = threadIdx.x; b < a.n_seqs; b += blockDim.x) {
+    for (int b = threadIdx.x; b < a.n_seqs; b += kAppendWaves * OPA_WAVE) {
       const int n = span_of(a.cu, b, a.n_new).count;
       const int64_t first = a.lens[b], last = first + n;
       if (a.lens_out) a.lens_out[b] = a.lens[b] + n;

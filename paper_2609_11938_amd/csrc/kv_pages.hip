@@ -15,7 +15,7 @@ namespace opa {
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   const int lane = lane_id();
   if (blockIdx.x == 0) {
-    check_spans(a.cu, a.n_seqs, a.n_new, a.diag);
+    check_spans(a.cu, a.n_seqs, a.n_new, a.diag, blockDim.x);
     if (a.lens_out)
       for (int b = threadIdx.x; b < a.n_seqs; b += blockDim.x)
         a.lens_out[b] = a.lens[b] + span_of(a.cu, b, a.n_new).count;
