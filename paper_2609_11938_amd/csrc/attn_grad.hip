@@ -385,7 +385,13 @@ __device__ __forceinline__ int tile_splits(const PromptArgs &a, const Span &sq, 
 struct Steps {
   int first, past;
 };
+template <bool W>
 __device__ __forceinline__ Steps split_steps(int all, int split, int splits) {
+  if constexpr (W) {  // (one division for all of a tile's splits)
+    const int each = all / splits, more = all - each * splits;
+    const int first = split * each + (split < more ? split : more);
+    return {first, first + each + (split < more)};
+  }
   return {(int)((int64_t)all * split / splits), (int)((int64_t)all * (split + 1) / splits)};
 }
 
@@ -483,7 +489,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   const int t0 = met.first, per = met.count;
   const int splits = tile_splits<DP, W>(a, sq, sk, part), all = per * a.group;
   if (split >= splits) return;
-  const Steps part_steps = split_steps(all, split, splits);
+  const Steps part_steps = split_steps<W>(all, split, splits);
   const int first = part_steps.first, steps = part_steps.past;
   s16x8 kf[KS], vf[KS];
   {
@@ -621,20 +627,67 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
                     sk.count - key0, a.head_dim);
 }
 
-// dk and dv of a sinks' tile, of which there are few and of many parts: a wave takes 32
-// columns of dk or dv of 32 keys, with several parts' loads on their way (12 documents,
-// window 512, 4 sinks, parts of 16 heads on 4 of 128: 13 us, 25 by the tiles' way).
+// A key tile's dk and dv from those of its blocks, added in order; a tile of one
+// block is done already. A wave takes dk or dv of 32 keys.
 template <class E, int DP>
-__device__ __forceinline__ void sink_sum(const PromptArgs &a, int id) {
+__global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArgs a) {
   constexpr int DB = DP / 32;
+  __shared__ __align__(16) uint16_t rows[2 * kGradWaves][32 * DP];
+  const int hk = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv;
+  const int all = uniform(wave_id()), wave = all / 2, which = all % 2;
+  Span sq, sk;
+  int part, seq;
+  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part, &seq)) return;
+  const int splits = tile_splits<DP, false>(a, sq, sk, part);
+  const int key0 = part * kHeld + wave * 32;
+  if (splits == 1 || key0 >= sk.count) return;
+  f32x16 sum[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) sum[d] = (f32x16)(0.f);
+  for (int k = 0; k < splits; ++k) {
+    const f32x4 *p =
+        part_of<DP, false>(a, k, tile, seq, part, hk, wave) + which * 4 * DB * OPA_WAVE;
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) {
+      const f32x4 v = p[i * OPA_WAVE];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[i / 4][i % 4 * 4 + e] += v[e];
+    }
+  }
+  const Rows &o = which ? a.dv : a.dk;
+  store_rows<E, DP>(rows[all], sum, 1.f,
+                    o.p + (int64_t)(sk.first + key0) * o.ts + (int64_t)hk * o.hs, o.ts,
+                    sk.count - key0, a.head_dim);
+}
+
+// The same through a window: the sinks' tiles first, of which there are few and of many
+// parts, then, where tiles are split, all the others. A wave takes 32 columns of dk or dv
+// of 32 keys, with several parts' loads on their way: 12 documents' sinks 10 us (25 by
+// whole rows, one part after another), 4 of up to 2000, window 2000, 19 us and not 24, one
+// of 521, 8 heads on 1 of 64, 10 and not 13; where all of many tiles are split whole rows
+// are read faster (12 documents, window 8192, 40 us and not 49).
+template <class E, int DP>
+__global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_window_sum(PromptArgs a) {
+  constexpr int DB = DP / 32;
+  const int lane = lane_id(), r = lane & 31, h = lane >> 5;
+  const int all = uniform(wave_id()), wave = all / 2, which = all % 2;
+  int id = blockIdx.x;
   const int hk = id % a.n_kv;
   id /= a.n_kv;
-  const int d = id % DB, tile = id / DB, lane = lane_id(), r = lane & 31, h = lane >> 5;
-  const int all = uniform(wave_id()), wave = all / 2, which = all % 2;
-  const int seq = tile / a.sink_tiles, part = tile % a.sink_tiles, key0 = part * kHeld + wave * 32;
+  const int d = id % DB;
+  int tile = id / DB, seq, part;
   Span sq, sk;
-  if (!sink_tile(a, seq, part, sk, sq)) return;
-  const int splits = tile_splits<DP, true>(a, sq, sk, part);
+  if (tile < a.n_seqs * a.sink_tiles) {
+    seq = tile / a.sink_tiles;
+    part = tile % a.sink_tiles;
+    if (!sink_tile(a, seq, part, sk, sq)) return;
+  } else {
+    tile -= a.n_seqs * a.sink_tiles;
+    if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part, &seq))
+      return;
+    if (part < a.sink_tiles) return;
+  }
+  const int splits = tile_splits<DP, true>(a, sq, sk, part), key0 = part * kHeld + wave * 32;
   if (splits == 1 || key0 >= sk.count) return;
   const Met mine(a, sq, sk.count - sq.count, key0);
   const Span met = tile_queries<DP, true>(a, sq, sk, part);
@@ -648,8 +701,8 @@ __device__ __forceinline__ void sink_sum(const PromptArgs &a, int id) {
     for (int k = 0; k < kAhead; ++k) {
       const bool there =
           k0 + k < splits &&
-          split_meets<DP>(mine, met, split_steps(met.count * a.group, k0 + k, splits));
-      const f32x4 *p = part_of<DP, true>(a, k0 + k, 0, seq, part, hk, wave) +
+          split_meets<DP>(mine, met, split_steps<true>(met.count * a.group, k0 + k, splits));
+      const f32x4 *p = part_of<DP, true>(a, k0 + k, tile, seq, part, hk, wave) +
                        (which * 4 * DB + 4 * d) * OPA_WAVE;
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[k][i] = there ? p[i * OPA_WAVE] : (f32x4)(0.f);
@@ -671,52 +724,6 @@ __device__ __forceinline__ void sink_sum(const PromptArgs &a, int id) {
   }
 }
 
-// A key tile's dk and dv from those of its blocks, added in order; a tile of one
-// block is done already. A wave takes dk or dv of 32 keys. The sinks' tiles' blocks
-// are the first.
-template <class E, int DP, bool W>
-__global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArgs a) {
-  constexpr int DB = DP / 32;
-  __shared__ __align__(16) uint16_t rows[2 * kGradWaves][32 * DP];
-  int id = blockIdx.x;
-  if constexpr (W) {
-    const int first = a.n_seqs * a.sink_tiles * DB * a.n_kv;
-    if (id < first) {
-      sink_sum<E, DP>(a, id);
-      return;
-    }
-    id -= first;
-  }
-  const int hk = id % a.n_kv, tile = id / a.n_kv;
-  const int all = uniform(wave_id()), wave = all / 2, which = all % 2;
-  Span sq, sk;
-  int part, seq;
-  if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part, &seq)) return;
-  if (W && part < a.sink_tiles) return;
-  const int splits = tile_splits<DP, W>(a, sq, sk, part);
-  const int key0 = part * kHeld + wave * 32;
-  if (splits == 1 || key0 >= sk.count) return;
-  f32x16 sum[DB];
-#pragma unroll
-  for (int d = 0; d < DB; ++d) sum[d] = (f32x16)(0.f);
-  const Met mine(a, sq, sk.count - sq.count, key0);
-  const Span met = tile_queries<DP, W>(a, sq, sk, part);
-  for (int k = 0; k < splits; ++k) {
-    if (W && !split_meets<DP>(mine, met, split_steps(met.count * a.group, k, splits))) continue;
-    const f32x4 *p = part_of<DP, W>(a, k, tile, seq, part, hk, wave) + which * 4 * DB * OPA_WAVE;
-#pragma unroll
-    for (int i = 0; i < 4 * DB; ++i) {
-      const f32x4 v = p[i * OPA_WAVE];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[i / 4][i % 4 * 4 + e] += v[e];
-    }
-  }
-  const Rows &o = which ? a.dv : a.dk;
-  store_rows<E, DP>(rows[all], sum, 1.f,
-                    o.p + (int64_t)(sk.first + key0) * o.ts + (int64_t)hk * o.hs, o.ts,
-                    sk.count - key0, a.head_dim);
-}
-
 template <class E, int DP, bool W>
 static void launch(const PromptArgs &a, hipStream_t s) {
   const int hs = W ? a.head_shift : 0;
@@ -735,9 +742,13 @@ static void launch(const PromptArgs &a, hipStream_t s) {
   const int64_t parts = kt * a.splits + sinks * a.sink_splits;
   hipLaunchKernelGGL((k_attn_dkv<E, DP, W>), dim3((uint32_t)(parts * a.n_kv)), block, 0, s, a);
   const dim3 twice(2 * kGradWaves * OPA_WAVE);
-  const int64_t sums = ((a.splits > 1 ? kt : 0) + sinks * (DP / 32)) * a.n_kv;
-  if (sums > 0)
-    hipLaunchKernelGGL((k_dkv_sum<E, DP, W>), dim3((uint32_t)sums), twice, 0, s, a);
+  if constexpr (W) {
+    const int64_t sums = ((a.splits > 1 ? kt : 0) + sinks) * (DP / 32) * a.n_kv;
+    if (sums > 0)
+      hipLaunchKernelGGL((k_window_sum<E, DP>), dim3((uint32_t)sums), twice, 0, s, a);
+  } else if (a.splits > 1) {
+    hipLaunchKernelGGL((k_dkv_sum<E, DP>), dim3((uint32_t)(kt * a.n_kv)), twice, 0, s, a);
+  }
 }
 
 template <class E>
@@ -790,7 +801,7 @@ static GradSplits causal_splits(int64_t n_q, int64_t n_k, int n_seqs, int group,
 // of 16000: through 4096 986 and 1018, through all 3315 and 2070.
 //
 // The sinks' tiles meet every query: they have blocks of sink_steps steps besides,
-// kMostSinks each and kSinkBlocks in all at most, which begin first. 12 documents, window
+// kMostSinks each and kSinkBlocks in all at most, which begin last. 12 documents, window
 // 512, 4 sinks, with the sums: 254 us with 64 steps, 233 with 32; one of 4000, whose tiles
 // are few, 100 us without the sums with 32 and 75 with 8.
 constexpr int kRound = 512, kMostSinks = 31, kSinkBlocks = 1024, kSinkSteps = 32;
@@ -803,7 +814,7 @@ static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group,
   const int64_t steps = (met * group + 31) / 32;
   x.most = most_splits(kRound / blocks < steps / kFewSteps ? kRound / blocks : steps / kFewSteps);
   const int64_t each = (steps + x.most - 1) / x.most;
-  if (each >= kSplitSteps || (x.most > 1 && each > kFewSteps)) x.steps = (int)each;
+  if (x.most > 1 || each > kSplitSteps) x.steps = (int)(each < kFewSteps ? kFewSteps : each);
   if (window >= n_q / n_seqs) {  // the mean length
     const GradSplits y = causal_splits(n_q, n_k, n_seqs, group, n_kv);
     if (y.most > x.most) return y;  // (the sinks' tiles are then like the first ones)
