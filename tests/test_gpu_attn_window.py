@@ -120,6 +120,14 @@ def test_window_near_the_mean_length(lens, window, sinks):
     _check(_case(lens, lens, 8, 2, 64, window, sinks, "bfloat16"))
 
 
+@pytest.mark.parametrize("n,window,sinks", [(64, 13, 0), (64, 13, 5), (300, 100, 0),
+                                            (521, 773, 0), (521, 200, 130)])
+@pytest.mark.parametrize("d,dtype", [(64, "bfloat16"), (128, "float16")])
+def test_window_one_sequence_of_many_heads(n, window, sinks, d, dtype):
+    """One key head, whose few key tiles are split into blocks of few steps."""
+    _check(_case([n], [n], 8, 1, d, window, sinks, dtype))
+
+
 def test_window_as_long_as_the_sequences_is_the_causal_mask():
     """By the bounds of attention without a window: which of two products joins a sum by
     a fused operation is the compiler's choice in each kernel, so bits may differ."""
