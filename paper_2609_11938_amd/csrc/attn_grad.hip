@@ -7,7 +7,7 @@
 //   k_attn_dkv  a wave holds 32 keys of one key head, and their dk and dv, and
 //               passes over the queries that see them, of every query head of
 //               the group; where key tiles are few, a tile's passes are split
-//               over several blocks and added up by k_dkv_sum
+//               over several blocks and added up by k_dkv_sum (k_window_sum)
 // Ten products where seven are needed (with the forward pass): the scores and dp
 // are computed by both passes, because adding dq in the second needs float32 atomics,
 // whose order changes the result; and sum_j p_j k_j, which takes the rounding of
@@ -126,7 +126,7 @@ constexpr int kFewBlocks = 256, kManyKeys = 768;
 // goes to the second pass with the scaled lse.
 // W: through a window with sinks, with heads and keys as in the forward pass: 12
 // documents of up to 4001 tokens, 16 heads on 4 of 128, window 512, 4 sinks, float16: 172
-// us, dk and dv 204 and the sinks' sums 13 (without a window 346, 346 and 39).
+// us, dk and dv 204 and the sinks' sums 10 (without a window 346, 346 and 39).
 template <class E, int DP, int G, bool W>
 __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;
@@ -802,7 +802,7 @@ static GradSplits causal_splits(int64_t n_q, int64_t n_k, int n_seqs, int group,
 //
 // The sinks' tiles meet every query: they have blocks of sink_steps steps besides,
 // kMostSinks each and kSinkBlocks in all at most, which begin last. 12 documents, window
-// 512, 4 sinks, with the sums: 254 us with 64 steps, 233 with 32; one of 4000, whose tiles
+// 512, 4 sinks, with sums of 14 and 25 us: 254 us with 64 steps, 233 with 32; one of 4000, whose tiles
 // are few, 100 us without the sums with 32 and 75 with 8.
 constexpr int kRound = 512, kMostSinks = 31, kSinkBlocks = 1024, kSinkSteps = 32;
 constexpr int64_t kManyBlocks = 1 << 16;  // past these a few blocks more say nothing
