@@ -802,10 +802,12 @@ static GradSplits causal_splits(int64_t n_q, int64_t n_k, int n_seqs, int group,
 //
 // The sinks' tiles meet every query: they have blocks of sink_steps steps besides,
 // kMostSinks each and kSinkBlocks in all at most, which begin last. 12 documents, window
-// 512, 4 sinks, with sums of 14 and 25 us: 254 us with 64 steps, 233 with 32; one of 4000, whose tiles
-// are few, 100 us without the sums with 32 and 75 with 8.
+// 512, 4 sinks, with the sums: 206 us with 16 steps, 212 with 32, 211 with 48; 32 of up to
+// 4000 321, 314 and 309, 6 of 16 key heads 137, 142 and 159; one of 4000, whose tiles are
+// few, 100 us without the sums with 32 and 75 with 8.
 constexpr int kRound = 512, kMostSinks = 31, kSinkBlocks = 1024, kSinkSteps = 32;
-constexpr int64_t kManyBlocks = 1 << 16;  // past these a few blocks more say nothing
+constexpr int64_t kManyBlocks = 1 << 16;  // past these more blocks say nothing (and one launch
+                                          // takes as many)
 static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group, int n_kv,
                                 int window, int sinks) {
   const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
