@@ -16,9 +16,9 @@
 // Products, exponentials and fragment reads follow one another in a wave, as in the
 // forward pass: 12 documents of up to 4001 tokens, 16 heads on 4 of 128: dq 346 us, dk
 // and dv 346, their sums 39, the matrix units busy 54% and 52% of the first two; with
-// the forward pass 887 us, in float16 (two launches more, which read dout and v once
+// the forward pass 887 us, in float16 (two launches more, for few rows one: dout and v once
 // more: 25 us) 961. 8 sequences of 512, 8 heads of 64: 16 and 18 us, one round of
-// blocks; a training pass 43 us, in float16 53. head_dim 72 to 120 costs nearly what 128
+// blocks; a training pass 43 us, in float16 49. head_dim 72 to 120 costs nearly what 128
 // does.
 #include "attn_dev.h"
 #include "attn_impl.h"
@@ -70,9 +70,17 @@ struct Scales<F16> {
 // head (the bits of non-negative floats order as integers, so the maximum is the same
 // in any order). A block takes kNormRows rows of a sequence and one head: blockIdx.y
 // is a query head, and past those a key head. 4 lanes a row.
+//
+// kAll: a block takes a whole sequence, so that nothing has to be cleared before: for few
+// rows, of sequences that are no longer than a block likes. 8 heads of 64, with the launch
+// that clears and without: one sequence of 64 8.1 us and 4.0, 8 of 512 10.9 and 4.4, 2 of
+// 2048 10.9 and 9.6, one of 4096 11.3 and 13.4; 100 of 40, 16 heads and 16 key heads of
+// 128: 13.8 and 17.8.
 constexpr int kNormRows = 512;
-__global__ __launch_bounds__(256) void k_attn_norms(PromptArgs a) {
-  __shared__ float most[4];
+template <bool kAll>
+__global__ __launch_bounds__(kAll ? 1024 : 256) void k_attn_norms(PromptArgs a) {
+  constexpr int kThreads = kAll ? 1024 : 256;
+  __shared__ float most[kThreads / OPA_WAVE];
   const int sub = threadIdx.x & 3;
   const bool q = (int)blockIdx.y < a.n_heads;
   const int head = q ? blockIdx.y : blockIdx.y - a.n_heads;
@@ -80,11 +88,14 @@ __global__ __launch_bounds__(256) void k_attn_norms(PromptArgs a) {
   const Rows x = q ? a.dout : a.v;
   const int32_t *cu = q ? a.cu_q : a.cu_k;
   Span s, same;
-  int part, seq;
-  if (!find_tile(cu, n, cu, n, a.n_seqs, kNormRows, blockIdx.x, s, same, part, &seq)) return;
+  int part = 0, seq = blockIdx.x;
+  if constexpr (kAll)
+    s = span_of(cu, seq, n);
+  else if (!find_tile(cu, n, cu, n, a.n_seqs, kNormRows, blockIdx.x, s, same, part, &seq))
+    return;
+  const int past = kAll || s.count < (part + 1) * kNormRows ? s.count : (part + 1) * kNormRows;
   float top = 0.f;
-  for (int t = part * kNormRows + (threadIdx.x >> 2); t < s.count && t < (part + 1) * kNormRows;
-       t += 64) {
+  for (int t = part * kNormRows + (threadIdx.x >> 2); t < past; t += kThreads / 4) {
     const uint16_t *px = x.p + (int64_t)(s.first + t) * x.ts + (int64_t)head * x.hs;
     float norm = 0.f;
     for (int c = sub * 8; c < a.head_dim; c += 32) {
@@ -103,9 +114,14 @@ __global__ __launch_bounds__(256) void k_attn_norms(PromptArgs a) {
   for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
   if (lane_id() == 0) most[wave_id()] = top;
   __syncthreads();
-  if (threadIdx.x == 0)
-    atomicMax(&a.norms[(int64_t)seq * (a.n_heads + a.n_kv) + blockIdx.y],
-              __float_as_uint(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]))));
+  if (threadIdx.x) return;
+#pragma unroll
+  for (int w = 1; w < kThreads / OPA_WAVE; ++w) top = fmaxf(top, most[w]);
+  uint32_t *to = &a.norms[(int64_t)seq * (a.n_heads + a.n_kv) + blockIdx.y];
+  if (kAll)
+    *to = __float_as_uint(top);
+  else
+    atomicMax(to, __float_as_uint(top));
 }
 
 __global__ void k_attn_zero(uint32_t *p, int n) {
@@ -751,14 +767,24 @@ static void launch(const PromptArgs &a, hipStream_t s) {
   }
 }
 
+static bool whole_norms(const PromptArgs &a, int rows) {
+  return rows <= 4096 && rows <= 1024 * (int64_t)a.n_seqs &&
+         (int64_t)a.n_seqs * (a.n_heads + a.n_kv) <= 2048;
+}
+
 template <class E>
 static void grad(const PromptArgs &a, hipStream_t s) {
   if (a.norms) {
     const int n = a.n_seqs * (a.n_heads + a.n_kv);
-    hipLaunchKernelGGL(k_attn_zero, dim3((n + 63) / 64), dim3(64), 0, s, a.norms, n);
     const int most = a.n_k > a.n_q ? a.n_k : a.n_q;
-    const dim3 grid(most / kNormRows + a.n_seqs, a.n_heads + a.n_kv);
-    if (most > 0) hipLaunchKernelGGL(k_attn_norms, grid, dim3(256), 0, s, a);
+    if (whole_norms(a, most)) {
+      hipLaunchKernelGGL(k_attn_norms<true>, dim3(a.n_seqs, a.n_heads + a.n_kv), dim3(1024), 0, s,
+                         a);
+    } else {
+      hipLaunchKernelGGL(k_attn_zero, dim3((n + 63) / 64), dim3(64), 0, s, a.norms, n);
+      const dim3 grid(most / kNormRows + a.n_seqs, a.n_heads + a.n_kv);
+      if (most > 0) hipLaunchKernelGGL(k_attn_norms<false>, grid, dim3(256), 0, s, a);
+    }
   }
   if (a.window)
     a.head_dim <= 64 ? launch<E, 64, true>(a, s) : launch<E, 128, true>(a, s);
