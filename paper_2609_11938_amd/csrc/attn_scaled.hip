@@ -281,7 +281,8 @@ __device__ __forceinline__ int code_swz(int row) {
 // Blocks go round the 8 chiplets: a share's key heads lie 8 blocks apart, on one chiplet,
 // so that a token's heads, side by side in memory, are read through one cache.
 template <class E, int DP, bool R>
-__global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 64 ? 4 : 3) void k_attn_scaled(ScaledArgs a) {
+__global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 64 ? 4 : 3) void k_attn_scaled(
+    ScaledArgs a) {
   constexpr int KS = DP / 32, DB = DP / 16, C = DP / 16, N = kTile * C / OPA_WAVE;
   constexpr int kBytes = kTile * DP;  // a wave's tile
   // the tiles of the waves, two in turn; at the end the waves' sums, two waves' in each

@@ -263,8 +263,9 @@ def serve(rec, lens=(100, 37, 64), steps=8, layers=2, heads=8, kv_heads=4, head_
           page_size=16, dtype=torch.bfloat16, seed=0, window=None, sinks=0, scaled=False):
     """Prompts of the given lengths, `steps` tokens each, a turn in which the
     first sequence is forked into the place of the second, and `steps` more; through a
-    window with sinks, if one is given, and from a cache of 8 bits, if scaled. Returns, for every sequence alive at the end, its layers' queries, keys,
-    values and outputs, each [tokens, heads, head_dim]."""
+    window with sinks, if one is given, and from a cache of 8 bits, if scaled. Returns,
+    for every sequence alive at the end, its layers' queries, keys, values and outputs,
+    each [tokens, heads, head_dim]."""
     gen = torch.Generator(device="cuda:0")
     gen.manual_seed(seed)
     rows, most = len(lens), max(lens) + 2 * steps
