@@ -349,8 +349,10 @@ static int prompt_grad(const opattr_attn_shape *a, int32_t window, int32_t sinks
   p.splits = x.most;
   p.split_steps = x.steps;
   p.sink_tiles = x.sink_tiles;
-  p.sink_splits = x.sink_most;
-  p.sink_steps = x.sink_steps;
+  p.sink_shift = x.sink_shift;
+  p.sink_most = x.sink_most;
+  p.sink_slots = x.sink_slots;
+  p.sink_sums = x.sink_sums;
   run_prompt_grad(p, a->dtype, (hipStream_t)stream);
   return launched();
 }

@@ -20,6 +20,8 @@
 // more: 25 us) 961. 8 sequences of 512, 8 heads of 64: 16 and 18 us, one round of
 // blocks; a training pass 43 us, in float16 49. head_dim 72 to 120 costs nearly what 128
 // does.
+#include <algorithm>
+
 #include "attn_dev.h"
 #include "attn_impl.h"
 
@@ -392,9 +394,56 @@ template <int DP, bool W>
 __device__ __forceinline__ int tile_splits(const PromptArgs &a, const Span &sq, const Span &sk,
                                            int part) {
   const int steps = tile_queries<DP, W>(a, sq, sk, part).count * a.group * (kStep(DP) / 32);
-  if (W && part < a.sink_tiles)
-    return clamp_to((steps + a.sink_steps - 1) / a.sink_steps, 1, a.splits + a.sink_splits);
   return clamp_to((steps + a.split_steps - 1) / a.split_steps, 1, a.splits);
+}
+
+// Through a window the sinks' key tiles meet every query. Of a sequence whose first tile
+// has the steps for more blocks than other tiles have, such tiles are shared by blocks of
+// their own, `blocks` each: slots, counted through the sequences, their tiles, and a
+// tile's blocks. tiles 0: none are.
+struct Sinks {
+  int tiles, blocks;
+};
+template <int DP>
+__device__ __forceinline__ Sinks sinks_of(const PromptArgs &a, const Span &sq, const Span &sk) {
+  if (a.sink_tiles == 0) return {0, 0};
+  const int steps = tile_queries<DP, true>(a, sq, sk, 0).count * a.group * (kStep(DP) / 32);
+  int blocks = (steps + (1 << a.sink_shift) - 1) >> a.sink_shift;
+  if (blocks <= a.splits) return {0, 0};
+  if (blocks > a.sink_most) blocks = a.sink_most;
+  const int tiles = tiles_of(sk.count, kHeld);
+  return {tiles < a.sink_tiles ? tiles : a.sink_tiles, blocks};
+}
+// Of the sequences' slots, or of their shared tiles, the one numbered `at`: its sequence and
+// tile, and the tile's first slot; false past the last. By whole waves.
+template <int DP, bool kSlots>
+__device__ __forceinline__ bool find_sink(const PromptArgs &a, int at, Span &sk, Span &sq,
+                                          int &seq, int &part, int &slot, int &blocks) {
+  const int lane = lane_id();
+  int before = 0;  // slots of the sequences so far
+  for (int base = 0; base < a.n_seqs && before < a.sink_slots; base += OPA_WAVE) {
+    const int b = base + lane < a.n_seqs ? base + lane : a.n_seqs - 1;
+    const Span k = span_of(a.cu_k, b, a.n_k), q = span_of(a.cu_q, b, a.n_q);
+    const Sinks x = base + lane < a.n_seqs ? sinks_of<DP>(a, q, k) : Sinks{0, 0};
+    const int slots = x.tiles * x.blocks, past = wave_sums(slots);
+    const int n = kSlots ? slots : x.tiles, inc = kSlots ? past : wave_sums(n);
+    const uint64_t m = __ballot(inc > at);
+    if (m) {
+      const int w = __ffsll((unsigned long long)m) - 1;
+      const auto from = [&](int v) { return __builtin_amdgcn_readlane(v, w); };
+      sk = {from(k.first), from(k.count)};
+      sq = {from(q.first), from(q.count)};
+      seq = base + w;
+      blocks = from(x.blocks);
+      at -= from(inc - n);
+      part = kSlots ? at / blocks : at;
+      slot = before + from(past - slots) + part * blocks;
+      return slot + blocks <= a.sink_slots;  // (offsets that overlap may ask for more)
+    }
+    at -= __builtin_amdgcn_readlane(inc, OPA_WAVE - 1);
+    before += __builtin_amdgcn_readlane(past, OPA_WAVE - 1);
+  }
+  return false;
 }
 
 // A split's steps of a tile: a head's tiles of queries, then the next head's.
@@ -433,26 +482,17 @@ __device__ __forceinline__ bool split_meets(const Met &m, const Span &tiles, con
 
 // Where a wave of one of a tile's blocks leaves its dk and dv, as its registers hold
 // them: [parts][n_kv][waves][dk, dv][DP / 8][64 lanes] of four values, the parts
-// [splits][tiles], none where splits is 1, and then those of the sinks' tiles,
-// [splits + sink_splits][sequences][sink_tiles].
-template <int DP, bool W>
-__device__ __forceinline__ f32x4 *part_of(const PromptArgs &a, int split, int tile, int seq,
-                                          int part, int hk, int wave) {
-  const int64_t tiles = a.n_k / kHeld + a.n_seqs;
-  int64_t at = split * tiles + tile;
-  if (W && part < a.sink_tiles)
-    at = (a.splits > 1 ? a.splits * tiles : 0) +
-         ((int64_t)split * a.n_seqs + seq) * a.sink_tiles + part;
+// [splits][tiles], none where splits is 1, and then the slots of the sinks' tiles.
+template <int DP>
+__device__ __forceinline__ f32x4 *part_at(const PromptArgs &a, int64_t at, int hk, int wave) {
   at = (at * a.n_kv + hk) * kGradWaves + wave;
   return reinterpret_cast<f32x4 *>(a.part) + at * (2 * DP / 8 * OPA_WAVE) + lane_id();
 }
-
-// Sequence `seq`'s key tile `part` without a search; false if it has none.
-__device__ __forceinline__ bool sink_tile(const PromptArgs &a, int seq, int part, Span &sk,
-                                          Span &sq) {
-  sk = span_of(a.cu_k, seq, a.n_k);
-  sq = span_of(a.cu_q, seq, a.n_q);
-  return part * kHeld < sk.count;
+__device__ __forceinline__ int64_t tile_part(const PromptArgs &a, int split, int tile) {
+  return split * (a.n_k / kHeld + (int64_t)a.n_seqs) + tile;
+}
+__device__ __forceinline__ int64_t sink_part(const PromptArgs &a, int slot) {
+  return (a.splits > 1 ? tile_part(a, a.splits, 0) : 0) + slot;
 }
 
 // dk and dv of 32 keys a wave: S = Q K^T with the wave's keys as columns, so
@@ -471,21 +511,24 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   id /= a.n_kv;
   Span sq, sk;
   int part, seq, split;
-  // W: past the blocks of every tile those that the sinks' tiles have besides
-  const int64_t more = W ? id - (a.n_k / kHeld + (int64_t)a.n_seqs) * a.splits : -1;
-  bool found;
-  if (more >= 0) {
-    const int x = (int)more / a.sink_splits;
-    split = a.splits + (int)more % a.sink_splits;
-    part = x % a.sink_tiles;
-    seq = x / a.sink_tiles;
-    found = sink_tile(a, seq, part, sk, sq);
+  // W: past the blocks of every tile those of the sinks' tiles
+  const int64_t past_tiles = W ? id - tile_part(a, a.splits, 0) : -1;
+  int splits;
+  int64_t place;  // of this block's part
+  if (past_tiles >= 0) {
+    int slot;
+    if (!find_sink<DP, true>(a, (int)past_tiles, sk, sq, seq, part, slot, splits)) return;
+    split = (int)past_tiles - slot;
+    place = sink_part(a, (int)past_tiles);
   } else {
     split = id % a.splits;
-    found = find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, id / a.splits, sk, sq, part,
-                      &seq);
+    const int tile = id / a.splits;
+    if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part, &seq))
+      return;
+    if (W && part < sinks_of<DP>(a, sq, sk).tiles) return;
+    splits = tile_splits<DP, W>(a, sq, sk, part);
+    place = tile_part(a, split, tile);
   }
-  if (!found) return;
   const int lead = sk.count - sq.count;
   const int key0 = part * kHeld + wave * 32, key = key0 + r;
   const bool live = key < sk.count;
@@ -503,7 +546,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   const Met mine(a, sq, lead, key0);
   const Span met = tile_queries<DP, W>(a, sq, sk, part);
   const int t0 = met.first, per = met.count;
-  const int splits = tile_splits<DP, W>(a, sq, sk, part), all = per * a.group;
+  const int all = per * a.group;
   if (split >= splits) return;
   const Steps part_steps = split_steps<W>(all, split, splits);
   const int first = part_steps.first, steps = part_steps.past;
@@ -614,7 +657,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   const float fk = a.scale / up;
   if (splits > 1) {
     if (W && !split_meets<DP>(mine, met, part_steps)) return;
-    f32x4 *p = part_of<DP, W>(a, split, id / a.splits, seq, part, hk, wave);
+    f32x4 *p = part_at<DP>(a, place, hk, wave);
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -632,14 +675,14 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   }
   block_sync();  // the tiles' last readers are done
   constexpr int kFit = kTile / (32 * DP);  // waves' rows in one tile's place
-  uint16_t *const place = (wave / kFit == 0 ? tq0 : wave / kFit == 1 ? tq1
-                                                  : wave / kFit == 2 ? td0
-                                                                     : td1) +
-                          wave % kFit * 32 * DP;
+  uint16_t *const room = (wave / kFit == 0 ? tq0 : wave / kFit == 1 ? tq1
+                                                 : wave / kFit == 2 ? td0
+                                                                    : td1) +
+                         wave % kFit * 32 * DP;
   const int64_t tok = sk.first + key0;
-  store_rows<E, DP>(place, dk, fk, a.dk.p + tok * a.dk.ts + (int64_t)hk * a.dk.hs, a.dk.ts,
+  store_rows<E, DP>(room, dk, fk, a.dk.p + tok * a.dk.ts + (int64_t)hk * a.dk.hs, a.dk.ts,
                     sk.count - key0, a.head_dim);
-  store_rows<E, DP>(place, dv, fv, a.dv.p + tok * a.dv.ts + (int64_t)hk * a.dv.hs, a.dv.ts,
+  store_rows<E, DP>(room, dv, fv, a.dv.p + tok * a.dv.ts + (int64_t)hk * a.dv.hs, a.dv.ts,
                     sk.count - key0, a.head_dim);
 }
 
@@ -662,7 +705,7 @@ __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_dkv_sum(PromptArg
   for (int d = 0; d < DB; ++d) sum[d] = (f32x16)(0.f);
   for (int k = 0; k < splits; ++k) {
     const f32x4 *p =
-        part_of<DP, false>(a, k, tile, seq, part, hk, wave) + which * 4 * DB * OPA_WAVE;
+        part_at<DP>(a, tile_part(a, k, tile), hk, wave) + which * 4 * DB * OPA_WAVE;
 #pragma unroll
     for (int i = 0; i < 4 * DB; ++i) {
       const f32x4 v = p[i * OPA_WAVE];
@@ -691,19 +734,23 @@ __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_window_sum(Prompt
   const int hk = id % a.n_kv;
   id /= a.n_kv;
   const int d = id % DB;
-  int tile = id / DB, seq, part;
+  int tile = id / DB, seq, part, splits;
   Span sq, sk;
-  if (tile < a.n_seqs * a.sink_tiles) {
-    seq = tile / a.sink_tiles;
-    part = tile % a.sink_tiles;
-    if (!sink_tile(a, seq, part, sk, sq)) return;
+  int64_t place, step = 1;  // of the tile's first part, and to its next
+  if (tile < a.sink_sums) {
+    int slot;
+    if (!find_sink<DP, false>(a, tile, sk, sq, seq, part, slot, splits)) return;
+    place = sink_part(a, slot);
   } else {
-    tile -= a.n_seqs * a.sink_tiles;
+    tile -= a.sink_sums;
     if (!find_tile(a.cu_k, a.n_k, a.cu_q, a.n_q, a.n_seqs, kHeld, tile, sk, sq, part, &seq))
       return;
-    if (part < a.sink_tiles) return;
+    if (part < sinks_of<DP>(a, sq, sk).tiles) return;
+    splits = tile_splits<DP, true>(a, sq, sk, part);
+    place = tile_part(a, 0, tile);
+    step = tile_part(a, 1, 0);
   }
-  const int splits = tile_splits<DP, true>(a, sq, sk, part), key0 = part * kHeld + wave * 32;
+  const int key0 = part * kHeld + wave * 32;
   if (splits == 1 || key0 >= sk.count) return;
   const Met mine(a, sq, sk.count - sq.count, key0);
   const Span met = tile_queries<DP, true>(a, sq, sk, part);
@@ -718,8 +765,8 @@ __global__ __launch_bounds__(2 * kGradWaves * OPA_WAVE) void k_window_sum(Prompt
       const bool there =
           k0 + k < splits &&
           split_meets<DP>(mine, met, split_steps<true>(met.count * a.group, k0 + k, splits));
-      const f32x4 *p = part_of<DP, true>(a, k0 + k, tile, seq, part, hk, wave) +
-                       (which * 4 * DB + 4 * d) * OPA_WAVE;
+      const f32x4 *p =
+          part_at<DP>(a, place + (k0 + k) * step, hk, wave) + (which * 4 * DB + 4 * d) * OPA_WAVE;
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[k][i] = there ? p[i * OPA_WAVE] : (f32x4)(0.f);
     }
@@ -754,12 +801,11 @@ static void launch(const PromptArgs &a, hipStream_t s) {
   else if (a.n_q > 0)
     hipLaunchKernelGGL((k_attn_dq<E, DP, 1, W>), rows, block, 0, s, a);
   if (a.n_k == 0) return;
-  const int64_t sinks = (int64_t)a.n_seqs * a.sink_tiles;
-  const int64_t parts = kt * a.splits + sinks * a.sink_splits;
+  const int64_t parts = kt * a.splits + a.sink_slots;
   hipLaunchKernelGGL((k_attn_dkv<E, DP, W>), dim3((uint32_t)(parts * a.n_kv)), block, 0, s, a);
   const dim3 twice(2 * kGradWaves * OPA_WAVE);
   if constexpr (W) {
-    const int64_t sums = ((a.splits > 1 ? kt : 0) + sinks) * (DP / 32) * a.n_kv;
+    const int64_t sums = ((a.splits > 1 ? kt : 0) + a.sink_sums) * (DP / 32) * a.n_kv;
     if (sums > 0)
       hipLaunchKernelGGL((k_window_sum<E, DP>), dim3((uint32_t)sums), twice, 0, s, a);
   } else if (a.splits > 1) {
@@ -809,7 +855,7 @@ constexpr int kSplitSteps = 24, kFewSteps = 8, kFewTiles = 192;
 static int most_splits(int64_t n) { return n < 1 ? 1 : n > 16 ? 16 : (int)n; }
 static GradSplits causal_splits(int64_t n_q, int64_t n_k, int n_seqs, int group, int n_kv) {
   const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
-  GradSplits x{1, kSplitSteps, 0, 0, 0};
+  GradSplits x{1, kSplitSteps, 0, 0, 0, 0, 0};
   const int64_t steps = n_q * group / 32 / n_seqs;
   if (blocks <= kFewTiles && steps >= kSplitSteps) x.steps = kFewSteps;
   const int64_t n = (2048 + blocks - 1) / blocks;
@@ -826,18 +872,21 @@ static GradSplits causal_splits(int64_t n_q, int64_t n_k, int n_seqs, int group,
 // the causal rule, sums included; through 2048 449 and 370, through 4096 706 and 408; one
 // of 16000: through 4096 986 and 1018, through all 3315 and 2070.
 //
-// The sinks' tiles meet every query: they have blocks of sink_steps steps besides,
-// kMostSinks each and kSinkBlocks in all at most, which begin last. 12 documents, window
-// 512, 4 sinks, with the sums: 206 us with 16 steps, 212 with 32, 211 with 48; 32 of up to
-// 4000 321, 314 and 309, 6 of 16 key heads 137, 142 and 159; one of 4000, whose tiles are
-// few, 100 us without the sums with 32 and 75 with 8.
-constexpr int kRound = 512, kMostSinks = 31, kSinkBlocks = 1024, kSinkSteps = 32;
+// The sinks' tiles meet every query: where that is more than a block is to have, they are
+// shared by blocks of 2^sink_shift steps, kMostSinks more than other tiles have at most, and
+// of all key heads about kSinkBlocks at most, which begin last. Their room goes by the
+// steps that there are, as the slots are counted through the sequences that have them: of
+// 32 steps it is about half of the queries' own. dk and dv with the sums: 12 documents,
+// window 512, 4 sinks, 190 us by 16 steps, 191 by 32, 214 by 64; 6 documents of 16 key heads
+// 84, 101 and 144; with 300 sinks 12 documents 270, 245 and 263. Where tiles are few, by 8
+// and by 32 steps: one of 4000 74 and 86 us, 3 of up to 609, one key head, 22 and 33.
+constexpr int kRound = 512, kMostSinks = 31, kSinkBlocks = 2048, kSinkShift = 5, kFewShift = 3;
 constexpr int64_t kManyBlocks = 1 << 16;  // past these more blocks say nothing (and one launch
                                           // takes as many)
 static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group, int n_kv,
                                 int window, int sinks) {
   const int64_t blocks = (n_k / kHeld + n_seqs) * n_kv;
-  GradSplits x{1, kSplitSteps, 0, 0, 0};
+  GradSplits x{1, kSplitSteps, 0, 0, 0, 0, 0};
   const int64_t met = n_q < (int64_t)window + kHeld ? n_q : (int64_t)window + kHeld;
   const int64_t steps = (met * group + 31) / 32;
   x.most = most_splits(kRound / blocks < steps / kFewSteps ? kRound / blocks : steps / kFewSteps);
@@ -847,28 +896,39 @@ static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group,
     const GradSplits y = causal_splits(n_q, n_k, n_seqs, group, n_kv);
     if (y.most > x.most) return y;  // (the sinks' tiles are then like the first ones)
   }
-  if (sinks && blocks < kManyBlocks) {
-    const int64_t tiles = ((sinks < n_k ? sinks : n_k) + kHeld - 1) / kHeld;
-    x.sink_steps = blocks <= kFewTiles ? kFewSteps : kSinkSteps;
-    int64_t more = (n_q * group / 32 + x.sink_steps - 1) / x.sink_steps - x.most;
-    const int64_t room = kSinkBlocks / (n_seqs * tiles);
-    if (more > room) more = room;
-    if (more > 0) {
-      x.sink_tiles = (int)tiles;
-      x.sink_most = more > kMostSinks ? kMostSinks : (int)more;
-    }
-  }
+  if (!sinks || blocks >= kManyBlocks) return x;
+  const int64_t tiles = ((sinks < n_k ? sinks : n_k) + kHeld - 1) / kHeld;  // of a sequence
+  int shift = blocks <= kFewTiles ? kFewShift : kSinkShift;
+  // A sequence of n queries has (n + kMostEnd) group / 32 steps at most; to share its tiles
+  // it has more than 2^shift, so that not every sequence of a batch can
+  constexpr int64_t kMostEnd = 63;
+  int64_t least = ((int64_t)32 << shift) / group - kMostEnd;
+  if (least < 1) least = 1;
+  const int64_t seqs = n_q / least < n_seqs ? n_q / least : n_seqs;
+  const int64_t all = tiles * ((n_q + kMostEnd * seqs) * group / 32 + 1);  // steps, of them
+  while (all >> shift > kSinkBlocks / n_kv) ++shift;
+  // of S = ceil(steps / 2^shift) blocks, more than one: less than 2 steps / 2^shift, and
+  // than steps / 2^shift + 1
+  const int64_t held = std::min(seqs * tiles, n_k / kHeld + seqs);
+  const int64_t slots = std::min(std::min(2 * all >> shift, (all >> shift) + held),
+                                 held * (x.most + kMostSinks));
+  const int64_t most = ((n_q + kMostEnd) * group / 32 + (1 << shift)) >> shift;  // of a tile
+  if (most <= x.most || slots <= x.most) return x;
+  x.sink_tiles = (int)tiles;
+  x.sink_shift = shift;
+  x.sink_most = x.most + kMostSinks;
+  x.sink_slots = (int)slots;
+  x.sink_sums = (int)std::min(held, slots / (x.most + 1));
   return x;
 }
 
 int64_t grad_parts(const GradSplits &x, int64_t n_k, int n_seqs) {
-  const int64_t tiles = n_k / kHeld + n_seqs, sinks = (int64_t)n_seqs * x.sink_tiles;
-  return (x.most > 1 ? x.most * tiles : 0) + (x.sink_tiles ? sinks * (x.most + x.sink_most) : 0);
+  return (x.most > 1 ? x.most * (n_k / kHeld + n_seqs) : 0) + x.sink_slots;
 }
 
 GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv, int window,
                        int sinks) {
-  if (n_seqs == 0 || n_k == 0) return {1, kSplitSteps, 0, 0, 0};
+  if (n_seqs == 0 || n_k == 0) return {1, kSplitSteps, 0, 0, 0, 0, 0};
   const int group = n_heads / n_kv;
   return window ? window_splits(n_q, n_k, n_seqs, group, n_kv, window, sinks)
                 : causal_splits(n_q, n_k, n_seqs, group, n_kv);

@@ -28,8 +28,9 @@ struct PromptArgs {
   float *rows, *part;
   uint32_t *norms;
   int splits, split_steps;
-  // key tiles with sinks; blocks for each beyond `splits`, and their steps
-  int sink_tiles, sink_splits, sink_steps;
+  // key tiles of a sequence with sinks; where blocks share them, the log2 of a block's
+  // steps and how many share one at most; such blocks and tiles of the call at most
+  int sink_tiles, sink_shift, sink_most, sink_slots, sink_sums;
 };
 
 // Query heads of a key head that a block takes, as a power of two: a block passes over
@@ -39,10 +40,9 @@ struct PromptArgs {
 inline int window_heads(int group) { return group % 4 == 0 ? 2 : group % 2 == 0 ? 1 : 0; }
 
 // Blocks that share a key tile of the gradient at most, and the steps of 32 queries
-// that each is to have, or fewer; through a window, the key tiles of a sequence that
-// hold sinks, as many blocks more for each, and the steps that each of those is to have.
+// that each is to have, or fewer; through a window, what PromptArgs has of the sinks'.
 struct GradSplits {
-  int most, steps, sink_tiles, sink_most, sink_steps;
+  int most, steps, sink_tiles, sink_shift, sink_most, sink_slots, sink_sums;
 };
 GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv, int window,
                        int sinks);
