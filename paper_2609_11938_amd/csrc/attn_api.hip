@@ -122,10 +122,11 @@ static PromptArgs prompt_args(const opattr_attn_shape *a, int32_t window, int32_
   return p;
 }
 
-// float16: the largest norms of each sequence and head
+// float16: the largest norms
 static size_t norms_bytes(const opattr_attn_shape *a) {
   return a->dtype == OPATTR_F16
-             ? align256((size_t)a->n_seqs * (a->n_heads + a->n_kv_heads) * 4)
+             ? align256((size_t)norm_slots(a->n_q, a->n_k, a->n_seqs) *
+                        (a->n_heads + a->n_kv_heads) * 4)
              : 0;
 }
 
@@ -343,6 +344,7 @@ static int prompt_grad(const opattr_attn_shape *a, int32_t window, int32_t sinks
   p.rows = reinterpret_cast<float *>(at);
   at += align256((size_t)a->n_q * a->n_heads * 8);
   if (a->dtype == OPATTR_F16) p.norms = reinterpret_cast<uint32_t *>(at);
+  p.norm_slots = (int)norm_slots(a->n_q, a->n_k, a->n_seqs);
   p.part = reinterpret_cast<float *>(at + norms_bytes(a));
   const GradSplits x = grad_splits(a->n_q, a->n_k, a->n_seqs, a->n_heads, a->n_kv_heads, p.window,
                                    p.sinks);

@@ -294,6 +294,23 @@ __device__ __forceinline__ int wave_sums(int x) {
   return x;
 }
 
+// The largest over the wave, uniform: the same moves.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  const auto moved = [&](auto how, auto rows) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(how)::value,
+                                                 decltype(rows)::value, 0xf, false);
+  };
+  using std::integral_constant;
+  const integral_constant<int, 0xf> all;
+  x = max(x, moved(integral_constant<int, 0x111>(), all));
+  x = max(x, moved(integral_constant<int, 0x112>(), all));
+  x = max(x, moved(integral_constant<int, 0x114>(), all));
+  x = max(x, moved(integral_constant<int, 0x118>(), all));
+  x = max(x, moved(integral_constant<int, 0x142>(), integral_constant<int, 0xa>()));
+  x = max(x, moved(integral_constant<int, 0x143>(), integral_constant<int, 0xc>()));
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, OPA_WAVE - 1);
+}
+
 // Tile `tile` of the tiles of `rows` rows that the sequences of `cu` have: which
 // of the sequence's tiles it is, the sequence's spans in both offset arrays, and
 // which sequence; false past the last. By whole waves; the result is uniform. Each lane loads a

@@ -16,10 +16,9 @@
 // Products, exponentials and fragment reads follow one another in a wave, as in the
 // forward pass: 12 documents of up to 4001 tokens, 16 heads on 4 of 128: dq 346 us, dk
 // and dv 346, their sums 39, the matrix units busy 54% and 52% of the first two; with
-// the forward pass 887 us, in float16 (two launches more, for few rows one: dout and v once
-// more: 25 us) 961. 8 sequences of 512, 8 heads of 64: 16 and 18 us, one round of
-// blocks; a training pass 43 us, in float16 49. head_dim 72 to 120 costs nearly what 128
-// does.
+// the forward pass 887 us, in float16 (one launch more: dout and v once more: 21 us)
+// 956. 8 sequences of 512, 8 heads of 64: 16 and 18 us, one round of blocks; a training
+// pass 43 us, in float16 50. head_dim 72 to 120 costs nearly what 128 does.
 #include <algorithm>
 
 #include "attn_dev.h"
@@ -33,6 +32,42 @@ constexpr int kHeld = 32 * kGradWaves;  // keys (queries) a block holds
 // scores of 32 at a time of head_dim 128.
 constexpr int kStep(int dp) { return dp <= 64 ? 64 : 32; }
 
+// float16: the largest squared norms of dout's and v's rows, in pieces of kNormRows rows of a
+// sequence and head: [n_heads + n_kv][slots] as the bits of non-negative floats, whose order
+// is that of integers. Piece p of sequence b is in slot b + first / kNormRows + p, first its
+// first row, which leaves room for every sequence's, and each has one writer: nothing is
+// cleared before, and a long sequence's pieces are many blocks'.
+constexpr int kNormRows = 128, kNormThreads = 256;
+int64_t norm_slots(int64_t n_q, int64_t n_k, int n_seqs) {
+  return std::max(n_q, n_k) / kNormRows + n_seqs;
+}
+__device__ __forceinline__ int norms_at(const PromptArgs &a, int head, int seq, const Span &s) {
+  return head * a.norm_slots + seq + s.first / kNormRows;
+}
+// The product of the largest norms of dout, of n query heads from `head` on, and of v; by
+// whole waves.
+__device__ __forceinline__ float most_norms(const PromptArgs &a, int seq, const Span &sq,
+                                            const Span &sk, int head, int n, int hk) {
+  const uint32_t *dout = a.norms + norms_at(a, head, seq, sq);
+  const uint32_t *v = a.norms + norms_at(a, a.n_heads + hk, seq, sk);
+  const int pieces = tiles_of(sq.count, kNormRows), douts = pieces * n;
+  const int vs = tiles_of(sk.count, kNormRows), most = douts > vs ? douts : vs;
+  uint32_t x = 0, y = 0;
+  if (douts == 1 && vs == 1) {  // by scalars (1000 sequences of 20: 331 us, 320 so)
+    x = dout[0];
+    y = v[0];
+  } else {
+    for (int i = lane_id(); i < most; i += OPA_WAVE) {
+      const int h = n == 1 || i >= douts ? 0 : i / pieces;
+      if (i < douts) x = max(x, dout[h * a.norm_slots + i - h * pieces]);
+      if (i < vs) y = max(y, v[i]);
+    }
+    x = wave_max(x);
+    y = wave_max(y);
+  }
+  return sqrtf(__uint_as_float(x)) * sqrtf(__uint_as_float(y));
+}
+
 // Weights and their gradients are rounded to 16 bits for the products. For
 // float16 both are scaled by powers of two first: the weights by 2^kWeight, and
 // ds by 2^e with |ds| <= 2 |dout_i| |v_j|, so that its largest stays below
@@ -42,25 +77,17 @@ constexpr int kStep(int dp) { return dp <= 64 ? 64 : 32; }
 template <class E>
 struct Scales {
   static constexpr float kWeight = 0.f;
-  static __device__ __forceinline__ float ds(const PromptArgs &, int, int, int, int) {
+  static __device__ __forceinline__ float ds(const PromptArgs &, int, const Span &, const Span &,
+                                             int, int, int) {
     return 1.f;
   }
 };
 template <>
 struct Scales<F16> {
   static constexpr float kWeight = 10.f;
-  static __device__ __forceinline__ float ds(const PromptArgs &a, int seq, int head, int n,
-                                             int hk) {
-    const uint32_t *norms = a.norms + (int64_t)seq * (a.n_heads + a.n_kv);
-    uint32_t dout = norms[head];
-    if (n > 1) {
-      for (int i = lane_id(); i < n; i += OPA_WAVE) dout = max(dout, norms[head + i]);
-#pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) dout = max(dout, (uint32_t)__shfl_xor((int)dout, d));
-      dout = (uint32_t)uniform((int)dout);
-    }
-    const float most = sqrtf(__uint_as_float(dout)) *
-                       sqrtf(__uint_as_float(norms[a.n_heads + hk]));
+  static __device__ __forceinline__ float ds(const PromptArgs &a, int seq, const Span &sq,
+                                             const Span &sk, int head, int n, int hk) {
+    const float most = most_norms(a, seq, sq, sk, head, n, hk);
     if (!(most > 0.f) || !(most < 1e30f)) return 1.f;
     int e;
     frexpf(most, &e);  // most < 2^e
@@ -68,21 +95,13 @@ struct Scales<F16> {
   }
 };
 
-// float16: the largest squared norms of dout's and v's rows, of each sequence and
-// head (the bits of non-negative floats order as integers, so the maximum is the same
-// in any order). A block takes kNormRows rows of a sequence and one head: blockIdx.y
-// is a query head, and past those a key head. 4 lanes a row.
-//
-// kAll: a block takes a whole sequence, so that nothing has to be cleared before: for few
-// rows, of sequences that are no longer than a block likes. 8 heads of 64, with the launch
-// that clears and without: one sequence of 64 8.1 us and 4.0, 8 of 512 10.9 and 4.4, 2 of
-// 2048 10.9 and 9.6, one of 4096 11.3 and 13.4; 100 of 40, 16 heads and 16 key heads of
-// 128: 13.8 and 17.8.
-constexpr int kNormRows = 512;
-template <bool kAll>
-__global__ __launch_bounds__(kAll ? 1024 : 256) void k_attn_norms(PromptArgs a) {
-  constexpr int kThreads = kAll ? 1024 : 256;
-  __shared__ float most[kThreads / OPA_WAVE];
+// A block takes a piece of one head: blockIdx.y is a query head, and past those a key
+// head. 4 lanes a row. 8 heads of 64: 8 sequences of 512 4.1 us, one of 4000 beside three
+// of 20 4.2 (16 heads on 4 of 128: 7.6); 12 documents of up to 4001 of those 20.6, 95 MB at
+// 4.6 TB/s. Pieces of 512 rows by 1024 threads find 1000 sequences of 20 in 142 us and not
+// 53, by 256 threads those of 512 in 6.6.
+__global__ __launch_bounds__(kNormThreads) void k_attn_norms(PromptArgs a) {
+  __shared__ float most[kNormThreads / OPA_WAVE];
   const int sub = threadIdx.x & 3;
   const bool q = (int)blockIdx.y < a.n_heads;
   const int head = q ? blockIdx.y : blockIdx.y - a.n_heads;
@@ -90,45 +109,36 @@ __global__ __launch_bounds__(kAll ? 1024 : 256) void k_attn_norms(PromptArgs a) 
   const Rows x = q ? a.dout : a.v;
   const int32_t *cu = q ? a.cu_q : a.cu_k;
   Span s, same;
-  int part = 0, seq = blockIdx.x;
-  if constexpr (kAll)
-    s = span_of(cu, seq, n);
-  else if (!find_tile(cu, n, cu, n, a.n_seqs, kNormRows, blockIdx.x, s, same, part, &seq))
-    return;
-  const int past = kAll || s.count < (part + 1) * kNormRows ? s.count : (part + 1) * kNormRows;
+  int part, seq;
+  if (!find_tile(cu, n, cu, n, a.n_seqs, kNormRows, blockIdx.x, s, same, part, &seq)) return;
+  const int past = s.count < (part + 1) * kNormRows ? s.count : (part + 1) * kNormRows;
   float top = 0.f;
-  for (int t = part * kNormRows + (threadIdx.x >> 2); t < past; t += kThreads / 4) {
+  for (int t = part * kNormRows + (threadIdx.x >> 2); t < past; t += kNormThreads / 4) {
     const uint16_t *px = x.p + (int64_t)(s.first + t) * x.ts + (int64_t)head * x.hs;
-    float norm = 0.f;
-    for (int c = sub * 8; c < a.head_dim; c += 32) {
-      const s16x8 u = *reinterpret_cast<const s16x8 *>(px + c);
+    s16x8 u[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float f = F16::widen((uint16_t)u[i]);
-        norm = fmaf(f, f, norm);
-      }
+    for (int j = 0; j < 4; ++j) {
+      u[j] = (s16x8)(0);
+      if (sub * 8 + 32 * j < a.head_dim)
+        u[j] = *reinterpret_cast<const s16x8 *>(px + sub * 8 + 32 * j);
+    }
+    float norm = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float f = F16::widen((uint16_t)u[i / 8][i % 8]);
+      norm = fmaf(f, f, norm);
     }
     norm += __shfl_xor(norm, 1);
     norm += __shfl_xor(norm, 2);
     top = fmaxf(top, norm);
   }
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  top = __uint_as_float(wave_max(__float_as_uint(top)));
   if (lane_id() == 0) most[wave_id()] = top;
   __syncthreads();
   if (threadIdx.x) return;
 #pragma unroll
-  for (int w = 1; w < kThreads / OPA_WAVE; ++w) top = fmaxf(top, most[w]);
-  uint32_t *to = &a.norms[(int64_t)seq * (a.n_heads + a.n_kv) + blockIdx.y];
-  if (kAll)
-    *to = __float_as_uint(top);
-  else
-    atomicMax(to, __float_as_uint(top));
-}
-
-__global__ void k_attn_zero(uint32_t *p, int n) {
-  const int i = blockIdx.x * blockDim.x + threadIdx.x;
-  if (i < n) p[i] = 0;
+  for (int w = 1; w < kNormThreads / OPA_WAVE; ++w) top = fmaxf(top, most[w]);
+  a.norms[norms_at(a, blockIdx.y, seq, s) + part] = __float_as_uint(top);
 }
 
 // Two groups of waves share the keys where the blocks are this few (one sequence
@@ -228,7 +238,7 @@ __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(Prompt
   const uint16_t *k0p = a.k.p + (int64_t)sk.first * a.k.ts + (int64_t)hk * a.k.hs;
   const uint16_t *v0p = a.v.p + (int64_t)sk.first * a.v.ts + (int64_t)hk * a.v.hs;
   const float c = a.scale * kLog2e;
-  const float up = Scales<E>::ds(a, seq, head, 1, hk);
+  const float up = Scales<E>::ds(a, seq, sq, sk, head, 1, hk);
   const float fw = exp2_fast(-Scales<E>::kWeight), upw = up * fw;
   const int nat0 = nat_place<DP>(), tr0 = tr_place<DP>();
   f32x16 dq[DB], kp[DB];
@@ -550,6 +560,7 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
   if (split >= splits) return;
   const Steps part_steps = split_steps<W>(all, split, splits);
   const int first = part_steps.first, steps = part_steps.past;
+  const float up = Scales<E>::ds(a, seq, sq, sk, hk * a.group, a.group, hk);
   s16x8 kf[KS], vf[KS];
   {
     const int64_t tok = sk.first + (live ? key : 0);
@@ -566,7 +577,6 @@ __global__ __launch_bounds__(kGradWaves * OPA_WAVE, 2) void k_attn_dkv(PromptArg
     }
   }
   const float c = a.scale * kLog2e;
-  const float up = Scales<E>::ds(a, seq, hk * a.group, a.group, hk);
   const float fv = exp2_fast(-Scales<E>::kWeight), upw = up * fv;
   const int nat0 = nat_place<DP>(), tr0 = tr_place<DP>();
   f32x16 dk[DB], dv[DB];
@@ -813,25 +823,11 @@ static void launch(const PromptArgs &a, hipStream_t s) {
   }
 }
 
-static bool whole_norms(const PromptArgs &a, int rows) {
-  return rows <= 4096 && rows <= 1024 * (int64_t)a.n_seqs &&
-         (int64_t)a.n_seqs * (a.n_heads + a.n_kv) <= 2048;
-}
-
 template <class E>
 static void grad(const PromptArgs &a, hipStream_t s) {
-  if (a.norms) {
-    const int n = a.n_seqs * (a.n_heads + a.n_kv);
-    const int most = a.n_k > a.n_q ? a.n_k : a.n_q;
-    if (whole_norms(a, most)) {
-      hipLaunchKernelGGL(k_attn_norms<true>, dim3(a.n_seqs, a.n_heads + a.n_kv), dim3(1024), 0, s,
-                         a);
-    } else {
-      hipLaunchKernelGGL(k_attn_zero, dim3((n + 63) / 64), dim3(64), 0, s, a.norms, n);
-      const dim3 grid(most / kNormRows + a.n_seqs, a.n_heads + a.n_kv);
-      if (most > 0) hipLaunchKernelGGL(k_attn_norms<false>, grid, dim3(256), 0, s, a);
-    }
-  }
+  if (a.norms && (a.n_q > 0 || a.n_k > 0))
+    hipLaunchKernelGGL(k_attn_norms, dim3(a.norm_slots, a.n_heads + a.n_kv), dim3(kNormThreads), 0,
+                       s, a);
   if (a.window)
     a.head_dim <= 64 ? launch<E, 64, true>(a, s) : launch<E, 128, true>(a, s);
   else

@@ -24,9 +24,10 @@ struct PromptArgs {
   opattr_diag *diag;
   Rows dout, dq, dk, dv;
   // the gradient's workspace: pairs (lse in binary digits, D)
-  // [heads][n_q]; bounds [n_seqs][n_heads + n_kv] (float16); the splits' dk and dv
+  // [heads][n_q]; largest norms [n_heads + n_kv][norm_slots] (float16); the splits' dk and dv
   float *rows, *part;
   uint32_t *norms;
+  int norm_slots;
   int splits, split_steps;
   // key tiles of a sequence with sinks; where blocks share them, the log2 of a block's
   // steps and how many share one at most; such blocks and tiles of the call at most
@@ -46,6 +47,8 @@ struct GradSplits {
 };
 GradSplits grad_splits(int64_t n_q, int64_t n_k, int n_seqs, int n_heads, int n_kv, int window,
                        int sinks);
+// Pieces of rows whose largest norms a gradient in float16 looks up, of a head.
+int64_t norm_slots(int64_t n_q, int64_t n_k, int n_seqs);
 // Key tiles' parts that the blocks leave for the sums: of 128 keys of a key head, at most.
 int64_t grad_parts(const GradSplits &x, int64_t n_k, int n_seqs);
 
