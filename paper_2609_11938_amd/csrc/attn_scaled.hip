@@ -199,10 +199,12 @@ void run_append_scaled(const AppendScaledArgs &a, int dtype, hipStream_t s) {
 // --------------------------------------------------------------------------
 // attention
 // --------------------------------------------------------------------------
-// The weights that meet the codes are 2^(x_j + e_j - m'), e_j the value's exponent and
-// m' the largest x_j + e_j so far; those of the sum are 2^(x_j - m) as elsewhere. So
-// no scale, however large or small, takes a weight past the 16 bits of its product:
-// out = 2^(m' - m) sum_j 2^(x_j + e_j - m') c_j / sum_j 2^(x_j - m).
+// The weights that meet the codes are 2^((x_j - m) + (e_j - n)), e_j the value's exponent and
+// n a whole number near the largest x_j + e_j so far, less m; those of the sum are
+// 2^(x_j - m) as elsewhere. So no scale, however large or small, takes a weight past the 16
+// bits of its product, and exponents are added to differences of scores, never to
+// scores, whose size would round them:
+// out = 2^n sum_j 2^((x_j - m) + (e_j - n)) c_j / sum_j 2^(x_j - m).
 //
 // Bound by the cache's bytes, half of those of 16 bits: 2 sequences of 131000 tokens, 32
 // heads on 8 of 128: 108 us, 537 MB at 5.0 TB/s, and 6 us to join the shares; 96 of up to
@@ -229,17 +231,14 @@ __device__ __forceinline__ s16x8 eight_values(uint32_t w0, uint32_t w1) {
   return __builtin_bit_cast(s16x8, v);
 }
 
-// A row's result from its values' sum and its weights' sum, with their references.
+// A row's result from its values' sum, of 2^n, and its weights' sum and reference.
 template <class E>
 __device__ __forceinline__ void scaled_store(const PagedArgs &a, int seq, int head, int d, f32x4 v,
-                                             float vtop, float top, float l) {
+                                             float n, float top, float l) {
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  // 2^(vtop - top) as a power within one and a whole exponent
-  const float by = l == 0.f ? 0.f : vtop - top;
-  const float whole = rintf(by), f = exp2_fast(by - whole) * inv;
-  const int n = (int)whole;
-  const u32x2 w = {E::pack(ldexpf(v[0] * f, n), ldexpf(v[1] * f, n)),
-                   E::pack(ldexpf(v[2] * f, n), ldexpf(v[3] * f, n))};
+  const int by = (int)n;
+  const u32x2 w = {E::pack(ldexpf(v[0] * inv, by), ldexpf(v[1] * inv, by)),
+                   E::pack(ldexpf(v[2] * inv, by), ldexpf(v[3] * inv, by))};
   if (d < a.head_dim)
     *reinterpret_cast<u32x2 *>(a.out.p + seq * a.out.ts + (int64_t)head * a.out.hs + d) = w;
   if (d == 0 && a.lse)
@@ -263,7 +262,7 @@ __device__ __forceinline__ int code_swz(int row) {
                    : ((row >> 2) & 1) | ((row >> 4) & 1) << 1;
 }
 
-// As k_attn_paged, which see; a share's results end in m', m and l. Keys' codes come to
+// As k_attn_paged, which see; a share's results end in n, m and l. Keys' codes come to
 // registers, values' straight to LDS, from where the transposing read gives a lane the
 // codes of one column of the 8 tokens whose weights it holds: they become 16-bit values
 // only as operands. The references follow the maxima only when those have passed them
@@ -319,7 +318,8 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 64 ? 4 : 3) void k_at
   f32x4 o[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) o[d] = (f32x4)(0.f);
-  float m = -INFINITY, mv = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f;  // the weights' reference, and this lane's sum
+  float n = 0.f;                 // the values' reference is 2^n beside it
   int bad = 0;
 
   constexpr int kNone = INT_MIN;
@@ -486,7 +486,7 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 64 ? 4 : 3) void k_at
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         x[u][i] = __builtin_amdgcn_ldexpf(x[u][i] * c, (R ? xk[u] : ex[i] & 255) - 127);
-        if constexpr (!R) y[u][i] = x[u][i] + (float)((ex[i] >> 8) - 127);
+        if constexpr (!R) y[u][i] = (float)((ex[i] >> 8) - 127);
       }
     }
     if (there != ~0ull || (nan_k | nan_v)) {
@@ -506,8 +506,9 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 64 ? 4 : 3) void k_at
           }
         }
     }
-    const auto with_value = [&](int u, int i) __attribute__((always_inline)) {
-      return R ? x[u][i] + xv[u] : y[R ? 0 : u][i];
+    // a value's exponent
+    const auto value_e = [&](int u, int i) __attribute__((always_inline)) {
+      return R ? xv[u] : y[R ? 0 : u][i];
     };
     float top = -INFINITY, vtop = -INFINITY;
 #pragma unroll
@@ -516,33 +517,35 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 64 ? 4 : 3) void k_at
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         t = fmaxf(t, x[u][i]);
-        if (!R) vtop = fmaxf(vtop, with_value(u, i));
+        if (!R) vtop = fmaxf(vtop, x[u][i] + value_e(u, i));
       }
       top = fmaxf(top, t);
       if (R) vtop = fmaxf(vtop, t + xv[u]);
     }
-    if (__any(top > m + 8.f || vtop > mv + 8.f)) {
-      const float mn = fmaxf(m, column_max(top)), mvn = fmaxf(mv, column_max(vtop));
-      l *= mn == -INFINITY ? 1.f : exp2_fast(m - mn);
-      const float by = mvn == -INFINITY ? 1.f : exp2_fast(mv - mvn);
+    if (__any(top > m + 8.f || vtop > m + n + 8.f)) {
+      const float mn = fmaxf(m, column_max(top)), both = fmaxf(m + n, column_max(vtop));
+      const float to = both == -INFINITY ? 0.f : rintf(both - mn);
+      const float by = mn == -INFINITY ? 1.f : exp2_fast(m - mn);
+      const float vby = mn == -INFINITY ? 1.f : exp2_fast((m - mn) + (n - to));
+      l *= by;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[d][e] *= by;
+        for (int e = 0; e < 4; ++e) o[d][e] *= vby;
       m = mn;
-      mv = mvn;
+      n = to;
     }
-    const float ref = E::kShift - (m == -INFINITY ? 0.f : m);
-    const float vref = E::kShift - (mv == -INFINITY ? 0.f : mv);
+    const float ref = m == -INFINITY ? 0.f : m;
     float sum = 0.f;
     u32x4 w;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        sum += exp2_fast(x[u][2 * i] + ref) + exp2_fast(x[u][2 * i + 1] + ref);
-        w[2 * u + i] = E::pack(exp2_fast(with_value(u, 2 * i) + vref),
-                               exp2_fast(with_value(u, 2 * i + 1) + vref));
+        const float p0 = x[u][2 * i] - ref, p1 = x[u][2 * i + 1] - ref;
+        sum += exp2_fast(p0 + E::kShift) + exp2_fast(p1 + E::kShift);
+        w[2 * u + i] = E::pack(exp2_fast(p0 + (value_e(u, 2 * i) + (E::kShift - n))),
+                               exp2_fast(p1 + (value_e(u, 2 * i + 1) + (E::kShift - n))));
       }
     l += sum;
     const s16x8 pf = __builtin_bit_cast(s16x8, w);
@@ -581,7 +584,7 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 64 ? 4 : 3) void k_at
   for (int d = 0; d < DB; ++d) *sums(wave, r, 4 * d + g) = o[d];
   if (g == 0) {
     sm[wave][r] = m;
-    sv[wave][r] = mv;
+    sv[wave][r] = n;
     sl[wave][r] = l;
   }
   __syncthreads();
@@ -592,22 +595,23 @@ __global__ __launch_bounds__(kPagedWaves * OPA_WAVE, DP == 64 ? 4 : 3) void k_at
 #pragma unroll
     for (int w = 0; w < kPagedWaves; ++w) {
       top = fmaxf(top, sm[w][row]);
-      vtop = fmaxf(vtop, sv[w][row]);
+      vtop = fmaxf(vtop, sm[w][row] + sv[w][row]);
     }
-    const float ref = top == -INFINITY ? 0.f : top, vref = vtop == -INFINITY ? 0.f : vtop;
+    const float ref = top == -INFINITY ? 0.f : top;
+    const float to = vtop == -INFINITY ? 0.f : rintf(vtop - ref);
     f32x4 v = (f32x4)(0.f);
     float ls = 0.f;
 #pragma unroll
     for (int w = 0; w < kPagedWaves; ++w) {
-      v += *sums(w, row, p) * exp2_fast(sv[w][row] - vref);
+      v += *sums(w, row, p) * exp2_fast((sm[w][row] - ref) + (sv[w][row] - to));
       ls = fmaf(sl[w][row], exp2_fast(sm[w][row] - ref), ls);
     }
     if (whole) {
-      scaled_store<E>(a, seq, head, 4 * p, v, vtop, top, ls);
+      scaled_store<E>(a, seq, head, 4 * p, v, to, top, ls);
     } else {
-      float *to = a.part + ((int64_t)item * a.n_heads + head) * (DP + 4);
-      *reinterpret_cast<f32x4 *>(to + 4 * p) = v;
-      if (p == 0) *reinterpret_cast<f32x4 *>(to + DP) = f32x4{vtop, top, ls, 0.f};
+      float *part = a.part + ((int64_t)item * a.n_heads + head) * (DP + 4);
+      *reinterpret_cast<f32x4 *>(part + 4 * p) = v;
+      if (p == 0) *reinterpret_cast<f32x4 *>(part + DP) = f32x4{to, top, ls, 0.f};
     }
   }
 }
@@ -631,7 +635,7 @@ __global__ __launch_bounds__(kJoin * DP / 4) void k_scaled_join(ScaledArgs a) {
   for (int k = threadIdx.x; k < n; k += kThreads) {
     fv[k] = p[k * step + DP];
     f[k] = p[k * step + DP + 1];
-    vtop = fmaxf(vtop, fv[k]);
+    vtop = fmaxf(vtop, f[k] + fv[k]);
     top = fmaxf(top, f[k]);
   }
 #pragma unroll
@@ -649,13 +653,14 @@ __global__ __launch_bounds__(kJoin * DP / 4) void k_scaled_join(ScaledArgs a) {
     top = fmaxf(top, wave_top[w][0]);
     vtop = fmaxf(vtop, wave_top[w][1]);
   }
-  const float ref = top == -INFINITY ? 0.f : top, vref = vtop == -INFINITY ? 0.f : vtop;
+  const float ref = top == -INFINITY ? 0.f : top;
+  const float to = vtop == -INFINITY ? 0.f : rintf(vtop - ref);
   const int run = threadIdx.x / (DP / 4), d = threadIdx.x % (DP / 4) * 4;
   f32x4 v = (f32x4)(0.f);
   float l = 0.f;
 #pragma unroll 4
   for (int k = run; k < n; k += kJoin) {
-    v += *reinterpret_cast<const f32x4 *>(p + k * step + d) * exp2_fast(fv[k] - vref);
+    v += *reinterpret_cast<const f32x4 *>(p + k * step + d) * exp2_fast((f[k] - ref) + (fv[k] - to));
     l = fmaf(p[k * step + DP + 2], exp2_fast(f[k] - ref), l);
   }
   sums[run][d / 4] = v;
@@ -668,7 +673,7 @@ __global__ __launch_bounds__(kJoin * DP / 4) void k_scaled_join(ScaledArgs a) {
     v += sums[k][d / 4];
     l += run_l[k];
   }
-  scaled_store<E>(a, seq, head, d, v, vtop, top, l);
+  scaled_store<E>(a, seq, head, d, v, to, top, l);
 }
 
 constexpr int64_t kMaxRunStride = 1 << 26;  // 16 tokens within 2^31 bytes
