@@ -10,7 +10,8 @@ forward pass and its gradient over packed documents. Both take a sliding window 
 sinks, and ``serve`` a cache of 8 bits. Rows of random numbers
 stand for the projections' outputs. Every call is recorded by a ``Recorder``
 (device time by events, with the host kept ahead; bytes as the call has to move them, computed from its
-sizes and results, not counted in the memory) inside the operator range that
+sizes and results, not counted in the memory: rows, and of a cache what is in it; an append's
+exponents, and what it rounds again as they grow, are not among them) inside the operator range that
 issued it; ``profile`` attributes the trace and builds the profile document.
 """
 from __future__ import annotations
@@ -217,6 +218,15 @@ class Cache:
                            self.data[layer, 0], self.data[layer, 1], self.table, self.lens,
                            lens_out=lens_out)
 
+    def _blocks(self, n, window, sinks):
+        """Blocks with one exponent of which a query that comes after n - 1 tokens sees a
+        token."""
+        block = self.page_size // self.scales.shape[3]
+        first = 0 if window is None else max(0, n - window)
+        blocks = -(-n // block) - first // block
+        sinks = -(-min(sinks, first) // block)  # the last of them may be the window's first
+        return blocks + min(sinks, first // block)
+
     def attend(self, rec, layer, q, lens, sizes, scale, window=None, sinks=0):
         """Attention of one token a sequence over the layer's cache, of the given
         lengths (on the device, and as numbers): (out, lse)."""
@@ -227,6 +237,7 @@ class Cache:
         read = 2 * seen * k.shape[2] * k.shape[3] * k.element_size() + rows
         kw = dict(scale=scale, ws=self.ws)
         if self.scales is not None:
+            read += 2 * k.shape[2] * sum(self._blocks(n, window, sinks) for n in sizes)
             return rec.launch("attn_paged_scaled", read, rows, attn.opattr_attn_paged_scaled, q, k,
                               v, *self.scales[layer], self.table, lens, window=window,
                               sinks=sinks, **kw)
