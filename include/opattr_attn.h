@@ -48,8 +48,8 @@
  * before its division by the weights' in float32's range.
  *
  * float16 gradients: ds is rounded after a power of two by the largest |dout| and |v|
- * of its sequence and head, so neither another sequence nor, for dq, another query
- * head costs it bits.
+ * of its sequence and head (for dk of the key head's query heads together), so neither
+ * another sequence nor, for dq, another query head costs it bits.
  */
 #ifndef OPATTR_ATTN_H
 #define OPATTR_ATTN_H
@@ -97,7 +97,9 @@ int opattr_attn_prompt(const opattr_attn_shape *a, const opattr_rows *q, const o
      dv_j = sum_i p_ij dout_i,   ds_ij = scale p_ij (dout_i.v_j - D_i),
      dq_i = sum_j ds_ij k_j,     dk_j = sum_i ds_ij q_i,
    key heads summing over the query heads that read them. The same bits on
-   every run. out and lse are opattr_attn_prompt's for the same inputs. */
+   every run of a call: the parts that dk and dv are summed in go by n_q, n_k and n_seqs,
+   so that in buffers of other sizes a sequence's may be rounded otherwise. out and lse are
+   opattr_attn_prompt's for the same inputs. */
 size_t opattr_attn_prompt_grad_workspace_bytes(const opattr_attn_shape *a);
 int opattr_attn_prompt_grad(const opattr_attn_shape *a, const opattr_rows *dout,
                             const opattr_rows *q, const opattr_rows *k, const opattr_rows *v,
@@ -211,7 +213,8 @@ int opattr_kv_append_scaled(const opattr_kv_scaled *c, int64_t n_new, const int3
 /* opattr_attn_paged_window over a cache of 8 bits (a window of 2^30 sees every token).
    The codes are exact in the products, whose sums are q.code in float32; scores and
    values are scaled there, and weights are rounded to 16 bits with the value's scale in
-   them. */
+   them, the largest about 1: of float16's those below 2^-20 of it lose bits, and below
+   2^-30 all. */
 size_t opattr_attn_paged_scaled_workspace_bytes(const opattr_kv_scaled *c, int32_t n_heads,
                                                 int32_t window, int32_t sinks);
 int opattr_attn_paged_scaled(const opattr_kv_scaled *c, int32_t n_heads, int32_t window,

@@ -16,7 +16,7 @@
 // Products, exponentials and fragment reads follow one another in a wave, as in the
 // forward pass: 12 documents of up to 4001 tokens, 16 heads on 4 of 128: dq 346 us, dk
 // and dv 346, their sums 39, the matrix units busy 54% and 52% of the first two; with
-// the forward pass 887 us, in float16 (one launch more: dout and v once more: 21 us)
+// the forward pass 887 us, in float16 (one launch more: dout and v once more: 18 us)
 // 956. 8 sequences of 512, 8 heads of 64: 16 and 18 us, one round of blocks; a training
 // pass 43 us, in float16 50. head_dim 72 to 120 costs nearly what 128 does.
 #include <algorithm>
@@ -97,8 +97,8 @@ struct Scales<F16> {
 
 // A block takes a piece of one head: blockIdx.y is a query head, and past those a key
 // head. 4 lanes a row. 8 heads of 64: 8 sequences of 512 4.1 us, one of 4000 beside three
-// of 20 4.2 (16 heads on 4 of 128: 7.6); 12 documents of up to 4001 of those 20.6, 95 MB at
-// 4.6 TB/s. Pieces of 512 rows by 1024 threads find 1000 sequences of 20 in 142 us and not
+// of 20 4.2 (16 heads on 4 of 128: 7.6); 12 documents of up to 4001 of those 18 to 21, 77 MB
+// at 4 TB/s. Pieces of 512 rows by 1024 threads find 1000 sequences of 20 in 142 us and not
 // 53, by 256 threads those of 512 in 6.6.
 __global__ __launch_bounds__(kNormThreads) void k_attn_norms(PromptArgs a) {
   __shared__ float most[kNormThreads / OPA_WAVE];
@@ -153,8 +153,8 @@ constexpr int kFewBlocks = 256, kManyKeys = 768;
 // the plain form rounded to 16 bits once: 1.65 without, 1.4 to 1.5 with). The exact D
 // goes to the second pass with the scaled lse.
 // W: through a window with sinks, with heads and keys as in the forward pass: 12
-// documents of up to 4001 tokens, 16 heads on 4 of 128, window 512, 4 sinks, float16: 172
-// us, dk and dv 204 and the sinks' sums 10 (without a window 346, 346 and 39).
+// documents of up to 4001 tokens, 16 heads on 4 of 128, window 512, 4 sinks, float16: 168
+// us, dk and dv 175 and the sinks' sums 10 (without a window 360, 353 and 40).
 template <class E, int DP, int G, bool W>
 __global__ __launch_bounds__(G * kGradWaves * OPA_WAVE, 2) void k_attn_dq(PromptArgs a) {
   constexpr int KS = DP / 16, DB = DP / 32;

@@ -13,8 +13,8 @@ constexpr int kTile = 32;        // tokens a wave takes at a time
 constexpr int kMinShare = 256;   // tokens of the smallest share
 // Blocks that the shares come to: few enough that a block's start is a small part of it,
 // enough that the last ones leave no chiplet idle for long. Over 8 bits a share of as many
-// tokens is done sooner: 96 sequences of up to 9001 tokens, 8 key heads of 128, 64 us in
-// 2048 blocks, 68 us in 1024 and 67 us in 4096.
+// tokens is done sooner: 96 sequences of up to 9001 tokens, 8 key heads of 128, 65 us in
+// 2048 blocks, 68 us in 1024 and 67 us in 4096, whose join takes 7 us and not 5.
 constexpr int kBlocks = 1024, kScaledBlocks = 2048;
 
 // Tokens of sequence b, as many as its table can name; of these, as many as its

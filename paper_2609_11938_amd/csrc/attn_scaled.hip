@@ -208,10 +208,11 @@ void run_append_scaled(const AppendScaledArgs &a, int dtype, hipStream_t s) {
 //
 // Bound by the cache's bytes, half of those of 16 bits: 2 sequences of 131000 tokens, 32
 // heads on 8 of 128: 108 us, 537 MB at 5.0 TB/s, and 6 us to join the shares; 96 of up to
-// 9001, 275 MB: 65 us, 4.2 TB/s, and 5 us. At half the bytes a tile's conversions, softmax
-// and products are no longer hidden by themselves, so the work is what the loop looks
-// after: codes become 16-bit values only as operands, an exponent is added and not
-// multiplied, a run's addresses and exponents are scalars.
+// 9001, 275 MB: 65 us, 4.2 TB/s, and 5 us; 64 of up to 32000 through a window of 4096 with 4
+// sinks, 210 MB: 51 us, 4.1 TB/s, and 4 us (127 and 6 without a window). At half the bytes a
+// tile's conversions, softmax and products are no longer hidden by themselves, so the work
+// is what the loop looks after: codes become 16-bit values only as operands, an exponent is
+// added and not multiplied, a run's addresses and exponents are scalars.
 
 // The two codes of half h of a word as 16-bit values (exact).
 template <class E>
@@ -271,11 +272,12 @@ __device__ __forceinline__ int code_swz(int row) {
 // R: pages and blocks of 16 tokens or more. A run of 16 then has one page and one scale:
 // its addresses are scalars and a lane's own offsets, its exponents scalars. Otherwise
 // each token has its own (ts of any size too). 2 sequences of 131000 tokens: 108 us by
-// runs, 111 us otherwise; 96 of up to 9001: 65 and 68 us; 4 of 150, heads of 64: 5.5 and
-// 7.0 us.
+// runs, 111 us otherwise; 96 of up to 9001: 65 and 68 us; 4 of 300 through a window of 64,
+// heads of 64: 4.5 and 5.7 us.
 //
 // Three waves a SIMD for heads of 128: the registers of four hold a tile's loads no more
-// (2 of 131000: 115 us and not 108; 96 of up to 9001: 68 and not 64).
+// (2 of 131000: 112 us and not 108; 64 of up to 32000: 131 and not 127; 96 of up to 9001:
+// 65 us either way).
 //
 // Blocks go round the 8 chiplets: a share's key heads lie 8 blocks apart, on one chiplet,
 // so that a token's heads, side by side in memory, are read through one cache.
@@ -660,7 +662,8 @@ __global__ __launch_bounds__(kJoin * DP / 4) void k_scaled_join(ScaledArgs a) {
   float l = 0.f;
 #pragma unroll 4
   for (int k = run; k < n; k += kJoin) {
-    v += *reinterpret_cast<const f32x4 *>(p + k * step + d) * exp2_fast((f[k] - ref) + (fv[k] - to));
+    v += *reinterpret_cast<const f32x4 *>(p + k * step + d) *
+         exp2_fast((f[k] - ref) + (fv[k] - to));
     l = fmaf(p[k * step + DP + 2], exp2_fast(f[k] - ref), l);
   }
   sums[run][d / 4] = v;
