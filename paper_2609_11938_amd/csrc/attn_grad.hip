@@ -903,6 +903,7 @@ static GradSplits window_splits(int64_t n_q, int64_t n_k, int n_seqs, int group,
   const int64_t seqs = n_q / least < n_seqs ? n_q / least : n_seqs;
   const int64_t all = tiles * ((n_q + kMostEnd * seqs) * group / 32 + 1);  // steps, of them
   while (all >> shift > kSinkBlocks / n_kv) ++shift;
+  if (shift > 30) return x;  // (no tile has as many steps)
   // of S = ceil(steps / 2^shift) blocks, more than one: less than 2 steps / 2^shift, and
   // than steps / 2^shift + 1
   const int64_t held = std::min(seqs * tiles, n_k / kHeld + seqs);

@@ -35,3 +35,12 @@ def test_sinks_of_many_key_tiles(lib, shape, sinks):  # noqa: F811
     sequence's last block has few steps."""
     g, d = shape[3:5]
     assert _extra(lib, shape, sinks) <= 2 * (2048 + g) * 128 * 2 * d * 4
+
+
+@pytest.mark.parametrize("n", [4000, 1 << 18])
+def test_more_key_heads_than_shared_blocks(lib, n):  # noqa: F811
+    """No tile is shared then."""
+    a = _shape(n_q=n, n_k=1000, n_seqs=2, n_heads=4096, n_kv_heads=4096, head_dim=64)
+    need = lib.opattr_attn_prompt_window_grad_workspace_bytes
+    assert need(a, 50, 0) > 0
+    assert all(need(a, 50, sinks) == need(a, 50, 0) for sinks in (1, 200, 1 << 29))
